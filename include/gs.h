@@ -398,6 +398,168 @@ int gs_linear_noalloc(const void *x, const void *w, void *y, int M, int N, int K
  * nothing.  Errors: GS_ERR_CUDA. */
 int gs_linear_noalloc_status(void *stream);
 
+/* ---------------------------------------------------------------------------
+ * One sampled decoding step over a paged cache, for decoders whose heads the
+ * engine above does not cover and for sampling several continuations of one
+ * prompt.  The paper has no counterpart: its rounds take the argmax or plain
+ * temperature samples of one fixed decoder.  The four operators take a layer's
+ * projected rows to the next token; the matrix products between them are
+ * gs_linear's.  They need no handle: work is enqueued on the given stream, no
+ * device memory is allocated, and every call may be captured in a CUDA graph.
+ *
+ * `err` (or the first int32 of the scratch) is a device error word: a kernel
+ * that meets an index out of range stores 1, one whose bounded wait runs out
+ * stores 2, and goes on with the index clamped or the write left out.  It is
+ * never cleared by a call: zero it once, read it when convenient.
+ * ------------------------------------------------------------------------ */
+
+/* Element types. */
+enum { GS_F16 = 0, GS_BF16 = 1, GS_F32 = 2 };
+
+/* One layer of a paged cache.  A page holds 64 tokens, [2][n_kv_heads][64 *
+ * head_dim] elements: keys as [64 tokens][head_dim], values transposed, as
+ * [head_dim][64 tokens] (for head_dim 64 and fp16 the layout of the engine and
+ * of gs_attention).  Token t of sequence s lies in page page_table[s][t / 64].
+ *   kv          device, 16-byte aligned, n_pages pages
+ *   head_dim    64 or 128; dtype GS_F16 or GS_BF16
+ *   page_table  device int32 [n_seq, pt_stride]
+ * Pages may be shared between sequences as long as no call writes them. */
+typedef struct {
+  void *kv;
+  int n_pages, n_kv_heads, head_dim, dtype;
+  const int32_t *page_table;
+  int n_seq, pt_stride;
+} gs_cache;
+
+/* Rotary positions: the first rotary_dim dims of a head (a multiple of 16, at
+ * most head_dim) are rotated in pairs, (i, i + rotary_dim / 2) in the half
+ * layout or (2i, 2i + 1) in the interleaved one; the rest pass through.
+ *   table   device fp32 [table_rows][rotary_dim / 2][2], 16-byte aligned: cos
+ *           and sin of each position's angles (gs_rope_table) */
+enum { GS_ROPE_HALF = 0, GS_ROPE_INTERLEAVED = 1 };
+typedef struct {
+  const void *table;
+  int table_rows, rotary_dim, layout;
+} gs_rope;
+
+/* Frequencies theta^(-2i / rotary_dim) of pair i, stretched for contexts longer
+ * than the trained one by `factor` (>= 1):
+ *   GS_ROPE_LINEAR  every frequency divided by factor
+ *   GS_ROPE_NTK     theta * factor^(R / (R - 2)) instead of theta
+ *   GS_ROPE_YARN    pairs that turn more than beta_fast times in original_ctx
+ *                   positions kept, those below beta_slow divided, a linear
+ *                   ramp over the pairs between; cos and sin times magnitude
+ *                   (0: 0.1 ln(factor) + 1)
+ * Fields that a kind does not name are not read. */
+enum { GS_ROPE_PLAIN = 0, GS_ROPE_LINEAR = 1, GS_ROPE_NTK = 2, GS_ROPE_YARN = 3 };
+typedef struct {
+  int kind;
+  float theta, factor;
+  int original_ctx;
+  float beta_fast, beta_slow, magnitude;
+} gs_rope_scaling;
+
+/* Fill a rotary table: angles, cos and sin in 64 bits, rounded once to fp32.
+ *   table  device fp32 [rows][rotary_dim / 2][2], 16-byte aligned
+ * rotary_dim is a multiple of 16, at most 128.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_CUDA. */
+int gs_rope_table(const gs_rope_scaling *scaling, int rotary_dim, int rows, void *table,
+                  void *stream);
+
+/* Per-head RMS norm of queries and keys, their rotation, and the write of keys
+ * and values into the cache, for T tokens of any sequences (a decode batch, a
+ * prompt, or a mix).  Arithmetic in fp32, each output rounded once.
+ *   qkv     device [T, (n_heads + 2 n_kv_heads) * head_dim] of the cache's
+ *           type: query heads, key heads, value heads; row stride ld_qkv
+ *           elements (a multiple of 8), 16-byte aligned
+ *   q_gain, k_gain  device bf16 [head_dim], 16-byte aligned; both NULL: no norm
+ *   seq     device int32 [T]: the token's row of the page table
+ *   slot    device int32 [T]: its place in the sequence's cache; negative: the
+ *           token's key and value are not written.  Two tokens of one call must
+ *           not name the same place.
+ *   pos     device int32 [T]: the position it is rotated to (row of the table)
+ *   q_out   device [T, n_heads * head_dim], row stride ld_q (a multiple of 8);
+ *           may be qkv itself with ld_q == ld_qkv
+ *   err     device int32, see above (seq, slot, page or pos out of range: a
+ *           write is left out, a position clamped)
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (head_dim, too many rows),
+ * GS_ERR_CUDA. */
+int gs_rope_append(const gs_cache *cache, const gs_rope *rope, const void *qkv, int64_t ld_qkv,
+                   int T, int n_heads, const void *q_gain, const void *k_gain, float eps,
+                   const int32_t *seq, const int32_t *slot, const int32_t *pos, void *q_out,
+                   int64_t ld_q, int32_t *err, void *stream);
+
+/* Attention of one token per row over the paged cache:
+ *   out = softmax(scale * q K^T) V over the keys max(0, n - window) .. n - 1
+ * (all n keys if window is 0).  A row with n = 0 gives zeros and lse -inf.
+ *   q       device [rows, n_heads * head_dim] of the cache's type, row stride
+ *           ld_q (a multiple of 8), 16-byte aligned; out likewise with ld_out
+ *   seq     device int32 [rows]: the row's sequence (page-table row), or NULL:
+ *           row r is sequence r
+ *   n       device int32 [rows]: cached keys, the new token's own included
+ *   lse     device fp32 [rows, n_heads] or NULL: ln of the sum of exp of the
+ *           scores (to join with attention over other keys)
+ *   split_pages  pages per work item, 0 = chosen from rows, heads and pt_stride
+ *           (or window).  Items are reduced independently and joined in a fixed
+ *           order: a row's result depends on its own keys and the split only.
+ *   scratch device, 256-byte aligned, at least
+ *           gs_decode_attention_scratch_bytes(...) bytes (0 on a bad argument);
+ *           its first int32 is the error word, the rest may hold anything.
+ *           Calls that may run at the same time need scratch of their own.
+ * What the cache holds at or beyond n, or before the window, has no influence.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (head_dim, rows > 65535),
+ * GS_ERR_OOM (scratch too small), GS_ERR_CUDA. */
+size_t gs_decode_attention_scratch_bytes(const gs_cache *cache, int rows, int n_heads,
+                                         int split_pages);
+int gs_decode_attention(const gs_cache *cache, const void *q, int64_t ld_q, const int32_t *seq,
+                        const int32_t *n, int rows, int n_heads, float scale, int window, void *out,
+                        int64_t ld_out, float *lse, int split_pages, void *scratch,
+                        size_t scratch_bytes, void *stream);
+
+/* Per-row sampling settings: device arrays of `rows` entries, each may be NULL.
+ *   temperature fp32, > 0 (NULL: 1).  0, negative or NaN: the row takes its
+ *               largest logit, and u is not used
+ *   top_p       fp32: below 1, the shortest prefix whose mass is at least top_p
+ *   min_p       fp32: above 0, only tokens with at least min_p times the
+ *               largest probability (at most 1 is used)
+ *   top_k       int32: above 0, the k most likely tokens */
+typedef struct {
+  const float *temperature, *top_p, *min_p;
+  const int32_t *top_k;
+} gs_sample_params;
+
+/* Draw one token per row.  With M the row's largest logit, token i has weight
+ * w = exp((l_i - M) * (1 / T)), counted as the integer floor(w * 2^40): sums of
+ * weights are exact, whatever their order, so a draw does not depend on how the
+ * row was divided.  The tokens are ordered by falling logit, equal ones by
+ * index; of that order min_p, then top_k, then top_p (a share of what is left)
+ * keep a prefix of mass Z, and the draw is its first token whose cumulative
+ * mass exceeds min(floor(u Z), Z - 1).
+ *   logits   device [rows, vocab] of dtype, row stride ld elements; NaN counts
+ *            as -inf.  Rows need no alignment beyond the element's.
+ *   u        device fp32 [rows], in [0, 1) (others are clamped, NaN is 0)
+ *   token    device int32 [rows]; -1 where every logit is -inf
+ *   logprob  device fp32 [rows] or NULL: ln of the token's share of Z
+ *   kept     device int32 [rows] or NULL: tokens in the prefix
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (vocab > 262,144),
+ * GS_ERR_CUDA. */
+int gs_sample(const void *logits, int64_t ld, int rows, int vocab, int dtype,
+              const gs_sample_params *params, const float *u, int32_t *token, float *logprob,
+              int32_t *kept, void *stream);
+
+/* Copy n pages in every layer: page dst_ids[i] of dst becomes page src_ids[i]
+ * of src, in one launch.  Both pools are [n_layers][pages][page_bytes] and may
+ * be the same one; no page may be a destination twice, or a source and a
+ * destination of one pool.
+ *   page_bytes  a multiple of 16; src, dst 16-byte aligned
+ *   src_ids, dst_ids  device int32 [n] (an index out of range: nothing is
+ *               copied for it and *err is raised)
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (n_layers > 65535),
+ * GS_ERR_CUDA. */
+int gs_pages_copy(const void *src, int src_pages, void *dst, int dst_pages, int n_layers,
+                  int64_t page_bytes, const int32_t *src_ids, const int32_t *dst_ids, int n,
+                  int32_t *err, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

@@ -1,0 +1,68 @@
+// pages.cu -- gs_pages_copy: whole pages of a paged cache copied in every
+// layer by one launch (forks of a sequence, moves that close a pool's gaps).
+//
+// A page of one layer is contiguous, so the copy is a streaming one: the floor
+// is each distinct source read once and each destination written once.  A
+// block moves one 16 KB piece of one page of one layer: 256 threads, four
+// independent 16-byte loads each before the first store, which keeps 32 KB or
+// more in flight on every SM with two resident blocks; HBM is what bounds it.
+#include "internal.h"
+#include "step_common.cuh"
+
+namespace gs {
+namespace {
+
+constexpr int kCopyThreads = 256;
+constexpr int kCopyUnroll = 4;
+constexpr int kCopyVecs = kCopyThreads * kCopyUnroll;   // 16-byte vectors per block
+
+__global__ void __launch_bounds__(kCopyThreads)
+pages_copy_kernel(const uint4* src, int src_pages, uint4* dst, int dst_pages, int page_vecs,
+                  const int32_t* src_ids, const int32_t* dst_ids, int* err) {
+  const int i = blockIdx.y;
+  const int s = src_ids[i], d = dst_ids[i];
+  if (s < 0 || s >= src_pages || d < 0 || d >= dst_pages) {
+    if (threadIdx.x == 0 && blockIdx.x == 0) atomicExch(err, kErrBounds);
+    return;
+  }
+  const uint4* from = src + (static_cast<int64_t>(blockIdx.z) * src_pages + s) * page_vecs;
+  uint4* to = dst + (static_cast<int64_t>(blockIdx.z) * dst_pages + d) * page_vecs;
+  const int v0 = blockIdx.x * kCopyVecs + threadIdx.x;
+  uint4 r[kCopyUnroll];
+#pragma unroll
+  for (int u = 0; u < kCopyUnroll; ++u) {
+    const int v = v0 + u * kCopyThreads;
+    if (v < page_vecs) r[u] = from[v];
+  }
+#pragma unroll
+  for (int u = 0; u < kCopyUnroll; ++u) {
+    const int v = v0 + u * kCopyThreads;
+    if (v < page_vecs) to[v] = r[u];
+  }
+}
+
+}  // namespace
+}  // namespace gs
+
+extern "C" int gs_pages_copy(const void* src, int src_pages, void* dst, int dst_pages, int n_layers,
+                             int64_t page_bytes, const int32_t* src_ids, const int32_t* dst_ids,
+                             int n, int32_t* err, void* stream) {
+  using namespace gs;
+  if (!src || !dst || !src_ids || !dst_ids || !err || src_pages < 1 || dst_pages < 1 ||
+      n_layers < 1 || n < 0 || page_bytes < 16 || page_bytes % 16)
+    return GS_ERR_INVALID_ARG;
+  if (!aligned16(src) || !aligned16(dst)) return GS_ERR_INVALID_ARG;
+  // the grid holds a layer and a page per index
+  if (n_layers > 65535 || page_bytes > (1ll << 30)) return GS_ERR_UNSUPPORTED;
+  const int page_vecs = static_cast<int>(page_bytes / 16);
+  const int pieces = (page_vecs + kCopyVecs - 1) / kCopyVecs;
+  for (int at = 0; at < n; at += 65535) {
+    const int m = n - at < 65535 ? n - at : 65535;
+    pages_copy_kernel<<<dim3(pieces, m, n_layers), kCopyThreads, 0,
+                        static_cast<cudaStream_t>(stream)>>>(
+        static_cast<const uint4*>(src), src_pages, static_cast<uint4*>(dst), dst_pages, page_vecs,
+        src_ids + at, dst_ids + at, err);
+    if (cudaGetLastError() != cudaSuccess) return GS_ERR_CUDA;
+  }
+  return GS_OK;
+}

@@ -24,6 +24,9 @@ GS_ACCEPT_GREEDY = 0
 GS_ACCEPT_STOCHASTIC = 1
 EPI_STORE_F16, EPI_RESID_F32, EPI_SWIGLU, EPI_ARGMAX = 0, 1, 2, 3
 ATTN_DRAFT, ATTN_VERIFY = 0, 1
+GS_F16, GS_BF16, GS_F32 = 0, 1, 2
+ROPE_HALF, ROPE_INTERLEAVED = 0, 1
+ROPE_PLAIN, ROPE_LINEAR, ROPE_NTK, ROPE_YARN = 0, 1, 2, 3
 KIND_NAMES = ("window", "embed", "qkv", "attention", "o_proj", "gate_up", "down", "lm_head",
               "accept")
 
@@ -65,11 +68,33 @@ class gs_debug(ctypes.Structure):
                 ("verify_logits", ctypes.c_void_p)]
 
 
+class gs_cache(ctypes.Structure):
+    _fields_ = [("kv", ctypes.c_void_p)] + [
+        (n, ctypes.c_int) for n in ("n_pages", "n_kv_heads", "head_dim", "dtype")] + [
+        ("page_table", ctypes.c_void_p), ("n_seq", ctypes.c_int), ("pt_stride", ctypes.c_int)]
+
+
+class gs_rope(ctypes.Structure):
+    _fields_ = [("table", ctypes.c_void_p), ("table_rows", ctypes.c_int),
+                ("rotary_dim", ctypes.c_int), ("layout", ctypes.c_int)]
+
+
+class gs_rope_scaling(ctypes.Structure):
+    _fields_ = [("kind", ctypes.c_int), ("theta", ctypes.c_float), ("factor", ctypes.c_float),
+                ("original_ctx", ctypes.c_int), ("beta_fast", ctypes.c_float),
+                ("beta_slow", ctypes.c_float), ("magnitude", ctypes.c_float)]
+
+
+class gs_sample_params(ctypes.Structure):
+    _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_p", "min_p", "top_k")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libgs.so not built at {LIB_PATH}; run __graft_entry__.build()")
     lib = ctypes.CDLL(LIB_PATH)
     vp, i32, sz = ctypes.c_void_p, ctypes.c_int, ctypes.c_size_t
+    i64 = ctypes.c_int64
     sig = {
         "gs_workspace_bytes": (sz, [ctypes.POINTER(gs_config)]),
         "gs_create": (i32, [ctypes.POINTER(gs_config), ctypes.POINTER(gs_weights), vp, sz, vp,
@@ -99,6 +124,15 @@ def _load():
         "gs_linear": (i32, [vp, vp, vp, i32, i32, i32, i32, i32, vp, sz, vp]),
         "gs_linear_noalloc": (i32, [vp, vp, vp, i32, i32, i32, i32, i32, vp]),
         "gs_linear_noalloc_status": (i32, [vp]),
+        "gs_rope_table": (i32, [ctypes.POINTER(gs_rope_scaling), i32, i32, vp, vp]),
+        "gs_rope_append": (i32, [ctypes.POINTER(gs_cache), ctypes.POINTER(gs_rope), vp, i64, i32,
+                                 i32, vp, vp, ctypes.c_float, vp, vp, vp, vp, i64, vp, vp]),
+        "gs_decode_attention_scratch_bytes": (sz, [ctypes.POINTER(gs_cache), i32, i32, i32]),
+        "gs_decode_attention": (i32, [ctypes.POINTER(gs_cache), vp, i64, vp, vp, i32, i32,
+                                      ctypes.c_float, i32, vp, i64, vp, i32, vp, sz, vp]),
+        "gs_sample": (i32, [vp, i64, i32, i32, i32, ctypes.POINTER(gs_sample_params), vp, vp, vp,
+                            vp, vp]),
+        "gs_pages_copy": (i32, [vp, i32, vp, i32, i32, i64, vp, vp, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -112,7 +146,9 @@ EXPORTED = ("gs_workspace_bytes", "gs_create", "gs_destroy", "gs_last_error", "g
             "gs_round", "gs_set_sampling", "gs_diffusion_block", "gs_round_refined", "gs_seq_restore", "gs_round_launches", "gs_round_profile", "gs_seq_state",
             "gs_release", "gs_sync_check", "gs_wait_probe",
             "gs_attention_scratch_bytes", "gs_attention", "gs_linear_scratch_bytes", "gs_linear",
-            "gs_linear_noalloc", "gs_linear_noalloc_status")
+            "gs_linear_noalloc", "gs_linear_noalloc_status", "gs_rope_table", "gs_rope_append",
+            "gs_decode_attention_scratch_bytes", "gs_decode_attention", "gs_sample",
+            "gs_pages_copy")
 
 
 def lib():
@@ -260,3 +296,57 @@ def gs_linear_noalloc(x_ptr, w_ptr, y_ptr, M, N, K, epilogue, split_k, stream_pt
 def gs_linear_noalloc_status(stream_ptr) -> int:
     """GS_OK or the kernel-side failure code of the last gs_linear_noalloc (synchronises)."""
     return int(_lib.gs_linear_noalloc_status(stream_ptr))
+
+
+# ------------------------------------------------------------------ the sampled single-token step
+# Pointers may be 0 where include/gs.h lets them be NULL.  Descriptors (gs_cache,
+# gs_rope, gs_sample_params) are made once and passed to every call.
+def gs_rope_table(scaling: gs_rope_scaling, rotary_dim: int, rows: int, table_ptr: int,
+                  stream_ptr: int) -> None:
+    """Fill an fp32 [rows, rotary_dim / 2, 2] table of cos and sin."""
+    rc = _lib.gs_rope_table(scaling, rotary_dim, rows, table_ptr, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_rope_table")
+
+
+def gs_rope_append(cache: gs_cache, rope: gs_rope, qkv_ptr, ld_qkv, T, n_heads, q_gain_ptr,
+                   k_gain_ptr, eps, seq_ptr, slot_ptr, pos_ptr, q_out_ptr, ld_q, err_ptr,
+                   stream_ptr) -> None:
+    """Norm and rotate T tokens' query and key heads, write keys and values to their pages."""
+    rc = _lib.gs_rope_append(cache, rope, qkv_ptr, ld_qkv, T, n_heads, q_gain_ptr, k_gain_ptr, eps,
+                             seq_ptr, slot_ptr, pos_ptr, q_out_ptr, ld_q, err_ptr, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_rope_append")
+
+
+def gs_decode_attention_scratch_bytes(cache: gs_cache, rows, n_heads, split_pages) -> int:
+    return int(_lib.gs_decode_attention_scratch_bytes(cache, rows, n_heads, split_pages))
+
+
+def gs_decode_attention(cache: gs_cache, q_ptr, ld_q, seq_ptr, n_ptr, rows, n_heads, scale, window,
+                        out_ptr, ld_out, lse_ptr, split_pages, scratch_ptr, scratch_bytes,
+                        stream_ptr) -> None:
+    """Attention of one token per row over its sequence's pages."""
+    rc = _lib.gs_decode_attention(cache, q_ptr, ld_q, seq_ptr, n_ptr, rows, n_heads, scale, window,
+                                  out_ptr, ld_out, lse_ptr, split_pages, scratch_ptr, scratch_bytes,
+                                  stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_decode_attention")
+
+
+def gs_sample(logits_ptr, ld, rows, vocab, dtype, params: gs_sample_params, u_ptr, token_ptr,
+              logprob_ptr, kept_ptr, stream_ptr) -> None:
+    """Draw one token per row under temperature, min-p, top-k and top-p."""
+    rc = _lib.gs_sample(logits_ptr, ld, rows, vocab, dtype, params, u_ptr, token_ptr, logprob_ptr,
+                        kept_ptr, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_sample")
+
+
+def gs_pages_copy(src_ptr, src_pages, dst_ptr, dst_pages, n_layers, page_bytes, src_ids_ptr,
+                  dst_ids_ptr, n, err_ptr, stream_ptr) -> None:
+    """Copy n pages of every layer, src_ids[i] of one pool to dst_ids[i] of another (or the same)."""
+    rc = _lib.gs_pages_copy(src_ptr, src_pages, dst_ptr, dst_pages, n_layers, page_bytes,
+                            src_ids_ptr, dst_ids_ptr, n, err_ptr, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_pages_copy")
