@@ -1,0 +1,233 @@
+"""Several sampled continuations of one prompt, token by token.
+
+A decoder that the round engine does not cover -- RMS-normed query and key
+heads, rotary positions on part of the head, 64 or 128 dims per head -- run
+from the library's operators: projections by ``gs_linear``, heads into the cache
+by ``gs_rope_append``, one-token attention by ``gs_decode_attention``, tokens by
+``gs_sample``.  The prompt is run once; its pages are then shared by all
+continuations (``PagePool.fork``), each of which copies only the page that it
+goes on writing.
+
+    python -m paper_2609_26638_gb300.best_of_n --n 8 --new 32
+"""
+from __future__ import annotations
+
+import argparse
+import dataclasses
+from typing import Dict, List, Optional
+
+import torch
+
+from . import gs
+from .cache import PAGE_TOKENS, PagePool
+
+EPS = 1e-6
+
+
+@dataclasses.dataclass(frozen=True)
+class Shape:
+    """d_model, d_ffn and the projections' widths are multiples of 128, the vocabulary too."""
+    n_layers: int = 2
+    d_model: int = 256
+    n_heads: int = 8
+    n_kv_heads: int = 2
+    head_dim: int = 64
+    d_ffn: int = 512
+    vocab: int = 4096
+    rotary_dim: int = 32
+    rope_layout: int = gs.ROPE_INTERLEAVED
+    rope_theta: float = 10000.0
+
+    @property
+    def qkv_dim(self) -> int:
+        return (self.n_heads + 2 * self.n_kv_heads) * self.head_dim
+
+
+def random_weights(shape: Shape, seed: int = 0, device: str = "cuda:0") -> Dict[str, object]:
+    """fp16 matrices N(0, 0.02 .. 0.05), gains near 1."""
+    g = torch.Generator(device="cpu").manual_seed(seed)
+
+    def mat(rows, cols, std):
+        return (std * torch.randn(rows, cols, generator=g)).half().to(device)
+
+    def gain(n):
+        return (1 + 0.1 * torch.randn(n, generator=g)).bfloat16().to(device)
+
+    s = shape
+    layers = [dict(norm1=gain(s.d_model), qkv=mat(s.qkv_dim, s.d_model, 0.05), q_gain=gain(s.head_dim),
+                   k_gain=gain(s.head_dim), o=mat(s.d_model, s.n_heads * s.head_dim, 0.05),
+                   norm2=gain(s.d_model), gate_up=mat(2 * s.d_ffn, s.d_model, 0.05),
+                   down=mat(s.d_model, s.d_ffn, 0.05)) for _ in range(s.n_layers)]
+    return dict(embed=mat(s.vocab, s.d_model, 1.0), layers=layers, norm=gain(s.d_model),
+                lm_head=mat(s.vocab, s.d_model, 0.1))
+
+
+class StepDecoder:
+    """Feeds tokens of any sequences through the decoder, one call per step.
+
+    ``feed`` takes (sequence, first slot, tokens) runs: a prompt is one long run,
+    a decode step one token per sequence.  Runs of one token go through
+    ``gs_decode_attention`` together; in a longer run the tokens are rows over
+    the same pages, each seeing the keys up to its own."""
+
+    def __init__(self, shape: Shape, weights: Dict[str, object], *, n_pages: int, max_seqs: int,
+                 max_ctx: int, max_rows: int = 512, device: str = "cuda:0"):
+        self.shape, self.w, self.max_rows = shape, weights, max_rows
+        self.device = torch.device(device)
+        self.stream = torch.cuda.Stream(self.device)
+        torch.cuda.synchronize(self.device)
+        self.pool = PagePool(n_layers=shape.n_layers, n_pages=n_pages, n_kv_heads=shape.n_kv_heads,
+                             head_dim=shape.head_dim, dtype=torch.float16, max_seqs=max_seqs,
+                             max_ctx=max_ctx, device=device, stream=self.stream)
+        with torch.cuda.stream(self.stream):
+            self.table = torch.empty(max_ctx, shape.rotary_dim // 2, 2, device=self.device)
+            scaling = gs.gs_rope_scaling(kind=gs.ROPE_PLAIN, theta=shape.rope_theta)
+            gs.gs_rope_table(scaling, shape.rotary_dim, max_ctx, self.table.data_ptr(),
+                             self.stream.cuda_stream)
+            need = max(gs.gs_decode_attention_scratch_bytes(self.pool.layer(0), r, shape.n_heads, 0)
+                       for r in range(1, max_rows + 1))
+            self.attn_scratch = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            wide = max(shape.qkv_dim, shape.d_model, 2 * shape.d_ffn, shape.vocab)
+            need = max(gs.gs_linear_scratch_bytes(r, wide, 1) for r in range(1, max_rows + 1))
+            self.gemm_scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
+        self.rope = gs.gs_rope(self.table.data_ptr(), max_ctx, shape.rotary_dim, shape.rope_layout)
+
+    def _linear(self, x, w, y, n_out: int, epilogue: int) -> None:
+        gs.gs_linear(x.data_ptr(), w.data_ptr(), y.data_ptr(), x.shape[0], n_out, x.shape[1], epilogue,
+                     1, self.gemm_scratch.data_ptr(), self.gemm_scratch.numel(),
+                     self.stream.cuda_stream)
+
+    @staticmethod
+    def _norm(h, gain):
+        return (h * torch.rsqrt(h.square().mean(-1, keepdim=True) + EPS) * gain.float()).half()
+
+    def feed(self, runs) -> torch.Tensor:
+        """fp16 logits [runs, vocab] after the last token of each run."""
+        runs = list(runs)
+        rows = sum(len(t) for _, _, t in runs)
+        if rows > self.max_rows:
+            raise gs.GsError(gs.GS_ERR_INVALID_ARG, "more tokens than max_rows")
+        self.pool.prepare([(s, first, len(t)) for s, first, t in runs])
+        with torch.cuda.stream(self.stream):
+            return self._feed(runs, rows)
+
+    def _feed(self, runs, rows):
+        s, st = self.shape, self.stream.cuda_stream
+        dev = self.device
+
+        def ids(values):
+            return torch.tensor(values, dtype=torch.int32).to(dev)
+        seq = ids([q for q, _, t in runs for _ in t])
+        slot = ids([first + i for _, first, t in runs for i in range(len(t))])
+        n = slot + 1                       # a token sees itself and what lies before it
+        token = torch.cat([torch.as_tensor(t, dtype=torch.int64, device=dev) for _, _, t in runs])
+        h = self.w["embed"][token].float()
+        qkv = torch.empty(rows, s.qkv_dim, dtype=torch.float16, device=dev)
+        out = torch.empty(rows, s.n_heads * s.head_dim, dtype=torch.float16, device=dev)
+        act = torch.empty(rows, s.d_ffn, dtype=torch.float16, device=dev)
+        width = s.n_heads * s.head_dim
+        for i, w in enumerate(self.w["layers"]):
+            cache = self.pool.layer(i)
+            self._linear(self._norm(h, w["norm1"]), w["qkv"], qkv, s.qkv_dim, gs.EPI_STORE_F16)
+            # queries in place: the key and value parts of qkv are read by the same call
+            gs.gs_rope_append(cache, self.rope, qkv.data_ptr(), s.qkv_dim, rows, s.n_heads,
+                              w["q_gain"].data_ptr(), w["k_gain"].data_ptr(), EPS, seq.data_ptr(),
+                              slot.data_ptr(), slot.data_ptr(), qkv.data_ptr(), s.qkv_dim,
+                              self.pool.err.data_ptr(), st)
+            gs.gs_decode_attention(cache, qkv.data_ptr(), s.qkv_dim, seq.data_ptr(), n.data_ptr(), rows,
+                                   s.n_heads, s.head_dim ** -0.5, 0, out.data_ptr(), width, 0, 0,
+                                   self.attn_scratch.data_ptr(), self.attn_scratch.numel(), st)
+            self._linear(out, w["o"], h, s.d_model, gs.EPI_RESID_F32)
+            self._linear(self._norm(h, w["norm2"]), w["gate_up"], act, s.d_ffn, gs.EPI_SWIGLU)
+            self._linear(act, w["down"], h, s.d_model, gs.EPI_RESID_F32)
+        last = torch.tensor([len(t) for _, _, t in runs]).cumsum(0).to(dev) - 1
+        x = self._norm(h[last], self.w["norm"])
+        logits = torch.empty(len(runs), s.vocab, dtype=torch.float16, device=dev)
+        self._linear(x, self.w["lm_head"], logits, s.vocab, gs.EPI_STORE_F16)
+        return logits
+
+    def check(self) -> None:
+        """Synchronise and raise if a kernel met an index out of range."""
+        self.pool.check()
+        word = int(self.attn_scratch[:4].view(torch.int32).item())
+        if word:
+            with torch.cuda.stream(self.stream):
+                self.attn_scratch[:4].zero_()
+            raise gs.GsError(gs.GS_ERR_TIMEOUT if word == 2 else gs.GS_ERR_DEVICE_CHECK,
+                             "gs_decode_attention")
+
+
+class Sampler:
+    """gs_sample with one set of settings for every row."""
+
+    def __init__(self, rows: int, *, temperature: float = 1.0, top_k: int = 0, top_p: float = 1.0,
+                 min_p: float = 0.0, device: str = "cuda:0"):
+        def full(v, dtype=torch.float32):
+            return torch.full((rows,), v, dtype=dtype, device=device)
+        self._t = [full(temperature), full(top_p), full(min_p), full(top_k, torch.int32)]
+        self._p = gs.gs_sample_params(*[t.data_ptr() for t in self._t])
+        self.token = full(0, torch.int32)
+        self.logprob = full(0.0)
+
+    def draw(self, logits: torch.Tensor, u: torch.Tensor, stream) -> None:
+        """token and logprob of each row, from uniforms ``u`` on ``stream``."""
+        gs.gs_sample(logits.data_ptr(), logits.stride(0), logits.shape[0], logits.shape[1], gs.GS_F16,
+                     self._p, u.data_ptr(), self.token.data_ptr(), self.logprob.data_ptr(), 0,
+                     stream.cuda_stream)
+
+
+def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: Optional[torch.Tensor]
+              = None, seed: int = 0, **settings):
+    """n continuations of ``new`` tokens; (tokens [n, new], sum of log-probabilities [n]).
+
+    uniforms: [new, n] fp32 on the decoder's device, or drawn from ``seed``."""
+    dec.stream.wait_stream(torch.cuda.current_stream(dec.device))
+    with torch.cuda.stream(dec.stream):
+        if uniforms is None:
+            g = torch.Generator(device=dec.device).manual_seed(seed)
+            uniforms = torch.rand(new, n, device=dec.device, generator=g)
+        sampler = Sampler(n, device=str(dec.device), **settings)
+        total = torch.zeros(n, device=dec.device)
+        tokens = torch.empty(n, new, dtype=torch.int32, device=dec.device)
+    root = dec.pool.open()
+    step = dec.max_rows
+    for at in range(0, len(prompt), step):
+        logits = dec.feed([(root, at, prompt[at: at + step])])
+    seqs = [root] + dec.pool.fork(root, n - 1)
+    with torch.cuda.stream(dec.stream):
+        logits = logits.expand(n, -1).contiguous()
+    for i in range(new):
+        with torch.cuda.stream(dec.stream):
+            sampler.draw(logits, uniforms[i], dec.stream)
+            tokens[:, i] = sampler.token
+            total += sampler.logprob
+        if i + 1 < new:
+            logits = dec.feed([(q, len(prompt) + i, sampler.token[j: j + 1])
+                               for j, q in enumerate(seqs)])
+    dec.check()
+    for q in seqs:
+        dec.pool.close(q)
+    return tokens, total
+
+
+def main() -> None:
+    ap = argparse.ArgumentParser(description=__doc__, formatter_class=argparse.RawDescriptionHelpFormatter)
+    ap.add_argument("--n", type=int, default=8)
+    ap.add_argument("--new", type=int, default=32)
+    ap.add_argument("--prompt", type=int, default=300)
+    ap.add_argument("--temperature", type=float, default=0.8)
+    ap.add_argument("--top-p", type=float, default=0.95)
+    a = ap.parse_args()
+    shape = Shape()
+    ctx = a.prompt + a.new
+    pages = (a.prompt // PAGE_TOKENS + 1) + a.n * (a.new // PAGE_TOKENS + 2)
+    dec = StepDecoder(shape, random_weights(shape), n_pages=pages, max_seqs=a.n, max_ctx=ctx)
+    prompt = torch.randint(0, shape.vocab, (a.prompt,), generator=torch.Generator().manual_seed(1)).tolist()
+    tokens, logprob = best_of_n(dec, prompt, a.n, a.new, temperature=a.temperature, top_p=a.top_p)
+    best = int(logprob.argmax())
+    print(f"best of {a.n}: continuation {best}, log-probability {float(logprob[best]):.2f}")
+    print(tokens[best].tolist())
+
+
+if __name__ == "__main__":
+    main()
