@@ -61,21 +61,29 @@ struct Span {
   int lo, n, page0, pages;
   const int32_t* table;
 };
+// The row's numbers are read by one lane and broadcast: every lane of a warp
+// goes through the same pages whatever happens to the arrays meanwhile.
 __device__ __forceinline__ Span find_span(const DecodeArgs& a, int row) {
   Span s;
-  int seq = a.seq ? a.seq[row] : row;
-  s.n = a.n[row];
-  bool bad = false;
-  if (seq < 0 || seq >= a.cache.n_seq) {
-    bad = true;
-    seq = 0;
-    s.n = 0;
+  const int lane = threadIdx.x & 31;
+  int seq = 0, n = 0;
+  if (lane == 0) {
+    seq = a.seq ? a.seq[row] : row;
+    n = a.n[row];
+    bool bad = false;
+    if (seq < 0 || seq >= a.cache.n_seq) {
+      bad = true;
+      seq = 0;
+      n = 0;
+    }
+    if (n < 0 || n > a.cache.pt_stride * kPageTokens) {
+      bad = true;
+      n = n < 0 ? 0 : a.cache.pt_stride * kPageTokens;
+    }
+    if (bad) atomicExch(a.err, kErrBounds);
   }
-  if (s.n < 0 || s.n > a.cache.pt_stride * static_cast<int64_t>(kPageTokens)) {
-    bad = true;
-    s.n = s.n < 0 ? 0 : a.cache.pt_stride * kPageTokens;
-  }
-  if (bad) atomicExch(a.err, kErrBounds);
+  seq = __shfl_sync(0xFFFFFFFFu, seq, 0);
+  s.n = __shfl_sync(0xFFFFFFFFu, n, 0);
   s.lo = a.window > 0 && s.n > a.window ? s.n - a.window : 0;
   s.page0 = s.lo / kPageTokens;
   s.pages = (s.n + kPageTokens - 1) / kPageTokens - s.page0;
@@ -141,7 +149,7 @@ struct DecodeShape {
 
 // WIDE: more than 8 query rows (the upper half of the tile is in use).
 template <bool BF16, int D, bool WIDE>
-__global__ void __launch_bounds__(DecodeShape<D>::kThreads)
+__global__ void __launch_bounds__(DecodeShape<D>::kThreads, 2)
 decode_attention_kernel(const DecodeArgs a) {
   using S = DecodeShape<D>;
   extern __shared__ uint8_t smem_raw[];
@@ -189,21 +197,19 @@ decode_attention_kernel(const DecodeArgs a) {
   int ids = 0;
   auto load_ids = [&](int j0) {
     const int j = j0 + lane;
-    if (j < cnt) {
-      ids = sp.table[sp.page0 + p0 + warp + j * S::kWarps];
-      if (ids < 0 || ids >= a.cache.n_pages) {
-        atomicExch(a.err, kErrBounds);
-        ids = 0;
-      }
-    }
+    if (j < cnt) ids = sp.table[sp.page0 + p0 + warp + j * S::kWarps];
   };
   // Block b of the warp's stream: K of page b / 2, then its V^T.
   auto issue = [&](int b) {
     const int j = b >> 1;
     if (j >= cnt) return;
     if (!(b & 1) && !(j & 31)) load_ids(j);
-    const int page = __shfl_sync(0xFFFFFFFFu, ids, j & 31);
+    int page = __shfl_sync(0xFFFFFFFFu, ids, j & 31);
     if (lane == 0) {
+      if (page < 0 || page >= a.cache.n_pages) {
+        atomicExch(a.err, kErrBounds);
+        page = 0;
+      }
       const int st = b % S::kRing;
       // of the last page's keys only the rows that exist
       const int tok = (sp.page0 + p0 + warp + j * S::kWarps) * kPageTokens;

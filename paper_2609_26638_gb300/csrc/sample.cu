@@ -1,28 +1,30 @@
 // sample.cu -- temperature, min-p, top-k and top-p, and the draw of a token
-// from a given uniform number, in one launch and one pass over the logits.
+// from a given uniform number, in one launch.
 //
 //   w_i = exp((l_i - M) / T),  q_i = floor(w_i 2^40),  order: l falling, i rising
 //
 // Every step is a search for the token at which a running total of that order
 // passes a target: top-k in the count, top-p in the mass, the draw in the mass
-// that is left.  No row is sorted for it.  A row's logits stay in the shared
-// memory of a cluster of blocks (a slice each); one pass puts mass and count
-// into 2048 bins of equal width in d = (l - M) / T, which the blocks add up;
-// prefix sums over the bins give the bin in which a target is passed, and only
-// the tokens of that bin (typically 20 to 200) are gathered, ranked by counting
-// and searched.  Where the bins up to it hold few tokens in all, they are
-// gathered together and serve the later searches too.  A bin too full for the
-// list (equal logits, a hot row) is divided further by the bits of the logit.
+// that is left.  No row is sorted for it.  A row is one block's, or, where there
+// are few, a cluster's, a slice each.  The first pass finds the largest logit
+// and, from the maxima of the threads' first logits, a level that about 3500
+// logits of the row exceed, whatever its distribution.  The second (the row is
+// in L2 by then) notes these, the head, in shared memory and adds up the
+// weights of the others.  The head goes into 512 bins of equal width in d = (l - M) / T; the
+// blocks add up their bins; prefix sums over them give the bin in which a
+// target is passed, and only the tokens of that bin are gathered in block 0,
+// ranked by counting and searched.  Where the bins up to it hold few tokens in
+// all, they are gathered together and serve the later searches too.  A target
+// behind the head takes a pass for each 8 nats; a bin too full for the list
+// (equal logits, a hot row) is divided further by the bits of the logit, and a
+// logit too frequent for it by index.
 //
 // Masses are integers of 40 bits, so sums are exact and the result does not
 // depend on the order of atomics, the slices or the cluster.  (A 64-bit add in
 // shared memory is a compare-and-swap loop: the low and the high word are added
 // apart, the high one only when it changes.)
-//
-// Bound: the row is read once; what is left is the exponential and two or three
-// shared-memory adds per logit, which is what the time goes into for many rows,
-// and the chain of cluster barriers for few.
 #include <cmath>
+#include <cstddef>
 
 #include "internal.h"
 #include "step_common.cuh"
@@ -31,9 +33,15 @@ namespace gs {
 namespace {
 
 constexpr int kThreads = 512;
-constexpr int kBins = 2048;                 // four per thread
-constexpr int kList = 512;                  // gathered tokens
-constexpr float kBinsPerNat = 73.f;         // 2^-40 is at 27.73 nats: bin 2024
+constexpr int kBins = kThreads;             // one per thread
+constexpr int kBinBits = 9;
+constexpr float kNats = 8.f;                // of a window behind the head
+constexpr float kBinsPerNat = kBins / kNats;
+constexpr int kWindows = 5;                 // the head, and 32 nats: 2^-40 is at 27.73
+constexpr int kList = 256;                  // gathered tokens
+constexpr int kPrefix = 128;                // of which the order's first ones, kept for later searches
+constexpr int kHead = 4096;                 // head tokens that a block notes
+constexpr double kTarget = 3500.;           // head tokens of a row that the level aims at
 constexpr int kMostVocab = 262144;
 constexpr int kMostCluster = 8;
 
@@ -41,6 +49,7 @@ struct SampleArgs {
   const void* logits;
   int64_t ld;
   int vocab, slice;                         // tokens of a block's slice, a multiple of 16
+  int level_vecs, level_rank;               // of 32 threads' maxima over so many vectors, which sets the level
   const float *temperature, *top_p, *min_p;
   const int32_t* top_k;
   const float* u;
@@ -49,9 +58,9 @@ struct SampleArgs {
   int32_t* kept;
 };
 
-struct Entry {
+struct alignas(16) Entry {
+  unsigned long long mass;
   uint32_t key, idx;
-  unsigned long long mass, before;          // own mass, mass of the list's entries ahead of it
 };
 
 // The place where a running total passed its target: the token, and the totals
@@ -62,23 +71,47 @@ struct Cut {
   unsigned long long mass;
 };
 
+// A row's settings, read once: all blocks of its cluster take the same branches
+// whatever happens to the arrays meanwhile.
+struct Settings {
+  float t, top_p, min_p, u;
+  int top_k;
+};
+
 struct Shared {
-  uint32_t lo[kBins], hi[kBins], cnt[kBins];
   Entry list[kList];
-  uint32_t rank[kList];                     // list entries ahead of each entry
-  int list_n;
-  float block_max;
+  unsigned long long before[kList];         // mass of the list's entries ahead of each
+  uint32_t rank[kList];                     // and their number
+  alignas(16) uint32_t lo[kBins], hi[kBins], cnt[kBins];    // read four at a time
+  unsigned long long head_upto_m[kBins];    // the head's merged bins: totals up to and with each
+  uint32_t head_upto_c[kBins];
+  float2 head[kHead];                       // the slice's logits in the head, and (as bits) their places
+  alignas(16) uint4 edge[2];                            // the slice's first and last vector
   unsigned long long warp_mass[kThreads / 32];
+  // of every block, written by it: the mass and number of its other tokens
+  unsigned long long tail_mass[kMostCluster];
+  uint32_t tail_cnt[kMostCluster];
+  float block_max[kMostCluster], block_level[kMostCluster];
+  unsigned long long own_tail_mass;
+  uint32_t own_tail_cnt;
   uint32_t warp_cnt[kThreads / 32];
-  float warp_max[kThreads / 32];
+  float warp_max[kThreads / 32], warp_level[kThreads / 32];
+  int head_n;                               // may pass kHead: then the list is not used
+  int list_n;
   int best;                                 // lowest index of the largest logit
   // the crossing bin of a search: totals ahead of it, and its count
   int bin;
-  unsigned long long bin_mass;
   uint32_t bin_before, bin_cnt;
+  unsigned long long bin_mass;
   uint32_t tie_cnt;                         // tokens of the crossing key in this block's slice
-  Cut cut;
+  Settings set;
+  Cut cut[3];                               // of each search
 };
+
+static_assert(offsetof(Shared, lo) % 16 == 0 && offsetof(Shared, hi) % 16 == 0 &&
+                  offsetof(Shared, cnt) % 16 == 0 && offsetof(Shared, edge) % 16 == 0 &&
+                  sizeof(Entry) == 16 && offsetof(Shared, list) % 16 == 0,
+              "read as vectors");
 
 __device__ __forceinline__ uint32_t cluster_rank() {
   uint32_t r;
@@ -103,15 +136,73 @@ __device__ __forceinline__ void cluster_barrier() {
   cluster_sync_all();
 }
 
-// What a row's logits are measured with.
-struct Scale {
-  float top, inv_t;
-  // d = (l - M) / T, the same two roundings everywhere
-  __device__ __forceinline__ float d(float x) const {
-    return x == top ? 0.f : __fmul_rn(__fsub_rn(x, top), inv_t);
+template <int TYPE> struct Elem;             // GS_F16, GS_BF16, GS_F32
+template <> struct Elem<GS_F16> { static constexpr int kBytes = 2, kVec = 8; };
+template <> struct Elem<GS_BF16> { static constexpr int kBytes = 2, kVec = 8; };
+template <> struct Elem<GS_F32> { static constexpr int kBytes = 4, kVec = 4; };
+
+template <int TYPE>
+__device__ __forceinline__ float load_logit(const void* p, int64_t i) {
+  if constexpr (TYPE == GS_F32)
+    return static_cast<const float*>(p)[i];
+  else if constexpr (TYPE == GS_F16)
+    return __half2float(static_cast<const __half*>(p)[i]);
+  else
+    return __bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]);
+}
+
+template <int TYPE>
+__device__ __forceinline__ void unpack(const uint4& v, float (&x)[Elem<TYPE>::kVec]) {
+  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
+#pragma unroll
+  for (int i = 0; i < 4; ++i) {
+    if constexpr (TYPE == GS_F32) {
+      x[i] = __uint_as_float(w[i]);
+    } else {
+      const float2 f = unpack2<TYPE == GS_BF16>(w[i]);
+      x[2 * i] = f.x;
+      x[2 * i + 1] = f.y;
+    }
   }
-  __device__ __forceinline__ static float weight(float x, float d) {
-    return x == -INFINITY ? 0.f : expf(d);
+}
+
+// Elementwise maximum of packed logits (a NaN gives the other operand).
+template <int TYPE>
+__device__ __forceinline__ uint32_t max_packed(uint32_t a, uint32_t b) {
+  uint32_t r;
+  if constexpr (TYPE == GS_F32) {
+    r = __float_as_uint(fmaxf(__uint_as_float(a), __uint_as_float(b)));
+  } else if constexpr (TYPE == GS_F16) {
+    asm("max.f16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  } else {
+    asm("max.bf16x2 %0, %1, %2;" : "=r"(r) : "r"(a), "r"(b));
+  }
+  return r;
+}
+// The larger half of a packed pair.
+template <int TYPE>
+__device__ __forceinline__ float widest(uint32_t v) {
+  if constexpr (TYPE == GS_F32) {
+    return __uint_as_float(v);
+  } else {
+    const float2 f = unpack2<TYPE == GS_BF16>(v);
+    return fmaxf(f.x, f.y);
+  }
+}
+template <int TYPE>
+constexpr uint32_t kEmpty = TYPE == GS_F32 ? 0xFF800000u : (TYPE == GS_BF16 ? 0xFF80FF80u : 0xFC00FC00u);
+
+// What a row's logits are weighed with.  1 / T is kept within fp32's normal
+// range, so that a logit of -inf is at d = -inf for every T.
+struct Scale {
+  float top, inv_t, min_p;
+  float edge, per_nat;       // the head: d >= edge, and its bins
+  // d = (l - M) / T, the same two roundings everywhere
+  __device__ __forceinline__ float d(float x) const { return __fmul_rn(__fsub_rn(x, top), inv_t); }
+  // the weight, 0 if min-p drops it
+  __device__ __forceinline__ float weight(float d) const {
+    const float w = expf(d);
+    return w >= min_p ? w : 0.f;
   }
   // floor(w 2^40) from the bits of w (0 <= w <= 1)
   __device__ __forceinline__ static unsigned long long mass(float w) {
@@ -121,50 +212,38 @@ struct Scale {
     if (s < 0) return s < -23 ? 0ull : m >> -s;
     return static_cast<unsigned long long>(m) << s;
   }
-  // bins rise as the logit falls; rounded by adding 1.5 * 2^23
-  __device__ __forceinline__ static int bin(float d) {
-    const float y = fminf(-d * kBinsPerNat, static_cast<float>(kBins - 1));
-    return static_cast<int>(__float_as_uint(y + 12582912.f) & 0xFFFFu);
+  // The windows: 0 is the head, w >= 1 the w-th 8 nats behind it.
+  __device__ __forceinline__ float end_of(int w) const { return fmaf(-kNats, w, edge); }
+  __device__ __forceinline__ bool in(int w, float d) const {
+    return d >= end_of(w) && (w == 0 || d < end_of(w - 1));
   }
+  // bins rise as the logit falls; rounded by adding 1.5 * 2^23
+  __device__ __forceinline__ int bin(int w, float d) const {
+    const float y = w == 0 ? -d * per_nat : (end_of(w - 1) - d) * kBinsPerNat;
+    return static_cast<int>(
+        __float_as_uint(fminf(fmaxf(y, 0.f), static_cast<float>(kBins - 1)) + 12582912.f) & 0xFFFFu);
+  }
+  __device__ __forceinline__ static uint32_t key(float x) { return float_order_key(x + 0.f); }
 };
 
-template <int TYPE> struct Elem;             // GS_F16, GS_BF16, GS_F32
-template <> struct Elem<GS_F16> { static constexpr int kBytes = 2, kVec = 8; };
-template <> struct Elem<GS_BF16> { static constexpr int kBytes = 2, kVec = 8; };
-template <> struct Elem<GS_F32> { static constexpr int kBytes = 4, kVec = 4; };
-
-// A logit as it counts: NaN is -inf, -0 is 0.
-__device__ __forceinline__ float as_logit(float x) { return x != x ? -INFINITY : x + 0.f; }
-
-template <int TYPE>
-__device__ __forceinline__ float load_logit(const void* p, int64_t i) {
-  if constexpr (TYPE == GS_F32)
-    return as_logit(static_cast<const float*>(p)[i]);
-  else if constexpr (TYPE == GS_F16)
-    return as_logit(__half2float(static_cast<const __half*>(p)[i]));
-  else
-    return as_logit(__bfloat162float(static_cast<const __nv_bfloat16*>(p)[i]));
-}
-
-template <int TYPE>
-__device__ __forceinline__ void unpack(const uint4& v, float (&x)[Elem<TYPE>::kVec]) {
-  const uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    if constexpr (TYPE == GS_F32) {
-      x[i] = as_logit(__uint_as_float(w[i]));
-    } else {
-      const float2 f = unpack2<TYPE == GS_BF16>(w[i]);
-      x[2 * i] = as_logit(f.x);
-      x[2 * i + 1] = as_logit(f.y);
-    }
+// floor(p Z) for 0 <= p <= 1, exactly; `whole` if nothing is cut off.  (In
+// integers: this GPU's 64-bit floating-point units are few, and a block's 16
+// warps would queue for them.)
+__device__ __forceinline__ unsigned long long share_of(float p, unsigned long long z, bool& whole) {
+  const uint32_t u = __float_as_uint(p), e = u >> 23;
+  if (e < 23) {              // below 2^-104: p Z < 1
+    whole = p == 0.f;
+    return 0;
   }
-}
-
-template <int TYPE>
-__device__ __forceinline__ uint4 all_empty() {   // a vector of -inf
-  const uint32_t w = TYPE == GS_F32 ? 0xFF800000u : (TYPE == GS_BF16 ? 0xFF80FF80u : 0xFC00FC00u);
-  return make_uint4(w, w, w, w);
+  const unsigned long long m = (u & 0x7FFFFFu) | 0x800000u;
+  const int s = 150 - static_cast<int>(e);      // p = m 2^-s, 23 <= s <= 127
+  const unsigned long long lo = z * m, hi = __umul64hi(z, m);
+  if (s < 64) {
+    whole = lo << (64 - s) == 0;
+    return hi << (64 - s) | lo >> s;
+  }
+  whole = lo == 0 && (s == 64 || hi << (128 - s) == 0);
+  return hi >> (s - 64);
 }
 
 // Inclusive prefix sum over the block's threads of (mass, count); totals too.
@@ -203,101 +282,84 @@ __device__ __forceinline__ void block_scan(Shared& sh, unsigned long long& m, ui
   c += before_c;
 }
 
-// A histogram of the whole row, four bins to a thread: exclusive totals ahead
-// of the thread's first bin, and the bins.
-struct Histogram {
-  unsigned long long before_m, m[4];
-  uint32_t before_c, c[4];
+// The whole row's bins, one to a thread: totals up to and with it, and its own.
+struct Bins {
+  unsigned long long upto_m, m, total_m;
+  uint32_t upto_c, c, total_c;
 };
 
-// Adds up the cluster's bins (every block gets all of them).
-__device__ void merge_bins(Shared& sh, Histogram& h, unsigned long long& total_m, uint32_t& total_c) {
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    h.m[i] = 0;
-    h.c[i] = 0;
-  }
+// Adds up the cluster's bins (every block gets all of them).  Not inlined, like
+// the searches' rarer parts: a block goes through most of this code once, and
+// the fewer instructions there are to fetch, the sooner it is through.
+__device__ __noinline__ Bins merge_bins(Shared& sh) {
+  Bins h;
   const uint32_t n = cluster_size();
-  for (uint32_t r = 0; r < n; ++r) {
-    const Shared* p = peer(&sh, r);
-    const uint4 lo = reinterpret_cast<const uint4*>(p->lo)[threadIdx.x];
-    const uint4 hi = reinterpret_cast<const uint4*>(p->hi)[threadIdx.x];
-    const uint4 c = reinterpret_cast<const uint4*>(p->cnt)[threadIdx.x];
-    const uint32_t l4[4] = {lo.x, lo.y, lo.z, lo.w}, h4[4] = {hi.x, hi.y, hi.z, hi.w},
-                   c4[4] = {c.x, c.y, c.z, c.w};
+  unsigned long long m = 0;
+  uint32_t c = 0;
+  if (n == 1) {
+    __syncthreads();
+    m = (static_cast<unsigned long long>(sh.hi[threadIdx.x]) << 32) + sh.lo[threadIdx.x];
+    c = sh.cnt[threadIdx.x];
+  } else {
+    // Four neighbouring threads take the same four bins, 16 bytes a load, of
+    // every fourth peer, and exchange sums: one round trip through the cluster.
+    const int quad = threadIdx.x / 4, part = threadIdx.x % 4;
+    unsigned long long ms[4] = {};
+    uint32_t cs[4] = {};
+#pragma unroll
+    for (int k = 0; k < kMostCluster / 4; ++k) {
+      const uint32_t p = part + 4 * k;
+      if (p >= n) continue;
+      const Shared* from = peer(&sh, p);
+      const uint4 lo = reinterpret_cast<const uint4*>(from->lo)[quad];
+      const uint4 hi = reinterpret_cast<const uint4*>(from->hi)[quad];
+      const uint4 cn = reinterpret_cast<const uint4*>(from->cnt)[quad];
+      const uint32_t l[4] = {lo.x, lo.y, lo.z, lo.w}, u[4] = {hi.x, hi.y, hi.z, hi.w},
+                     w[4] = {cn.x, cn.y, cn.z, cn.w};
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        ms[i] += (static_cast<unsigned long long>(u[i]) << 32) + l[i];
+        cs[i] += w[i];
+      }
+    }
+    __syncwarp();
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      h.m[i] += (static_cast<unsigned long long>(h4[i]) << 32) + l4[i];
-      h.c[i] += c4[i];
+#pragma unroll
+      for (int s = 1; s < 4; s *= 2) {
+        ms[i] += __shfl_xor_sync(0xFFFFFFFFu, ms[i], s);
+        cs[i] += __shfl_xor_sync(0xFFFFFFFFu, cs[i], s);
+      }
+      if (i == part) {
+        m = ms[i];
+        c = cs[i];
+      }
     }
   }
-  unsigned long long m = h.m[0] + h.m[1] + h.m[2] + h.m[3];
-  uint32_t c = h.c[0] + h.c[1] + h.c[2] + h.c[3];
-  const unsigned long long own_m = m;
-  const uint32_t own_c = c;
-  block_scan(sh, m, c, total_m, total_c);
-  h.before_m = m - own_m;
-  h.before_c = c - own_c;
+  h.m = m;
+  h.c = c;
+  block_scan(sh, m, c, h.total_m, h.total_c);
+  h.upto_m = m;
+  h.upto_c = c;
+  return h;
 }
 
 // The bin in which base + running total passes `target` (in the count or the
-// mass): the first with a total above it.  Writes sh.bin, bin_mass, ...
-__device__ void find_bin(Shared& sh, const Histogram& h, bool by_count, unsigned long long target,
-                         unsigned long long base_m, uint32_t base_c) {
-  unsigned long long m = base_m + h.before_m;
-  uint32_t c = base_c + h.before_c;
-#pragma unroll
-  for (int i = 0; i < 4; ++i) {
-    const bool before = (by_count ? c : m) <= target;
-    const bool after = (by_count ? c + h.c[i] : m + h.m[i]) > target;
-    if (before && after) {
-      sh.bin = static_cast<int>(threadIdx.x) * 4 + i;
-      sh.bin_mass = m;
-      sh.bin_before = c;
-      sh.bin_cnt = h.c[i];
-    }
-    m += h.m[i];
-    c += h.c[i];
+// mass).  Writes sh.bin, bin_mass, bin_before, bin_cnt.
+__device__ __forceinline__ void find_bin(Shared& sh, const Bins& h, bool by_count,
+                                         unsigned long long target, unsigned long long base_m,
+                                         uint32_t base_c) {
+  const unsigned long long m = base_m + h.upto_m - h.m;
+  const uint32_t c = base_c + h.upto_c - h.c;
+  __syncthreads();           // the last search's numbers have been read
+  if (by_count ? c <= target && c + h.c > target : m <= target && m + h.m > target) {
+    sh.bin = static_cast<int>(threadIdx.x);
+    sh.bin_mass = m;
+    sh.bin_before = c;
+    sh.bin_cnt = h.c;
   }
   __syncthreads();
 }
-
-template <int TYPE>
-struct Row {
-  static constexpr int V = Elem<TYPE>::kVec;
-  const uint4* vecs;      // the slice in shared memory, padded with -inf to whole vectors
-  int n_vecs;
-  int first;              // index in the row of the first vector's first element
-  Scale sc;
-  float min_p;
-
-  // f(x, index) for every logit of the slice, vectors dealt to the threads in turn
-  template <class F>
-  __device__ __forceinline__ void each(F f) const {
-    for (int v = threadIdx.x; v < n_vecs; v += kThreads) {
-      float x[V];
-      unpack<TYPE>(vecs[v], x);
-#pragma unroll
-      for (int e = 0; e < V; ++e) f(x[e], first + v * V + e);
-    }
-  }
-  // the same, a run of neighbouring vectors to each thread, in index order
-  template <class F>
-  __device__ __forceinline__ void each_in_order(F f) const {
-    const int per = (n_vecs + kThreads - 1) / kThreads, v0 = threadIdx.x * per;
-    for (int v = v0; v < min(n_vecs, v0 + per); ++v) {
-      float x[V];
-      unpack<TYPE>(vecs[v], x);
-#pragma unroll
-      for (int e = 0; e < V; ++e) f(x[e], first + v * V + e);
-    }
-  }
-  // mass of a logit, 0 if min-p drops it
-  __device__ __forceinline__ unsigned long long mass(float x, float d) const {
-    const float w = Scale::weight(x, d);
-    return w >= min_p ? Scale::mass(w) : 0ull;
-  }
-};
 
 __device__ __forceinline__ void add_to_bin(Shared& sh, int b, unsigned long long m) {
   const uint32_t lo = static_cast<uint32_t>(m);
@@ -308,301 +370,624 @@ __device__ __forceinline__ void add_to_bin(Shared& sh, int b, unsigned long long
 }
 
 __device__ __forceinline__ void clear_bins(Shared& sh) {
-  const uint4 z = make_uint4(0, 0, 0, 0);
-  reinterpret_cast<uint4*>(sh.lo)[threadIdx.x] = z;
-  reinterpret_cast<uint4*>(sh.hi)[threadIdx.x] = z;
-  reinterpret_cast<uint4*>(sh.cnt)[threadIdx.x] = z;
+  sh.lo[threadIdx.x] = 0;
+  sh.hi[threadIdx.x] = 0;
+  sh.cnt[threadIdx.x] = 0;
 }
 
-// Tokens that a search still has in view: of bins first_bin .. bin, those with
-// a key in [key_lo, key_hi].
+// Tokens that a search still has in view: of a window's bins first .. last,
+// those with a key in [key_lo, key_hi].
 struct View {
-  int first_bin, bin;
+  int window, first, last;
   uint32_t key_lo, key_hi;
-  __device__ __forceinline__ bool has(int b, uint32_t key) const {
-    return b >= first_bin && b <= bin && key >= key_lo && key <= key_hi;
-  }
 };
 
-// Gathers the view's tokens in block 0's list.
+// A block's slice of a row, as aligned vectors.  What the first and the last
+// vector hold of other slices, or of beyond the row, counts as -inf: these two
+// are in shared memory, the others are read where they are.
 template <int TYPE>
-__device__ void gather(Shared& sh, const Row<TYPE>& row, const View& view) {
-  Shared* home = peer(&sh, 0);
-  // a logit whose d is this far below is in no bin of the view (half a bin of slack)
-  const float least = -(static_cast<float>(view.bin) + 1.f) / kBinsPerNat;
-  row.each([&](float x, int i) {
-    const float d = row.sc.d(x);
-    if (d < least) return;
-    const uint32_t key = float_order_key(x);
-    if (!view.has(Scale::bin(d), key)) return;
-    const unsigned long long m = row.mass(x, d);
-    if (m == 0) return;
-    const int at = atomicAdd(&home->list_n, 1);
-    if (at < kList) {
-      Entry e;
-      e.key = key;
-      e.idx = static_cast<uint32_t>(i);
-      e.mass = m;
-      e.before = 0;
-      home->list[at] = e;
-    }
-  });
-  cluster_barrier();
-}
+struct Slice {
+  static constexpr int V = Elem<TYPE>::kVec;
+  const uint4* vecs;
+  const uint4* edge;
+  int n_vecs, v0, v1;     // vectors v0 .. v1 - 1 are whole
+  int first;              // index in the row of the first vector's first element
+  Scale sc;
 
-// Block 0: each entry's rank, and the mass ahead of it, by counting.
-__device__ void rank_list(Shared& sh) {
-  const int n = sh.list_n;
-  for (int e = threadIdx.x; e < n; e += kThreads) {
-    const uint32_t key = sh.list[e].key, idx = sh.list[e].idx;
-    unsigned long long before = 0;
-    uint32_t rank = 0;
-    for (int k = 0; k < n; ++k) {
-      const Entry& o = sh.list[k];
-      if (o.key > key || (o.key == key && o.idx < idx)) {
-        before += o.mass;
-        ++rank;
+  __device__ __forceinline__ uint4 load(int v) const {
+    const uint4* p = v >= v0 && v < v1 ? vecs + v : edge + (v == 0 ? 0 : 1);
+    return *p;
+  }
+  // NaN as -inf
+  __device__ __forceinline__ static uint4 no_nan(uint4 x) {
+    x.x = max_packed<TYPE>(x.x, kEmpty<TYPE>);
+    x.y = max_packed<TYPE>(x.y, kEmpty<TYPE>);
+    x.z = max_packed<TYPE>(x.z, kEmpty<TYPE>);
+    x.w = max_packed<TYPE>(x.w, kEmpty<TYPE>);
+    return x;
+  }
+  // f(vector's first element, its logits), vectors dealt to the threads in
+  // turn; the next two are on their way meanwhile
+  template <class F>
+  __device__ __forceinline__ void each_vec(F f) const {
+    int v = threadIdx.x;
+    uint4 q0 = {}, q1 = {};
+    if (v < n_vecs) q0 = load(v);
+    if (v + kThreads < n_vecs) q1 = load(v + kThreads);
+#pragma unroll 1
+    for (; v < n_vecs; v += kThreads) {
+      uint4 q2 = {};
+      if (v + 2 * kThreads < n_vecs) q2 = load(v + 2 * kThreads);
+      float x[V];
+      unpack<TYPE>(no_nan(q0), x);
+      f(v * V, x);
+      q0 = q1;
+      q1 = q2;
+    }
+  }
+  // a logit by its place, which is one of the slice's own
+  __device__ __forceinline__ float at(int i) const {
+    const float x = load_logit<TYPE>(vecs, i);
+    return x == x ? x : -INFINITY;
+  }
+  // f(x, d, element) for the logits with d in [least, most): few of them, so a
+  // vector's are marked first and then taken one by one, and a warp goes
+  // through f as often as its fullest lane, not once per element.
+  template <class F>
+  __device__ __forceinline__ void each_within(float least, float most, F f) const {
+    each_vec([&](int i, const float (&x)[V]) {
+      uint32_t marked = 0;
+#pragma unroll
+      for (int e = 0; e < V; ++e) {
+        const float d = sc.d(x[e]);
+        if (d >= least && d < most) marked |= 1u << e;
       }
+      while (marked) {
+        const int k = i + __ffs(marked) - 1;
+        marked &= marked - 1;
+        const float y = at(k);
+        f(y, sc.d(y), k);
+      }
+    });
+  }
+  // f(key, mass, element) for the tokens of a view that have a weight
+  template <class F>
+  __device__ __forceinline__ void each_in(const Shared& sh, const View& view, F f) const {
+    auto take = [&](float x, float d, int i) {
+      if (!sc.in(view.window, d)) return;
+      const int b = sc.bin(view.window, d);
+      const uint32_t key = Scale::key(x);
+      if (b < view.first || b > view.last || key < view.key_lo || key > view.key_hi) return;
+      const unsigned long long m = Scale::mass(sc.weight(d));
+      if (m) f(key, m, i);
+    };
+    if (view.window == 0 && sh.head_n <= kHead) {
+      for (int k = threadIdx.x; k < sh.head_n; k += kThreads) {
+        const float2 h = sh.head[k];
+        take(h.x, sc.d(h.x), __float_as_int(h.y));
+      }
+    } else {
+      // half a bin and more on either side; the bin itself decides
+      const float from = view.window == 0 ? 0.f : sc.end_of(view.window - 1);
+      const float width = view.window == 0 ? 1.f / sc.per_nat : 1.f / kBinsPerNat;
+      const float least = from - (static_cast<float>(view.last) + 1.f) * width;
+      const float most =
+          view.first == 0 ? INFINITY : from - (static_cast<float>(view.first) - 1.f) * width;
+      each_within(view.last == kBins - 1 ? sc.end_of(view.window) : least, most, take);
     }
-    sh.list[e].before = before;
-    sh.rank[e] = rank;
   }
-  __syncthreads();
-}
-
-// Block 0: the list's entry at which the total passes the target.
-__device__ void cut_list(Shared& sh, bool by_count, unsigned long long target,
-                         unsigned long long base_m, uint32_t base_c) {
-  for (int e = threadIdx.x; e < sh.list_n; e += kThreads) {
-    const unsigned long long m = base_m + sh.list[e].before, own = sh.list[e].mass;
-    const uint32_t c = base_c + sh.rank[e];
-    const bool here = by_count ? c == target : m <= target && target < m + own;
-    if (here) sh.cut = {sh.list[e].idx, c + 1, m + own};
+  // f(element) for the tokens of this key in the thread's run of neighbouring
+  // vectors, in index order
+  template <class F>
+  __device__ __forceinline__ void each_tie(uint32_t key, F f) const {
+    const int per = (n_vecs + kThreads - 1) / kThreads, begin = threadIdx.x * per;
+#pragma unroll 1
+    for (int v = begin; v < min(n_vecs, begin + per); ++v) {
+      float x[V];
+      unpack<TYPE>(no_nan(load(v)), x);
+#pragma unroll
+      for (int e = 0; e < V; ++e)
+        if (Scale::key(x[e]) == key) f(v * V + e);
+    }
   }
-  __syncthreads();
-}
+};
 
 // One row's searches.  Every block of the cluster takes the same branches: the
 // merged totals are the same in all of them.
 template <int TYPE>
 struct Search {
   Shared& sh;
-  const Row<TYPE>& row;
-  const Histogram& bins;     // of the row
+  const Slice<TYPE>& row;
+  Bins bins;                 // of the window below, and the totals ahead of it
+  unsigned long long ahead_m = 0;
+  uint32_t ahead_c = 0;
+  int window = 0;
+  bool dirty = false;        // peers may still be reading this block's bins
   bool listed = false;       // block 0's list is the order's first tokens
-  bool clean = true;         // list_n is 0
+  int n_cuts = 0;
 
-  // The cut at which the total passes `target`; valid in every block.
-  __device__ Cut cross(bool by_count, unsigned long long target) {
+  // The merged bins at hand are the head's.
+  __device__ void keep_head() {
+    const int i = threadIdx.x;
+    sh.head_upto_m[i] = bins.upto_m;
+    sh.head_upto_c[i] = bins.upto_c;
+    __syncthreads();
+  }
+
+  // The cut at which the total passes `target`, in every block, or in block 0
+  // alone if it is the last one.
+  __device__ Cut cross(bool by_count, unsigned long long target, bool last) {
     const uint32_t rank = cluster_rank();
-    if (listed) {            // the list covers every later target: it only gets smaller
-      if (rank == 0) cut_list(sh, by_count, target, 0, 0);
-      return share();
+    if (listed) {            // the list covers every later target: they only get smaller
+      if (rank == 0) cut_list(by_count, target, 0, 0, last);
+      return share(last);
     }
-    find_bin(sh, bins, by_count, target, 0, 0);
-    View view = {sh.bin, sh.bin, 0u, 0xFFFFFFFFu};
+    move_window(by_count, target);
+    find_bin(sh, bins, by_count, target, ahead_m, ahead_c);
+    View view = {window, sh.bin, sh.bin, 0u, 0xFFFFFFFFu};
     unsigned long long base_m = sh.bin_mass;
     uint32_t base_c = sh.bin_before, count = sh.bin_cnt;
-    if (base_c + count <= kList) {
-      view.first_bin = 0;
+    if (window == 0 && base_c + count <= kPrefix) {
+      view.first = 0;
       base_m = 0;
       base_c = 0;
       listed = true;
-    }
-    __syncthreads();         // sh.bin .. have been read
-    if (!listed && count > kList) {
-      // divide the bin by the logits' bits, eleven at a time
-      for (int shift = 21; count > kList; shift = shift > 11 ? shift - 11 : 0) {
-        clear_bins(sh);
-        __syncthreads();
-        row.each([&](float x, int) {
-          const float d = row.sc.d(x);
-          const uint32_t key = float_order_key(x);
-          if (!view.has(Scale::bin(d), key)) return;
-          const unsigned long long m = row.mass(x, d);
-          if (m) add_to_bin(sh, (view.key_hi - key) >> shift, m);
+    } else if (count > kList) {
+      // divide the bin by the logits' bits
+      for (int shift = 32 - kBinBits;; shift = shift > kBinBits ? shift - kBinBits : 0) {
+        const Bins part = fill_bins([&] {
+          row.each_in(sh, view, [&](uint32_t key, unsigned long long m, int) {
+            add_to_bin(sh, (view.key_hi - key) >> shift, m);
+          });
         });
-        cluster_barrier();
-        Histogram h;
-        unsigned long long total_m;
-        uint32_t total_c;
-        merge_bins(sh, h, total_m, total_c);
-        find_bin(sh, h, by_count, target, base_m, base_c);
-        const uint32_t bin = static_cast<uint32_t>(sh.bin);
-        view.key_hi -= bin << shift;
+        find_bin(sh, part, by_count, target, base_m, base_c);
+        view.key_hi -= static_cast<uint32_t>(sh.bin) << shift;
         view.key_lo = view.key_hi - ((1u << shift) - 1u);
         base_m = sh.bin_mass;
         base_c = sh.bin_before;
         count = sh.bin_cnt;
-        cluster_barrier();  // the peers have read this block's bins
-        if (shift == 0) break;
+        if (count <= kList || shift == 0) break;
       }
-      if (count > kList) return cross_ties(view.key_hi, by_count, target, base_m, base_c);
+      if (count > kList) return cross_ties(view.key_hi, by_count, target, base_m, base_c, last);
     }
-    if (!clean) {
-      if (rank == 0 && threadIdx.x == 0) sh.list_n = 0;
-      cluster_barrier();
-    }
-    clean = false;
-    gather(sh, row, view);
+    gather(view);
     if (rank == 0) {
-      rank_list(sh);
-      cut_list(sh, by_count, target, base_m, base_c);
+      rank_list();
+      cut_list(by_count, target, base_m, base_c, last);
+      if (!listed) {
+        __syncthreads();
+        if (threadIdx.x == 0) sh.list_n = 0;
+      }
     }
-    return share();
+    return share(last);
   }
 
  private:
-  // Block 0's cut to all of them.
-  __device__ Cut share() {
+  // The whole row's bins, filled anew.
+  template <class F>
+  __device__ Bins fill_bins(F fill) {
+    if (dirty) cluster_barrier();
+    dirty = true;
+    clear_bins(sh);
+    __syncthreads();
+    fill();
     cluster_barrier();
-    const Cut c = peer(&sh, 0)->cut;
-    cluster_barrier();      // and it may be written again
-    return c;
+    return merge_bins(sh);
+  }
+
+  // Brings the target into the window's bins.
+  __device__ void move_window(bool by_count, unsigned long long target) {
+    if (target < (by_count ? ahead_c : ahead_m)) {       // back to the head
+      window = 0;
+      ahead_m = 0;
+      ahead_c = 0;
+      const int i = threadIdx.x;
+      bins = {sh.head_upto_m[i], sh.head_upto_m[i] - (i ? sh.head_upto_m[i - 1] : 0),
+              sh.head_upto_m[kBins - 1], sh.head_upto_c[i],
+              sh.head_upto_c[i] - (i ? sh.head_upto_c[i - 1] : 0), sh.head_upto_c[kBins - 1]};
+    }
+    while (window + 1 < kWindows &&
+           target >= (by_count ? ahead_c + bins.total_c : ahead_m + bins.total_m)) {
+      ahead_m += bins.total_m;
+      ahead_c += bins.total_c;
+      ++window;
+      bins = fill_bins([&] {
+        row.each_within(row.sc.end_of(window), row.sc.end_of(window - 1), [&](float, float d, int) {
+          const unsigned long long m = Scale::mass(row.sc.weight(d));
+          if (m) add_to_bin(sh, row.sc.bin(window, d), m);
+        });
+      });
+    }
+  }
+
+  // Gathers the view's tokens in block 0's list.
+  __device__ void gather(const View& view) {
+    Shared* home = peer(&sh, 0);
+    row.each_in(sh, view, [&](uint32_t key, unsigned long long m, int i) {
+      const int to = atomicAdd(&home->list_n, 1);
+      if (to < kList) home->list[to] = {m, key, static_cast<uint32_t>(row.first + i)};
+    });
+    cluster_barrier();
+    dirty = false;           // all blocks are past their merges
+  }
+
+  // Block 0: each entry's rank, and the mass ahead of it, by counting; an
+  // entry's comparisons are shared by as many neighbouring threads as there are.
+  __device__ void rank_list() {
+    const int n = sh.list_n;
+    int share = 32;
+    while (share > 1 && share * n > kThreads) share /= 2;
+    const int e = threadIdx.x / share, part = threadIdx.x % share;
+    unsigned long long before = 0;
+    uint32_t rank = 0;
+    const Entry own = sh.list[min(e, kList - 1)];
+    for (int k = part; k < n; k += share) {
+      const Entry o = sh.list[k];
+      if (o.key > own.key || (o.key == own.key && o.idx < own.idx)) {
+        before += o.mass;
+        ++rank;
+      }
+    }
+    __syncwarp();
+    for (int s = 1; s < share; s *= 2) {
+      before += __shfl_xor_sync(0xFFFFFFFFu, before, s);
+      rank += __shfl_xor_sync(0xFFFFFFFFu, rank, s);
+    }
+    if (e < n && part == 0) {
+      sh.before[e] = before;
+      sh.rank[e] = rank;
+    }
+    __syncthreads();
+  }
+
+  // Block 0: the list's entry at which the total passes the target.
+  __device__ void cut_list(bool by_count, unsigned long long target, unsigned long long base_m,
+                           uint32_t base_c, bool last) {
+    const int e = threadIdx.x;
+    if (e >= sh.list_n) return;
+    const unsigned long long m = base_m + sh.before[e], own = sh.list[e].mass;
+    const uint32_t c = base_c + sh.rank[e];
+    if (by_count ? c == target : m <= target && target < m + own)
+      tell({sh.list[e].idx, c + 1, m + own}, last);
+  }
+
+  // Every block has the cut once all are past the barrier.  Each search has a
+  // place of its own for it, so the next one's does not overwrite what a peer
+  // still reads; the last one's is block 0's alone.
+  __device__ void tell(const Cut& c, bool last) {
+    const uint32_t n = last ? 1 : cluster_size();        // the peers may have ended
+    for (uint32_t p = 0; p < n; ++p) peer(&sh, p)->cut[n_cuts] = c;
+  }
+  __device__ Cut share(bool last) {
+    const int i = n_cuts++;
+    if (last)
+      __syncthreads();
+    else
+      cluster_barrier();
+    return sh.cut[i];
   }
 
   // More than kList tokens of one logit: all have the same mass, and the one in
   // question is found by its place among them in index order.
-  __device__ Cut cross_ties(uint32_t key, bool by_count, unsigned long long target,
-                            unsigned long long base_m, uint32_t base_c) {
+  __device__ __noinline__ Cut cross_ties(uint32_t key, bool by_count, unsigned long long target,
+                                         unsigned long long base_m, uint32_t base_c, bool last) {
     const float x = __uint_as_float((key & 0x80000000u) ? (key & 0x7FFFFFFFu) : ~key);
-    const unsigned long long own = row.mass(x, row.sc.d(x));
+    const unsigned long long own = Scale::mass(row.sc.weight(row.sc.d(x)));
     const uint32_t want =
         static_cast<uint32_t>(by_count ? target - base_c : (target - base_m) / own);
-    uint32_t c = 0;
-    row.each_in_order([&](float y, int) { c += float_order_key(y) == key; });
-    unsigned long long unused = 0, total_m;
+    uint32_t c;
+    uint32_t at = count_ties(key, c);
+    if (want >= at && want < at + c)
+      row.each_tie(key, [&](int i) {
+        if (at++ == want)
+          tell({static_cast<uint32_t>(row.first + i), base_c + want + 1,
+                base_m + own * (want + 1ull)}, last);
+      });
+    cluster_barrier();       // the cut is there, and every peer's count has been read
+    return share(last);
+  }
+
+  // Tokens of this key in the thread's run, and in the row ahead of it.
+  __device__ __forceinline__ uint32_t count_ties(uint32_t key, uint32_t& c) {
+    c = 0;
+    row.each_tie(key, [&](int) { ++c; });
+    unsigned long long none = 0, total_m;
     uint32_t upto = c, total;
-    block_scan(sh, unused, upto, total_m, total);
+    block_scan(sh, none, upto, total_m, total);
     if (threadIdx.x == 0) sh.tie_cnt = total;
     cluster_barrier();
-    uint32_t before = upto - c;
-    for (uint32_t r = 0; r < cluster_rank(); ++r) before += peer(&sh, r)->tie_cnt;
-    if (want >= before && want < before + c) {
-      uint32_t at = before;
-      row.each_in_order([&](float y, int i) {
-        if (float_order_key(y) != key) return;
-        if (at++ == want)
-          peer(&sh, 0)->cut = {static_cast<uint32_t>(i), base_c + want + 1,
-                               base_m + own * (want + 1ull)};
-      });
+    uint32_t at = upto - c;
+    for (uint32_t r = 0; r < cluster_rank(); ++r) at += peer(&sh, r)->tie_cnt;
+    return at;
+  }
+
+ public:
+  // A row with infinite logits: a draw between these, which weigh the same.
+  __device__ __noinline__ Cut draw_infinite(const Settings& set) {
+    const uint32_t key = Scale::key(INFINITY);
+    uint32_t c;
+    uint32_t at = count_ties(key, c), kept = 0;
+    for (uint32_t r = 0; r < cluster_size(); ++r) kept += peer(&sh, r)->tie_cnt;
+    if (set.top_k > 0) kept = min(kept, static_cast<uint32_t>(set.top_k));
+    bool whole;
+    if (set.top_p < 1.f) {
+      const uint32_t n = static_cast<uint32_t>(share_of(fmaxf(set.top_p, 0.f), kept, whole));
+      kept = max(n + (whole ? 0u : 1u), 1u);
     }
-    return share();
+    const uint32_t want = min(
+        static_cast<uint32_t>(share_of(set.u > 0.f ? fminf(set.u, 1.f) : 0.f, kept, whole)), kept - 1);
+    if (want >= at && want < at + c)
+      row.each_tie(key, [&](int i) {
+        if (at++ == want) tell({static_cast<uint32_t>(row.first + i), kept, 0}, true);
+      });
+    cluster_barrier();
+    return sh.cut[0];
   }
 };
 
+// One pass over the slice.  HEAD: the elements at or above the edge are noted.
+// TAIL: the mass of the others, and (COUNT) their number.  A weight's 40 bits are taken as two
+// sums: adding 8 (then 2^-17, to the rest) with rounding toward zero leaves
+// floor(w 2^20) (then the next 20 bits) in the low bits of the result.
+template <int TYPE, bool HEAD, bool TAIL, bool COUNT>
+__device__ __forceinline__ void weigh(Shared& sh, const Slice<TYPE>& row) {
+  constexpr int V = Elem<TYPE>::kVec;
+  uint32_t hi = 0, lo = 0, n = 0;            // at most 528 elements a thread: below 2^30
+  row.each_vec([&](int i, const float (&x)[V]) {
+    uint32_t head = 0;
+#pragma unroll
+    for (int e = 0; e < V; ++e) {
+      const float d = row.sc.d(x[e]);
+      const bool is = d >= row.sc.edge;
+      if (is) head |= 1u << e;
+      if constexpr (TAIL) {
+        const float w = is ? 0.f : row.sc.weight(d);
+        const float h = __fadd_rz(w, 8.f);
+        const float l = __fadd_rz(__fsub_rn(w, __fsub_rn(h, 8.f)), 0x1p-17f);
+        hi += __float_as_uint(h) - 0x41000000u;
+        lo += __float_as_uint(l) - 0x37000000u;
+        if constexpr (COUNT) n += w >= 0x1p-40f;
+      }
+    }
+    if (HEAD && head) {
+      int to = atomicAdd(&sh.head_n, __popc(head));
+      do {
+        if (to < kHead) sh.head[to].y = __int_as_float(i + __ffs(head) - 1);
+        ++to;
+        head &= head - 1;
+      } while (head);
+    }
+  });
+  if constexpr (TAIL) {
+    unsigned long long m = (static_cast<unsigned long long>(hi) << 20) + lo;
+#pragma unroll
+    for (int s = 16; s; s >>= 1) {
+      m += __shfl_xor_sync(0xFFFFFFFFu, m, s);
+      n += __shfl_xor_sync(0xFFFFFFFFu, n, s);
+    }
+    if ((threadIdx.x & 31) == 0) {
+      atomicAdd(&sh.own_tail_mass, m);
+      atomicAdd(&sh.own_tail_cnt, n);
+    }
+  }
+  __syncthreads();
+  if (TAIL && threadIdx.x < cluster_size()) {
+    Shared* to = peer(&sh, threadIdx.x);
+    to->tail_mass[cluster_rank()] = sh.own_tail_mass;
+    to->tail_cnt[cluster_rank()] = sh.own_tail_cnt;
+  }
+}
+
+// The head into the block's bins: from the noted elements, or, if there were
+// too many, from all of the slice.
 template <int TYPE>
-__global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
+__device__ __forceinline__ void bin_head(Shared& sh, const Slice<TYPE>& row) {
+  auto take = [&](float d) {
+    const unsigned long long m = Scale::mass(row.sc.weight(d));
+    if (m) add_to_bin(sh, row.sc.bin(0, d), m);
+  };
+  if (sh.head_n <= kHead) {
+#pragma unroll 4
+    for (int k = threadIdx.x; k < sh.head_n; k += kThreads) {
+      const float x = row.at(__float_as_int(sh.head[k].y));
+      sh.head[k].x = x;
+      take(row.sc.d(x));
+    }
+  } else {
+    row.each_within(row.sc.edge, INFINITY, [&](float, float d, int) { take(d); });
+  }
+}
+
+template <int TYPE>
+__global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a) {
   constexpr int V = Elem<TYPE>::kVec, B = Elem<TYPE>::kBytes;
   extern __shared__ __align__(16) uint8_t smem[];
   Shared& sh = *reinterpret_cast<Shared*>(smem);
-  uint4* vecs = reinterpret_cast<uint4*>(smem + (sizeof(Shared) + 15) / 16 * 16);
+  cluster_arrive_relaxed();
   const uint32_t rank = cluster_rank(), n_blocks = cluster_size();
   const int r = blockIdx.x / n_blocks;
   const int lane = threadIdx.x & 31, warp = threadIdx.x >> 5;
 
-  // ---- the slice into shared memory.  Global vectors are aligned: the slice
-  // begins `skew` elements into its first vector, and what a vector holds of
-  // other slices or of beyond the row counts as -inf.
+  // ---- the slice: its first and last vector, which may hold other slices'
+  // logits or lie beyond the row, are put together from its own elements
   const int begin = min(a.vocab, static_cast<int>(rank) * a.slice);
-  const int end = min(a.vocab, begin + a.slice);
+  const int len = min(a.vocab, begin + a.slice) - begin;
   const uintptr_t addr = reinterpret_cast<uintptr_t>(a.logits) + (r * a.ld + begin) * B;
-  const int skew = static_cast<int>(addr % 16) / B;
-  const uint4* src = reinterpret_cast<const uint4*>(addr - addr % 16);
-  const int n_vecs = end > begin ? (end - begin + skew + V - 1) / V : 0;
-  float top = -INFINITY;
-#pragma unroll 4
-  for (int v = threadIdx.x; v < n_vecs; v += kThreads) {
-    const int e0 = v * V - skew;
-    uint4 x = all_empty<TYPE>();
-    if (e0 >= 0 && e0 + V <= end - begin) {
-      x = src[v];
-    } else {                 // the first or the last vector: its own elements only
-      uint8_t* to = reinterpret_cast<uint8_t*>(&x);
-      const uint8_t* from = reinterpret_cast<const uint8_t*>(src + v);
-      for (int e = 0; e < V; ++e)
-        if (e0 + e >= 0 && e0 + e < end - begin)
-          for (int k = 0; k < B; ++k) to[e * B + k] = from[e * B + k];
-    }
-    vecs[v] = x;
-    float f[V];
-    unpack<TYPE>(x, f);
-#pragma unroll
-    for (int e = 0; e < V; ++e) top = fmaxf(top, f[e]);
-  }
-  clear_bins(sh);
-#pragma unroll
-  for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
-  if (lane == 0) sh.warp_max[warp] = top;
+  const int skew = static_cast<int>(addr % 16) / B;       // elements ahead of the slice's first
+  Slice<TYPE> row;
+  row.vecs = reinterpret_cast<const uint4*>(addr - addr % 16);
+  row.edge = sh.edge;
+  row.n_vecs = (len + skew + V - 1) / V;
+  row.v0 = skew ? 1 : 0;
+  row.v1 = (len + skew) / V;
+  row.first = begin - skew;
   if (threadIdx.x == 0) {
+    sh.head_n = 0;
     sh.list_n = 0;
     sh.best = kMostVocab;
+    sh.own_tail_mass = 0;
+    sh.own_tail_cnt = 0;
+    if (rank == 0)           // the others' copies are written below
+      sh.set = {a.temperature ? a.temperature[r] : 1.f, a.top_p ? a.top_p[r] : 1.f,
+                a.min_p ? a.min_p[r] : 0.f, a.u[r], a.top_k ? a.top_k[r] : 0};
+  }
+  if (threadIdx.x < kMostCluster) {
+    sh.tail_mass[threadIdx.x] = 0;
+    sh.tail_cnt[threadIdx.x] = 0;
+  }
+  if (threadIdx.x < 2 * V) {
+    const int at = (threadIdx.x < V ? 0 : (row.n_vecs - 1) * V) + threadIdx.x % V;
+    const bool own = at >= skew && at - skew < len;
+    const int64_t i = r * a.ld + begin + (at - skew);
+    if constexpr (B == 4)
+      reinterpret_cast<uint32_t*>(sh.edge)[threadIdx.x] =
+          own ? static_cast<const uint32_t*>(a.logits)[i] : kEmpty<TYPE>;
+    else
+      reinterpret_cast<uint16_t*>(sh.edge)[threadIdx.x] =
+          own ? static_cast<const uint16_t*>(a.logits)[i] : static_cast<uint16_t>(kEmpty<TYPE>);
+  }
+  clear_bins(sh);
+  __syncthreads();
+
+  // ---- the largest logit
+  uint32_t best = kEmpty<TYPE>, early = best;             // early: of the thread's first vectors
+  const int early_end = a.level_vecs * kThreads;
+#pragma unroll 8
+  for (int v = threadIdx.x; v < row.n_vecs; v += kThreads) {
+    const uint4 x = Slice<TYPE>::no_nan(row.load(v));
+    best = max_packed<TYPE>(best, max_packed<TYPE>(max_packed<TYPE>(x.x, x.y), max_packed<TYPE>(x.z, x.w)));
+    if (v < early_end) early = best;
+  }
+  float top = widest<TYPE>(best);
+  // ---- the row's largest logit, and a level that a given share of the threads'
+  // maxima exceed: each warp's value of that rank, averaged
+  {
+    const float mine = widest<TYPE>(early);
+    int before = 0;          // lanes of larger maximum
+#pragma unroll
+    for (int i = 0; i < 32; ++i) {
+      const float o = __shfl_sync(0xFFFFFFFFu, mine, i);
+      before += o > mine || (o == mine && i < lane) ? 1 : 0;
+    }
+    if (before == a.level_rank) sh.warp_level[warp] = mine;
+#pragma unroll
+    for (int m = 16; m; m >>= 1) top = fmaxf(top, __shfl_xor_sync(0xFFFFFFFFu, top, m));
+    if (lane == 0) sh.warp_max[warp] = top;
   }
   __syncthreads();
+  float level = 0.f;
+  int levels = 0;
 #pragma unroll
-  for (int w = 0; w < kThreads / 32; ++w) top = fmaxf(top, sh.warp_max[w]);
-  if (threadIdx.x == 0) sh.block_max = top;
+  for (int w = 0; w < kThreads / 32; ++w) {
+    top = fmaxf(top, sh.warp_max[w]);
+    if (fabsf(sh.warp_level[w]) < INFINITY) {
+      level += sh.warp_level[w];
+      ++levels;
+    }
+  }
+  level = levels ? level / levels : -INFINITY;
+  __syncwarp();
+  cluster_wait();            // every block runs
+  if (threadIdx.x < n_blocks) {
+    Shared* to = peer(&sh, threadIdx.x);
+    to->block_max[rank] = top;
+    to->block_level[rank] = level;
+    if (rank == 0) to->set = sh.set;
+  }
   cluster_barrier();
-  for (uint32_t p = 0; p < n_blocks; ++p) top = fmaxf(top, peer(&sh, p)->block_max);
+  level = 0.f;
+  for (uint32_t p = 0; p < n_blocks; ++p) {
+    top = fmaxf(top, sh.block_max[p]);
+    level += sh.block_level[p];              // -inf if a block has none
+  }
+  level /= n_blocks;
+  const Settings set = sh.set;
 
-  const float t = a.temperature ? a.temperature[r] : 1.f;
-  const bool greedy = !(t > 0.f);
-  Row<TYPE> row;
-  row.vecs = vecs;
-  row.n_vecs = n_vecs;
-  row.first = begin - skew;
-  row.sc = {top, greedy ? 0.f : __fdiv_rn(1.f, t)};
-  row.min_p = a.min_p ? a.min_p[r] : 0.f;
-  row.min_p = row.min_p > 0.f ? fminf(row.min_p, 1.f) : 0.f;   // NaN: none
-
+  row.sc = {top, 0.f, set.min_p > 0.f ? fminf(set.min_p, 1.f) : 0.f, 0.f, 0.f};   // a NaN min_p: none
   int token = -1;
   float logprob = -INFINITY;
   uint32_t kept = 0;
   if (top == -INFINITY) {
-    cluster_barrier();       // nothing to draw from; the peers have read block_max
-  } else if (greedy) {
-    row.each([&](float x, int i) {
-      if (x == top) atomicMin(&peer(&sh, 0)->best, i);
+    // nothing to draw from
+  } else if (!(set.t > 0.f)) {
+    row.each_vec([&](int i, const float (&x)[V]) {
+      int e = V;
+#pragma unroll
+      for (int k = V - 1; k >= 0; --k)
+        if (x[k] == top) e = k;
+      if (e < V) atomicMin(&peer(&sh, 0)->best, row.first + i + e);
     });
     cluster_barrier();
     token = sh.best;         // block 0 writes it
     logprob = 0.f;
     kept = 1;
-  } else {
-    row.each([&](float x, int) {
-      const float d = row.sc.d(x);
-      const unsigned long long m = row.mass(x, d);
-      if (m) add_to_bin(sh, Scale::bin(d), m);
-    });
-    cluster_barrier();
-    Histogram bins;
-    unsigned long long mass;
-    merge_bins(sh, bins, mass, kept);
-    cluster_barrier();      // before any block clears its bins again
-    Search<TYPE> search{sh, row, bins};
-    const int k = a.top_k ? a.top_k[r] : 0;
-    if (k > 0 && static_cast<uint32_t>(k) < kept) {
-      const Cut c = search.cross(true, static_cast<unsigned long long>(k - 1));
-      mass = c.mass;
-      kept = c.count;
-    }
-    const float p = a.top_p ? a.top_p[r] : 1.f;
-    if (p < 1.f) {
-      const double need = ceil(static_cast<double>(p) * static_cast<double>(mass));
-      const Cut c = search.cross(false, need > 1.0 ? static_cast<unsigned long long>(need) - 1 : 0);
-      mass = c.mass;
-      kept = c.count;
-    }
-    float u = a.u[r];
-    u = u > 0.f ? fminf(u, 1.f) : 0.f;
-    unsigned long long at =
-        static_cast<unsigned long long>(static_cast<double>(u) * static_cast<double>(mass));
-    if (at >= mass) at = mass - 1;
-    const Cut c = search.cross(false, at);
+  } else if (top == INFINITY) {
+    Search<TYPE> search{sh, row};
+    const Cut c = search.draw_infinite(set);
     token = static_cast<int>(c.idx);
-    if (rank == 0 && threadIdx.x == 0)       // from d: the integer weight of an unlikely token is coarse
-      logprob = static_cast<float>(row.sc.d(load_logit<TYPE>(a.logits, r * a.ld + token)) -
-                                   log(static_cast<double>(mass) * 0x1p-40));
+    kept = c.count;
+    logprob = -logf(static_cast<float>(kept));
+  } else {
+    row.sc.inv_t = fminf(fmaxf(__fdiv_rn(1.f, set.t), 1.17549435e-38f), 3.40282347e38f);
+    // ---- the head; the others' total, if it can matter (min-p and top-k mostly
+    // end a row within the head)
+    row.sc.edge = a.vocab <= kHead ? -28.f : fminf(row.sc.d(level), -1e-6f);
+    row.sc.edge = fmaxf(row.sc.edge, -28.f);             // nothing behind it has a weight
+    row.sc.per_nat = (kBins - 1) / -row.sc.edge;
+    const bool tail = !(row.sc.min_p > 1.001f * expf(row.sc.edge));
+    if (!tail || set.top_k > 0)
+      weigh<TYPE, true, false, false>(sh, row);
+    else if (set.top_p < 1.f)                            // which ends in a count of its own
+      weigh<TYPE, true, true, false>(sh, row);
+    else
+      weigh<TYPE, true, true, true>(sh, row);
+    bin_head(sh, row);
+    cluster_barrier();
+    Search<TYPE> search{sh, row};
+    search.dirty = true;
+    search.bins = merge_bins(sh);
+    search.keep_head();
+    if (tail && set.top_k > 0 && static_cast<uint32_t>(set.top_k) > search.bins.total_c) {
+      weigh<TYPE, false, true, true>(sh, row);
+      cluster_barrier();
+    }
+    unsigned long long mass = search.bins.total_m;
+    kept = search.bins.total_c;
+    for (uint32_t p = 0; p < n_blocks; ++p) {
+      mass += sh.tail_mass[p];
+      kept += sh.tail_cnt[p];
+    }
+    Cut c;
+#pragma unroll 1
+    for (int step = 0; step < 3; ++step) {   // top-k, top-p, the draw
+      unsigned long long target;
+      if (step == 0) {
+        if (!(set.top_k > 0 && static_cast<uint32_t>(set.top_k) < kept)) continue;
+        target = static_cast<unsigned long long>(set.top_k - 1);
+      } else if (step == 1) {
+        if (!(set.top_p < 1.f)) continue;
+        // passed where the total reaches ceil(p Z): where it passes ceil(p Z) - 1
+        bool whole;
+        target = share_of(fmaxf(set.top_p, 0.f), mass, whole);
+        if (whole && target > 0) --target;
+      } else {
+        bool whole;
+        target = share_of(set.u > 0.f ? fminf(set.u, 1.f) : 0.f, mass, whole);
+        if (target >= mass) target = mass - 1;
+      }
+      c = search.cross(step == 0, target, step == 2);
+      if (step < 2) {
+        mass = c.mass;
+        kept = c.count;
+      }
+    }
+    if (rank == 0 && threadIdx.x == 0) {
+      token = static_cast<int>(c.idx);
+      // from d, as the integer weight of an unlikely token is coarse; the best
+      // token's 2^40 is always part of the mass
+      const float d = row.sc.d(load_logit<TYPE>(a.logits, r * a.ld + token));
+      logprob = d - log1pf(__ull2float_rn(mass - (1ull << 40)) * 0x1p-40f);
+    }
   }
   if (rank == 0 && threadIdx.x == 0) {
     a.token[r] = token;
@@ -611,33 +996,33 @@ __global__ void __launch_bounds__(kThreads) sample_kernel(const SampleArgs a) {
   }
 }
 
-// Blocks that share a row: as many as keep one wave of the GPU busy (three
-// blocks fit an SM while a slice is at most 32 KB), at least what holds the
-// row in shared memory.
-constexpr int kSliceBytes = 96 * 1024;
-int cluster_for(int rows, int vocab, int bytes) {
+// Blocks that share a row: one, or as many as one wave of the GPU holds (two
+// blocks an SM) while each still has a few thousand logits.
+int cluster_for(int rows, int vocab) {
   int n = 1;
-  while (n < kMostCluster &&
-         (static_cast<int64_t>(vocab) * bytes > static_cast<int64_t>(n) * kSliceBytes ||
-          (rows * static_cast<int64_t>(n) < 2 * kNumSMs && vocab > n * 4096)))
-    n *= 2;
+  while (n < kMostCluster && rows * 2 * static_cast<int64_t>(n) <= 2 * kNumSMs && vocab > n * 4096) n *= 2;
   return n;
 }
 
 template <int TYPE>
 cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t s) {
-  constexpr int B = Elem<TYPE>::kBytes;
-  constexpr size_t head = (sizeof(Shared) + 15) / 16 * 16;
-  constexpr int wide = kMostVocab / kMostCluster * B, most = wide > kSliceBytes ? wide : kSliceBytes;
+  constexpr size_t smem = sizeof(Shared);
   static DeviceOnce once;
   cudaError_t e = once.run([] {
     return cudaFuncSetAttribute(sample_kernel<TYPE>, cudaFuncAttributeMaxDynamicSharedMemorySize,
-                                static_cast<int>(head) + most + 64);
+                                static_cast<int>(sizeof(Shared)));
   });
   if (e != cudaSuccess) return e;
-  const int n = cluster_for(rows, a.vocab, B);
+  const int n = cluster_for(rows, a.vocab);
   a.slice = ((a.vocab + n - 1) / n + 15) / 16 * 16;
-  const size_t smem = head + static_cast<size_t>(a.slice) * B + 32;
+  // The head's size, no more than the blocks can note, and the sample that finds
+  // its level: with `each` of its tokens among so many vectors of a thread, a
+  // share of 1 - exp(-each) of the threads has one.
+  constexpr int V = Elem<TYPE>::kVec;
+  const double want = fmin(kTarget, 0.88 * kHead * n), per_vec = V * want / a.vocab;
+  a.level_vecs = per_vec > 1.0 ? 1 : static_cast<int>(1.0 / per_vec + 0.5);
+  const double each = per_vec * a.level_vecs;
+  a.level_rank = static_cast<int>(fmin(32.0 * (1.0 - exp(-each)), 31.0) - 0.5);
   return launch_ex(sample_kernel<TYPE>, dim3(rows * n), dim3(kThreads), smem, s, false, dim3(n, 1, 1),
                    a);
 }
