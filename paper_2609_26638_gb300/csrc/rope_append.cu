@@ -18,8 +18,8 @@
 namespace gs {
 namespace {
 
-constexpr int kAppendThreads = 256;
-constexpr int kHeadIters = 4;     // heads one lane group of a warp handles
+constexpr int kAppendThreads = 128;
+constexpr int kAhead = 4;         // heads of a lane group that are loaded together
 constexpr int kVRows = 32;        // tokens of one V tile
 
 struct AppendArgs {
@@ -33,7 +33,9 @@ struct AppendArgs {
   float eps;
   const int32_t *seq, *slot, *pos;
   int* err;
-  int T, Hq, qk_blocks, chunks;   // chunks of heads per token in the Q/K part
+  int T, Hq, v_blocks, iters;
+  int v_heads;                    // KV heads that a block of the V part takes in turn
+  int q_chunks, chunks;           // a token's chunks of query heads, and of all heads, in the Q/K part
   CacheView cache;
 };
 
@@ -58,27 +60,61 @@ __device__ __forceinline__ Target find_target(const AppendArgs& a, int t) {
   return {page, slot % kPageTokens};
 }
 
+// Two fp32 values in a 64-bit register pair: one instruction for both.
+typedef unsigned long long F32x2;
+__device__ __forceinline__ F32x2 join2(float a, float b) {
+  F32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 split2(F32x2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ F32x2 mul2(F32x2 a, F32x2 b) {
+  F32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F32x2 fma2(F32x2 a, F32x2 b, F32x2 c) {
+  F32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
 // Queries and keys.  A head's D dims lie on D / 8 neighbouring lanes, 16 bytes
 // each, so a warp holds 32 / (D / 8) heads of one token at once and goes
-// through kHeadIters such groups: its loads are issued together, and the
-// lane's cos and sin are read once for all of them.  A half-layout pair sits
-// on two lanes R / 16 apart: the partner's raw 16-bit values come by shuffle.
+// through `iters` such groups, all of queries or all of keys, four loads at a
+// time.  Gain and rotation are the same for all heads, so they are made into two
+// factors per element once, and two elements go through each instruction:
+//   out = rsqrt(...) * (x * A + partner * B),  A = gain cos, B = -+ partner's gain sin
+// A half-layout pair sits on two lanes R / 16 apart: the partner's raw 16-bit
+// values come by shuffle.
 template <bool BF16, int D, bool HALF>
 __device__ void rotate_heads(const AppendArgs& a) {
   constexpr int LPH = D / 8, HPW = 32 / LPH;
   const int lane = threadIdx.x & 31, sub = lane % LPH;
-  const int warp = blockIdx.x * (kAppendThreads / 32) + (threadIdx.x >> 5);
-  const int t = warp / a.chunks;
+  const int warp = (blockIdx.x - a.v_blocks) * (kAppendThreads / 32) + (threadIdx.x >> 5);
+  const int t = warp / a.chunks, chunk = warp % a.chunks;
   if (t >= a.T) return;
-  const int heads = a.Hq + a.cache.Hkv;
-  const int h0 = (warp % a.chunks) * (HPW * kHeadIters) + lane / LPH;
-  const uint16_t* row = a.qkv + t * a.ld_qkv + sub * 8;
-  uint4 x[kHeadIters];
+  const bool keys = chunk >= a.q_chunks;
+  // heads h0, h0 + HPW, ... below `heads`, of the queries or of the keys
+  const int first = (keys ? chunk - a.q_chunks : chunk) * HPW * a.iters;
+  const int h0 = first + lane / LPH;
+  const int heads = keys ? a.cache.Hkv : a.Hq;
+  const int iters = min(a.iters, (heads - first + HPW - 1) / HPW);
+  const uint16_t* row = a.qkv + t * a.ld_qkv + (keys ? a.Hq * D : 0) + sub * 8;
+  uint4 x[kAhead];
+  auto load = [&](int i0) {
 #pragma unroll
-  for (int i = 0; i < kHeadIters; ++i) {
-    const int h = h0 + i * HPW;
-    x[i] = h < heads ? *reinterpret_cast<const uint4*>(row + h * D) : make_uint4(0, 0, 0, 0);
-  }
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + (i0 + i) * HPW;
+      x[i] = make_uint4(0, 0, 0, 0);
+      if (h < heads) x[i] = *reinterpret_cast<const uint4*>(row + h * D);
+    }
+  };
+  load(0);
   int pos = a.pos[t];
   if (pos < 0 || pos >= a.table_rows) {
     if (lane == 0) atomicExch(a.err, kErrBounds);
@@ -87,87 +123,104 @@ __device__ void rotate_heads(const AppendArgs& a) {
   const bool turns = sub * 8 < 2 * a.half;
   const bool second = HALF && sub * 8 >= a.half;
   const int partner = HALF && turns ? (second ? sub - a.half / 8 : sub + a.half / 8) : sub;
-  float2 cs[HALF ? 8 : 4];
-  if (turns) {
-    const float2* r = a.table + static_cast<int64_t>(pos) * a.half +
-                      (HALF ? sub * 8 - (second ? a.half : 0) : sub * 4);
+  const __nv_bfloat16* gain = keys ? a.k_gain : a.q_gain;
+  float A[8], B[8];
 #pragma unroll
-    for (int e = 0; e < (HALF ? 8 : 4); e += 2) {
-      const float4 v = *reinterpret_cast<const float4*>(r + e);
-      cs[e] = make_float2(v.x, v.y);
-      cs[e + 1] = make_float2(v.z, v.w);
+  for (int e = 0; e < 8; ++e) {
+    A[e] = 1.f;
+    B[e] = 0.f;
+  }
+  if (turns) {
+    const float4* r = reinterpret_cast<const float4*>(
+        a.table + static_cast<int64_t>(pos) * a.half +
+        (HALF ? sub * 8 - (second ? a.half : 0) : sub * 4));
+#pragma unroll
+    for (int e = 0; e < (HALF ? 4 : 2); ++e) {
+      const float4 v = r[e];
+      if constexpr (HALF) {
+        A[2 * e] = v.x;
+        A[2 * e + 1] = v.z;
+        B[2 * e] = second ? v.y : -v.y;
+        B[2 * e + 1] = second ? v.w : -v.w;
+      } else {
+        A[4 * e] = A[4 * e + 1] = v.x;
+        A[4 * e + 2] = A[4 * e + 3] = v.z;
+        B[4 * e] = -v.y;
+        B[4 * e + 1] = v.y;
+        B[4 * e + 2] = -v.w;
+        B[4 * e + 3] = v.w;
+      }
     }
   }
-  const Target to = find_target(a, t);
-#pragma unroll
-  for (int i = 0; i < kHeadIters; ++i) {
-    const int h = h0 + i * HPW;
-    const uint32_t raw[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
-    float y[8];
+  if (gain) {
+    const uint4 own = *reinterpret_cast<const uint4*>(gain + sub * 8);
+    const uint4 oth = *reinterpret_cast<const uint4*>(gain + partner * 8);
+    const uint32_t w[4] = {own.x, own.y, own.z, own.w}, p[4] = {oth.x, oth.y, oth.z, oth.w};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float2 f = unpack2<BF16>(raw[e]);
-      y[2 * e] = f.x;
-      y[2 * e + 1] = f.y;
+      const float2 f = unpack2<true>(w[e]), q = unpack2<true>(p[e]);
+      A[2 * e] *= f.x;
+      A[2 * e + 1] *= f.y;
+      B[2 * e] *= HALF ? q.x : q.y;
+      B[2 * e + 1] *= HALF ? q.y : q.x;
     }
-    float z[8];   // the partner's values (half layout)
-    if constexpr (HALF) {
+  }
+  F32x2 A2[4], B2[4];
+#pragma unroll
+  for (int e = 0; e < 4; ++e) {
+    A2[e] = join2(A[2 * e], A[2 * e + 1]);
+    B2[e] = join2(B[2 * e], B[2 * e + 1]);
+  }
+  // where head 0 goes, and from there the next one
+  uint16_t* out = nullptr;
+  int64_t step = D;
+  if (!keys) {
+    out = a.q_out + t * a.ld_q + sub * 8;
+  } else {
+    const Target to = find_target(a, t);
+    if (to.page >= 0) out = a.cache.block(to.page, 0, 0, D) + to.at * D + sub * 8;
+    step = kPageTokens * D;
+  }
+#pragma unroll 1
+  for (int i0 = 0; i0 < iters; i0 += kAhead) {
+    if (i0) load(i0);
+#pragma unroll
+    for (int i = 0; i < kAhead; ++i) {
+      const int h = h0 + (i0 + i) * HPW;
+      const uint32_t raw[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      F32x2 y[4], ss = join2(0.f, 0.f);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 f =
-            unpack2<BF16>(__shfl_sync(0xFFFFFFFFu, raw[e], lane - sub + partner));
-        z[2 * e] = f.x;
-        z[2 * e + 1] = f.y;
+        const float2 f = unpack2<BF16>(raw[e]);
+        y[e] = join2(f.x, f.y);
+        ss = fma2(y[e], y[e], ss);
       }
-    }
-    const __nv_bfloat16* gain = h < a.Hq ? a.q_gain : a.k_gain;
-    if (a.q_gain) {
-      float ss = 0.f;
+      float r = 1.f;
+      if (gain) {
+        const float2 s2 = split2(ss);
+        float s = s2.x + s2.y;
 #pragma unroll
-      for (int e = 0; e < 8; ++e) ss = fmaf(y[e], y[e], ss);
-#pragma unroll
-      for (int m = 1; m < LPH; m *= 2) ss += __shfl_xor_sync(0xFFFFFFFFu, ss, m);
-      const float r = rsqrtf(ss * (1.f / D) + a.eps);
-      const uint4 g = *reinterpret_cast<const uint4*>(gain + sub * 8);
-      const uint32_t gw[4] = {g.x, g.y, g.z, g.w};
+        for (int m = 1; m < LPH; m *= 2) s += __shfl_xor_sync(0xFFFFFFFFu, s, m);
+        r = rsqrtf(s * (1.f / D) + a.eps);
+      }
+      const F32x2 r2 = join2(r, r);
+      uint32_t o[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack2<true>(gw[e]);
-        y[2 * e] *= r * f.x;
-        y[2 * e + 1] *= r * f.y;
-      }
-      if constexpr (HALF) {
-        const uint4 p = *reinterpret_cast<const uint4*>(gain + partner * 8);
-        const uint32_t pw[4] = {p.x, p.y, p.z, p.w};
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float2 f = unpack2<true>(pw[e]);
-          z[2 * e] *= r * f.x;
-          z[2 * e + 1] *= r * f.y;
+        F32x2 z;   // the partners' values; where nothing turns, 0 (B is 0, but x may be infinite)
+        if constexpr (HALF) {
+          const uint32_t p = __shfl_sync(0xFFFFFFFFu, raw[e], lane - sub + partner);
+          const float2 f = unpack2<BF16>(turns ? p : 0u);
+          z = join2(f.x, f.y);
+        } else {
+          const float2 f = unpack2<BF16>(turns ? raw[e] : 0u);
+          z = join2(f.y, f.x);
         }
+        const float2 v = split2(mul2(fma2(z, B2[e], mul2(y[e], A2[e])), r2));
+        o[e] = pack2<BF16>(v.x, v.y);
       }
-    }
-    if (turns) {
-      if constexpr (HALF) {
-        const float sign = second ? 1.f : -1.f;
-#pragma unroll
-        for (int e = 0; e < 8; ++e) y[e] = fmaf(y[e], cs[e].x, sign * z[e] * cs[e].y);
-      } else {
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          const float p = y[2 * e], q = y[2 * e + 1];
-          y[2 * e] = fmaf(p, cs[e].x, -q * cs[e].y);
-          y[2 * e + 1] = fmaf(q, cs[e].x, p * cs[e].y);
-        }
-      }
-    }
-    if (h >= heads) continue;
-    const uint4 o = make_uint4(pack2<BF16>(y[0], y[1]), pack2<BF16>(y[2], y[3]),
-                               pack2<BF16>(y[4], y[5]), pack2<BF16>(y[6], y[7]));
-    if (h < a.Hq) {
-      *reinterpret_cast<uint4*>(a.q_out + t * a.ld_q + h * D + sub * 8) = o;
-    } else if (to.page >= 0) {
-      *reinterpret_cast<uint4*>(a.cache.block(to.page, 0, h - a.Hq, D) + to.at * D + sub * 8) = o;
+      if (h < heads && out)
+        *reinterpret_cast<uint4*>(out + h * step) = make_uint4(o[0], o[1], o[2], o[3]);
     }
   }
 }
@@ -182,16 +235,16 @@ __device__ void rotate_heads(const AppendArgs& a) {
 template <int D>
 __device__ void write_values(const AppendArgs& a) {
   constexpr int P = D + 2, kBack = 8, kSpan = kBack + kVRows + 8;
-  __shared__ uint16_t tile[(kVRows + 8) * P];
+  __shared__ alignas(16) uint16_t tile[(kVRows + 8) * P];
   __shared__ Target to[kSpan];          // rows t0 - 8 .. t0 + 39
   __shared__ bool starts[kSpan];        // a full aligned run starts at this row
   __shared__ uint8_t run[kVRows], single[kVRows];
   __shared__ int n_run, n_single;
-  const int block = blockIdx.x - a.qk_blocks;
-  const int head = block % a.cache.Hkv, t0 = (block / a.cache.Hkv) * kVRows;
+  const int block = blockIdx.x, groups = (a.cache.Hkv + a.v_heads - 1) / a.v_heads;
+  const int head0 = block % groups * a.v_heads, t0 = (block / groups) * kVRows;
   const int rows = min(kVRows, a.T - t0);
-  const uint16_t* src = a.qkv + (a.Hq + a.cache.Hkv + head) * D;
-  auto load_rows = [&](int r0, int r1) {
+  auto load_rows = [&](int head, int r0, int r1) {
+    const uint16_t* src = a.qkv + (a.Hq + a.cache.Hkv + head) * D;
     for (int v = r0 * (D / 8) + threadIdx.x; v < r1 * (D / 8); v += kAppendThreads) {
       const int r = v / (D / 8), c = v % (D / 8) * 8;
       const uint4 x = *reinterpret_cast<const uint4*>(src + (t0 + r) * a.ld_qkv + c);
@@ -202,7 +255,7 @@ __device__ void write_values(const AppendArgs& a) {
       s[3] = x.w;
     }
   };
-  load_rows(0, rows);
+  load_rows(head0, 0, rows);
   if (threadIdx.x < kSpan) {
     const int t = t0 - kBack + static_cast<int>(threadIdx.x);
     to[threadIdx.x] = t >= 0 && t < a.T ? find_target(a, t) : Target{-1, 0};
@@ -233,34 +286,48 @@ __device__ void write_values(const AppendArgs& a) {
     }
   }
   __syncthreads();
-  const int last = n_run ? run[n_run - 1] + 8 : 0;
-  if (last > kVRows) {                  // a run that ends in the next tile
-    load_rows(kVRows, last);
-    __syncthreads();
-  }
-  for (int w = threadIdx.x; w < D * n_run; w += kAppendThreads) {
-    const int d = w / n_run, r = run[w % n_run];
-    uint32_t p[4];
+  const int last = n_run ? run[n_run - 1] + 8 : 0;   // past 32: a run that ends in the next tile
+  for (int head = head0; head < min(head0 + a.v_heads, a.cache.Hkv); ++head) {
+    if (head > head0) {
+      __syncthreads();                 // the tile has been read
+      load_rows(head, 0, max(rows, last));
+      __syncthreads();
+    } else if (last > kVRows) {
+      load_rows(head, kVRows, last);
+      __syncthreads();
+    }
+    // at most four runs of eight rows start in a tile; two dims at a time
+    for (int w = threadIdx.x; w < D / 2 * 4; w += kAppendThreads) {
+      if ((w & 3) >= n_run) continue;
+      const int d = w >> 2, r = run[w & 3];
+      const uint32_t* s = reinterpret_cast<const uint32_t*>(tile) + r * (P / 2) + d;
+      uint32_t lo[4], hi[4];
 #pragma unroll
-    for (int i = 0; i < 4; ++i)
-      p[i] = tile[(r + 2 * i) * P + d] | static_cast<uint32_t>(tile[(r + 2 * i + 1) * P + d]) << 16;
-    const Target at = to[kBack + r];
-    *reinterpret_cast<uint4*>(a.cache.block(at.page, 1, head, D) + d * kPageTokens + at.at) =
-        make_uint4(p[0], p[1], p[2], p[3]);
-  }
-  for (int w = threadIdx.x; w < n_single * D; w += kAppendThreads) {
-    const int r = single[w / D], d = w % D;
-    const Target at = to[kBack + r];
-    a.cache.block(at.page, 1, head, D)[d * kPageTokens + at.at] = tile[r * P + d];
+      for (int i = 0; i < 4; ++i) {
+        const uint32_t u = s[2 * i * (P / 2)], v = s[(2 * i + 1) * (P / 2)];
+        lo[i] = __byte_perm(u, v, 0x5410);
+        hi[i] = __byte_perm(u, v, 0x7632);
+      }
+      const Target at = to[kBack + r];
+      uint16_t* out = a.cache.block(at.page, 1, head, D) + 2 * d * kPageTokens + at.at;
+      *reinterpret_cast<uint4*>(out) = make_uint4(lo[0], lo[1], lo[2], lo[3]);
+      *reinterpret_cast<uint4*>(out + kPageTokens) = make_uint4(hi[0], hi[1], hi[2], hi[3]);
+    }
+    for (int w = threadIdx.x; w < n_single * D; w += kAppendThreads) {
+      const int r = single[w / D], d = w % D;
+      const Target at = to[kBack + r];
+      a.cache.block(at.page, 1, head, D)[d * kPageTokens + at.at] = tile[r * P + d];
+    }
   }
 }
 
 template <bool BF16, int D, bool HALF>
-__global__ void __launch_bounds__(kAppendThreads) rope_append_kernel(const AppendArgs a) {
-  if (static_cast<int>(blockIdx.x) < a.qk_blocks)
-    rotate_heads<BF16, D, HALF>(a);
-  else
+__global__ void __launch_bounds__(kAppendThreads, 8) rope_append_kernel(const AppendArgs a) {
+  // the values' blocks take longest: they come first
+  if (static_cast<int>(blockIdx.x) < a.v_blocks)
     write_values<D>(a);
+  else
+    rotate_heads<BF16, D, HALF>(a);
 }
 
 template <bool BF16, int D>
@@ -354,7 +421,6 @@ extern "C" int gs_rope_append(const gs_cache* cache, const gs_rope* rope, const 
       (q_out == qkv && ld_q != ld_qkv))
     return GS_ERR_INVALID_ARG;
   if (T == 0) return GS_OK;
-  const int per_warp = 32 / (D / 8) * kHeadIters;
   AppendArgs a;
   a.qkv = static_cast<const uint16_t*>(qkv);
   a.ld_qkv = ld_qkv;
@@ -372,14 +438,24 @@ extern "C" int gs_rope_append(const gs_cache* cache, const gs_rope* rope, const 
   a.err = err;
   a.T = T;
   a.Hq = n_heads;
-  a.chunks = (n_heads + Hkv + per_warp - 1) / per_warp;
+  // A warp takes twice as many heads where that still leaves two waves of warps
+  // (32 an SM): what it sets up for a token then serves more of them.
+  const int hpw = 32 / (D / 8);
+  for (a.iters = 2 * kAhead;; a.iters /= 2) {
+    a.q_chunks = (n_heads + hpw * a.iters - 1) / (hpw * a.iters);
+    a.chunks = a.q_chunks + (Hkv + hpw * a.iters - 1) / (hpw * a.iters);
+    if (a.iters == kAhead || static_cast<int64_t>(T) * a.chunks >= 2 * 32 * kNumSMs) break;
+  }
+  a.v_heads = static_cast<int64_t>((T + kVRows - 1) / kVRows) * Hkv >= 8 * kNumSMs ? 4 : 1;
   a.cache = cache_view(*cache);
   constexpr int warps = kAppendThreads / 32;
   const int64_t qk_blocks = (static_cast<int64_t>(T) * a.chunks + warps - 1) / warps;
-  const int64_t blocks = qk_blocks + static_cast<int64_t>((T + kVRows - 1) / kVRows) * Hkv;
+  const int64_t v_blocks =
+      static_cast<int64_t>((T + kVRows - 1) / kVRows) * ((Hkv + a.v_heads - 1) / a.v_heads);
+  const int64_t blocks = qk_blocks + v_blocks;
   if (static_cast<int64_t>(T) * a.chunks + warps >= (1ll << 31) || blocks >= (1ll << 31))
     return GS_ERR_UNSUPPORTED;
-  a.qk_blocks = static_cast<int>(qk_blocks);
+  a.v_blocks = static_cast<int>(v_blocks);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool half = rope->layout == GS_ROPE_HALF;
   const int n = static_cast<int>(blocks);
