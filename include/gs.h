@@ -408,9 +408,9 @@ int gs_linear_noalloc_status(void *stream);
  * device memory is allocated, and every call may be captured in a CUDA graph.
  *
  * `err` (or the first int32 of the scratch) is a device error word: a kernel
- * that meets an index out of range stores 1, one whose bounded wait runs out
- * stores 2, and goes on with the index clamped or the write left out.  It is
- * never cleared by a call: zero it once, read it when convenient.
+ * that meets an index out of range stores 1 and goes on with the index clamped
+ * or the write left out.  It is never cleared by a call: zero it once, read it
+ * when convenient.
  * ------------------------------------------------------------------------ */
 
 /* Element types. */

@@ -153,8 +153,7 @@ class StepDecoder:
         if word:
             with torch.cuda.stream(self.stream):
                 self.attn_scratch[:4].zero_()
-            raise gs.GsError(gs.GS_ERR_TIMEOUT if word == 2 else gs.GS_ERR_DEVICE_CHECK,
-                             "gs_decode_attention")
+            raise gs.GsError(gs.GS_ERR_DEVICE_CHECK, "gs_decode_attention")
 
 
 class Sampler:

@@ -8,11 +8,8 @@
 // flops per 4 bytes, so HBM bounds every group that shares a KV head.  The
 // work is cut into items of `split` pages; a block takes one item of one KV
 // head (and up to 16 of its query heads), its warps take the item's pages in
-// turn.  A warp is its own pipeline: lane 0 streams the warp's pages, K block
-// then V^T block (each contiguous), by bulk copies into a private ring of
-// shared-memory blocks, the warp computes and gives the block back with a
-// warp-level barrier, so no two warps ever wait for each other before the
-// item's end.
+// turn, 32 tokens at a time, and are joined at the item's end; until then no warp
+// waits for another.
 //
 // The products are m16n8k16 tensor instructions on the 16 query rows.  One
 // token fills at most 16 of the 128 rows of a tcgen05 tile, and its
@@ -20,14 +17,20 @@
 // scores and probabilities never leave the registers.  A dot product does not
 // care in which order its terms come, so each lane takes 16 contiguous bytes
 // as its share of the operand: of a K row, 8 dims (Q is held in the same
-// order); of a V^T row, 8 tokens.  The S tile's columns are given to the tokens
-// in the order in which the accumulators of one lane are again the P operand of
-// the 8 tokens whose values it reads, so P needs no exchange either.
+// order); of a V^T row, 8 tokens.  So keys and values come straight from global
+// memory into the registers that the products read, a step ahead of them, with
+// no shared memory, no barrier and every loaded byte used.  (Bulk copies into a
+// ring of shared memory moved the same bytes, but cost about 350 cycles to issue
+// and 190 to wait for, 8 KB at a time: 1.5 us per page and warp, where this
+// takes 0.9.)  The S tile's columns are given to the tokens in the order in
+// which the accumulators of one lane are again the P operand of the 8 tokens
+// whose values it reads, so P needs no exchange either.
 //
 // Running max (log2 units), sum and accumulators are fp32.  P is rounded to
 // the cache's type for the second product: at most 1, relative error 2^-12
 // (fp16) or 2^-9 (bf16), below the output's own rounding after averaging; the
 // sum l takes the unrounded P.
+#include <algorithm>
 #include <cmath>
 
 #include "internal.h"
@@ -49,6 +52,7 @@ struct DecodeArgs {
   int64_t ld_out;
   float* lse;
   int Hq, G, tiles, window, split, items;
+  int cluster;        // the items of a row and head are one cluster, and join there
   float scale_log2;
   float* part_o;      // [row][head][item][D]
   float2* part_ml;    // [row][head][item]
@@ -95,26 +99,15 @@ template <bool BF16>
 __device__ __forceinline__ void mma16816(float (&c)[4], uint32_t a0, uint32_t a1, uint32_t a2,
                                          uint32_t a3, uint32_t b0, uint32_t b1) {
   if constexpr (BF16)
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.bf16.bf16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
         "{%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
   else
-    asm volatile(
-        "mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
+    asm("mma.sync.aligned.m16n8k16.row.col.f32.f16.f16.f32 {%0,%1,%2,%3}, {%4,%5,%6,%7}, "
         "{%8,%9}, {%0,%1,%2,%3};"
         : "+f"(c[0]), "+f"(c[1]), "+f"(c[2]), "+f"(c[3])
         : "r"(a0), "r"(a1), "r"(a2), "r"(a3), "r"(b0), "r"(b1));
-}
-
-__device__ __forceinline__ uint4 lds128(uint32_t addr) {
-  uint4 v;
-  asm volatile("ld.shared.v4.u32 {%0,%1,%2,%3}, [%4];"
-               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
-               : "r"(addr)
-               : "memory");
-  return v;
 }
 
 __device__ __forceinline__ float ex2(float x) {
@@ -123,61 +116,74 @@ __device__ __forceinline__ float ex2(float x) {
   return y;
 }
 
-// Contiguous copy of `bytes` (a multiple of 16) into shared memory.
-__device__ __forceinline__ void bulk_load(uint32_t dst, const void* src, uint32_t bytes,
-                                          uint32_t bar) {
-  asm volatile(
-      "cp.async.bulk.shared::cluster.global.mbarrier::complete_tx::bytes [%0], [%1], %2, [%3];" ::"r"(
-          dst),
-      "l"(reinterpret_cast<uint64_t>(src)), "r"(bytes), "r"(bar)
-      : "memory");
+// 16 bytes that are read once.
+__device__ __forceinline__ uint4 load_once(const uint16_t* p) {
+  uint4 v;
+  asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
+               : "=r"(v.x), "=r"(v.y), "=r"(v.z), "=r"(v.w)
+               : "l"(p));
+  return v;
 }
 
 // m = -inf means no weight at all: such a max is taken as 0, so that its
 // exponentials are 2^-inf = 0 and not 2^(inf - inf).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
-template <int D>
-struct DecodeShape {
-  static constexpr int kBlock = kPageTokens * D * 2;    // bytes of one K or V^T block
-  static constexpr int kWarps = D == 64 ? 4 : 2;
-  static constexpr int kRing = 3;                       // blocks of a warp's ring
-  static constexpr int kThreads = kWarps * 32;
-  static constexpr int kRingBytes = kWarps * kRing * kBlock;
-  static constexpr int kSmem = kRingBytes + 128;        // and the alignment of its start
-};
+// Four dims of a head's output, and with the first of them its log-sum-exp.
+template <bool BF16, int D>
+__device__ __forceinline__ void store_row(const DecodeArgs& a, int row, int head, int d, float m,
+                                          float l, const float4& acc) {
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(head) * D + d) =
+      make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
+  if (d == 0 && a.lse)
+    a.lse[static_cast<int64_t>(row) * a.Hq + head] =
+        l != 0.f ? (finite_max(m) + log2f(l)) * kLn2 : -INFINITY;
+}
+
+constexpr int kMostCluster = 8;
+
+// acc += f v, l += f l_v: products rounded before they are added, so that the
+// two ways of joining items give the same bits.
+__device__ __forceinline__ void add_scaled(float4& acc, float& l, const float4& v, float l_v, float f) {
+  l = __fadd_rn(l, __fmul_rn(f, l_v));
+  acc.x = __fadd_rn(acc.x, __fmul_rn(f, v.x));
+  acc.y = __fadd_rn(acc.y, __fmul_rn(f, v.y));
+  acc.z = __fadd_rn(acc.z, __fmul_rn(f, v.z));
+  acc.w = __fadd_rn(acc.w, __fmul_rn(f, v.w));
+}
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kStep = 32;            // tokens of a warp's step: half a page
 
 // WIDE: more than 8 query rows (the upper half of the tile is in use).
 template <bool BF16, int D, bool WIDE>
-__global__ void __launch_bounds__(DecodeShape<D>::kThreads, 2)
+__global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2)
 decode_attention_kernel(const DecodeArgs a) {
-  using S = DecodeShape<D>;
-  extern __shared__ uint8_t smem_raw[];
-  __shared__ uint64_t bars[S::kWarps * S::kRing];
-  __shared__ float2 s_ml[S::kWarps][kRows];
+  constexpr int P = D + 8;           // row pitch: 8-byte stores of 8 rows x 4 lanes on distinct banks
+  __shared__ alignas(16) float so[kWarps * kRows * P];   // the warps' parts
+  __shared__ alignas(16) float s_item[kRows * D];        // in a cluster: this item's part
+  __shared__ float2 s_ml[kWarps][kRows], s_item_ml[kRows];
   pdl_trigger();   // the joining kernel may take its place; it waits for this one's end
   const int row = blockIdx.z, head = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
   const int item = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const Span sp = find_span(a, row);
   const int items = (sp.pages + a.split - 1) / a.split;
-  if (item >= items && item > 0) return;
+  if (item >= items && item > 0) {
+    if (a.cluster) {                     // the barriers below want every block
+      cluster_sync_all();
+      cluster_sync_all();
+    }
+    return;
+  }
   const int h0 = head * a.G + tile * kRows;              // first query head of the block
   const int rows = min(kRows, a.G - tile * kRows);
-  const int p0 = item * a.split;                         // this item's pages, from page0
-  const int cnt_all = min(a.split, sp.pages - p0);       // 0 for an empty row
-  const int cnt = cnt_all > warp ? (cnt_all - warp + S::kWarps - 1) / S::kWarps : 0;
-
-  uint8_t* smem = reinterpret_cast<uint8_t*>(
-      (reinterpret_cast<uintptr_t>(smem_raw) + 127) & ~static_cast<uintptr_t>(127));
-  const uint32_t ring = smem_u32(smem) + warp * S::kRing * S::kBlock;
-  const uint32_t bar = smem_u32(bars) + warp * S::kRing * 8;
-  if (lane == 0) {
-    for (int i = 0; i < S::kRing; ++i) mbar_init(bar + 8 * i, 1);
-    fence_mbar_init();
-    fence_proxy_async_smem();
-  }
-  __syncwarp();
+  // this item's steps: the half pages of its pages that hold visible keys
+  const int t0 = (sp.page0 + item * a.split) * 2;
+  const int begin = max(t0, sp.lo / kStep);
+  const int steps = max(0, min(t0 + 2 * a.split, (sp.n + kStep - 1) / kStep) - begin);
+  const int cnt = steps > warp ? (steps - warp + kWarps - 1) / kWarps : 0;
 
   // Q in the operand's order: of each 32 dims, dims 8q .. 8q + 7 on lane q.
   uint32_t qa[D / 32][4], qb[D / 32][4];
@@ -192,84 +198,82 @@ decode_attention_kernel(const DecodeArgs a) {
     qb[c][0] = v.x, qb[c][1] = v.y, qb[c][2] = v.z, qb[c][3] = v.w;
   }
 
-  // The warp's j-th page is page p0 + warp + j * kWarps of the row; lane l
-  // holds the pool's page of j = 32 i + l.
+  // The warp's j-th step is half page begin + warp + j * kWarps; lane l holds
+  // the pool's page of j = 32 i + l.
   int ids = 0;
-  auto load_ids = [&](int j0) {
-    const int j = j0 + lane;
-    if (j < cnt) ids = sp.table[sp.page0 + p0 + warp + j * S::kWarps];
-  };
-  // Block b of the warp's stream: K of page b / 2, then its V^T.
-  auto issue = [&](int b) {
-    const int j = b >> 1;
+  const int k_lane = (8 * (g >> 1) + (g & 1)) * D + 8 * q, v_lane = g * kPageTokens + 8 * q;
+  const uint16_t *k_at = nullptr, *v_at = nullptr;       // this lane's place in a step's K, V^T
+  auto find_step = [&](int j) {
     if (j >= cnt) return;
-    if (!(b & 1) && !(j & 31)) load_ids(j);
+    if (!(j & 31) && j + lane < cnt) ids = sp.table[(begin + warp + (j + lane) * kWarps) / 2];
     int page = __shfl_sync(0xFFFFFFFFu, ids, j & 31);
-    if (lane == 0) {
-      if (page < 0 || page >= a.cache.n_pages) {
-        atomicExch(a.err, kErrBounds);
-        page = 0;
-      }
-      const int st = b % S::kRing;
-      // of the last page's keys only the rows that exist
-      const int tok = (sp.page0 + p0 + warp + j * S::kWarps) * kPageTokens;
-      const uint32_t bytes =
-          b & 1 ? S::kBlock : static_cast<uint32_t>(min(kPageTokens, sp.n - tok)) * (D * 2);
-      mbar_arrive_expect_tx(bar + 8 * st, bytes);
-      bulk_load(ring + st * S::kBlock, a.cache.block(page, b & 1, head, D), bytes, bar + 8 * st);
+    if (page < 0 || page >= a.cache.n_pages) {
+      if (lane == 0) atomicExch(a.err, kErrBounds);
+      page = 0;
     }
+    const int half = (begin + warp + j * kWarps) & 1;
+    k_at = a.cache.block(page, 0, head, D) + half * kStep * D + k_lane;
+    v_at = a.cache.block(page, 1, head, D) + half * kStep + v_lane;
   };
-  // Block b has landed; the same answer in every lane.
-  auto arrived = [&](int b) {
-    const bool here = mbar_wait(bar + 8 * (b % S::kRing), (b / S::kRing) & 1, a.err);
-    return __all_sync(0xFFFFFFFFu, here) != 0;
+  constexpr int C = D / 32;          // 32-dim chunks of a K row
+  uint4 k[4 * C], v[8];              // S tile i's chunk c; 8 rows of each of 8 V^T tiles
+  auto load_k = [&](int j) {
+    if (j >= cnt) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < C; ++c) k[i * C + c] = load_once(k_at + 2 * i * D + 32 * c);
   };
-  for (int b = 0; b < S::kRing; ++b) issue(b);
+  auto load_v = [&](int j) {
+    if (j >= cnt) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_once(v_at + 8 * i * kPageTokens);
+  };
+  find_step(0);
+  load_k(0);
+  load_v(0);
 
   float o[D / 8][4];
 #pragma unroll
   for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
   float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
-  int b = 0;
-  bool ok = true;
-  for (int j = 0; j < cnt && ok; ++j) {
-    const int tok0 = (sp.page0 + p0 + warp + j * S::kWarps) * kPageTokens;
-    const bool edge = tok0 < sp.lo || tok0 + kPageTokens > sp.n;
-    // ---- S = Q K^T
-    float s[8][4];
+  for (int j = 0; j < cnt; ++j) {
+    const int tok0 = (begin + warp + j * kWarps) * kStep;
+    const bool edge = tok0 < sp.lo || tok0 + kStep > sp.n;
+    // ---- S = Q K^T; column n of S tile i is token 8 (n/2) + 2 i + n%2
+    float s[4][4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
-    ok = arrived(b);
-    if (!ok) break;
-    {
-      const uint32_t kb = ring + (b % S::kRing) * S::kBlock + q * 16;
+    for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {      // column n of S tile i: token 32 (i/4) + 8 (n/2) + 2 (i%4) + n%2
-        const uint32_t r = kb + (32 * (i >> 2) + 8 * (g >> 1) + 2 * (i & 3) + (g & 1)) * (D * 2);
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
-        for (int c = 0; c < D / 32; ++c) {
-          const uint4 k = lds128(r + 64 * c);
-          mma16816<BF16>(s[i], qa[c][0], qb[c][0], qa[c][1], qb[c][1], k.x, k.y);
-          mma16816<BF16>(s[i], qa[c][2], qb[c][2], qa[c][3], qb[c][3], k.z, k.w);
-        }
-      }
+      for (int i = 0; i < 4; ++i)
+        mma16816<BF16>(s[i], qa[c][0], qb[c][0], qa[c][1], qb[c][1], k[i * C + c].x, k[i * C + c].y);
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        mma16816<BF16>(s[i], qa[c][2], qb[c][2], qa[c][3], qb[c][3], k[i * C + c].z, k[i * C + c].w);
     }
-    __syncwarp();                        // every lane has read the block
-    issue(b + S::kRing);
-    ++b;
+    const uint16_t* v_now = v_at;
+    find_step(j + 1);
+    if constexpr (D == 64) {
+      load_k(j + 1);
+    } else {   // K's registers take the other dims' values first
+#pragma unroll
+      for (int i = 0; i < 8; ++i) k[i] = load_once(v_now + 8 * (8 + i) * kPageTokens);
+    }
     // ---- softmax; this lane's columns 2q, 2q + 1 of tile i are tokens
-    //      tok0 + 32 (i/4) + 8 q + 2 (i%4) + {0, 1}
+    //      tok0 + 8 q + 2 i + {0, 1}
     if (edge) {
 #pragma unroll
-      for (int i = 0; i < 8; ++i) {
-        const int t = tok0 + 32 * (i >> 2) + 8 * q + 2 * (i & 3);
+      for (int i = 0; i < 4; ++i) {
+        const int t = tok0 + 8 * q + 2 * i;
         if (t < sp.lo || t >= sp.n) s[i][0] = s[i][2] = -INFINITY;
         if (t + 1 < sp.lo || t + 1 >= sp.n) s[i][1] = s[i][3] = -INFINITY;
       }
     }
     float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       x0 = fmaxf(x0, fmaxf(s[i][0], s[i][1]));
       if (WIDE) x1 = fmaxf(x1, fmaxf(s[i][2], s[i][3]));
     }
@@ -295,9 +299,9 @@ decode_attention_kernel(const DecodeArgs a) {
       m1 = n1;
     }
     const float z0 = finite_max(m0), z1 = finite_max(m1);
-    uint32_t pa[8], pb[8];
+    uint32_t pa[4], pb[4];
 #pragma unroll
-    for (int i = 0; i < 8; ++i) {
+    for (int i = 0; i < 4; ++i) {
       const float u = ex2(fmaf(s[i][0], a.scale_log2, -z0)), v = ex2(fmaf(s[i][1], a.scale_log2, -z0));
       l0 += u + v;
       pa[i] = pack2<BF16>(u, v);
@@ -310,40 +314,33 @@ decode_attention_kernel(const DecodeArgs a) {
       }
     }
     // ---- O += P V
-    ok = arrived(b);
-    if (!ok) break;
-    {
-      const uint32_t vb = ring + (b % S::kRing) * S::kBlock + q * 16;
+    auto multiply = [&](float (*acc)[4], uint4* x) {     // 8 tiles of 8 dims
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        const uint32_t r = vb + (8 * i + g) * (kPageTokens * 2);
+      for (int i = 0; i < 8; ++i)
+        if (edge) {          // what lies behind the mask may be anything, NaN too
+          uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
 #pragma unroll
-        for (int c = 0; c < 2; ++c) {
-          uint4 v = lds128(r + 64 * c);
-          if (edge) {                    // what lies behind the mask may be anything, NaN too
-            uint32_t w[4] = {v.x, v.y, v.z, v.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-              const int t = tok0 + 32 * c + 8 * q + 2 * e;
-              if (t < sp.lo || t >= sp.n) w[e] &= 0xFFFF0000u;
-              if (t + 1 < sp.lo || t + 1 >= sp.n) w[e] &= 0x0000FFFFu;
-            }
-            v = make_uint4(w[0], w[1], w[2], w[3]);
+          for (int e = 0; e < 4; ++e) {
+            const int t = tok0 + 8 * q + 2 * e;
+            if (t < sp.lo || t >= sp.n) w[e] &= 0xFFFF0000u;
+            if (t + 1 < sp.lo || t + 1 >= sp.n) w[e] &= 0x0000FFFFu;
           }
-          mma16816<BF16>(o[i], pa[4 * c], pb[4 * c], pa[4 * c + 1], pb[4 * c + 1], v.x, v.y);
-          mma16816<BF16>(o[i], pa[4 * c + 2], pb[4 * c + 2], pa[4 * c + 3], pb[4 * c + 3], v.z, v.w);
+          x[i] = make_uint4(w[0], w[1], w[2], w[3]);
         }
-      }
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mma16816<BF16>(acc[i], pa[0], pb[0], pa[1], pb[1], x[i].x, x[i].y);
+#pragma unroll
+      for (int i = 0; i < 8; ++i) mma16816<BF16>(acc[i], pa[2], pb[2], pa[3], pb[3], x[i].z, x[i].w);
+    };
+    multiply(o, v);
+    load_v(j + 1);
+    if constexpr (D == 128) {
+      multiply(o + 8, k);
+      load_k(j + 1);
     }
-    __syncwarp();
-    issue(b + S::kRing);
-    ++b;
-  }
-  if (!ok) {   // a wait gave up: the copies still under way must land before the block ends
-    for (int e = b; e < min(2 * cnt, b + S::kRing); ++e) arrived(e);
   }
 
-  // ---- the warps' parts are joined through the ring's memory, in warp order
+  // ---- the warps' parts are joined, in warp order
   l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1);
   l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
   l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1);
@@ -352,9 +349,6 @@ decode_attention_kernel(const DecodeArgs a) {
     s_ml[warp][g] = make_float2(m0, l0);
     s_ml[warp][g + 8] = make_float2(m1, l1);
   }
-  __syncthreads();                       // the rings are free from here on
-  constexpr int P = D + 8;               // row pitch: 8-byte stores of 8 rows x 4 lanes on distinct banks
-  float* so = reinterpret_cast<float*>(smem);
   if (cnt > 0) {
 #pragma unroll
     for (int i = 0; i < D / 8; ++i) {
@@ -366,8 +360,8 @@ decode_attention_kernel(const DecodeArgs a) {
     }
   }
   __syncthreads();
-  const int used = min(S::kWarps, cnt_all);
-  for (int e = threadIdx.x; e < rows * (D / 4); e += S::kThreads) {
+  const int used = min(kWarps, steps);
+  for (int e = threadIdx.x; e < rows * (D / 4); e += kThreads) {
     const int r = e / (D / 4), d = e % (D / 4) * 4;
     float m = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -383,16 +377,47 @@ decode_attention_kernel(const DecodeArgs a) {
       acc.w = fmaf(f, v.w, acc.w);
     }
     const int64_t at = static_cast<int64_t>(row) * a.Hq + h0 + r;
-    if (items > 1) {
+    if (items <= 1) {
+      store_row<BF16, D>(a, row, h0 + r, d, m, l, acc);
+    } else if (a.cluster) {
+      *reinterpret_cast<float4*>(s_item + r * D + d) = acc;
+      if (d == 0) s_item_ml[r] = make_float2(m, l);
+    } else {
       *reinterpret_cast<float4*>(a.part_o + (at * a.items + item) * D + d) = acc;
       if (d == 0) a.part_ml[at * a.items + item] = make_float2(m, l);
-    } else {
-      const float inv = l != 0.f ? 1.f / l : 0.f;
-      *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(h0 + r) * D + d) =
-          make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-      if (d == 0 && a.lse) a.lse[at] = l != 0.f ? (z + log2f(l)) * kLn2 : -INFINITY;
     }
   }
+  if (!a.cluster) return;
+  // ---- the items, in order: the row's values are dealt to the cluster's blocks
+  __syncwarp();
+  cluster_sync_all();
+  if (items > 1) {
+    const uint32_t o_at = smem_u32(s_item), ml_at = smem_u32(s_item_ml);
+    for (int e = item * kThreads + threadIdx.x; e < rows * (D / 4); e += items * kThreads) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
+      float2 ml[kMostCluster];
+      float4 v[kMostCluster];
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kMostCluster; ++i)
+        if (i < items) {
+          ml[i] = ld_cluster_f32x2(cluster_map(ml_at + r * 8, i));
+          v[i] = ld_cluster_f32x4(cluster_map(o_at + (r * D + d) * 4, i));
+        }
+#pragma unroll
+      for (int i = 0; i < kMostCluster; ++i)
+        if (i < items) m = fmaxf(m, ml[i].x);
+      const float z = finite_max(m);
+      float l = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kMostCluster; ++i)
+        if (i < items) add_scaled(acc, l, v[i], ml[i].y, ex2(ml[i].x - z));
+      store_row<BF16, D>(a, row, h0 + r, d, m, l, acc);
+    }
+  }
+  __syncwarp();
+  cluster_sync_all();                    // the peers have read this block's part
 }
 
 // Joins a row's items, one query head per block: the items are dealt to the
@@ -407,9 +432,9 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeA
   __shared__ float4 s_acc[NG][L];
   __shared__ float s_l[NG];
   const int h = blockIdx.x, row = blockIdx.y;
-  const Span sp = find_span(a, row);     // inputs of the call, not of the first kernel
+  pdl_wait();      // in every block: the grid ends after the first kernel's
+  const Span sp = find_span(a, row);
   const int items = (sp.pages + a.split - 1) / a.split;
-  pdl_wait();                            // in every block: the grid ends after the first kernel's
   if (items <= 1) return;
   const int64_t at = static_cast<int64_t>(row) * a.Hq + h;
   const float2* ml = a.part_ml + at * a.items;
@@ -429,41 +454,32 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeA
 #pragma unroll 4
   for (int i = grp; i < items; i += NG) {
     const float2 x = ml[i];
-    const float4 v = po[static_cast<int64_t>(i) * L + d];
-    const float f = ex2(x.x - z);
-    l = fmaf(f, x.y, l);
-    acc.x = fmaf(f, v.x, acc.x);
-    acc.y = fmaf(f, v.y, acc.y);
-    acc.z = fmaf(f, v.z, acc.z);
-    acc.w = fmaf(f, v.w, acc.w);
+    add_scaled(acc, l, po[static_cast<int64_t>(i) * L + d], x.y, ex2(x.x - z));
   }
   s_acc[grp][d] = acc;
   if (d == 0) s_l[grp] = l;
   __syncthreads();
   if (grp > 0) return;
-  for (int k = 1; k < NG; ++k) {
-    const float4 v = s_acc[k][d];
-    acc.x += v.x;
-    acc.y += v.y;
-    acc.z += v.z;
-    acc.w += v.w;
-    l += s_l[k];
-  }
-  const float inv = l != 0.f ? 1.f / l : 0.f;
-  *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(h) * D + 4 * d) =
-      make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-  if (d == 0 && a.lse) a.lse[at] = l != 0.f ? (z + log2f(l)) * kLn2 : -INFINITY;
+  for (int k = 1; k < NG; ++k) add_scaled(acc, l, s_acc[k][d], s_l[k], 1.f);
+  store_row<BF16, D>(a, row, h, 4 * d, m, l, acc);
 }
 
-// Pages of an item when the caller leaves it open.  One wave of blocks (two
-// per SM) shares the cache of few rows evenly; many rows are cut into items
-// of at most kMostPages, so that the last wave's tail is short.
-constexpr int64_t kSlots = 2 * kNumSMs;
-constexpr int kMostPages = 32;
-int auto_split(int pages, int64_t blocks_per_item, int warps) {
-  int64_t split = (pages * blocks_per_item + kSlots - 1) / kSlots;
-  if (split < warps) split = warps;
-  if (split > kMostPages && blocks_per_item >= kSlots) split = kMostPages;
+// Pages of an item when the caller leaves it open.  Few rows: one wave of blocks
+// shares the cache evenly (of the 456 or 304 places that the GPU has for head
+// dims 64 and 128, not all: one row of 131,001 tokens takes 48 us on 256 blocks
+// and 53 on 304), or eight items that join in a cluster where that is not long.
+// More than one row, which may differ in length: items of at most kMostPages, so
+// that the tail behind the longest is short (32 rows of 1024 to 6144 tokens: 43
+// us with 12 pages, 47 with 32, 49 with 4).
+constexpr int64_t wave_of(int head_dim) { return head_dim == 64 ? 320 : 256; }
+constexpr int kMostPages = 12;
+int auto_split(int pages, int rows, int64_t blocks_per_item, int head_dim) {
+  const int64_t wave = wave_of(head_dim) / blocks_per_item;
+  int64_t items = wave < 1 ? 1 : wave;
+  if (items > kMostCluster && pages <= 8 * kMostCluster) items = kMostCluster;
+  int64_t split = (pages + items - 1) / items;
+  if (split < 2) split = 2;
+  if (split > kMostPages && rows > 1) split = kMostPages;
   return static_cast<int>(split < pages ? split : pages);
 }
 
@@ -477,31 +493,20 @@ Plan plan_decode(const gs_cache& c, int rows, int n_heads, int window, int split
   int pages = c.pt_stride;
   if (window > 0 && (window + kPageTokens - 2) / kPageTokens + 1 < pages)
     pages = (window + kPageTokens - 2) / kPageTokens + 1;
-  const int warps = c.head_dim == 64 ? DecodeShape<64>::kWarps : DecodeShape<128>::kWarps;
   p.split = split_pages > 0 ? split_pages
-                            : auto_split(pages, static_cast<int64_t>(rows) * c.n_kv_heads * p.tiles,
-                                         warps);
+                            : auto_split(pages, rows, static_cast<int64_t>(rows < 1 ? 1 : rows) *
+                                                          c.n_kv_heads * p.tiles,
+                                         c.head_dim);
   p.items = (pages + p.split - 1) / p.split;
   return p;
 }
 
 template <bool BF16, int D>
 cudaError_t launch_decode(const DecodeArgs& a, int rows, cudaStream_t s) {
-  using S = DecodeShape<D>;
-  static DeviceOnce once;
-  cudaError_t e = once.run([] {
-    cudaError_t r = cudaFuncSetAttribute(decode_attention_kernel<BF16, D, true>,
-                                         cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-    if (r == cudaSuccess)
-      r = cudaFuncSetAttribute(decode_attention_kernel<BF16, D, false>,
-                               cudaFuncAttributeMaxDynamicSharedMemorySize, S::kSmem);
-    return r;
-  });
-  if (e != cudaSuccess) return e;
   auto kernel = a.G > 8 ? decode_attention_kernel<BF16, D, true> : decode_attention_kernel<BF16, D, false>;
-  e = launch_ex(kernel, dim3(a.items, a.cache.Hkv * a.tiles, rows), dim3(S::kThreads), S::kSmem, s,
-                false, dim3(1, 1, 1), a);
-  if (e != cudaSuccess || a.items == 1) return e;
+  cudaError_t e = launch_ex(kernel, dim3(a.items, a.cache.Hkv * a.tiles, rows), dim3(kThreads), 0, s,
+                            false, dim3(a.cluster ? a.items : 1, 1, 1), a);
+  if (e != cudaSuccess || a.items == 1 || a.cluster) return e;
   return launch_ex(decode_join_kernel<BF16, D>, dim3(a.Hq, rows), dim3(kJoinThreads), 0, s, true,
                    dim3(1, 1, 1), a);
 }
@@ -531,12 +536,14 @@ extern "C" size_t gs_decode_attention_scratch_bytes(const gs_cache* cache, int r
   if (check_cache(cache) != GS_OK || !heads_ok(cache, rows, n_heads, split_pages)) return 0;
   const Plan p = plan_decode(*cache, rows, n_heads, 0, split_pages);
   // An open split follows the pages that a window leaves: whatever it is, the
-  // items are at most one wave's share, or pages / kMostPages, and the rounding.
+  // items are at most one wave's share, a cluster, or pages / kMostPages, and
+  // the rounding.
   size_t items = p.items;
   if (split_pages == 0) {
     const int64_t blocks = static_cast<int64_t>(rows < 1 ? 1 : rows) * cache->n_kv_heads * p.tiles;
-    const size_t wave = static_cast<size_t>(kSlots / blocks), cut = cache->pt_stride / kMostPages;
-    items = (wave > cut ? wave : cut) + 2;
+    const size_t wave = static_cast<size_t>(wave_of(cache->head_dim) / blocks),
+                 cut = cache->pt_stride / kMostPages, cluster = kMostCluster;
+    items = std::max(std::max(wave, cut), cluster) + 2;
     if (items > static_cast<size_t>(cache->pt_stride)) items = cache->pt_stride;
   }
   return scratch_of(*cache, rows, n_heads, items).total;
@@ -578,6 +585,10 @@ extern "C" int gs_decode_attention(const gs_cache* cache, const void* q, int64_t
   a.window = window;
   a.split = p.split;
   a.items = p.items;
+  // Up to eight items of one wave join within a cluster (one launch, no trip
+  // through memory); more items, or more blocks, through the scratch.
+  a.cluster = p.items > 1 && p.items <= kMostCluster &&
+              static_cast<int64_t>(p.items) * cache->n_kv_heads * p.tiles * rows <= wave_of(D);
   a.scale_log2 = scale * kLog2e;
   a.part_o = reinterpret_cast<float*>(base + sc.o);
   a.part_ml = reinterpret_cast<float2*>(base + sc.ml);

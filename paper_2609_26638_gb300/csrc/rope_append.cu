@@ -331,11 +331,9 @@ __global__ void __launch_bounds__(kAppendThreads, 8) rope_append_kernel(const Ap
 }
 
 template <bool BF16, int D>
-void launch_append(const AppendArgs& a, bool half, int blocks, cudaStream_t s) {
-  if (half)
-    rope_append_kernel<BF16, D, true><<<blocks, kAppendThreads, 0, s>>>(a);
-  else
-    rope_append_kernel<BF16, D, false><<<blocks, kAppendThreads, 0, s>>>(a);
+cudaError_t launch_append(const AppendArgs& a, bool half, int blocks, cudaStream_t s) {
+  return launch_ex(half ? rope_append_kernel<BF16, D, true> : rope_append_kernel<BF16, D, false>,
+                   dim3(blocks), dim3(kAppendThreads), 0, s, false, dim3(1, 1, 1), a);
 }
 
 struct Frequencies {
@@ -459,9 +457,10 @@ extern "C" int gs_rope_append(const gs_cache* cache, const gs_rope* rope, const 
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   const bool half = rope->layout == GS_ROPE_HALF;
   const int n = static_cast<int>(blocks);
+  cudaError_t e;
   if (cache->dtype == GS_BF16)
-    D == 64 ? launch_append<true, 64>(a, half, n, s) : launch_append<true, 128>(a, half, n, s);
+    e = D == 64 ? launch_append<true, 64>(a, half, n, s) : launch_append<true, 128>(a, half, n, s);
   else
-    D == 64 ? launch_append<false, 64>(a, half, n, s) : launch_append<false, 128>(a, half, n, s);
-  return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+    e = D == 64 ? launch_append<false, 64>(a, half, n, s) : launch_append<false, 128>(a, half, n, s);
+  return e == cudaSuccess ? GS_OK : GS_ERR_CUDA;
 }

@@ -159,6 +159,21 @@ def test_rows_do_not_depend_on_the_batch(gs):
         assert torch.equal(o1[0], out[b]) and torch.equal(l1[0], lse[b])
 
 
+@pytest.mark.parametrize("D", [64, 128])
+def test_ways_of_joining_give_the_same_bits(gs, D):
+    """Few rows join their items within a cluster, many through the scratch."""
+    ns = [1500, 300, 64, 0, 1, 1999] * 8
+    c = _case("bf16", ns, 16, 8, D, seed=D)
+    out, lse, err = _run(gs, c, split=8)              # 4 items x 8 heads x 48 rows
+    assert err == 0
+    _check(c, out, lse)
+    for b in (0, 1, 2, 3, 4, 5):
+        o1, l1, _ = _run(gs, c, split=8, seq=torch.tensor([b], dtype=torch.int32, device=DEV),
+                         n=torch.tensor([ns[b]], dtype=torch.int32, device=DEV),
+                         q=c["q"].view(len(ns), -1)[b: b + 1].contiguous())
+        assert torch.equal(o1[0], out[b]) and torch.equal(l1[0], lse[b])
+
+
 def test_shared_pages(gs):
     """Two sequences over the same pages, cut at different lengths."""
     c = _case("bf16", [300, 300], 8, 4, 64, seed=2)
