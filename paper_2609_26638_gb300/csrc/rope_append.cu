@@ -60,29 +60,6 @@ __device__ __forceinline__ Target find_target(const AppendArgs& a, int t) {
   return {page, slot % kPageTokens};
 }
 
-// Two fp32 values in a 64-bit register pair: one instruction for both.
-typedef unsigned long long F32x2;
-__device__ __forceinline__ F32x2 join2(float a, float b) {
-  F32x2 r;
-  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
-  return r;
-}
-__device__ __forceinline__ float2 split2(F32x2 v) {
-  float2 r;
-  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
-  return r;
-}
-__device__ __forceinline__ F32x2 mul2(F32x2 a, F32x2 b) {
-  F32x2 r;
-  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
-  return r;
-}
-__device__ __forceinline__ F32x2 fma2(F32x2 a, F32x2 b, F32x2 c) {
-  F32x2 r;
-  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
-  return r;
-}
-
 // Queries and keys.  A head's D dims lie on D / 8 neighbouring lanes, 16 bytes
 // each, so a warp holds 32 / (D / 8) heads of one token at once and goes
 // through `iters` such groups, all of queries or all of keys, four loads at a

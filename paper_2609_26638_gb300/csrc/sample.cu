@@ -39,9 +39,11 @@ constexpr float kNats = 8.f;                // of a window behind the head
 constexpr float kBinsPerNat = kBins / kNats;
 constexpr int kWindows = 5;                 // the head, and 32 nats: 2^-40 is at 27.73
 constexpr int kList = 256;                  // gathered tokens
-constexpr int kPrefix = 128;                // of which the order's first ones, kept for later searches
+constexpr int kPrefix = 64;                // of which the order's first ones, kept for later searches
 constexpr int kHead = 4096;                 // head tokens that a block notes
-constexpr double kTarget = 3500.;           // head tokens of a row that the level aims at
+constexpr double kTarget = 3500.;           // head tokens of a row that the level aims at,
+constexpr double kShare = 0.125;            // or this share of a smaller vocabulary;
+constexpr int kSmall = 512;                 // one of so few tokens is all head
 constexpr int kMostVocab = 262144;
 constexpr int kMostCluster = 8;
 
@@ -735,18 +737,22 @@ __device__ __forceinline__ void weigh(Shared& sh, const Slice<TYPE>& row) {
   uint32_t hi = 0, lo = 0, n = 0;            // at most 528 elements a thread: below 2^30
   row.each_vec([&](int i, const float (&x)[V]) {
     uint32_t head = 0;
+    const F32x2 top = join2(-row.sc.top, -row.sc.top), inv = join2(row.sc.inv_t, row.sc.inv_t);
+    const F32x2 eight = join2(8.f, 8.f), low = join2(0x1p-17f, 0x1p-17f), minus = join2(-1.f, -1.f);
 #pragma unroll
-    for (int e = 0; e < V; ++e) {
-      const float d = row.sc.d(x[e]);
-      const bool is = d >= row.sc.edge;
-      if (is) head |= 1u << e;
+    for (int e = 0; e < V; e += 2) {
+      const float2 d = split2(mul2(add2(join2(x[e], x[e + 1]), top), inv));
+      const bool is0 = d.x >= row.sc.edge, is1 = d.y >= row.sc.edge;
+      if (is0) head |= 1u << e;
+      if (is1) head |= 2u << e;
       if constexpr (TAIL) {
-        const float w = is ? 0.f : row.sc.weight(d);
-        const float h = __fadd_rz(w, 8.f);
-        const float l = __fadd_rz(__fsub_rn(w, __fsub_rn(h, 8.f)), 0x1p-17f);
-        hi += __float_as_uint(h) - 0x41000000u;
-        lo += __float_as_uint(l) - 0x37000000u;
-        if constexpr (COUNT) n += w >= 0x1p-40f;
+        const float w0 = is0 ? 0.f : row.sc.weight(d.x), w1 = is1 ? 0.f : row.sc.weight(d.y);
+        const F32x2 w = join2(w0, w1), h = add2_rz(w, eight);
+        const F32x2 l = add2_rz(add2(w, fma2(h, minus, eight)), low);
+        const float2 hf = split2(h), lf = split2(l);
+        hi += __float_as_uint(hf.x) + __float_as_uint(hf.y) - 2u * 0x41000000u;
+        lo += __float_as_uint(lf.x) + __float_as_uint(lf.y) - 2u * 0x37000000u;
+        if constexpr (COUNT) n += (w0 >= 0x1p-40f) + (w1 >= 0x1p-40f);
       }
     }
     if (HEAD && head) {
@@ -931,7 +937,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     row.sc.inv_t = fminf(fmaxf(__fdiv_rn(1.f, set.t), 1.17549435e-38f), 3.40282347e38f);
     // ---- the head; the others' total, if it can matter (min-p and top-k mostly
     // end a row within the head)
-    row.sc.edge = a.vocab <= kHead ? -28.f : fminf(row.sc.d(level), -1e-6f);
+    row.sc.edge = a.vocab <= kSmall ? -28.f : fminf(row.sc.d(level), -1e-6f);
     row.sc.edge = fmaxf(row.sc.edge, -28.f);             // nothing behind it has a weight
     row.sc.per_nat = (kBins - 1) / -row.sc.edge;
     const bool tail = !(row.sc.min_p > 1.001f * expf(row.sc.edge));
@@ -996,11 +1002,15 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
   }
 }
 
-// Blocks that share a row: one, or as many as one wave of the GPU holds (two
-// blocks an SM) while each still has a few thousand logits.
+// Blocks that share a row: more while the GPU has an SM for each and each still
+// has a few thousand logits; eight only for a few rows, as clusters of eight wait
+// for room in one GPC (17 rows of 59,392: 19 us with four blocks, 24 with eight;
+// 64 rows of 32,001: 14 us with two, 17 with four).
 int cluster_for(int rows, int vocab) {
   int n = 1;
-  while (n < kMostCluster && rows * 2 * static_cast<int64_t>(n) <= 2 * kNumSMs && vocab > n * 4096) n *= 2;
+  while (n < kMostCluster && vocab > n * 4096 &&
+         rows * 2 * static_cast<int64_t>(n) <= (n == 4 ? kNumSMs / 2 : kNumSMs))
+    n *= 2;
   return n;
 }
 
@@ -1019,7 +1029,7 @@ cudaError_t launch_sample(SampleArgs a, int rows, cudaStream_t s) {
   // its level: with `each` of its tokens among so many vectors of a thread, a
   // share of 1 - exp(-each) of the threads has one.
   constexpr int V = Elem<TYPE>::kVec;
-  const double want = fmin(kTarget, 0.88 * kHead * n), per_vec = V * want / a.vocab;
+  const double want = fmin(fmin(kTarget, kShare * a.vocab), 0.88 * kHead * n), per_vec = V * want / a.vocab;
   a.level_vecs = per_vec > 1.0 ? 1 : static_cast<int>(1.0 / per_vec + 0.5);
   const double each = per_vec * a.level_vecs;
   a.level_rank = static_cast<int>(fmin(32.0 * (1.0 - exp(-each)), 31.0) - 0.5);

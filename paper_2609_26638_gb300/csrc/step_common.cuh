@@ -40,6 +40,41 @@ __device__ __forceinline__ uint32_t pack2(float a, float b) {
   return r;
 }
 
+// Two fp32 values in a 64-bit register pair: one instruction for both.
+typedef unsigned long long F32x2;
+__device__ __forceinline__ F32x2 join2(float a, float b) {
+  F32x2 r;
+  asm("mov.b64 %0, {%1, %2};" : "=l"(r) : "f"(a), "f"(b));
+  return r;
+}
+__device__ __forceinline__ float2 split2(F32x2 v) {
+  float2 r;
+  asm("mov.b64 {%0, %1}, %2;" : "=f"(r.x), "=f"(r.y) : "l"(v));
+  return r;
+}
+__device__ __forceinline__ F32x2 mul2(F32x2 a, F32x2 b) {
+  F32x2 r;
+  asm("mul.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+__device__ __forceinline__ F32x2 fma2(F32x2 a, F32x2 b, F32x2 c) {
+  F32x2 r;
+  asm("fma.rn.f32x2 %0, %1, %2, %3;" : "=l"(r) : "l"(a), "l"(b), "l"(c));
+  return r;
+}
+
+__device__ __forceinline__ F32x2 add2(F32x2 a, F32x2 b) {
+  F32x2 r;
+  asm("add.rn.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+// rounded toward zero
+__device__ __forceinline__ F32x2 add2_rz(F32x2 a, F32x2 b) {
+  F32x2 r;
+  asm("add.rz.f32x2 %0, %1, %2;" : "=l"(r) : "l"(a), "l"(b));
+  return r;
+}
+
 // One layer of the paged cache.  A page holds [2][Hkv][64 * D] elements: keys
 // as [64 tokens][D], values transposed as [D][64 tokens].
 struct CacheView {
