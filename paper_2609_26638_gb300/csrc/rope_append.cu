@@ -20,7 +20,7 @@ namespace {
 
 constexpr int kAppendThreads = 128;
 constexpr int kAhead = 4;         // heads of a lane group that are loaded together
-constexpr int kVRows = 32;        // tokens of one V tile
+constexpr int kVRows = 32;        // tokens of one V tile at most
 
 struct AppendArgs {
   const uint16_t* qkv;
@@ -34,7 +34,7 @@ struct AppendArgs {
   const int32_t *seq, *slot, *pos;
   int* err;
   int T, Hq, v_blocks, iters;
-  int v_heads;                    // KV heads that a block of the V part takes in turn
+  int v_rows, v_heads;            // tokens of a V tile, KV heads that its block takes in turn
   int q_chunks, chunks;           // a token's chunks of query heads, and of all heads, in the Q/K part
   CacheView cache;
 };
@@ -202,7 +202,7 @@ __device__ void rotate_heads(const AppendArgs& a) {
   }
 }
 
-// Values: a tile of 32 tokens of one KV head goes through shared memory and is
+// Values: a tile of up to 32 tokens of one KV head goes through shared memory and is
 // written transposed.  Eight tokens that fill an aligned run of slots (same
 // page, consecutive rows and slots, the first slot a multiple of 8) are one
 // 16-byte store per dim, by the tile in which the run starts (it reads up to 7
@@ -218,8 +218,8 @@ __device__ void write_values(const AppendArgs& a) {
   __shared__ uint8_t run[kVRows], single[kVRows];
   __shared__ int n_run, n_single;
   const int block = blockIdx.x, groups = (a.cache.Hkv + a.v_heads - 1) / a.v_heads;
-  const int head0 = block % groups * a.v_heads, t0 = (block / groups) * kVRows;
-  const int rows = min(kVRows, a.T - t0);
+  const int head0 = block % groups * a.v_heads, t0 = (block / groups) * a.v_rows;
+  const int rows = min(a.v_rows, a.T - t0);
   auto load_rows = [&](int head, int r0, int r1) {
     const uint16_t* src = a.qkv + (a.Hq + a.cache.Hkv + head) * D;
     for (int v = r0 * (D / 8) + threadIdx.x; v < r1 * (D / 8); v += kAppendThreads) {
@@ -263,14 +263,14 @@ __device__ void write_values(const AppendArgs& a) {
     }
   }
   __syncthreads();
-  const int last = n_run ? run[n_run - 1] + 8 : 0;   // past 32: a run that ends in the next tile
+  const int last = n_run ? run[n_run - 1] + 8 : 0;   // past v_rows: a run that ends in the next tile
   for (int head = head0; head < min(head0 + a.v_heads, a.cache.Hkv); ++head) {
     if (head > head0) {
       __syncthreads();                 // the tile has been read
       load_rows(head, 0, max(rows, last));
       __syncthreads();
-    } else if (last > kVRows) {
-      load_rows(head, kVRows, last);
+    } else if (last > a.v_rows) {
+      load_rows(head, a.v_rows, last);
       __syncthreads();
     }
     // at most four runs of eight rows start in a tile; two dims at a time
@@ -421,12 +421,14 @@ extern "C" int gs_rope_append(const gs_cache* cache, const gs_rope* rope, const 
     a.chunks = a.q_chunks + (Hkv + hpw * a.iters - 1) / (hpw * a.iters);
     if (a.iters == kAhead || static_cast<int64_t>(T) * a.chunks >= 2 * 32 * kNumSMs) break;
   }
+  // a decode batch's values are scattered 2-byte stores: small tiles on many SMs
+  a.v_rows = static_cast<int64_t>(T) * Hkv >= kVRows * kNumSMs ? kVRows : 8;
   a.v_heads = static_cast<int64_t>((T + kVRows - 1) / kVRows) * Hkv >= 8 * kNumSMs ? 4 : 1;
   a.cache = cache_view(*cache);
   constexpr int warps = kAppendThreads / 32;
   const int64_t qk_blocks = (static_cast<int64_t>(T) * a.chunks + warps - 1) / warps;
   const int64_t v_blocks =
-      static_cast<int64_t>((T + kVRows - 1) / kVRows) * ((Hkv + a.v_heads - 1) / a.v_heads);
+      static_cast<int64_t>((T + a.v_rows - 1) / a.v_rows) * ((Hkv + a.v_heads - 1) / a.v_heads);
   const int64_t blocks = qk_blocks + v_blocks;
   if (static_cast<int64_t>(T) * a.chunks + warps >= (1ll << 31) || blocks >= (1ll << 31))
     return GS_ERR_UNSUPPORTED;
