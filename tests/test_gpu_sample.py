@@ -170,6 +170,19 @@ def test_ties(gs, dtype):
     assert kept[0] == 5000 and token[0] == int(float(np.float32(0.99)) * 5000)
 
 
+@pytest.mark.parametrize("rows", [1, 5, 200])
+def test_top_p_between_close_totals(gs, rows):
+    """Nearly flat rows, where a token weighs less than an estimate of the row's
+    mass may be off: top-p ends within and behind the tokens that are noted."""
+    vocab = 59392
+    g = torch.Generator(device=DEV).manual_seed(rows)
+    x = (0.02 * torch.randn(rows, vocab, device=DEV, generator=g)).to(torch.float32)
+    rng = np.random.default_rng(rows)
+    for p in (0.001, 0.01, 0.03, 0.055, 0.06, 0.3, 0.999):
+        par = dict(top_p=[p] * rows)
+        _check(x, _run(gs, x, rng.random(rows).astype(np.float32), **par), **par)
+
+
 def test_masked_and_infinite_logits(gs):
     """-inf and the type's lowest value are never drawn next to ordinary
     logits; NaN counts as -inf; +inf takes the row; a row of -inf gives -1."""
