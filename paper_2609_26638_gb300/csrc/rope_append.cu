@@ -10,6 +10,12 @@
 // is rounded once at the store.  cos and sin come from a table that is built
 // in 64 bits (gs_rope_table): the fp32 product position * frequency is off by
 // up to 2^-25 of the angle, 0.004 rad at position 131,072.
+//
+// Measured: 8191 prompt tokens (32 query and 8 KV heads of 128, bf16, norm, full
+// rotation) 38 us, 5.3 TB/s, with issue slots 53% busy and the loads' latency the
+// largest stall (46 us with blocks of 256 threads, whose warps end together; 41
+// with 16 instead of 8 heads a lane group); a batch of 256 single tokens 4.2 us;
+// one token 2.9 us, the launch.
 #include <cmath>
 
 #include "internal.h"

@@ -10,19 +10,25 @@
 // and, from the maxima of the threads' first logits, a level that about 3500
 // logits of the row exceed, whatever its distribution.  The second (the row is
 // in L2 by then) notes these, the head, in shared memory and adds up the
-// weights of the others.  The head goes into 512 bins of equal width in d = (l - M) / T; the
-// blocks add up their bins; prefix sums over them give the bin in which a
-// target is passed, and only the tokens of that bin are gathered in block 0,
-// ranked by counting and searched.  Where the bins up to it hold few tokens in
-// all, they are gathered together and serve the later searches too.  A target
-// behind the head takes a pass for each 8 nats; a bin too full for the list
-// (equal logits, a hot row) is divided further by the bits of the logit, and a
-// logit too frequent for it by index.
+// weights of the others.  The head goes into 512 bins of equal width in
+// d = (l - M) / T; the blocks add up their bins; prefix sums over them give the
+// bin in which a target is passed, and only the tokens of that bin are gathered
+// in block 0, ranked by counting and searched.  Where the bins up to it hold few
+// tokens in all, they are gathered together and serve the later searches too.  A
+// target behind the head takes a pass for each 8 nats; a bin too full for the
+// list (equal logits, a hot row) is divided further by the bits of the logit,
+// and a logit too frequent for it by index.
 //
 // Masses are integers of 40 bits, so sums are exact and the result does not
 // depend on the order of atomics, the slices or the cluster.  (A 64-bit add in
 // shared memory is a compare-and-swap loop: the low and the high word are added
 // apart, the high one only when it changes.)
+//
+// Many rows are bound by instruction issue, about 55 a logit, 25 of them its
+// weight: 544 rows of 59,392 (bf16, top-p) take 93 us, 10% of the copy rate; a
+// head of 2000 tokens instead of 3500 makes it 178 us, as more rows end behind
+// it.  Few rows are bound by the chain of passes and barriers: one row of 4096
+// takes 10 us, 32 rows of 59,392 (fp32, mixed settings) 22 us.
 #include <cmath>
 #include <cstddef>
 
@@ -39,7 +45,7 @@ constexpr float kNats = 8.f;                // of a window behind the head
 constexpr float kBinsPerNat = kBins / kNats;
 constexpr int kWindows = 5;                 // the head, and 32 nats: 2^-40 is at 27.73
 constexpr int kList = 256;                  // gathered tokens
-constexpr int kPrefix = 64;                // of which the order's first ones, kept for later searches
+constexpr int kPrefix = 64;                 // of which the order's first ones, kept for later searches
 constexpr int kHead = 4096;                 // head tokens that a block notes
 constexpr double kTarget = 3500.;           // head tokens of a row that the level aims at,
 constexpr double kShare = 0.125;            // or this share of a smaller vocabulary;
@@ -51,7 +57,8 @@ struct SampleArgs {
   const void* logits;
   int64_t ld;
   int vocab, slice;                         // tokens of a block's slice, a multiple of 16
-  int level_vecs, level_rank;               // of 32 threads' maxima over so many vectors, which sets the level
+  // of 32 threads' maxima over their first level_vecs vectors, which sets the level
+  int level_vecs, level_rank;
   const float *temperature, *top_p, *min_p;
   const int32_t* top_k;
   const float* u;
@@ -88,7 +95,7 @@ struct Shared {
   unsigned long long head_upto_m[kBins];    // the head's merged bins: totals up to and with each
   uint32_t head_upto_c[kBins];
   float2 head[kHead];                       // the slice's logits in the head, and (as bits) their places
-  alignas(16) uint4 edge[2];                            // the slice's first and last vector
+  alignas(16) uint4 edge[2];                // the slice's first and last vector
   unsigned long long warp_mass[kThreads / 32];
   // of every block, written by it: the mass and number of its other tokens
   unsigned long long tail_mass[kMostCluster];
@@ -616,7 +623,7 @@ struct Search {
   // Block 0: each entry's rank, and the mass ahead of it, by counting; an
   // entry's comparisons are shared by as many neighbouring threads as there are.
   __device__ void rank_list() {
-    const int n = sh.list_n;
+    const int n = min(sh.list_n, kList);
     int share = 32;
     while (share > 1 && share * n > kThreads) share /= 2;
     const int e = threadIdx.x / share, part = threadIdx.x % share;
@@ -646,7 +653,7 @@ struct Search {
   __device__ void cut_list(bool by_count, unsigned long long target, unsigned long long base_m,
                            uint32_t base_c, bool last) {
     const int e = threadIdx.x;
-    if (e >= sh.list_n) return;
+    if (e >= min(sh.list_n, kList)) return;
     const unsigned long long m = base_m + sh.before[e], own = sh.list[e].mass;
     const uint32_t c = base_c + sh.rank[e];
     if (by_count ? c == target : m <= target && target < m + own)
@@ -728,9 +735,9 @@ struct Search {
 };
 
 // One pass over the slice.  HEAD: the elements at or above the edge are noted.
-// TAIL: the mass of the others, and (COUNT) their number.  A weight's 40 bits are taken as two
-// sums: adding 8 (then 2^-17, to the rest) with rounding toward zero leaves
-// floor(w 2^20) (then the next 20 bits) in the low bits of the result.
+// TAIL: the mass of the others, and (COUNT) their number.  A weight's 40 bits
+// are taken as two sums: adding 8 (then 2^-17, to the rest) with rounding toward
+// zero leaves floor(w 2^20) (then the next 20 bits) in the low bits of the result.
 template <int TYPE, bool HEAD, bool TAIL, bool COUNT>
 __device__ __forceinline__ void weigh(Shared& sh, const Slice<TYPE>& row) {
   constexpr int V = Elem<TYPE>::kVec;
@@ -831,6 +838,11 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
     sh.head_n = 0;
     sh.list_n = 0;
     sh.best = kMostVocab;
+    sh.bin = 0;
+    sh.bin_mass = 0;
+    sh.bin_before = 0;
+    sh.bin_cnt = 0;
+    for (Cut& c : sh.cut) c = {0u, 0u, 0ull};
     sh.own_tail_mass = 0;
     sh.own_tail_cnt = 0;
     if (rank == 0)           // the others' copies are written below
@@ -988,7 +1000,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
       }
     }
     if (rank == 0 && threadIdx.x == 0) {
-      token = static_cast<int>(c.idx);
+      // (a row that someone writes meanwhile may give any index: not beyond it)
+      token = min(static_cast<int>(c.idx), a.vocab - 1);
       // from d, as the integer weight of an unlikely token is coarse; the best
       // token's 2^40 is always part of the mass
       const float d = row.sc.d(load_logit<TYPE>(a.logits, r * a.ld + token));
