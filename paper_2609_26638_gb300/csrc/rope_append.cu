@@ -12,10 +12,10 @@
 // up to 2^-25 of the angle, 0.004 rad at position 131,072.
 //
 // Measured: 8191 prompt tokens (32 query and 8 KV heads of 128, bf16, norm, full
-// rotation) 38 us, 5.3 TB/s, with issue slots 53% busy and the loads' latency the
-// largest stall (46 us with blocks of 256 threads, whose warps end together; 41
-// with 16 instead of 8 heads a lane group); a batch of 256 single tokens 4.2 us;
-// one token 2.9 us, the launch.
+// rotation) 37 us, 5.5 TB/s, with issue slots 58% busy and the loads' latency the
+// largest stall (45 us with blocks of 256 threads, whose warps end together; 38
+// with 16 instead of 8 heads a lane group); a batch of 256 single tokens 4.3 us;
+// one token 2.7 us, the launch.
 #include <cmath>
 
 #include "internal.h"
@@ -66,14 +66,14 @@ __device__ __forceinline__ Target find_target(const AppendArgs& a, int t) {
   return {page, slot % kPageTokens};
 }
 
-// Queries and keys.  A head's D dims lie on D / 8 neighbouring lanes, 16 bytes
-// each, so a warp holds 32 / (D / 8) heads of one token at once and goes
-// through `iters` such groups, all of queries or all of keys, four loads at a
-// time.  Gain and rotation are the same for all heads, so they are made into two
-// factors per element once, and two elements go through each instruction:
-//   out = rsqrt(...) * (x * A + partner * B),  A = gain cos, B = -+ partner's gain sin
-// A half-layout pair sits on two lanes R / 16 apart: the partner's raw 16-bit
-// values come by shuffle.
+// Queries and keys.  A head's D dims lie on D / 8 neighbouring lanes, so a warp
+// holds 32 / (D / 8) heads of one token at once and goes through `iters` such
+// groups, all of queries or all of keys, four at a time.  A lane's eight dims are
+// two fours a and b: neighbours, or in the half layout dims i and i + R / 2, so
+// that pairs never lie on two lanes.  Gain and rotation are the same for all
+// heads; they are made into two factors per element once, and two elements go
+// through each instruction:
+//   out_a = rsqrt(...) * (a * A_a + b * B_a),  A = gain cos, B = -+ partner's gain sin
 template <bool BF16, int D, bool HALF>
 __device__ void rotate_heads(const AppendArgs& a) {
   constexpr int LPH = D / 8, HPW = 32 / LPH;
@@ -87,15 +87,21 @@ __device__ void rotate_heads(const AppendArgs& a) {
   const int h0 = first + lane / LPH;
   const int heads = keys ? a.cache.Hkv : a.Hq;
   const int iters = min(a.iters, (heads - first + HPW - 1) / HPW);
-  const uint16_t* row = a.qkv + t * a.ld_qkv + (keys ? a.Hq * D : 0) + sub * 8;
-  uint4 x[kAhead];
-  auto load = [&](int i0) {
+  const int mine = min(iters, (heads - h0 + HPW - 1) / HPW);   // of them, with a head for this lane
+  const bool turns = sub * 8 < 2 * a.half;
+  const int da = HALF && turns ? sub * 4 : sub * 8, db = HALF && turns ? a.half + sub * 4 : da + 4;
+  const uint16_t* src = a.qkv + t * a.ld_qkv + ((keys ? a.Hq : 0) + h0) * D + da;
+  uint2 xa[kAhead], xb[kAhead];
+  auto load = [&](int i0) {   // the next kAhead heads
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int h = h0 + (i0 + i) * HPW;
-      x[i] = make_uint4(0, 0, 0, 0);
-      if (h < heads) x[i] = *reinterpret_cast<const uint4*>(row + h * D);
+      xa[i] = xb[i] = make_uint2(0, 0);
+      if (i0 + i < mine) {
+        xa[i] = *reinterpret_cast<const uint2*>(src + i * HPW * D);
+        xb[i] = *reinterpret_cast<const uint2*>(src + i * HPW * D + (db - da));
+      }
     }
+    src += kAhead * HPW * D;
   };
   load(0);
   int pos = a.pos[t];
@@ -103,28 +109,26 @@ __device__ void rotate_heads(const AppendArgs& a) {
     if (lane == 0) atomicExch(a.err, kErrBounds);
     pos = pos < 0 ? 0 : a.table_rows - 1;
   }
-  const bool turns = sub * 8 < 2 * a.half;
-  const bool second = HALF && sub * 8 >= a.half;
-  const int partner = HALF && turns ? (second ? sub - a.half / 8 : sub + a.half / 8) : sub;
   const __nv_bfloat16* gain = keys ? a.k_gain : a.q_gain;
-  float A[8], B[8];
+  float A[8], B[8];   // of a's four elements, then of b's
 #pragma unroll
   for (int e = 0; e < 8; ++e) {
     A[e] = 1.f;
     B[e] = 0.f;
   }
   if (turns) {
-    const float4* r = reinterpret_cast<const float4*>(
-        a.table + static_cast<int64_t>(pos) * a.half +
-        (HALF ? sub * 8 - (second ? a.half : 0) : sub * 4));
+    const float4* r = reinterpret_cast<const float4*>(a.table + static_cast<int64_t>(pos) * a.half +
+                                                      sub * 4);
 #pragma unroll
-    for (int e = 0; e < (HALF ? 4 : 2); ++e) {
-      const float4 v = r[e];
+    for (int e = 0; e < 2; ++e) {
+      const float4 v = r[e];   // cos, sin of the lane's pairs 2e and 2e + 1
       if constexpr (HALF) {
-        A[2 * e] = v.x;
-        A[2 * e + 1] = v.z;
-        B[2 * e] = second ? v.y : -v.y;
-        B[2 * e + 1] = second ? v.w : -v.w;
+        A[2 * e] = A[4 + 2 * e] = v.x;
+        A[2 * e + 1] = A[5 + 2 * e] = v.z;
+        B[2 * e] = -v.y;
+        B[2 * e + 1] = -v.w;
+        B[4 + 2 * e] = v.y;
+        B[5 + 2 * e] = v.w;
       } else {
         A[4 * e] = A[4 * e + 1] = v.x;
         A[4 * e + 2] = A[4 * e + 3] = v.z;
@@ -136,16 +140,17 @@ __device__ void rotate_heads(const AppendArgs& a) {
     }
   }
   if (gain) {
-    const uint4 own = *reinterpret_cast<const uint4*>(gain + sub * 8);
-    const uint4 oth = *reinterpret_cast<const uint4*>(gain + partner * 8);
-    const uint32_t w[4] = {own.x, own.y, own.z, own.w}, p[4] = {oth.x, oth.y, oth.z, oth.w};
+    const uint2 ga = *reinterpret_cast<const uint2*>(gain + da);
+    const uint2 gb = *reinterpret_cast<const uint2*>(gain + db);
+    const float2 g[4] = {unpack2<true>(ga.x), unpack2<true>(ga.y), unpack2<true>(gb.x),
+                         unpack2<true>(gb.y)};
 #pragma unroll
     for (int e = 0; e < 4; ++e) {
-      const float2 f = unpack2<true>(w[e]), q = unpack2<true>(p[e]);
-      A[2 * e] *= f.x;
-      A[2 * e + 1] *= f.y;
-      B[2 * e] *= HALF ? q.x : q.y;
-      B[2 * e + 1] *= HALF ? q.y : q.x;
+      const float2 q = HALF ? g[e ^ 2] : make_float2(g[e].y, g[e].x);   // the partners'
+      A[2 * e] *= g[e].x;
+      A[2 * e + 1] *= g[e].y;
+      B[2 * e] *= q.x;
+      B[2 * e + 1] *= q.y;
     }
   }
   F32x2 A2[4], B2[4];
@@ -154,28 +159,29 @@ __device__ void rotate_heads(const AppendArgs& a) {
     A2[e] = join2(A[2 * e], A[2 * e + 1]);
     B2[e] = join2(B[2 * e], B[2 * e + 1]);
   }
-  // where head 0 goes, and from there the next one
-  uint16_t* out = nullptr;
-  int64_t step = D;
+  // where the lane's first head goes, and from there the next one; how many go
+  uint16_t* out;
+  int64_t step = HPW * D;
+  int stored = mine;
   if (!keys) {
-    out = a.q_out + t * a.ld_q + sub * 8;
+    out = a.q_out + t * a.ld_q + h0 * D + da;
   } else {
     const Target to = find_target(a, t);
-    if (to.page >= 0) out = a.cache.block(to.page, 0, 0, D) + to.at * D + sub * 8;
-    step = kPageTokens * D;
+    if (to.page < 0) stored = 0;
+    out = a.cache.block(max(to.page, 0), 0, h0, D) + to.at * D + da;
+    step = HPW * (kPageTokens * D);
   }
 #pragma unroll 1
   for (int i0 = 0; i0 < iters; i0 += kAhead) {
     if (i0) load(i0);
 #pragma unroll
     for (int i = 0; i < kAhead; ++i) {
-      const int h = h0 + (i0 + i) * HPW;
-      const uint32_t raw[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+      const float2 f[4] = {unpack2<BF16>(xa[i].x), unpack2<BF16>(xa[i].y), unpack2<BF16>(xb[i].x),
+                           unpack2<BF16>(xb[i].y)};
       F32x2 y[4], ss = join2(0.f, 0.f);
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        const float2 f = unpack2<BF16>(raw[e]);
-        y[e] = join2(f.x, f.y);
+        y[e] = join2(f[e].x, f[e].y);
         ss = fma2(y[e], y[e], ss);
       }
       float r = 1.f;
@@ -187,23 +193,25 @@ __device__ void rotate_heads(const AppendArgs& a) {
         r = rsqrtf(s * (1.f / D) + a.eps);
       }
       const F32x2 r2 = join2(r, r);
+      F32x2 v[4];
+#pragma unroll
+      for (int e = 0; e < 4; ++e) v[e] = mul2(y[e], A2[e]);
+      if (turns) {   // (else B is 0, but the partner may be infinite)
+#pragma unroll
+        for (int e = 0; e < 4; ++e)
+          v[e] = fma2(HALF ? y[e ^ 2] : join2(f[e].y, f[e].x), B2[e], v[e]);
+      }
       uint32_t o[4];
 #pragma unroll
       for (int e = 0; e < 4; ++e) {
-        F32x2 z;   // the partners' values; where nothing turns, 0 (B is 0, but x may be infinite)
-        if constexpr (HALF) {
-          const uint32_t p = __shfl_sync(0xFFFFFFFFu, raw[e], lane - sub + partner);
-          const float2 f = unpack2<BF16>(turns ? p : 0u);
-          z = join2(f.x, f.y);
-        } else {
-          const float2 f = unpack2<BF16>(turns ? raw[e] : 0u);
-          z = join2(f.y, f.x);
-        }
-        const float2 v = split2(mul2(fma2(z, B2[e], mul2(y[e], A2[e])), r2));
-        o[e] = pack2<BF16>(v.x, v.y);
+        const float2 w = split2(mul2(v[e], r2));
+        o[e] = pack2<BF16>(w.x, w.y);
       }
-      if (h < heads && out)
-        *reinterpret_cast<uint4*>(out + h * step) = make_uint4(o[0], o[1], o[2], o[3]);
+      if (i0 + i < stored) {
+        *reinterpret_cast<uint2*>(out) = make_uint2(o[0], o[1]);
+        *reinterpret_cast<uint2*>(out + (db - da)) = make_uint2(o[2], o[3]);
+      }
+      out += step;
     }
   }
 }
