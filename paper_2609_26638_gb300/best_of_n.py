@@ -180,6 +180,8 @@ def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: O
     """n continuations of ``new`` tokens; (tokens [n, new], sum of log-probabilities [n]).
 
     uniforms: [new, n] fp32 on the decoder's device, or drawn from ``seed``."""
+    if not prompt or n < 1 or new < 0:
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "an empty prompt, n < 1 or new < 0")
     dec.stream.wait_stream(torch.cuda.current_stream(dec.device))
     with torch.cuda.stream(dec.stream):
         if uniforms is None:

@@ -498,7 +498,7 @@ Plan plan_decode(const gs_cache& c, int rows, int n_heads, int window, int split
   int pages = c.pt_stride;
   if (window > 0 && (window + kPageTokens - 2) / kPageTokens + 1 < pages)
     pages = (window + kPageTokens - 2) / kPageTokens + 1;
-  p.split = split_pages > 0 ? split_pages
+  p.split = split_pages > 0 ? std::min(split_pages, c.pt_stride)
                             : auto_split(pages, rows, static_cast<int64_t>(rows < 1 ? 1 : rows) *
                                                           c.n_kv_heads * p.tiles,
                                          c.head_dim);
@@ -528,7 +528,7 @@ Scratch scratch_of(const gs_cache& c, int rows, int n_heads, size_t items) {
 }
 
 bool heads_ok(const gs_cache* c, int rows, int n_heads, int split_pages) {
-  return rows >= 0 && n_heads >= 1 && n_heads <= (1 << 16) && n_heads % c->n_kv_heads == 0 &&
+  return rows >= 0 && n_heads >= 1 && n_heads < (1 << 16) && n_heads % c->n_kv_heads == 0 &&
          split_pages >= 0;
 }
 
@@ -569,7 +569,9 @@ extern "C" int gs_decode_attention(const gs_cache* cache, const void* q, int64_t
   if (ld_q < width || ld_out < width || ld_q % 8 || ld_out % 8 || !aligned16(q) || !aligned16(out) ||
       (reinterpret_cast<uintptr_t>(scratch) & 255))
     return GS_ERR_INVALID_ARG;
+  if (!aligned4(seq, n, lse)) return GS_ERR_INVALID_ARG;
   if (rows > 65535) return GS_ERR_UNSUPPORTED;
+  if (window >= cache->pt_stride * kPageTokens) window = 0;   // no row is longer
   if (scratch_bytes < gs_decode_attention_scratch_bytes(cache, rows, n_heads, split_pages))
     return GS_ERR_OOM;
   if (rows == 0) return GS_OK;

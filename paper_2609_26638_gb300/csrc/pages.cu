@@ -53,7 +53,8 @@ extern "C" int gs_pages_copy(const void* src, int src_pages, void* dst, int dst_
   if (!src || !dst || !src_ids || !dst_ids || !err || src_pages < 1 || dst_pages < 1 ||
       n_layers < 1 || n < 0 || page_bytes < 16 || page_bytes % 16)
     return GS_ERR_INVALID_ARG;
-  if (!aligned16(src) || !aligned16(dst)) return GS_ERR_INVALID_ARG;
+  if (!aligned16(src) || !aligned16(dst) || !aligned4(src_ids, dst_ids, err))
+    return GS_ERR_INVALID_ARG;
   // the grid holds a layer and a page per index
   if (n_layers > 65535 || page_bytes > (1ll << 30)) return GS_ERR_UNSUPPORTED;
   const int page_vecs = static_cast<int>(page_bytes / 16);

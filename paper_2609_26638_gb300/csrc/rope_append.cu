@@ -402,7 +402,8 @@ extern "C" int gs_rope_append(const gs_cache* cache, const gs_rope* rope, const 
     return GS_ERR_INVALID_ARG;
   if (!qkv || !seq || !slot || !pos || !q_out || !err || T < 0 || n_heads < 1 || n_heads % Hkv)
     return GS_ERR_INVALID_ARG;
-  if (!q_gain != !k_gain || !(eps >= 0.f)) return GS_ERR_INVALID_ARG;
+  if (!q_gain != !k_gain || !(eps >= 0.f) || !aligned4(seq, slot, pos, err))
+    return GS_ERR_INVALID_ARG;
   const int64_t width = (static_cast<int64_t>(n_heads) + 2 * Hkv) * D;
   if (width > (1 << 24)) return GS_ERR_UNSUPPORTED;
   if (ld_qkv < width || ld_q < static_cast<int64_t>(n_heads) * D || ld_qkv % 8 || ld_q % 8 ||

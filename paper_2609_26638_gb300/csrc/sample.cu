@@ -1060,6 +1060,9 @@ extern "C" int gs_sample(const void* logits, int64_t ld, int rows, int vocab, in
   if (!logits || !params || !u || !token || rows < 0 || vocab < 1 || ld < vocab)
     return GS_ERR_INVALID_ARG;
   if (dtype != GS_F16 && dtype != GS_BF16 && dtype != GS_F32) return GS_ERR_INVALID_ARG;
+  if (!aligned4(params->temperature, params->top_p, params->min_p, params->top_k, u, token, logprob,
+                kept))
+    return GS_ERR_INVALID_ARG;
   if (reinterpret_cast<uintptr_t>(logits) % (dtype == GS_F32 ? 4 : 2)) return GS_ERR_INVALID_ARG;
   if (vocab > kMostVocab || rows > (1 << 24)) return GS_ERR_UNSUPPORTED;
   if (rows == 0) return GS_OK;

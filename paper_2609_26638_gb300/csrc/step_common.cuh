@@ -115,10 +115,15 @@ class DeviceOnce {
 };
 
 inline bool aligned16(const void* p) { return (reinterpret_cast<uintptr_t>(p) & 15) == 0; }
+// All of them aligned for 32-bit elements (NULL is).
+template <class... P>
+inline bool aligned4(const P*... p) {
+  return ((reinterpret_cast<uintptr_t>(p) | ...) & 3) == 0;
+}
 
 // GS_OK, or what is wrong with a cache descriptor.
 inline int check_cache(const gs_cache* c) {
-  if (!c || !c->kv || !c->page_table || !aligned16(c->kv) || c->n_pages < 1 || c->n_kv_heads < 1 ||
+  if (!c || !c->kv || !c->page_table || !aligned16(c->kv) || !aligned4(c->page_table) || c->n_pages < 1 || c->n_kv_heads < 1 ||
       c->n_seq < 1 || c->pt_stride < 1 || c->pt_stride > (1 << 24))
     return GS_ERR_INVALID_ARG;
   if (c->dtype != GS_F16 && c->dtype != GS_BF16) return GS_ERR_INVALID_ARG;

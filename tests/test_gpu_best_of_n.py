@@ -103,10 +103,68 @@ def test_continuations(bn):
     assert same >= 4
 
 
+def test_graph_replay(bn):
+    """The four operators captured in one graph: replays give the eager results."""
+    from paper_2609_26638_gb300 import gs
+    from paper_2609_26638_gb300.cache import PagePool
+    g = torch.Generator(device=DEV).manual_seed(0)
+    st = torch.cuda.Stream()
+    pool = PagePool(n_layers=1, n_pages=8, n_kv_heads=2, head_dim=64, dtype=torch.float16, max_seqs=2,
+                    max_ctx=256, stream=st)
+    seq = pool.open()
+    pool.prepare([(seq, 0, 100)])
+    table = torch.empty(256, 32, 2, device=DEV)
+    qkv = torch.randn(1, 8 * 64, device=DEV, generator=g).half()
+    logits = torch.randn(1, 999, device=DEV, generator=g).half()
+    i32 = [torch.tensor([v], dtype=torch.int32, device=DEV) for v in (seq, 99, 100, 0, 7)]
+    u = torch.full((1,), 0.37, device=DEV)
+    q, out = torch.zeros(2, 1, 4 * 64, dtype=torch.float16, device=DEV)
+    token = torch.zeros(1, dtype=torch.int32, device=DEV)
+    cache = pool.layer(0)
+    scratch = torch.zeros(gs.gs_decode_attention_scratch_bytes(cache, 1, 4, 1), dtype=torch.uint8,
+                          device=DEV)
+    rope, par = gs.gs_rope(table.data_ptr(), 256, 64, gs.ROPE_HALF), gs.gs_sample_params(0, 0, 0, 0)
+    gs.gs_rope_table(gs.gs_rope_scaling(kind=gs.ROPE_PLAIN, theta=1e4), 64, 256, table.data_ptr(),
+                     torch.cuda.current_stream().cuda_stream)
+    torch.cuda.synchronize()
+
+    def step():
+        s = torch.cuda.current_stream().cuda_stream
+        gs.gs_rope_append(cache, rope, qkv.data_ptr(), 8 * 64, 1, 4, 0, 0, 1e-6, i32[0].data_ptr(),
+                          i32[1].data_ptr(), i32[1].data_ptr(), q.data_ptr(), 4 * 64,
+                          pool.err.data_ptr(), s)
+        gs.gs_decode_attention(cache, q.data_ptr(), 4 * 64, i32[0].data_ptr(), i32[2].data_ptr(), 1, 4,
+                               0.125, 0, out.data_ptr(), 4 * 64, 0, 1, scratch.data_ptr(),
+                               scratch.numel(), s)
+        gs.gs_sample(logits.data_ptr(), 999, 1, 999, gs.GS_F16, par, u.data_ptr(), token.data_ptr(), 0,
+                     0, s)
+        gs.gs_pages_copy(pool.kv.data_ptr(), 8, pool.kv.data_ptr(), 8, 1, pool.kv[0, 0].numel() * 2,
+                         i32[3].data_ptr(), i32[4].data_ptr(), 1, pool.err.data_ptr(), s)
+
+    with torch.cuda.stream(st):
+        step()
+        st.synchronize()
+        want = [t.clone() for t in (q, out, token, pool.kv)]
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=st):
+            step()
+        for t in (q, out, token):
+            t.zero_()
+        pool.kv[0, 7].zero_()
+        graph.replay()
+    st.synchronize()
+    assert all(torch.equal(a, b) for a, b in zip(want, (q, out, token, pool.kv)))
+    assert (out != 0).any() and (pool.kv[0, 7] == pool.kv[0, 0]).all()
+
+
 def test_greedy_is_the_argmax(bn):
     shape = bn.Shape()
     dec = _decoder(bn, shape)
     prompt = list(range(40))
+    from paper_2609_26638_gb300 import gs
+    for bad in (([], 2, 6), (prompt, 0, 6), (prompt, 2, -1)):
+        with pytest.raises(gs.GsError):
+            bn.best_of_n(dec, *bad)
     tokens, total = bn.best_of_n(dec, prompt, 2, 6, temperature=0.0)
     assert torch.equal(tokens[0], tokens[1]) and (total == 0).all()
     seq = dec.pool.open()

@@ -107,7 +107,7 @@ def test_lengths_and_groups(gs, dtype, D, Hq, Hkv):
 
 
 @pytest.mark.parametrize("D", [64, 128])
-@pytest.mark.parametrize("window", [1, 2, 63, 64, 65, 100, 640, 5000])
+@pytest.mark.parametrize("window", [1, 2, 63, 64, 65, 100, 640, 5000, 2 ** 31 - 1])
 def test_window(gs, D, window):
     """Keys before the window have no influence: they are NaN."""
     ns = [0, 1, 64, 65, 200, 777, 1290]
@@ -124,7 +124,7 @@ def test_window(gs, D, window):
         _check(c, out, lse, window)
 
 
-@pytest.mark.parametrize("split", [1, 2, 5, 40, 1000])
+@pytest.mark.parametrize("split", [1, 2, 5, 40, 1000, 2 ** 31 - 1])
 def test_splits(gs, split):
     """Any division of the length, the joining kernel's many items included."""
     c = _case("fp16", [4500, 64, 0, 321], 16, 2, 64, seed=split)

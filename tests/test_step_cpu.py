@@ -29,7 +29,7 @@ def _refused(gs, code, f, *args):
 
 
 BAD_CACHES = [dict(kv=0), dict(kv=P + 8), dict(n_pages=0), dict(n_kv_heads=0), dict(page_table=0),
-              dict(n_seq=0), dict(pt_stride=0), dict(dtype=2), dict(dtype=-1)]
+              dict(n_seq=0), dict(pt_stride=0), dict(dtype=2), dict(dtype=-1), dict(page_table=P + 2)]
 
 
 def test_rope_append_refuses(gs):
@@ -47,7 +47,7 @@ def test_rope_append_refuses(gs):
     for bad in ((0, 100, 64, 0), (P + 4, 100, 64, 0), (P, 0, 64, 0), (P, 100, 64, 2), (P, 100, 8, 0),
                 (P, 100, 40, 0), (P, 100, 80, 0)):
         _refused(gs, gs.GS_ERR_INVALID_ARG, lambda: call(rp=gs.gs_rope(*bad)))
-    for bad in (dict(qkv=0), dict(qkv=P + 2), dict(ld=8 * 64 - 8), dict(ld=8 * 64 + 4), dict(T=-1),
+    for bad in (dict(seq=P + 2), dict(slot=P + 1), dict(pos=P + 2), dict(err=P + 2), dict(qkv=0), dict(qkv=P + 2), dict(ld=8 * 64 - 8), dict(ld=8 * 64 + 4), dict(T=-1),
                 dict(Hq=3), dict(Hq=0), dict(qg=0), dict(kg=0), dict(qg=P + 2), dict(eps=-1.0),
                 dict(eps=float("nan")), dict(seq=0), dict(slot=0), dict(pos=0), dict(q=0),
                 dict(ldq=4 * 64 - 8), dict(ldq=4 * 64 + 2), dict(err=0),
@@ -83,7 +83,8 @@ def test_decode_attention_refuses(gs):
     for bad in (dict(q=0), dict(q=P + 2), dict(ldq=4 * 64 - 8), dict(ldq=4 * 64 + 4), dict(n=0),
                 dict(rows=-1), dict(Hq=3), dict(scale=0.0), dict(scale=-1.0), dict(scale=float("inf")),
                 dict(scale=float("nan")), dict(window=-1), dict(out=0), dict(out=P + 8),
-                dict(ldo=4 * 64 - 8), dict(split=-1), dict(scratch=0), dict(scratch=P + 16)):
+                dict(ldo=4 * 64 - 8), dict(split=-1), dict(scratch=0), dict(scratch=P + 16),
+                dict(seq=P + 2), dict(n=P + 2), dict(lse=P + 1)):
         _refused(gs, gs.GS_ERR_INVALID_ARG, lambda: call(**bad))
     _refused(gs, gs.GS_ERR_UNSUPPORTED, lambda: call(rows=65536, nb=1 << 60))
     need = gs.gs_decode_attention_scratch_bytes(_cache(gs), 3, 4, 0)
@@ -91,6 +92,11 @@ def test_decode_attention_refuses(gs):
     _refused(gs, gs.GS_ERR_OOM, lambda: call(nb=need - 1))
     assert gs.gs_decode_attention_scratch_bytes(_cache(gs), 3, 4, 1) > \
         gs.gs_decode_attention_scratch_bytes(_cache(gs), 3, 4, 8)
+    # the largest numbers are not added up
+    most = 2 ** 31 - 1
+    assert gs.gs_decode_attention_scratch_bytes(_cache(gs), 3, 4, most) == \
+        gs.gs_decode_attention_scratch_bytes(_cache(gs), 3, 4, 8)
+    call(rows=0, window=most, split=most)
     call(rows=0)
 
 
@@ -103,7 +109,10 @@ def test_sample_refuses(gs):
         gs.gs_sample(*{**base, **kw}.values())
 
     for bad in (dict(x=0), dict(ld=999), dict(rows=-1), dict(vocab=0), dict(dt=3), dict(dt=-1),
-                dict(u=0), dict(token=0), dict(x=P + 1), dict(x=P + 2, dt=gs.GS_F32)):
+                dict(u=0), dict(token=0), dict(x=P + 1), dict(x=P + 2, dt=gs.GS_F32), dict(u=P + 2),
+                dict(token=P + 2), dict(logprob=P + 2), dict(kept=P + 1),
+                dict(params=gs.gs_sample_params(P + 2, 0, 0, 0)),
+                dict(params=gs.gs_sample_params(0, 0, 0, P + 1))):
         _refused(gs, gs.GS_ERR_INVALID_ARG, lambda: call(**bad))
     _refused(gs, gs.GS_ERR_UNSUPPORTED, lambda: call(vocab=262145, ld=262145))
     call(rows=0)
@@ -116,7 +125,8 @@ def test_pages_copy_refuses(gs):
         gs.gs_pages_copy(*{**base, **kw}.values())
 
     for bad in (dict(src=0), dict(src=P + 8), dict(dst=0), dict(dst=P + 4), dict(sp=0), dict(dp=0),
-                dict(layers=0), dict(nb=0), dict(nb=24), dict(s=0), dict(d=0), dict(n=-1), dict(err=0)):
+                dict(layers=0), dict(nb=0), dict(nb=24), dict(s=0), dict(d=0), dict(n=-1), dict(err=0),
+                dict(s=P + 2), dict(d=P + 1), dict(err=P + 2)):
         _refused(gs, gs.GS_ERR_INVALID_ARG, lambda: call(**bad))
     _refused(gs, gs.GS_ERR_UNSUPPORTED, lambda: call(layers=65536))
     call(n=0)
