@@ -24,11 +24,11 @@
 // shared memory is a compare-and-swap loop: the low and the high word are added
 // apart, the high one only when it changes.)
 //
-// Many rows are bound by instruction issue, about 55 a logit, 25 of them its
-// weight: 544 rows of 59,392 (bf16, top-p) take 93 us, 10% of the copy rate; a
-// head of 2000 tokens instead of 3500 makes it 178 us, as more rows end behind
-// it.  Few rows are bound by the chain of passes and barriers: one row of 4096
-// takes 10 us, 32 rows of 59,392 (fp32, mixed settings) 22 us.
+// Many rows are bound by instruction issue, about 59 a logit, half of them for
+// its weight: 544 rows of 59,392 (bf16, top-p) take 81 us, 12% of the copy rate
+// (98 us with a head of 3000 tokens instead of 3500: more rows end behind it).
+// Few rows are bound by the chain of passes and barriers: one row of 4096 takes
+// 9 us, 32 rows of 59,392 (fp32, mixed settings) 17 us.
 #include <cmath>
 #include <cstddef>
 
@@ -866,7 +866,7 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
   // ---- the largest logit
   uint32_t best = kEmpty<TYPE>, early = best;             // early: of the thread's first vectors
   const int early_end = a.level_vecs * kThreads;
-#pragma unroll 8
+#pragma unroll 4
   for (int v = threadIdx.x; v < row.n_vecs; v += kThreads) {
     const uint4 x = Slice<TYPE>::no_nan(row.load(v));
     best = max_packed<TYPE>(best, max_packed<TYPE>(max_packed<TYPE>(x.x, x.y), max_packed<TYPE>(x.z, x.w)));
@@ -1012,8 +1012,8 @@ __global__ void __launch_bounds__(kThreads, 2) sample_kernel(const SampleArgs a)
 
 // Blocks that share a row: more while the GPU has an SM for each and each still
 // has a few thousand logits; eight only for a few rows, as clusters of eight wait
-// for room in one GPC (17 rows of 59,392: 19 us with four blocks, 24 with eight;
-// 64 rows of 32,001: 14 us with two, 17 with four).
+// for room in one GPC (17 rows of 59,392: 16.4 us with four blocks, 18.8 with
+// eight; 64 rows of 32,001: 12.4 us with two, 13.8 with four).
 int cluster_for(int rows, int vocab) {
   int n = 1;
   while (n < kMostCluster && vocab > n * 4096 &&
