@@ -536,7 +536,8 @@ typedef struct {
  * keep a prefix of mass Z, and the draw is its first token whose cumulative
  * mass exceeds min(floor(u Z), Z - 1).
  *   logits   device [rows, vocab] of dtype, row stride ld elements; NaN counts
- *            as -inf.  Rows need no alignment beyond the element's.
+ *            as -inf, logits of +inf have all the weight between them.  Rows
+ *            need no alignment beyond the element's.
  *   u        device fp32 [rows], in [0, 1) (others are clamped, NaN is 0)
  *   token    device int32 [rows]; -1 where every logit is -inf
  *   logprob  device fp32 [rows] or NULL: ln of the token's share of Z
