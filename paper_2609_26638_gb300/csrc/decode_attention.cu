@@ -3,6 +3,7 @@
 //
 //   s_j = scale * q . k_j over the visible keys j in [max(0, n - window), n)
 //   o = sum_j 2^(s_j' - m) v_j / l,  l = sum_j 2^(s_j' - m),  s' = s log2(e)
+//   (m the running maximum of s'; in fp16 15 less, see below)
 //
 // Each key and value is read once for its group of query heads, with 4 G
 // flops per 4 bytes, so HBM bounds every group that shares a KV head.  The
@@ -27,9 +28,13 @@
 // whose values it reads, so P needs no exchange either.
 //
 // Running max (log2 units), sum and accumulators are fp32.  P is rounded to
-// the cache's type for the second product: at most 1, relative error 2^-12
-// (fp16) or 2^-9 (bf16), below the output's own rounding after averaging; the
-// sum l takes the unrounded P.
+// the cache's type for the second product, relative error 2^-11 (fp16) or 2^-8
+// (bf16) at most, like the output's own rounding and averaged over the keys; the
+// sum l takes the unrounded P.  fp16 has no exponents for light keys (below 2^-14 it
+// loses bits, below 2^-25 all of them), so there the max is held 15 too low: P goes up
+// to 2^15, O and l with it, and a weight of 2^-29 still has all its bits.  (As
+// two products, P and what its rounding left, the error would vanish; but 0 times an
+// infinite value would make NaN of an infinite output.)
 //
 // Measured (16 query and 8 KV heads of 64, fp16, unless named): 64 rows of 8192
 // tokens 162 us, 6.6 TB/s; 32 rows of 1024 to 6144 43 us, 5.5 TB/s, and one row
@@ -134,6 +139,18 @@ __device__ __forceinline__ uint4 load_once(const uint16_t* p) {
 // exponentials are 2^-inf = 0 and not 2^(inf - inf).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
+// The max that a step's largest score (before scaling) asks for, held low as said
+// above.  Both roundings are upwards, so P is at most 2^15 (or 1) however large
+// the scores are: with 1.4 times that fp16 would come near its end, and scores
+// beyond 2^24 could pass it.
+template <bool BF16>
+constexpr float kHeld = BF16 ? 0.f : 15.f;
+template <bool BF16>
+__device__ __forceinline__ float held_max(float x, float scale_log2) {
+  const float m = __fmul_ru(x, scale_log2);
+  return BF16 ? m : __fsub_ru(m, kHeld<BF16>);
+}
+
 // Four dims of a head's output, and with the first of them its log-sum-exp.
 template <bool BF16, int D>
 __device__ __forceinline__ void store_row(const DecodeArgs& a, int row, int head, int d, float m,
@@ -141,9 +158,10 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int row, int head
   const float inv = l != 0.f ? 1.f / l : 0.f;
   *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(head) * D + d) =
       make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-  if (d == 0 && a.lse)
+  if (d == 0 && a.lse)     // (the 15 go out of m and l first, without a rounding)
     a.lse[static_cast<int64_t>(row) * a.Hq + head] =
-        l != 0.f ? (finite_max(m) + log2f(l)) * kLn2 : -INFINITY;
+        l != 0.f ? (finite_max(m) + kHeld<BF16> + log2f(l * (BF16 ? 1.f : 0x1p-15f))) * kLn2
+                 : -INFINITY;
 }
 
 constexpr int kMostCluster = 8;
@@ -290,7 +308,8 @@ decode_attention_kernel(const DecodeArgs a) {
       x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
       x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
     }
-    const float n0 = fmaxf(m0, x0 * a.scale_log2), n1 = fmaxf(m1, x1 * a.scale_log2);
+    const float n0 = fmaxf(m0, held_max<BF16>(x0, a.scale_log2)),
+                n1 = fmaxf(m1, held_max<BF16>(x1, a.scale_log2));
     const bool rises = n0 != m0 || (WIDE && n1 != m1);
     if (__any_sync(0xFFFFFFFFu, rises)) {
       const float f0 = ex2(m0 - finite_max(n0)), f1 = WIDE ? ex2(m1 - finite_max(n1)) : 1.f;
