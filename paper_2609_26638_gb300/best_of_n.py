@@ -68,7 +68,11 @@ class StepDecoder:
     ``feed`` takes (sequence, first slot, tokens) runs: a prompt is one long run,
     a decode step one token per sequence.  Runs of one token go through
     ``gs_decode_attention`` together; in a longer run the tokens are rows over
-    the same pages, each seeing the keys up to its own."""
+    the same pages, each seeing the keys up to its own.
+
+    The work runs on a stream of the decoder's own (``stream``), ordered with the
+    caller's current stream: tokens may come from work enqueued there, and what
+    ``feed`` returns may be used there without synchronising."""
 
     def __init__(self, shape: Shape, weights: Dict[str, object], *, n_pages: int, max_seqs: int,
                  max_ctx: int, max_rows: int = 512, device: str = "cuda:0"):
@@ -107,9 +111,17 @@ class StepDecoder:
         rows = sum(len(t) for _, _, t in runs)
         if rows > self.max_rows:
             raise gs.GsError(gs.GS_ERR_INVALID_ARG, "more tokens than max_rows")
+        caller = torch.cuda.current_stream(self.device)
+        self.stream.wait_stream(caller)
+        for _, _, t in runs:
+            if isinstance(t, torch.Tensor) and t.is_cuda:
+                t.record_stream(self.stream)
         self.pool.prepare([(s, first, len(t)) for s, first, t in runs])
         with torch.cuda.stream(self.stream):
-            return self._feed(runs, rows)
+            logits = self._feed(runs, rows)
+        caller.wait_stream(self.stream)
+        logits.record_stream(caller)
+        return logits
 
     def _feed(self, runs, rows):
         s, st = self.shape, self.stream.cuda_stream
@@ -179,10 +191,12 @@ def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: O
               = None, seed: int = 0, **settings):
     """n continuations of ``new`` tokens; (tokens [n, new], sum of log-probabilities [n]).
 
-    uniforms: [new, n] fp32 on the decoder's device, or drawn from ``seed``."""
+    uniforms: [new, n] fp32 on the decoder's device, or drawn from ``seed``.  The
+    results are complete when the call returns (it synchronises)."""
     if not prompt or n < 1 or new < 0:
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "an empty prompt, n < 1 or new < 0")
-    dec.stream.wait_stream(torch.cuda.current_stream(dec.device))
+    caller = torch.cuda.current_stream(dec.device)
+    dec.stream.wait_stream(caller)
     with torch.cuda.stream(dec.stream):
         if uniforms is None:
             g = torch.Generator(device=dec.device).manual_seed(seed)
@@ -208,6 +222,8 @@ def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: O
     dec.check()
     for q in seqs:
         dec.pool.close(q)
+    tokens.record_stream(caller)
+    total.record_stream(caller)
     return tokens, total
 
 

@@ -1,0 +1,90 @@
+"""StepDecoder as a caller uses it: streams, token ids, error words, refusals."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+SLEEP = 40_000_000           # cycles: about 20 ms, a bounded spin
+
+
+@pytest.fixture(scope="module")
+def bn():
+    from paper_2609_26638_gb300 import best_of_n
+    return best_of_n
+
+
+def _decoder(bn, shape=None, weights=None, **kw):
+    shape = shape or bn.Shape()
+    weights = weights or bn.random_weights(shape, 3)
+    return bn.StepDecoder(shape, weights, **{**dict(n_pages=60, max_seqs=8, max_ctx=400), **kw})
+
+
+def _prompt(n, vocab=4096, seed=5):
+    return np.random.default_rng(seed).integers(0, vocab, n).tolist()
+
+
+@pytest.mark.parametrize("side", [False, True])
+def test_logits_are_ordered_behind_the_callers_stream(bn, side):
+    """The last product comes late; the caller's stream reads the logits without
+    synchronising, frees them, and reads the next call's."""
+    dec = _decoder(bn)
+    a, b = _prompt(30), _prompt(30, seed=6)
+    want = []
+    for p in (a, b):
+        seq = dec.pool.open()
+        want.append(dec.feed([(seq, 0, p)]).clone())
+        dec.check()
+    linear = dec._linear
+
+    def late(x, w, *args):
+        if w is dec.w["lm_head"]:
+            torch.cuda._sleep(SLEEP)
+        linear(x, w, *args)
+    dec._linear = late
+    stream = torch.cuda.Stream() if side else torch.cuda.current_stream()
+    with torch.cuda.stream(stream):
+        got = []
+        for p in (a, b):
+            seq = dec.pool.open()
+            logits = dec.feed([(seq, 0, p)])
+            got.append(logits.clone())
+            del logits
+    stream.synchronize()
+    assert torch.equal(got[0], want[0]) and torch.equal(got[1], want[1])
+    dec.check()
+
+
+def test_tokens_are_read_behind_the_callers_stream(bn):
+    """A token that the caller's stream has yet to write, freed right after the call."""
+    dec = _decoder(bn)
+    prompt = _prompt(20)
+    one, two = dec.pool.open(), dec.pool.open()
+    dec.feed([(one, 0, prompt), (two, 0, prompt)])
+    want = dec.feed([(one, 20, [77])]).clone()
+    dec.check()
+    token = torch.zeros(1, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    torch.cuda._sleep(SLEEP)
+    token += 77
+    logits = dec.feed([(two, 20, token)])
+    del token
+    torch.full((1,), 5, dtype=torch.int32, device=DEV)         # may take the freed place
+    dec.check()
+    assert torch.equal(logits, want)
+
+
+def test_best_of_n_on_a_side_stream(bn):
+    """Uniforms that the caller's stream has yet to write; results used there."""
+    dec = _decoder(bn)
+    prompt = _prompt(70)
+    u = torch.rand(5, 3, generator=torch.Generator().manual_seed(1)).to(DEV)
+    want, total = bn.best_of_n(dec, prompt, 3, 5, uniforms=u)
+    want, total = want.clone(), total.clone()
+    torch.cuda.synchronize()
+    with torch.cuda.stream(torch.cuda.Stream()):
+        late = torch.zeros_like(u)
+        torch.cuda._sleep(SLEEP)
+        late += u
+        got, t2 = bn.best_of_n(dec, prompt, 3, 5, uniforms=late)
+        assert torch.equal(got, want) and torch.equal(t2, total)
