@@ -62,13 +62,24 @@ def random_weights(shape: Shape, seed: int = 0, device: str = "cuda:0") -> Dict[
                 lm_head=mat(s.vocab, s.d_model, 0.1))
 
 
+def check_tokens(tokens, vocab: int) -> None:
+    """Refuses ids outside the vocabulary.  Ids on the device are not read here."""
+    t = torch.as_tensor(tokens)
+    if t.dim() != 1 or t.is_floating_point() or t.is_complex():
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "tokens must be a list of whole numbers")
+    if not t.is_cuda and t.numel() and not (0 <= int(t.min()) and int(t.max()) < vocab):
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "token id outside the vocabulary")
+
+
 class StepDecoder:
     """Feeds tokens of any sequences through the decoder, one call per step.
 
     ``feed`` takes (sequence, first slot, tokens) runs: a prompt is one long run,
     a decode step one token per sequence.  Runs of one token go through
     ``gs_decode_attention`` together; in a longer run the tokens are rows over
-    the same pages, each seeing the keys up to its own.
+    the same pages, each seeing the keys up to its own.  A token id outside the
+    vocabulary is refused; where the ids are on the device, it is clamped, and the
+    next ``check`` raises.
 
     The work runs on a stream of the decoder's own (``stream``), ordered with the
     caller's current stream: tokens may come from work enqueued there, and what
@@ -111,6 +122,8 @@ class StepDecoder:
         rows = sum(len(t) for _, _, t in runs)
         if rows > self.max_rows:
             raise gs.GsError(gs.GS_ERR_INVALID_ARG, "more tokens than max_rows")
+        for _, _, t in runs:
+            check_tokens(t, self.shape.vocab)
         caller = torch.cuda.current_stream(self.device)
         self.stream.wait_stream(caller)
         for _, _, t in runs:
@@ -133,7 +146,9 @@ class StepDecoder:
         slot = ids([first + i for _, first, t in runs for i in range(len(t))])
         n = slot + 1                       # a token sees itself and what lies before it
         token = torch.cat([torch.as_tensor(t, dtype=torch.int64, device=dev) for _, _, t in runs])
-        h = self.w["embed"][token].float()
+        inside = token.clamp(0, s.vocab - 1)
+        self.pool.err.logical_or_((inside != token).any())
+        h = self.w["embed"][inside].float()
         qkv = torch.empty(rows, s.qkv_dim, dtype=torch.float16, device=dev)
         out = torch.empty(rows, s.n_heads * s.head_dim, dtype=torch.float16, device=dev)
         act = torch.empty(rows, s.d_ffn, dtype=torch.float16, device=dev)

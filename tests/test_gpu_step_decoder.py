@@ -88,3 +88,39 @@ def test_best_of_n_on_a_side_stream(bn):
         late += u
         got, t2 = bn.best_of_n(dec, prompt, 3, 5, uniforms=late)
         assert torch.equal(got, want) and torch.equal(t2, total)
+
+
+def test_token_ids_outside_the_vocabulary(bn):
+    """On the host: refused, and nothing has changed.  On the device: clamped,
+    and the next check raises, once."""
+    from paper_2609_26638_gb300 import gs
+    dec = _decoder(bn)
+    V = dec.shape.vocab
+    seq = dec.pool.open()
+    free = dec.pool.table.free_pages
+    for bad in ([V], [-1], [3, 2 ** 40], np.array([V, 0])):
+        with pytest.raises(gs.GsError) as e:
+            dec.feed([(seq, 0, bad)])
+        assert e.value.code == gs.GS_ERR_INVALID_ARG
+        assert dec.pool.table.free_pages == free
+    dec.check()
+    for bad, inside in ((V, V - 1), (-1, 0), (-2 ** 31, 0), (2 ** 31 - 1, V - 1)):
+        got = dec.feed([(seq, 0, torch.tensor([5, bad], dtype=torch.int32, device=DEV))]).clone()
+        with pytest.raises(gs.GsError) as e:
+            dec.check()
+        assert e.value.code == gs.GS_ERR_DEVICE_CHECK
+        dec.check()
+        assert torch.equal(got, dec.feed([(seq, 0, [5, inside])]))
+        dec.check()
+
+
+def test_a_row_without_logits_is_reported(bn):
+    """A language-model head of NaN: every draw is -1, which is no token to go on with."""
+    from paper_2609_26638_gb300 import gs
+    shape = bn.Shape()
+    w = bn.random_weights(shape, 3)
+    w["lm_head"].fill_(float("nan"))
+    dec = _decoder(bn, shape, w)
+    with pytest.raises(gs.GsError) as e:
+        bn.best_of_n(dec, _prompt(9), 2, 4)
+    assert e.value.code == gs.GS_ERR_DEVICE_CHECK
