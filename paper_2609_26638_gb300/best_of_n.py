@@ -104,13 +104,18 @@ class StepDecoder:
             self.attn_scratch = torch.zeros(need, dtype=torch.uint8, device=self.device)
             wide = max(shape.qkv_dim, shape.d_model, 2 * shape.d_ffn, shape.vocab)
             need = max(gs.gs_linear_scratch_bytes(r, wide, 1) for r in range(1, max_rows + 1))
-            self.gemm_scratch = torch.empty(need, dtype=torch.uint8, device=self.device)
+            # a scratch, and so an error word, for each product of a step: a call
+            # clears its own
+            self.gemm_scratch = torch.zeros(4 * shape.n_layers + 1, need, dtype=torch.uint8,
+                                            device=self.device)
+            self.gemm_err = torch.zeros((), dtype=torch.int32, device=self.device)
         self.rope = gs.gs_rope(self.table.data_ptr(), max_ctx, shape.rotary_dim, shape.rope_layout)
 
-    def _linear(self, x, w, y, n_out: int, epilogue: int) -> None:
+    def _linear(self, x, w, y, n_out: int, epilogue: int, at: int) -> None:
+        """y = x w^T as the step's ``at``-th product."""
+        scratch = self.gemm_scratch[at]
         gs.gs_linear(x.data_ptr(), w.data_ptr(), y.data_ptr(), x.shape[0], n_out, x.shape[1], epilogue,
-                     1, self.gemm_scratch.data_ptr(), self.gemm_scratch.numel(),
-                     self.stream.cuda_stream)
+                     1, scratch.data_ptr(), scratch.numel(), self.stream.cuda_stream)
 
     @staticmethod
     def _norm(h, gain):
@@ -155,7 +160,7 @@ class StepDecoder:
         width = s.n_heads * s.head_dim
         for i, w in enumerate(self.w["layers"]):
             cache = self.pool.layer(i)
-            self._linear(self._norm(h, w["norm1"]), w["qkv"], qkv, s.qkv_dim, gs.EPI_STORE_F16)
+            self._linear(self._norm(h, w["norm1"]), w["qkv"], qkv, s.qkv_dim, gs.EPI_STORE_F16, 4 * i)
             # queries in place: the key and value parts of qkv are read by the same call
             gs.gs_rope_append(cache, self.rope, qkv.data_ptr(), s.qkv_dim, rows, s.n_heads,
                               w["q_gain"].data_ptr(), w["k_gain"].data_ptr(), EPS, seq.data_ptr(),
@@ -164,23 +169,32 @@ class StepDecoder:
             gs.gs_decode_attention(cache, qkv.data_ptr(), s.qkv_dim, seq.data_ptr(), n.data_ptr(), rows,
                                    s.n_heads, s.head_dim ** -0.5, 0, out.data_ptr(), width, 0, 0,
                                    self.attn_scratch.data_ptr(), self.attn_scratch.numel(), st)
-            self._linear(out, w["o"], h, s.d_model, gs.EPI_RESID_F32)
-            self._linear(self._norm(h, w["norm2"]), w["gate_up"], act, s.d_ffn, gs.EPI_SWIGLU)
-            self._linear(act, w["down"], h, s.d_model, gs.EPI_RESID_F32)
+            self._linear(out, w["o"], h, s.d_model, gs.EPI_RESID_F32, 4 * i + 1)
+            self._linear(self._norm(h, w["norm2"]), w["gate_up"], act, s.d_ffn, gs.EPI_SWIGLU,
+                         4 * i + 2)
+            self._linear(act, w["down"], h, s.d_model, gs.EPI_RESID_F32, 4 * i + 3)
         last = torch.tensor([len(t) for _, _, t in runs]).cumsum(0).to(dev) - 1
         x = self._norm(h[last], self.w["norm"])
         logits = torch.empty(len(runs), s.vocab, dtype=torch.float16, device=dev)
-        self._linear(x, self.w["lm_head"], logits, s.vocab, gs.EPI_STORE_F16)
+        self._linear(x, self.w["lm_head"], logits, s.vocab, gs.EPI_STORE_F16, 4 * s.n_layers)
+        words = self.gemm_scratch[:, :4].view(torch.int32)
+        torch.maximum(self.gemm_err, words.amax(), out=self.gemm_err)
         return logits
 
     def check(self) -> None:
-        """Synchronise and raise if a kernel met an index out of range."""
+        """Synchronise and raise if a kernel met an index out of range, or a
+        product a value beyond fp16's.  All error words are clear afterwards."""
+        self.stream.synchronize()
+        with torch.cuda.stream(self.stream):
+            attn = self.attn_scratch[:4].view(torch.int32)
+            attend, linear = int(attn.item()), int(self.gemm_err.item())
+            attn.zero_()
+            self.gemm_err.zero_()
         self.pool.check()
-        word = int(self.attn_scratch[:4].view(torch.int32).item())
-        if word:
-            with torch.cuda.stream(self.stream):
-                self.attn_scratch[:4].zero_()
+        if attend:
             raise gs.GsError(gs.GS_ERR_DEVICE_CHECK, "gs_decode_attention")
+        if linear:
+            raise gs.GsError(gs.GS_ERR_TIMEOUT if linear == 2 else gs.GS_ERR_DEVICE_CHECK, "gs_linear")
 
 
 class Sampler:

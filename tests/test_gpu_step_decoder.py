@@ -124,3 +124,39 @@ def test_a_row_without_logits_is_reported(bn):
     with pytest.raises(gs.GsError) as e:
         bn.best_of_n(dec, _prompt(9), 2, 4)
     assert e.value.code == gs.GS_ERR_DEVICE_CHECK
+
+
+@pytest.mark.parametrize("which", ["qkv", "gate_up", "lm_head"])
+def test_a_product_beyond_fp16_is_reported(bn, which):
+    """Any product of a step, not the last one alone, and feeds after it do not hide it."""
+    from paper_2609_26638_gb300 import gs
+    shape = bn.Shape()
+    w = bn.random_weights(shape, 3)
+    m = w["lm_head"] if which == "lm_head" else w["layers"][0][which]
+    good = m.clone()
+    m.copy_(m.float().sign().half() * 60000)
+    dec = _decoder(bn, shape, w)
+    seq = dec.pool.open()
+    dec.feed([(seq, 0, _prompt(9))])
+    dec.stream.synchronize()
+    m.copy_(good)
+    torch.cuda.synchronize()
+    dec.feed([(seq, 9, [3])])
+    with pytest.raises(gs.GsError) as e:
+        dec.check()
+    assert e.value.code == gs.GS_ERR_DEVICE_CHECK
+    dec.check()                                    # reported once
+    dec.feed([(seq, 0, _prompt(9))])
+    dec.check()
+
+
+def test_one_check_clears_every_word(bn):
+    from paper_2609_26638_gb300 import gs
+    dec = _decoder(bn)
+    for words in ("pa", "ag", "pg", "pag"):
+        with torch.cuda.stream(dec.stream):
+            for x in words:
+                {"p": dec.pool.err, "a": dec.attn_scratch[:4].view(torch.int32), "g": dec.gemm_err}[x].fill_(1)
+        with pytest.raises(gs.GsError):
+            dec.check()
+        dec.check()
