@@ -236,11 +236,10 @@ class PagePool:
     def _copy(self, pairs: Pairs) -> None:
         if not pairs:
             return
-        with self._torch.cuda.stream(self.stream):
-            ids = self._torch.tensor(pairs, dtype=self._torch.int32).t().contiguous().to(self.device)
         layers, n_pages = self.kv.shape[:2]
         page_bytes = self.kv[0, 0].numel() * self.kv.element_size()
-        gs.gs_pages_copy(self.kv.data_ptr(), n_pages, self.kv.data_ptr(), n_pages, layers, page_bytes,
-                         ids[0].data_ptr(), ids[1].data_ptr(), len(pairs), self.err.data_ptr(),
-                         self.stream.cuda_stream)
-        ids.record_stream(self.stream)
+        with self._torch.cuda.stream(self.stream):     # (and its device)
+            ids = self._torch.tensor(pairs, dtype=self._torch.int32).t().contiguous().to(self.device)
+            gs.gs_pages_copy(self.kv.data_ptr(), n_pages, self.kv.data_ptr(), n_pages, layers,
+                             page_bytes, ids[0].data_ptr(), ids[1].data_ptr(), len(pairs),
+                             self.err.data_ptr(), self.stream.cuda_stream)
