@@ -224,9 +224,11 @@ class PagePool:
     def check(self) -> None:
         """Synchronise and raise if a kernel met an index out of range."""
         self.stream.synchronize()
-        word = int(self.err.item())
+        with self._torch.cuda.stream(self.stream):     # in order with the kernels that raise it
+            word = int(self.err.item())
+            if word:
+                self.err.zero_()
         if word:
-            self.err.zero_()
             raise gs.GsError(gs.GS_ERR_DEVICE_CHECK, "a kernel's bounds check fired")
 
     def _upload(self) -> None:

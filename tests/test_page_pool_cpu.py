@@ -77,3 +77,16 @@ def test_copies_run_within_the_pools_stream(pool):
     pool.close(a)
     pool.compact()
     assert _inside(pool.log, "copy")
+
+
+def test_check_reads_and_clears_within_the_pools_stream(pool):
+    """A word cleared on another stream could take a later kernel's report with it."""
+    from paper_2609_26638_gb300 import gs
+    pool.check()
+    pool.err.word = 1
+    with pytest.raises(gs.GsError) as e:
+        pool.check()
+    assert e.value.code == gs.GS_ERR_DEVICE_CHECK
+    assert pool.log.count("synchronize") == 2 and pool.err.word == 0
+    assert _inside(pool.log, "item") and _inside(pool.log, "zero")
+    pool.check()
