@@ -75,15 +75,19 @@ class PageTable:
         """Make slots [first, first + count) of each (seq, first, count) writable.
 
         Maps missing pages and replaces shared ones that the span touches;
-        returns the pages to copy.  Nothing changes if the pool is too small.
+        returns the pages to copy.  Nothing changes if the pool is too small.  Of
+        several spans of one sequence, a later one may start where an earlier one
+        ends.
         """
         spans = list(spans)
+        held: Dict[int, int] = {}                         # pages by then
         for seq, first, count in spans:
-            pages = self._of(seq)
+            have = held.get(seq, len(self._of(seq)))
             if count < 1 or first < 0 or first + count > self.max_ctx:
                 raise gs.GsError(gs.GS_ERR_INVALID_ARG, "slots out of range")
-            if first > len(pages) * PAGE_TOKENS:
+            if first > have * PAGE_TOKENS:
                 raise gs.GsError(gs.GS_ERR_INVALID_ARG, "slots start beyond the sequence's pages")
+            held[seq] = max(have, -(-(first + count) // PAGE_TOKENS))
         if self._need(spans) > len(self._free):
             raise gs.GsError(gs.GS_ERR_OOM, "page pool exhausted")
         pairs: Pairs = []
