@@ -71,13 +71,28 @@ def check_tokens(tokens, vocab: int) -> None:
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "token id outside the vocabulary")
 
 
+def check_runs(runs, max_rows: int) -> int:
+    """The tokens of all (sequence, first slot, tokens) runs; refuses runs that
+    are empty, too many, or name a slot twice."""
+    if not runs or any(len(t) == 0 for _, _, t in runs):
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "no tokens")
+    rows = sum(len(t) for _, _, t in runs)
+    if rows > max_rows:
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "more tokens than max_rows")
+    spans = sorted((s, first, first + len(t)) for s, first, t in runs)
+    if any(a[0] == b[0] and b[1] < a[2] for a, b in zip(spans, spans[1:])):
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "two runs name one slot")
+    return rows
+
+
 class StepDecoder:
     """Feeds tokens of any sequences through the decoder, one call per step.
 
     ``feed`` takes (sequence, first slot, tokens) runs: a prompt is one long run,
     a decode step one token per sequence.  Runs of one token go through
     ``gs_decode_attention`` together; in a longer run the tokens are rows over
-    the same pages, each seeing the keys up to its own.  A token id outside the
+    the same pages, each seeing the keys up to its own.  Runs of one call may
+    follow one another in a sequence, but not name a slot twice.  A token id outside the
     vocabulary is refused; where the ids are on the device, it is clamped, and the
     next ``check`` raises.
 
@@ -124,9 +139,7 @@ class StepDecoder:
     def feed(self, runs) -> torch.Tensor:
         """fp16 logits [runs, vocab] after the last token of each run."""
         runs = list(runs)
-        rows = sum(len(t) for _, _, t in runs)
-        if rows > self.max_rows:
-            raise gs.GsError(gs.GS_ERR_INVALID_ARG, "more tokens than max_rows")
+        rows = check_runs(runs, self.max_rows)
         for _, _, t in runs:
             check_tokens(t, self.shape.vocab)
         caller = torch.cuda.current_stream(self.device)

@@ -160,3 +160,13 @@ def test_one_check_clears_every_word(bn):
         with pytest.raises(gs.GsError):
             dec.check()
         dec.check()
+
+
+def test_a_prompt_in_two_runs(bn):
+    dec = _decoder(bn)
+    p = _prompt(90)
+    one, two = dec.pool.open(), dec.pool.open()
+    want = dec.feed([(one, 0, p)])
+    got = dec.feed([(two, 0, p[:33]), (two, 33, p[33:])])
+    dec.check()
+    assert torch.equal(got[1], want[0])

@@ -25,3 +25,15 @@ def test_token_ids(bn):
     for bad in ([100], [-1], [3, 2 ** 40], np.array([0, 100]), torch.tensor([-5]), [1.0], [[1]],
                 torch.tensor(3)):
         _refused(bn, bn.check_tokens, bad, 100)
+
+
+def test_runs(bn):
+    """Runs of one call name each place at most once."""
+    for good, rows in (([(0, 0, [1, 2, 3])], 3), ([(0, 0, [1]), (1, 0, [1])], 2),
+                       ([(0, 5, [1, 2]), (1, 3, [4]), (0, 7, [3, 4])], 5),
+                       ([(0, 7, [3, 4]), (0, 5, [1, 2])], 4)):
+        assert bn.check_runs(good, 5) == rows
+    for bad in ([], [(0, 0, [])], [(0, 0, [1]), (1, 0, [])], [(0, 0, [1] * 6)],
+                [(0, 0, [1, 2, 3]), (0, 2, [1])], [(0, 2, [1]), (1, 2, [1]), (0, 0, [1, 2, 3])],
+                [(0, 4, [1]), (0, 4, [1])]):
+        _refused(bn, bn.check_runs, bad, 5)
