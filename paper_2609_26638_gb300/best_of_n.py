@@ -237,6 +237,8 @@ def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: O
     results are complete when the call returns (it synchronises)."""
     if not prompt or n < 1 or new < 0:
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "an empty prompt, n < 1 or new < 0")
+    if (new > 1 and n > dec.max_rows) or len(prompt) + max(new - 1, 0) > dec.pool.table.max_ctx:
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "more sequences or tokens than the decoder was made for")
     caller = torch.cuda.current_stream(dec.device)
     dec.stream.wait_stream(caller)
     with torch.cuda.stream(dec.stream):
@@ -246,24 +248,26 @@ def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: O
         sampler = Sampler(n, device=str(dec.device), **settings)
         total = torch.zeros(n, device=dec.device)
         tokens = torch.empty(n, new, dtype=torch.int32, device=dec.device)
-    root = dec.pool.open()
-    step = dec.max_rows
-    for at in range(0, len(prompt), step):
-        logits = dec.feed([(root, at, prompt[at: at + step])])
-    seqs = [root] + dec.pool.fork(root, n - 1)
-    with torch.cuda.stream(dec.stream):
-        logits = logits.expand(n, -1).contiguous()
-    for i in range(new):
+    seqs: List[int] = []
+    try:
+        seqs.append(dec.pool.open())
+        for at in range(0, len(prompt), dec.max_rows):
+            logits = dec.feed([(seqs[0], at, prompt[at: at + dec.max_rows])])
+        seqs += dec.pool.fork(seqs[0], n - 1)
         with torch.cuda.stream(dec.stream):
-            sampler.draw(logits, uniforms[i], dec.stream)
-            tokens[:, i] = sampler.token
-            total += sampler.logprob
-        if i + 1 < new:
-            logits = dec.feed([(q, len(prompt) + i, sampler.token[j: j + 1])
-                               for j, q in enumerate(seqs)])
-    dec.check()
-    for q in seqs:
-        dec.pool.close(q)
+            logits = logits.expand(n, -1).contiguous()
+        for i in range(new):
+            with torch.cuda.stream(dec.stream):
+                sampler.draw(logits, uniforms[i], dec.stream)
+                tokens[:, i] = sampler.token
+                total += sampler.logprob
+            if i + 1 < new:
+                logits = dec.feed([(q, len(prompt) + i, sampler.token[j: j + 1])
+                                   for j, q in enumerate(seqs)])
+        dec.check()
+    finally:
+        for q in seqs:
+            dec.pool.close(q)
     tokens.record_stream(caller)
     total.record_stream(caller)
     return tokens, total

@@ -1,0 +1,55 @@
+"""best_of_n and its pool: what a failed call leaves behind, and each row's keys
+against the whole forward in 64 bits."""
+import numpy as np
+import pytest
+import torch
+
+from tests.test_gpu_best_of_n import DEV, _decoder, _forward
+
+pytestmark = pytest.mark.gpu
+
+
+@pytest.fixture(scope="module")
+def bn():
+    from paper_2609_26638_gb300 import best_of_n
+    return best_of_n
+
+
+def _prompt(n, seed=1):
+    return np.random.default_rng(seed).integers(0, 4096, n).tolist()
+
+
+def test_a_failed_call_gives_everything_back(bn, monkeypatch):
+    """The pool too small, too few rows, too many tokens, a bad id, an error in
+    a kernel: no page and no sequence stays taken, and the next call works."""
+    from paper_2609_26638_gb300 import gs
+    dec = _decoder(bn, bn.Shape(), n_pages=12, max_seqs=4, max_rows=70, max_ctx=400)
+    want = bn.best_of_n(dec, _prompt(40), 3, 4, seed=2)[0].clone()
+
+    def clean():
+        assert dec.pool.table.free_pages == 12 and not dec.pool.table._pages
+        assert torch.equal(bn.best_of_n(dec, _prompt(40), 3, 4, seed=2)[0], want)
+
+    def fails(code, *args, **kw):
+        with pytest.raises(gs.GsError) as e:
+            bn.best_of_n(dec, *args, **kw)
+        assert e.value.code == code
+        clean()
+
+    fails(gs.GS_ERR_INVALID_ARG, _prompt(390), 1, 40)            # past max_ctx
+    fails(gs.GS_ERR_OOM, _prompt(380), 4, 10)                    # forks need more pages than there are
+    fails(gs.GS_ERR_OOM, _prompt(10), 5, 2)                      # more rows than the table has
+    fails(gs.GS_ERR_INVALID_ARG, _prompt(10), 71, 2)             # more than one feed takes
+    fails(gs.GS_ERR_INVALID_ARG, _prompt(100) + [4096], 2, 2)    # in the prompt's second part
+    real = dec.pool.prepare
+    calls = []
+
+    def prepare(spans):
+        calls.append(1)
+        if len(calls) == 3:
+            with torch.cuda.stream(dec.stream):
+                dec.pool.err.fill_(1)                            # as a kernel would
+        return real(spans)
+    monkeypatch.setattr(dec.pool, "prepare", prepare)
+    fails(gs.GS_ERR_DEVICE_CHECK, _prompt(10), 2, 5)
+    assert len(calls) > 4
