@@ -229,11 +229,19 @@ class Sampler:
                      stream.cuda_stream)
 
 
+def uniform_table(uniforms, new: int, n: int, device) -> torch.Tensor:
+    """``uniforms`` as the kernel reads them: [new, n] contiguous fp32 on the device."""
+    u = torch.as_tensor(uniforms)
+    if u.shape != (new, n) or u.is_complex():
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "uniforms must be [new, n]")
+    return u.to(device=device, dtype=torch.float32).contiguous()
+
+
 def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: Optional[torch.Tensor]
               = None, seed: int = 0, **settings):
     """n continuations of ``new`` tokens; (tokens [n, new], sum of log-probabilities [n]).
 
-    uniforms: [new, n] fp32 on the decoder's device, or drawn from ``seed``.  The
+    uniforms: [new, n] numbers in [0, 1), or drawn from ``seed``.  The
     results are complete when the call returns (it synchronises)."""
     if not prompt or n < 1 or new < 0:
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "an empty prompt, n < 1 or new < 0")
@@ -245,6 +253,9 @@ def best_of_n(dec: StepDecoder, prompt: List[int], n: int, new: int, uniforms: O
         if uniforms is None:
             g = torch.Generator(device=dec.device).manual_seed(seed)
             uniforms = torch.rand(new, n, device=dec.device, generator=g)
+        else:
+            uniforms = uniform_table(uniforms, new, n, dec.device)
+            uniforms.record_stream(dec.stream)
         sampler = Sampler(n, device=str(dec.device), **settings)
         total = torch.zeros(n, device=dec.device)
         tokens = torch.empty(n, new, dtype=torch.int32, device=dec.device)

@@ -53,3 +53,17 @@ def test_a_failed_call_gives_everything_back(bn, monkeypatch):
     monkeypatch.setattr(dec.pool, "prepare", prepare)
     fails(gs.GS_ERR_DEVICE_CHECK, _prompt(10), 2, 5)
     assert len(calls) > 4
+
+
+def test_uniforms_of_any_layout(bn):
+    """On the host, in 64 bits or transposed: the same draws."""
+    from paper_2609_26638_gb300 import gs
+    dec = _decoder(bn, bn.Shape())
+    u = torch.rand(6, 3, generator=torch.Generator().manual_seed(4))
+    want, total = (t.clone() for t in bn.best_of_n(dec, _prompt(33), 3, 6, uniforms=u.to(DEV)))
+    for given in (u, u.double(), u.to(DEV).double(), u.to(DEV).t().contiguous().t(), u.numpy()):
+        tokens, t2 = bn.best_of_n(dec, _prompt(33), 3, 6, uniforms=given)
+        assert torch.equal(tokens, want) and torch.equal(t2, total)
+    with pytest.raises(gs.GsError):
+        bn.best_of_n(dec, _prompt(33), 3, 6, uniforms=u.t().contiguous())
+    assert dec.pool.table.free_pages == 60

@@ -37,3 +37,16 @@ def test_runs(bn):
                 [(0, 0, [1, 2, 3]), (0, 2, [1])], [(0, 2, [1]), (1, 2, [1]), (0, 0, [1, 2, 3])],
                 [(0, 4, [1]), (0, 4, [1])]):
         _refused(bn, bn.check_runs, bad, 5)
+
+
+def test_uniforms(bn):
+    """Any layout and type of the right shape becomes contiguous fp32 on the device."""
+    g = torch.Generator().manual_seed(0)
+    u = torch.rand(3, 5, generator=g)
+    for given in (u, u.double(), u.t().contiguous().t(), torch.cat([u, u], 1)[:, :5], u.numpy(),
+                  u.tolist()):
+        got = bn.uniform_table(given, 3, 5, torch.device("cpu"))
+        assert got.dtype == torch.float32 and got.is_contiguous() and torch.equal(got, u)
+    assert bn.uniform_table(torch.empty(0, 5), 0, 5, torch.device("cpu")).shape == (0, 5)
+    for bad in (u.t(), u[:2], u[:, :4], u[0], u[None], torch.tensor(0.5)):
+        _refused(bn, bn.uniform_table, bad, 3, 5, torch.device("cpu"))
