@@ -210,6 +210,9 @@ class StepDecoder:
             raise gs.GsError(gs.GS_ERR_TIMEOUT if linear == 2 else gs.GS_ERR_DEVICE_CHECK, "gs_linear")
 
 
+LOGIT_TYPES = {torch.float16: gs.GS_F16, torch.bfloat16: gs.GS_BF16, torch.float32: gs.GS_F32}
+
+
 class Sampler:
     """gs_sample with one set of settings for every row."""
 
@@ -223,10 +226,22 @@ class Sampler:
         self.logprob = full(0.0)
 
     def draw(self, logits: torch.Tensor, u: torch.Tensor, stream) -> None:
-        """token and logprob of each row, from uniforms ``u`` on ``stream``."""
-        gs.gs_sample(logits.data_ptr(), logits.stride(0), logits.shape[0], logits.shape[1], gs.GS_F16,
-                     self._p, u.data_ptr(), self.token.data_ptr(), self.logprob.data_ptr(), 0,
-                     stream.cuda_stream)
+        """token and logprob of each row, from uniforms ``u`` on ``stream``.
+
+        logits: [rows, vocab] in 16 or 32 bits, neighbouring columns, no more rows
+        than the sampler was made for; u: contiguous fp32 [rows]."""
+        code = LOGIT_TYPES.get(logits.dtype)
+        if (code is None or logits.dim() != 2 or logits.stride(1) != 1
+                or logits.stride(0) < logits.shape[1] or logits.shape[0] > self.token.shape[0]
+                or logits.device != self.token.device):
+            raise gs.GsError(gs.GS_ERR_INVALID_ARG, "logits do not fit the sampler")
+        if (u.dtype != torch.float32 or u.shape != logits.shape[:1] or not u.is_contiguous()
+                or u.device != self.token.device):
+            raise gs.GsError(gs.GS_ERR_INVALID_ARG, "uniforms do not fit the logits")
+        with torch.cuda.stream(stream):
+            gs.gs_sample(logits.data_ptr(), logits.stride(0), logits.shape[0], logits.shape[1], code,
+                         self._p, u.data_ptr(), self.token.data_ptr(), self.logprob.data_ptr(), 0,
+                         stream.cuda_stream)
 
 
 def uniform_table(uniforms, new: int, n: int, device) -> torch.Tensor:

@@ -1,5 +1,8 @@
 """Checks of best_of_n.py that need no GPU: what is refused before any device
 work."""
+import contextlib
+import types
+
 import numpy as np
 import pytest
 import torch
@@ -50,3 +53,32 @@ def test_uniforms(bn):
     assert bn.uniform_table(torch.empty(0, 5), 0, 5, torch.device("cpu")).shape == (0, 5)
     for bad in (u.t(), u[:2], u[:, :4], u[0], u[None], torch.tensor(0.5)):
         _refused(bn, bn.uniform_table, bad, 3, 5, torch.device("cpu"))
+
+
+def test_sampler_checks_what_it_passes_on(bn, monkeypatch):
+    """Logits and uniforms that do not fit the sampler's arrays, or that the
+    kernel would read as something else, are refused; the type follows the logits."""
+    gs = bn.gs
+    calls = []
+    monkeypatch.setattr(gs, "gs_sample", lambda *a: calls.append(a))
+
+    @contextlib.contextmanager
+    def within(stream):
+        yield
+    monkeypatch.setattr(torch.cuda, "stream", within)
+    stream = types.SimpleNamespace(cuda_stream=3)
+    s = bn.Sampler(4, top_k=7, device="cpu")
+    x, u = torch.zeros(4, 100, dtype=torch.float16), torch.zeros(4)
+    wide = torch.zeros(4, 128, dtype=torch.bfloat16)
+    for logits, uni, code in ((x, u, gs.GS_F16), (wide[:, :100], u, gs.GS_BF16),
+                              (x.float(), u, gs.GS_F32), (x[:2], u[:2], gs.GS_F16)):
+        s.draw(logits, uni, stream)
+        a = calls.pop()
+        assert a[:5] == (logits.data_ptr(), logits.stride(0), len(logits), 100, code)
+    one = x[:1].expand(4, -1)                            # every row the same memory: no row stride
+    for logits, uni in ((x.double(), u), (x[0], u), (x.t().contiguous().t(), u), (one, u),
+                        (torch.cat([x, x]), torch.zeros(8)), (x, u[:3]), (x, torch.zeros(5)),
+                        (x, u.double()), (x, torch.zeros(8)[::2]), (x, u[:, None]),
+                        (x.to("meta"), u), (x, u.to("meta"))):
+        _refused(bn, s.draw, logits, uni, stream)
+    assert not calls
