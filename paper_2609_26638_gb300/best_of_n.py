@@ -62,6 +62,28 @@ def random_weights(shape: Shape, seed: int = 0, device: str = "cuda:0") -> Dict[
                 lm_head=mat(s.vocab, s.d_model, 0.1))
 
 
+def check_weights(shape: Shape, weights: Dict[str, object], device) -> None:
+    """Refuses weights that are not what ``random_weights`` makes for this shape:
+    the kernels read them through pointers."""
+    s = shape
+    q, f, d = s.n_heads * s.head_dim, s.d_ffn, s.d_model
+    layer = dict(norm1=(d,), qkv=(s.qkv_dim, d), q_gain=(s.head_dim,), k_gain=(s.head_dim,), o=(d, q),
+                 norm2=(d,), gate_up=(2 * f, d), down=(d, f))
+    layers = weights.get("layers", ())
+    if len(layers) != s.n_layers:
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "weights of another number of layers")
+    want = [(weights, dict(embed=(s.vocab, d), norm=(d,), lm_head=(s.vocab, d)))]
+    for held, shapes in want + [(w, layer) for w in layers]:
+        for name, size in shapes.items():
+            t = held.get(name)
+            if (not isinstance(t, torch.Tensor) or t.shape != size or not t.is_contiguous()
+                    or t.dtype != (torch.float16 if len(size) == 2 else torch.bfloat16)
+                    or t.device != device or t.data_ptr() % 16):
+                raise gs.GsError(gs.GS_ERR_INVALID_ARG,
+                                 f"{name}: contiguous, 16-byte aligned "
+                                 f"{'fp16' if len(size) == 2 else 'bf16'} {list(size)} on {device} needed")
+
+
 def check_tokens(tokens, vocab: int) -> None:
     """Refuses ids outside the vocabulary.  Ids on the device are not read here."""
     t = torch.as_tensor(tokens)
@@ -87,6 +109,7 @@ def check_runs(runs, max_rows: int) -> int:
 
 class StepDecoder:
     """Feeds tokens of any sequences through the decoder, one call per step.
+    The weights are used where they are (``random_weights`` shows their form).
 
     ``feed`` takes (sequence, first slot, tokens) runs: a prompt is one long run,
     a decode step one token per sequence.  Runs of one token go through
@@ -103,7 +126,8 @@ class StepDecoder:
     def __init__(self, shape: Shape, weights: Dict[str, object], *, n_pages: int, max_seqs: int,
                  max_ctx: int, max_rows: int = 512, device: str = "cuda:0"):
         self.shape, self.w, self.max_rows = shape, weights, max_rows
-        self.device = torch.device(device)
+        self.device = torch.empty(0, device=device).device            # (with its index)
+        check_weights(shape, weights, self.device)
         self.stream = torch.cuda.Stream(self.device)
         torch.cuda.synchronize(self.device)
         self.pool = PagePool(n_layers=shape.n_layers, n_pages=n_pages, n_kv_heads=shape.n_kv_heads,

@@ -82,3 +82,33 @@ def test_sampler_checks_what_it_passes_on(bn, monkeypatch):
                         (x.to("meta"), u), (x, u.to("meta"))):
         _refused(bn, s.draw, logits, uni, stream)
     assert not calls
+
+
+def test_weights(bn):
+    """Weights reach the kernels as pointers: type, shape, layout and device are checked."""
+    shape = bn.Shape(n_layers=2, vocab=128)
+    device = torch.device("cpu")
+
+    def fresh():
+        return bn.random_weights(shape, 0, "cpu")
+    bn.check_weights(shape, fresh(), device)
+    names = {"embed", "norm", "lm_head"} | {"layers"}
+    assert set(fresh()) == names
+    cases = [(None, k) for k in ("embed", "norm", "lm_head")] + \
+        [(i, k) for i in (0, 1) for k in fresh()["layers"][0]]
+    for layer, k in cases:
+        t = (fresh() if layer is None else fresh()["layers"][layer])[k]
+        wrong = [t.float(), t[:-1].contiguous(), t[None], t.to("meta"), None,
+                 t.new_zeros(t.numel() + 1)[1:].view(t.shape)]          # 2 bytes off
+        if t.dim() == 2:
+            wrong += [t.new_zeros(t.shape[1], t.shape[0]).t(), t.new_zeros(t.shape[0], t.shape[1] + 8)[:, 8:]]
+        for bad in wrong:
+            w = fresh()
+            (w if layer is None else w["layers"][layer])[k] = bad
+            _refused(bn, bn.check_weights, shape, w, device)
+    w = fresh()
+    del w["layers"][1]
+    _refused(bn, bn.check_weights, shape, w, device)
+    w = fresh()
+    del w["layers"][0]["o"]
+    _refused(bn, bn.check_weights, shape, w, device)
