@@ -67,3 +67,44 @@ def test_uniforms_of_any_layout(bn):
     with pytest.raises(gs.GsError):
         bn.best_of_n(dec, _prompt(33), 3, 6, uniforms=u.t().contiguous())
     assert dec.pool.table.free_pages == 60
+
+
+@pytest.mark.parametrize("plen", [130, 128, 63])
+def test_every_row_of_a_shared_run(bn, plen):
+    """Each of five continuations, step by step over shared pages that begin
+    within a page, at its start and at its last slot: the logits after every
+    token are those of the whole forward of that row's own tokens in 64 bits
+    (3e-2, the tolerance of test_gpu_best_of_n.py), and best_of_n's tokens are the draws
+    from them.  A page that a row shared and another wrote would show in the
+    first, whichever row it is: one key of a neighbour's in place of its own moves
+    a row's logits by 0.22 (prompt of 130, two tokens later)."""
+    from paper_2609_26638_gb300 import gs
+    shape, n, new = bn.Shape(), 5, 12
+    prompt = _prompt(plen, seed=plen)
+    u = torch.rand(new, n, generator=torch.Generator().manual_seed(2)).to(DEV)
+    kw = dict(temperature=0.9, top_p=0.9, top_k=200)
+    dec = _decoder(bn, shape)
+    tokens, total = bn.best_of_n(dec, prompt, n, new, uniforms=u, **kw)
+    host = tokens.cpu().numpy()
+    assert len({tuple(r) for r in host[:, :4].tolist()}) == n    # rows part early: each its own keys
+    want = [_forward(bn, shape, dec.w, np.concatenate([prompt, host[j]]), gs) for j in range(n)]
+    sampler = bn.Sampler(n, **kw)
+    stream = torch.cuda.current_stream()
+    root = dec.pool.open()
+    logits = dec.feed([(root, 0, prompt)])
+    seqs = [root] + dec.pool.fork(root, n - 1)
+    logits = logits.expand(n, -1).contiguous()
+    mass = torch.zeros(n, device=DEV)
+    for i in range(new):
+        got = logits.cpu().double().numpy()
+        for j in range(n):
+            assert np.abs(got[j] - want[j][plen + i - 1]).max() <= 3e-2, (i, j)
+        sampler.draw(logits, u[i], stream)
+        assert torch.equal(sampler.token, tokens[:, i]), i
+        mass += sampler.logprob
+        logits = dec.feed([(q, plen + i, host[j, i: i + 1].tolist()) for j, q in enumerate(seqs)])
+    got = logits.cpu().double().numpy()
+    for j in range(n):
+        assert np.abs(got[j] - want[j][plen + new - 1]).max() <= 3e-2, j
+    assert torch.equal(mass, total)
+    dec.check()
