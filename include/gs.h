@@ -502,11 +502,16 @@ int gs_rope_append(const gs_cache *cache, const gs_rope *rope, const void *qkv, 
  *   split_pages  pages per work item, 0 = chosen from rows, heads and pt_stride
  *           (or window).  Items are reduced independently and joined in a fixed
  *           order: a row's result depends on its own keys and the split only.
+ *           The choice takes rows to be about as long as the table is wide: with
+ *           much shorter ones, a split made for them is faster.
  *   scratch device, 256-byte aligned, at least
  *           gs_decode_attention_scratch_bytes(...) bytes (0 on a bad argument);
  *           its first int32 is the error word, the rest may hold anything.
  *           Calls that may run at the same time need scratch of their own.
  * What the cache holds at or beyond n, or before the window, has no influence.
+ * Scores, maxima, sums and accumulators are fp32; the probabilities are rounded
+ * to the cache's type for the product with V (relative error 2^-11 in fp16, down
+ * to 2^-29 of the largest, 2^-8 in bf16), and the output to that type.
  * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (head_dim, rows > 65535),
  * GS_ERR_OOM (scratch too small), GS_ERR_CUDA. */
 size_t gs_decode_attention_scratch_bytes(const gs_cache *cache, int rows, int n_heads,
@@ -534,7 +539,8 @@ typedef struct {
  * row was divided.  The tokens are ordered by falling logit, equal ones by
  * index; of that order min_p, then top_k, then top_p (a share of what is left)
  * keep a prefix of mass Z, and the draw is its first token whose cumulative
- * mass exceeds min(floor(u Z), Z - 1).
+ * mass exceeds min(floor(u Z), Z - 1).  Tokens of weight 0 are neither drawn nor
+ * counted.
  *   logits   device [rows, vocab] of dtype, row stride ld elements; NaN counts
  *            as -inf, logits of +inf have all the weight between them.  Rows
  *            need no alignment beyond the element's.
@@ -542,8 +548,8 @@ typedef struct {
  *   token    device int32 [rows]; -1 where every logit is -inf
  *   logprob  device fp32 [rows] or NULL: ln of the token's share of Z
  *   kept     device int32 [rows] or NULL: tokens in the prefix
- * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (vocab > 262,144),
- * GS_ERR_CUDA. */
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (vocab > 262,144, rows >
+ * 2^24), GS_ERR_CUDA. */
 int gs_sample(const void *logits, int64_t ld, int rows, int vocab, int dtype,
               const gs_sample_params *params, const float *u, int32_t *token, float *logprob,
               int32_t *kept, void *stream);
@@ -552,11 +558,11 @@ int gs_sample(const void *logits, int64_t ld, int rows, int vocab, int dtype,
  * of src, in one launch.  Both pools are [n_layers][pages][page_bytes] and may
  * be the same one; no page may be a destination twice, or a source and a
  * destination of one pool.
- *   page_bytes  a multiple of 16; src, dst 16-byte aligned
+ *   page_bytes  a multiple of 16, at most 2^30; src, dst 16-byte aligned
  *   src_ids, dst_ids  device int32 [n] (an index out of range: nothing is
  *               copied for it and *err is raised)
- * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (n_layers > 65535),
- * GS_ERR_CUDA. */
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (n_layers > 65535, page_bytes
+ * > 2^30), GS_ERR_CUDA. */
 int gs_pages_copy(const void *src, int src_pages, void *dst, int dst_pages, int n_layers,
                   int64_t page_bytes, const int32_t *src_ids, const int32_t *dst_ids, int n,
                   int32_t *err, void *stream);

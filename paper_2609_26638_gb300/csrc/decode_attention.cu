@@ -5,8 +5,9 @@
 //   o = sum_j 2^(s_j' - m) v_j / l,  l = sum_j 2^(s_j' - m),  s' = s log2(e)
 //   (m the running maximum of s'; in fp16 15 less, see below)
 //
-// Each key and value is read once for its group of query heads, with 4 G
-// flops per 4 bytes, so HBM bounds every group that shares a KV head.  The
+// Each key and value is read once for a group of up to 16 query heads (once for
+// every 16 of a larger one), with 4 flops per query head and element of 2 bytes, so
+// HBM bounds every group that shares a KV head.  The
 // work is cut into items of `split` pages; a block takes one item of one KV
 // head (and up to 16 of its query heads), its warps take the item's pages in
 // turn, 32 tokens at a time, and are joined at the item's end; until then no warp
@@ -39,7 +40,11 @@
 // Measured (16 query and 8 KV heads of 64, fp16, unless named): 64 rows of 8192
 // tokens 162 us, 6.6 TB/s; 32 rows of 1024 to 6144 43 us, 5.5 TB/s, and one row
 // of 131,001 (32 / 4 heads of 128, bf16) 48 us, 5.6 TB/s: what is missing is the
-// wave's start and the tail of its last blocks; one row of 517 tokens 4.3 us.
+// wave's start and the tail of its last blocks; one row of 517 tokens 4.4 us.
+// These are tables as wide as the longest row.  An open split and the grid follow
+// the table's width, not the lengths, so a table with room to spare costs time:
+// 2048 pages wide, the 517 tokens take 7.2 us, 6144 tokens of one row 24 (7.7 at 96
+// pages), the 32 rows 87, and 64 rows of 400 tokens 124 (15.6 at 7 pages).
 #include <algorithm>
 #include <cmath>
 
@@ -494,6 +499,7 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeA
 // shares the cache evenly (of the 456 or 304 places that the GPU has for head
 // dims 64 and 128, not all: one row of 131,001 tokens takes 48 us on 256 blocks
 // and 53 on 304), or eight items that join in a cluster where that is not long.
+// (Measured on tables as wide as the row, one shape for each head dim.)
 // More than one row, which may differ in length: items of at most kMostPages, so
 // that the tail behind the longest is short (32 rows of 1024 to 6144 tokens: 43
 // us with 12 pages, 47 with 32, 49 with 4).
