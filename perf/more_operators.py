@@ -372,17 +372,17 @@ def _own_commit(s, gs):
 def _pack(s):
     from paper_2609_26638_gb300 import gs
     c = s["case"]
-    w = gs.gs_w4(0, s["q"].shape[0], c["inner"], c["group"], _dtype(gs, c), int(c["zeros"]),
-                 int(c["gated"]))
-    s["packed"] = torch.empty(gs.gs_w4_bytes(w), dtype=torch.uint8, device="cuda")
+    w = gs.gs_qweight(0, s["q"].shape[0], c["inner"], c["group"], _dtype(gs, c), int(c["zeros"]),
+                      int(c["gated"]))
+    s["packed"] = torch.empty(gs.gs_qweight_bytes(w), dtype=torch.uint8, device="cuda")
     w.packed = s["packed"].data_ptr()
-    gs.gs_w4_pack(w, s["q"].data_ptr(), s["scale"].data_ptr(), _ptr(s["zero"]), _stream())
+    gs.gs_qweight_pack(w, s["q"].data_ptr(), s["scale"].data_ptr(), _ptr(s["zero"]), _stream())
     s["w"] = w
 
 
 def _own_w4(s, gs):
     c = s["case"]
-    gs.gs_w4_linear(s["w"], s["x"].data_ptr(), c["inner"], s["y"].data_ptr(), c["out"], c["rows"],
+    gs.gs_qlinear(s["w"], s["x"].data_ptr(), c["inner"], s["y"].data_ptr(), c["out"], c["rows"],
                     gs.EPI_SWIGLU if c["gated"] else gs.EPI_STORE_F16, s["err"].data_ptr(), _stream())
     return s["y"]
 
