@@ -567,6 +567,130 @@ int gs_pages_copy(const void *src, int src_pages, void *dst, int dst_pages, int 
                   int64_t page_bytes, const int32_t *src_ids, const int32_t *dst_ids, int n,
                   int32_t *err, void *stream);
 
+/* ---------------------------------------------------------------------------
+ * Verification of drafted trees over the paged cache, and products with 4-bit
+ * weights.  The engine verifies one chain of its own drafts; these take a tree
+ * of candidates from anywhere through one step of a decoder of the caller's:
+ * its nodes are appended at slots n, n + 1, ... (gs_rope_append), attend to the
+ * cache and their ancestors (gs_tree_attention), choose a token each (gs_sample,
+ * or the largest logit), and the path of nodes that were chosen is kept
+ * (gs_tree_accept, gs_tree_commit).  As each node's token is drawn from the
+ * model's own distribution and a drafted one is only kept where it is that token,
+ * the output is distributed as without drafts, whatever drafted them.
+ *
+ * Trees of one call have up to `nodes` <= 64 nodes each; arrays by node are
+ * [trees, nodes].  Node 0 is the root: the last token chosen, not in the cache
+ * yet.  A parent comes before its children.  Like the operators above these need
+ * no handle, allocate nothing, may be captured, and raise an error word.
+ * ------------------------------------------------------------------------ */
+
+/* Attention of every node of each tree over the paged cache:
+ *   out = softmax(scale * q K^T) V over the cached keys 0 .. n - 1 and, of the
+ * nodes' own keys (at slots n .. n + count - 1), those in the node's mask.  A
+ * node that sees nothing gives zeros and lse -inf.
+ *   q       device [trees * nodes, n_heads * head_dim] of the cache's type, row
+ *           stride ld_q (a multiple of 8), 16-byte aligned; out likewise
+ *   seq     device int32 [trees]: the tree's row of the page table, or NULL: tree
+ *           b is sequence b
+ *   n       device int32 [trees]: cached keys before the tree
+ *   count   device int32 [trees]: nodes in use, or NULL: all.  Rows of the others
+ *           are left as they are, and their keys are not read.
+ *   mask    device uint64 [trees, nodes]: bit j: the node sees node j (its own
+ *           bit included, if it is to see itself).  Any pattern.
+ *   pos     device int32 [trees, nodes]: positions (n + depth), read only with a
+ *           window: cached keys at or below pos - window are not seen; a position
+ *           below n counts as n.  The mask alone decides about nodes.  May be NULL
+ *           without a window (0).
+ *   lse     device fp32 [trees * nodes, n_heads] or NULL: ln of the sum of exp of
+ *           the scores
+ *   split_pages, scratch  as in gs_decode_attention
+ * What the cache holds where a node does not see it has no influence on that node,
+ * infinities and NaN included.  Scores, maxima, sums and accumulators are fp32;
+ * the probabilities are rounded to the cache's type for the product with V.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (head_dim, nodes > 64, trees >
+ * 65535, n_heads > 16383), GS_ERR_OOM (scratch too small), GS_ERR_CUDA. */
+size_t gs_tree_attention_scratch_bytes(const gs_cache *cache, int trees, int nodes, int n_heads,
+                                       int split_pages);
+int gs_tree_attention(const gs_cache *cache, const void *q, int64_t ld_q, const int32_t *seq,
+                      const int32_t *n, const int32_t *count, const uint64_t *mask,
+                      const int32_t *pos, int trees, int nodes, int n_heads, float scale, int window,
+                      void *out, int64_t ld_out, float *lse, int split_pages, void *scratch,
+                      size_t scratch_bytes, void *stream);
+
+/* The path of each tree that its model chose: from the root to the first child (by
+ * number) whose token is its parent's choice, and so on.
+ *   parent  device int32 [trees, nodes]: a lower number; node 0's is not read
+ *   token   device int32 [trees, nodes]: drafted tokens; node 0's is not read
+ *   choice  device int32 [trees, nodes]: the token that the model chose to follow
+ *           each node; a negative one (gs_sample's -1) ends the path
+ *   count   device int32 [trees]: nodes in use, or NULL: all
+ *   most    device int32 [trees]: the longest path allowed, or NULL: any
+ *   eos     a path ends at a node whose choice this is; -1: none
+ *   path    device int32 [trees, nodes]: nodes on the path, then -1
+ *   next    device int32 [trees, nodes]: their choices, the tokens that this step
+ *           adds, then -1
+ *   length  device int32 [trees]: how many; at least 1 (the root) unless count or
+ *           most is 0
+ *   err     device int32, raised by a parent that is not a lower number (the node
+ *           is on no path) or a count out of range
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (nodes > 64), GS_ERR_CUDA. */
+int gs_tree_accept(const int32_t *parent, const int32_t *token, const int32_t *choice,
+                   const int32_t *count, const int32_t *most, int eos, int trees, int nodes,
+                   int32_t *path, int32_t *next, int32_t *length, int32_t *err, void *stream);
+
+/* Keys and values of accepted paths moved together, in every layer by one launch:
+ * slot n + path[i] goes to slot n + i for i < length.  Slots beyond are left as
+ * they are, and so is what does not move.
+ *   cache    layer 0; layer l lies l * n_pages pages behind it
+ *   seq, n   as in gs_tree_attention
+ *   path     device int32 [trees, nodes], rising, and length, device int32
+ *            [trees], as gs_tree_accept gives them
+ *   err      device int32, raised by a length, path, sequence, slot or page out of
+ *            range; nothing of that tree is moved then
+ * The slots' pages must not be shared with other sequences or trees.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (head_dim, nodes > 64, n_layers or
+ * trees > 65535), GS_ERR_CUDA. */
+int gs_tree_commit(const gs_cache *cache, int n_layers, const int32_t *seq, const int32_t *n,
+                   const int32_t *path, const int32_t *length, int trees, int nodes, int32_t *err,
+                   void *stream);
+
+/* A matrix [N, K] of 4-bit weights (q - z) * s: whole numbers q in 0 .. 15, and for
+ * each `group` of a row's neighbouring weights a scale s and a zero z in 0 .. 15.
+ *   packed  device, 16-byte aligned, gs_qweight_bytes bytes, made by gs_qweight_pack
+ *   group   32, 64 or 128; K is a multiple of it
+ *   dtype   GS_F16 or GS_BF16: type of scales, inputs and outputs
+ *   zeros   0: every z is 8
+ *   gated   1: rows 0 .. N / 2 - 1 are a SwiGLU's gate and the others its up
+ *           projection, laid out side by side for epilogue 2 */
+typedef struct {
+  void *packed;
+  int N, K, group, dtype, zeros, gated;
+} gs_qweight;
+
+/* Bytes of the packed form (0 on a bad argument; `packed` is not read). */
+size_t gs_qweight_bytes(const gs_qweight *w);
+
+/* Lay weights out, once, in the order in which gs_qlinear reads them.
+ *   q      device uint8 [N, K / 2]: two weights a byte, the first in the low bits
+ *   scale  device [N, K / group] of dtype
+ *   zero   device uint8 [N, K / group] (the low four bits count); NULL where zeros
+ *          is 0
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (another group, K > 2^20, N > 2^24),
+ * GS_ERR_CUDA. */
+int gs_qweight_pack(const gs_qweight *w, const void *q, const void *scale, const void *zero,
+                    void *stream);
+
+/* Y = X . W^T with 4-bit weights, made for the few rows of a decoding step.
+ *   x   device [M, K] of dtype, row stride ld_x (a multiple of 8), 16-byte aligned
+ *   y   device [M, N], row stride ld_y.  epilogue 0: dtype, y = acc; 1: fp32, y +=
+ *       acc; 2: dtype [M, N / 2], silu(gate) * up (gated weights, and only they)
+ *   err device int32: 3 is stored where an fp16 output is beyond the type's range
+ * q - z is exact, sums and the products with s are fp32: the output's rounding is
+ * the only one.  A row's result is the same for any M.
+ * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (as above, M > 2^21), GS_ERR_CUDA. */
+int gs_qlinear(const gs_qweight *w, const void *x, int64_t ld_x, void *y, int64_t ld_y, int M,
+               int epilogue, int32_t *err, void *stream);
+
 #ifdef __cplusplus
 }
 #endif

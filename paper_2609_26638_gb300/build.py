@@ -8,7 +8,7 @@ CSRC = os.path.join(HERE, "csrc")
 BUILD = os.path.join(HERE, "_build")
 LIB = os.path.join(HERE, "libgs.so")
 SOURCES = ["gemm.cu", "engine.cu", "noalloc.cu", "rope_append.cu", "decode_attention.cu", "sample.cu",
-           "pages.cu"]
+           "pages.cu", "tree_attention.cu", "tree.cu", "qlinear.cu"]
 ARCH = ["-gencode", "arch=compute_103a,code=sm_103a"]
 FLAGS = ["-O3", "-std=c++17", "-lineinfo", "-Xcompiler", "-fPIC", "--expt-relaxed-constexpr"]
 

@@ -1,0 +1,718 @@
+// tree_attention.cu -- attention of the nodes of a drafted tree over the paged
+// cache, split over the cache's length and joined.
+//
+//   s_ij = scale * q_i . k_j over the keys that node i sees: the cached ones
+//          (the window's, where there is one) and the nodes of its mask
+//   o_i = sum_j 2^(s'_ij - m_i) v_j / l_i,  l_i = sum_j 2^(s'_ij - m_i)
+//
+// (s' = s log2(e), m the running maximum, 15 less in fp16.)  A query row is one
+// query head of one node; the rows of a KV head, node by node, are cut into tiles
+// of 16 MT.  A block takes one tile and one item of `split` pages; its warps take
+// the item's half pages in turn, straight from global memory into the operand
+// registers of m16n8k16 instructions, and are joined at the item's end.
+//
+// Only steps that reach the tree's nodes, or a window's start, look at masks: a row's
+// view of the step's 32 tokens is one word, the cached range or'ed with its
+// mask shifted into place.  A masked score is replaced by -inf.  A value that no row
+// of the tile sees is cleared; one that some rows see is multiplied as it is, and
+// where it is not finite (0 times it would be NaN for the others) by itself, for the rows
+// that see it.
+#include <algorithm>
+#include <cmath>
+
+#include "attend_common.cuh"
+#include "internal.h"
+
+namespace gs {
+namespace {
+
+constexpr size_t kErrBytes = 256;    // the error word at the scratch's start
+constexpr int kMostNodes = 64;       // bits of a mask
+constexpr int kMostCluster = 8;
+
+struct TreeArgs {
+  const uint16_t* q;
+  int64_t ld_q;
+  const int32_t *seq, *n, *count, *pos;
+  const uint64_t* mask;
+  uint16_t* out;
+  int64_t ld_out;
+  float* lse;
+  int Hq, G, nodes, tiles, window, split, items;
+  int cluster;        // the items of a tile are one cluster, and join there
+  float scale_log2;
+  float* part_o;      // [row][head][item][D]
+  float2* part_ml;    // [row][head][item]
+  int* err;
+  CacheView cache;
+};
+
+// A tree's numbers: cached keys, keys in all, nodes in use, the first key that
+// any node sees, its page and the pages from there on.
+struct Span {
+  int n, keys, count, lo, lo_most, page0, pages;
+  const int32_t* table;
+};
+
+// The first cached key that a node at position `pos` sees; positions below n
+// count as n.
+__device__ __forceinline__ int first_key(int pos, int n, int window) {
+  const long long lo = static_cast<long long>(max(pos, n)) + 1 - window;
+  return lo < 0 ? 0 : lo > n ? n : static_cast<int>(lo);
+}
+
+// The tree's numbers are read by one warp for its block: all threads go through
+// the same pages and barriers whatever happens to the arrays meanwhile.
+__device__ __forceinline__ Span find_span(const TreeArgs& a, int tree) {
+  __shared__ int s_v[6];
+  if (threadIdx.x < 32) {
+    int seq = a.seq ? a.seq[tree] : tree, n = a.n[tree];
+    int count = a.count ? a.count[tree] : a.nodes;
+    const int most = a.cache.pt_stride * kPageTokens;
+    bool bad = count < 0 || count > a.nodes;
+    count = min(max(count, 0), a.nodes);
+    if (n < 0 || n > most - count) {
+      bad = true;
+      n = n < 0 ? 0 : min(n, most);
+    }
+    int keys = min(n + count, most);
+    if (seq < 0 || seq >= a.cache.n_seq) {
+      bad = true;
+      seq = 0;
+      n = keys = 0;
+    }
+    int lo = a.window > 0 ? n : 0, lo_most = 0;
+    if (a.window > 0) {
+      for (int i = threadIdx.x; i < count; i += 32) {
+        const int x = first_key(a.pos[static_cast<int64_t>(tree) * a.nodes + i], n, a.window);
+        lo = min(lo, x);
+        lo_most = max(lo_most, x);
+      }
+      lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+      lo_most = __reduce_max_sync(0xFFFFFFFFu, lo_most);
+    }
+    if (threadIdx.x == 0) {
+      if (bad) atomicExch(a.err, kErrBounds);
+      s_v[0] = seq, s_v[1] = n, s_v[2] = keys, s_v[3] = count, s_v[4] = lo, s_v[5] = lo_most;
+    }
+  }
+  __syncthreads();
+  Span s;
+  s.n = s_v[1];
+  s.keys = s_v[2];
+  s.count = s_v[3];
+  s.lo = s_v[4];
+  s.lo_most = s_v[5];
+  s.page0 = s.lo / kPageTokens;
+  s.pages = max(0, (s.keys + kPageTokens - 1) / kPageTokens - s.page0);
+  s.table = a.cache.page_table + static_cast<int64_t>(s_v[0]) * a.cache.pt_stride;
+  return s;
+}
+
+__device__ __forceinline__ uint32_t bits_below(int x) {
+  return x <= 0 ? 0u : x >= 32 ? 0xFFFFFFFFu : (1u << x) - 1u;
+}
+// Which of the tokens tok0 .. tok0 + 31 a row sees.  `mask` has no bits at or
+// beyond the tree's count.
+__device__ __forceinline__ uint32_t row_view(uint64_t mask, int lo, int n, int tok0) {
+  const int d = n - tok0;
+  uint32_t v = bits_below(d) & ~bits_below(lo - tok0);
+  if (d < 32 && d > -64)
+    v |= d >= 0 ? static_cast<uint32_t>(mask) << d : static_cast<uint32_t>(mask >> -d);
+  return v;
+}
+
+// Which of a register's two 16-bit values are infinite or NaN: all bits of their halves.
+template <bool BF16>
+__device__ __forceinline__ uint32_t not_finite(uint32_t v) {
+  constexpr uint32_t E = BF16 ? 0x7F80u : 0x7C00u;
+  return ((v & E) == E ? 0x0000FFFFu : 0u) | ((v & (E << 16)) == (E << 16) ? 0xFFFF0000u : 0u);
+}
+
+// Four dims of a row's output, and with the first of them its log-sum-exp.
+template <bool BF16, int D>
+__device__ __forceinline__ void store_row(const TreeArgs& a, int64_t row, int head, int d, float m,
+                                          float l, const float4& acc) {
+  const float inv = l != 0.f ? 1.f / l : 0.f;
+  *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(head) * D + d) =
+      make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
+  if (d == 0 && a.lse)     // (the 15 go out of m and l first, without a rounding)
+    a.lse[row * a.Hq + head] =
+        l != 0.f ? (finite_max(m) + kHeld<BF16> + log2f(l * (BF16 ? 1.f : 0x1p-15f))) * kLn2
+                 : -INFINITY;
+}
+
+constexpr int kWarps = 4, kThreads = kWarps * 32;
+constexpr int kStep = 32;            // tokens of a warp's step: half a page
+
+template <int D, int MT>
+struct Smem {
+  static constexpr int R = 16 * MT, P = D + 8;   // row pitch: 8 rows x 4 lanes on distinct banks
+  alignas(16) float so[kWarps * 16 * P];         // the warps' parts of 16 rows
+  alignas(16) float item[R * D];                 // in a cluster: this item's part
+  alignas(16) uint16_t q[MT > 1 ? R * P : 8];    // queries, where they do not fit in registers
+  float2 ml[kWarps][R], item_ml[R];
+  uint64_t mask[R];
+  int lo[R];
+};
+
+template <bool BF16, int D, int MT>
+__global__ void __launch_bounds__(kThreads, D == 64 && MT == 1 ? 3 : 2)
+tree_attention_kernel(const TreeArgs a) {
+  constexpr int R = 16 * MT, P = D + 8, C = D / 32;
+  extern __shared__ __align__(16) uint8_t smem_raw[];
+  Smem<D, MT>& sm = *reinterpret_cast<Smem<D, MT>*>(smem_raw);
+  pdl_trigger();   // the joining kernel may take its place; it waits for this one's end
+  const int tree = blockIdx.z, head = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
+  const int item = blockIdx.x;
+  const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
+  const Span sp = find_span(a, tree);
+  const int items = (sp.pages + a.split - 1) / a.split;
+  const int rows = min(R, sp.count * a.G - tile * R);     // query rows of this tile
+  if (rows <= 0 || (item >= items && item > 0)) {
+    if (a.cluster) {                     // the barriers below want every block
+      cluster_sync_all();
+      cluster_sync_all();
+    }
+    return;
+  }
+  const int64_t row0 = static_cast<int64_t>(tree) * a.nodes;   // the tree's first row
+  auto node_of = [&](int r) { return (tile * R + r) / a.G; };
+  auto q_head = [&](int r) { return head * a.G + (tile * R + r) % a.G; };
+  auto q_at = [&](int r) {
+    return a.q + (row0 + node_of(r)) * a.ld_q + static_cast<int64_t>(q_head(r)) * D;
+  };
+  // this item's steps: the half pages of its pages that hold visible keys
+  const int t0 = (sp.page0 + item * a.split) * 2;
+  const int begin = max(t0, sp.lo / kStep);
+  const int steps = max(0, min(t0 + 2 * a.split, (sp.keys + kStep - 1) / kStep) - begin);
+  const int cnt = steps > warp ? (steps - warp + kWarps - 1) / kWarps : 0;
+
+  // The warp's j-th step is half page begin + warp + j * kWarps; lane l holds
+  // the pool's page of j = 32 i + l.
+  int ids = 0;
+  const int k_lane = (8 * (g >> 1) + (g & 1)) * D + 8 * q, v_lane = g * kPageTokens + 8 * q;
+  const uint16_t *k_at = nullptr, *v_at = nullptr;       // this lane's place in a step's K, V^T
+  auto find_step = [&](int j) {
+    if (j >= cnt) return;
+    if (!(j & 31) && j + lane < cnt) ids = sp.table[(begin + warp + (j + lane) * kWarps) / 2];
+    int page = __shfl_sync(0xFFFFFFFFu, ids, j & 31);
+    if (page < 0 || page >= a.cache.n_pages) {
+      if (lane == 0) atomicExch(a.err, kErrBounds);
+      page = 0;
+    }
+    const int half = (begin + warp + j * kWarps) & 1;
+    k_at = a.cache.block(page, 0, head, D) + half * kStep * D + k_lane;
+    v_at = a.cache.block(page, 1, head, D) + half * kStep + v_lane;
+  };
+  uint4 k[4 * C], v[8];              // S tile i's chunk c; 8 rows of each of 8 V^T tiles
+  auto load_k = [&](int j) {
+    if (j >= cnt) return;
+#pragma unroll
+    for (int i = 0; i < 4; ++i)
+#pragma unroll
+      for (int c = 0; c < C; ++c) k[i * C + c] = load_once(k_at + 2 * i * D + 32 * c);
+  };
+  auto load_v = [&](int j) {
+    if (j >= cnt) return;
+#pragma unroll
+    for (int i = 0; i < 8; ++i) v[i] = load_once(v_at + 8 * i * kPageTokens);
+  };
+  find_step(0);
+  load_k(0);
+  load_v(0);
+
+  // each row's mask and first key, and Q in the operand's order: of each 32
+  // dims, dims 8q .. 8q + 7 on lane q
+  for (int r = threadIdx.x; r < R; r += kThreads) {
+    uint64_t mask = 0;
+    int lo = sp.n;
+    if (r < rows) {
+      const int node = node_of(r);
+      mask = a.mask[row0 + node];
+      if (sp.keys - sp.n < 64) mask &= (1ull << (sp.keys - sp.n)) - 1;
+      lo = a.window > 0 ? min(max(first_key(a.pos[row0 + node], sp.n, a.window), sp.lo), sp.lo_most)
+                        : 0;
+    }
+    sm.mask[r] = mask;
+    sm.lo[r] = lo;
+  }
+  uint32_t qa[MT > 1 ? 1 : C][4], qb[MT > 1 ? 1 : C][4];
+  const uint4 zero4 = make_uint4(0, 0, 0, 0);
+  if constexpr (MT == 1) {
+#pragma unroll
+    for (int c = 0; c < C; ++c) {
+      const uint4 u = g < rows ? *reinterpret_cast<const uint4*>(q_at(g) + 8 * q + 32 * c) : zero4;
+      const uint4 w =
+          g + 8 < rows ? *reinterpret_cast<const uint4*>(q_at(g + 8) + 8 * q + 32 * c) : zero4;
+      qa[c][0] = u.x, qa[c][1] = u.y, qa[c][2] = u.z, qa[c][3] = u.w;
+      qb[c][0] = w.x, qb[c][1] = w.y, qb[c][2] = w.z, qb[c][3] = w.w;
+    }
+  } else {
+    for (int e = threadIdx.x; e < R * (D / 8); e += kThreads) {
+      const int r = e / (D / 8), d = e % (D / 8) * 8;
+      *reinterpret_cast<uint4*>(sm.q + r * P + d) =
+          r < rows ? *reinterpret_cast<const uint4*>(q_at(r) + d) : zero4;
+    }
+  }
+  __syncthreads();
+
+  float o[MT][D / 8][4], m0[MT], m1[MT], l0[MT], l1[MT];
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+#pragma unroll
+    for (int i = 0; i < D / 8; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
+    m0[t] = m1[t] = -INFINITY;
+    l0[t] = l1[t] = 0.f;
+  }
+  for (int j = 0; j < cnt; ++j) {
+    const int tok0 = (begin + warp + j * kWarps) * kStep;
+    const bool edge = tok0 < sp.lo_most || tok0 + kStep > sp.n;
+    uint32_t some = 0u, all = 0xFFFFFFFFu;               // tokens that some row, every row sees
+    uint32_t pa[MT][4], pb[MT][4];
+#pragma unroll
+    for (int t = 0; t < MT; ++t) {
+      // ---- S = Q K^T; column n of S tile i is token 8 (n/2) + 2 i + n%2
+      float s[4][4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+#pragma unroll
+      for (int c = 0; c < C; ++c) {
+        uint4 u, w;
+        if constexpr (MT == 1) {
+          u = make_uint4(qa[c][0], qa[c][1], qa[c][2], qa[c][3]);
+          w = make_uint4(qb[c][0], qb[c][1], qb[c][2], qb[c][3]);
+        } else {
+          u = *reinterpret_cast<const uint4*>(sm.q + (16 * t + g) * P + 8 * q + 32 * c);
+          w = *reinterpret_cast<const uint4*>(sm.q + (16 * t + g + 8) * P + 8 * q + 32 * c);
+        }
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          mma16816<BF16>(s[i], u.x, w.x, u.y, w.y, k[i * C + c].x, k[i * C + c].y);
+#pragma unroll
+        for (int i = 0; i < 4; ++i)
+          mma16816<BF16>(s[i], u.z, w.z, u.w, w.w, k[i * C + c].z, k[i * C + c].w);
+      }
+      // ---- softmax; this lane's columns 2q, 2q + 1 of tile i are tokens
+      //      tok0 + 8 q + 2 i + {0, 1}
+      if (edge) {
+        const int r = 16 * t + g;
+        const uint32_t v0 = row_view(sm.mask[r], sm.lo[r], sp.n, tok0),
+                       v1 = row_view(sm.mask[r + 8], sm.lo[r + 8], sp.n, tok0);
+        if (r < rows) some |= v0, all &= v0;
+        if (r + 8 < rows) some |= v1, all &= v1;
+        const uint32_t w0 = v0 >> (8 * q), w1 = v1 >> (8 * q);
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+          if (!((w0 >> (2 * i)) & 1)) s[i][0] = -INFINITY;
+          if (!((w0 >> (2 * i + 1)) & 1)) s[i][1] = -INFINITY;
+          if (!((w1 >> (2 * i)) & 1)) s[i][2] = -INFINITY;
+          if (!((w1 >> (2 * i + 1)) & 1)) s[i][3] = -INFINITY;
+        }
+      }
+      float x0 = -INFINITY, x1 = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        x0 = fmaxf(x0, fmaxf(s[i][0], s[i][1]));
+        x1 = fmaxf(x1, fmaxf(s[i][2], s[i][3]));
+      }
+      x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1));
+      x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
+      x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
+      x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
+      const float n0 = fmaxf(m0[t], held_max<BF16>(x0, a.scale_log2)),
+                  n1 = fmaxf(m1[t], held_max<BF16>(x1, a.scale_log2));
+      if (__any_sync(0xFFFFFFFFu, n0 != m0[t] || n1 != m1[t])) {
+        const float f0 = ex2(m0[t] - finite_max(n0)), f1 = ex2(m1[t] - finite_max(n1));
+        l0[t] *= f0;
+        l1[t] *= f1;
+#pragma unroll
+        for (int i = 0; i < D / 8; ++i) {
+          o[t][i][0] *= f0;
+          o[t][i][1] *= f0;
+          o[t][i][2] *= f1;
+          o[t][i][3] *= f1;
+        }
+        m0[t] = n0;
+        m1[t] = n1;
+      }
+      const float z0 = finite_max(m0[t]), z1 = finite_max(m1[t]);
+#pragma unroll
+      for (int i = 0; i < 4; ++i) {
+        const float e0 = ex2(fmaf(s[i][0], a.scale_log2, -z0)),
+                    e1 = ex2(fmaf(s[i][1], a.scale_log2, -z0)),
+                    e2 = ex2(fmaf(s[i][2], a.scale_log2, -z1)),
+                    e3 = ex2(fmaf(s[i][3], a.scale_log2, -z1));
+        l0[t] += e0 + e1;
+        l1[t] += e2 + e3;
+        pa[t][i] = pack2<BF16>(e0, e1);
+        pb[t][i] = pack2<BF16>(e2, e3);
+      }
+    }
+    const uint16_t* v_now = v_at;
+    find_step(j + 1);
+    if constexpr (D == 64) {
+      load_k(j + 1);
+    } else {   // K's registers take the other dims' values first
+#pragma unroll
+      for (int i = 0; i < 8; ++i) k[i] = load_once(v_now + 8 * (8 + i) * kPageTokens);
+    }
+    // ---- O += P V, 8 tiles of 8 dims at a time
+    if (edge) {
+      some = __reduce_or_sync(0xFFFFFFFFu, some);
+      all = __reduce_and_sync(0xFFFFFFFFu, all);
+    }
+    auto multiply = [&](int i0, uint4* x) {
+      uint32_t odd = 0u;         // tokens with a value that is not finite, seen by some rows only
+      if (edge) {
+        const uint32_t keep = some >> (8 * q), part = (some & ~all) >> (8 * q);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            if (!((keep >> (2 * e)) & 1)) w[e] &= 0xFFFF0000u;
+            if (!((keep >> (2 * e + 1)) & 1)) w[e] &= 0x0000FFFFu;
+            if (not_finite<BF16>(w[e])) odd |= ((part >> (2 * e)) & 3u) << (8 * q + 2 * e);
+          }
+          x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+        }
+        odd = __reduce_or_sync(0xFFFFFFFFu, odd);
+      }
+      for (uint32_t left = odd; left; left &= left - 1) {
+        const int tok = __ffs(left) - 1;
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+          uint32_t w[4] = {x[i].x, x[i].y, x[i].z, x[i].w};
+          uint32_t one[4] = {0u, 0u, 0u, 0u};
+#pragma unroll
+          for (int e = 0; e < 4; ++e)
+            if (tok >> 1 == 4 * q + e) {
+              const uint32_t sel = not_finite<BF16>(w[e]) & (tok & 1 ? 0xFFFF0000u : 0x0000FFFFu);
+              one[e] = w[e] & sel;
+              w[e] &= ~sel;
+            }
+          x[i] = make_uint4(w[0], w[1], w[2], w[3]);
+#pragma unroll
+          for (int t = 0; t < MT; ++t) {
+            float p[4] = {0.f, 0.f, 0.f, 0.f};
+            mma16816<BF16>(p, pa[t][0], pb[t][0], pa[t][1], pb[t][1], one[0], one[1]);
+            mma16816<BF16>(p, pa[t][2], pb[t][2], pa[t][3], pb[t][3], one[2], one[3]);
+            const int r = 16 * t + g;
+            if ((row_view(sm.mask[r], sm.lo[r], sp.n, tok0) >> tok) & 1)
+              o[t][i0 + i][0] += p[0], o[t][i0 + i][1] += p[1];
+            if ((row_view(sm.mask[r + 8], sm.lo[r + 8], sp.n, tok0) >> tok) & 1)
+              o[t][i0 + i][2] += p[2], o[t][i0 + i][3] += p[3];
+          }
+        }
+      }
+#pragma unroll
+      for (int t = 0; t < MT; ++t) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          mma16816<BF16>(o[t][i0 + i], pa[t][0], pb[t][0], pa[t][1], pb[t][1], x[i].x, x[i].y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          mma16816<BF16>(o[t][i0 + i], pa[t][2], pb[t][2], pa[t][3], pb[t][3], x[i].z, x[i].w);
+      }
+    };
+    multiply(0, v);
+    load_v(j + 1);
+    if constexpr (D == 128) {
+      multiply(8, k);
+      load_k(j + 1);
+    }
+  }
+
+  // ---- the warps' parts are joined, in warp order, 16 rows at a time
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    l0[t] += __shfl_xor_sync(0xFFFFFFFFu, l0[t], 1);
+    l0[t] += __shfl_xor_sync(0xFFFFFFFFu, l0[t], 2);
+    l1[t] += __shfl_xor_sync(0xFFFFFFFFu, l1[t], 1);
+    l1[t] += __shfl_xor_sync(0xFFFFFFFFu, l1[t], 2);
+    if (q == 0) {
+      sm.ml[warp][16 * t + g] = make_float2(m0[t], l0[t]);
+      sm.ml[warp][16 * t + g + 8] = make_float2(m1[t], l1[t]);
+    }
+  }
+  const int used = min(kWarps, steps);
+#pragma unroll
+  for (int t = 0; t < MT; ++t) {
+    if (t > 0) __syncthreads();
+    if (cnt > 0) {
+#pragma unroll
+      for (int i = 0; i < D / 8; ++i) {
+        *reinterpret_cast<float2*>(sm.so + (warp * 16 + g) * P + 8 * i + 2 * q) =
+            make_float2(o[t][i][0], o[t][i][1]);
+        *reinterpret_cast<float2*>(sm.so + (warp * 16 + g + 8) * P + 8 * i + 2 * q) =
+            make_float2(o[t][i][2], o[t][i][3]);
+      }
+    }
+    __syncthreads();
+    const int here = min(16, rows - 16 * t);
+    for (int e = threadIdx.x; e < here * (D / 4); e += kThreads) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4, rt = 16 * t + r;
+      float m = -INFINITY, l = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+      for (int w = 0; w < used; ++w) m = fmaxf(m, sm.ml[w][rt].x);
+      const float z = finite_max(m);
+      for (int w = 0; w < used; ++w) {
+        const float f = ex2(sm.ml[w][rt].x - z);
+        const float4 x = *reinterpret_cast<const float4*>(sm.so + (w * 16 + r) * P + d);
+        l = fmaf(f, sm.ml[w][rt].y, l);
+        acc.x = fmaf(f, x.x, acc.x);
+        acc.y = fmaf(f, x.y, acc.y);
+        acc.z = fmaf(f, x.z, acc.z);
+        acc.w = fmaf(f, x.w, acc.w);
+      }
+      const int64_t row = row0 + node_of(rt);
+      if (items <= 1) {
+        store_row<BF16, D>(a, row, q_head(rt), d, m, l, acc);
+      } else if (a.cluster) {
+        *reinterpret_cast<float4*>(sm.item + rt * D + d) = acc;
+        if (d == 0) sm.item_ml[rt] = make_float2(m, l);
+      } else {
+        const int64_t at = row * a.Hq + q_head(rt);
+        *reinterpret_cast<float4*>(a.part_o + (at * a.items + item) * D + d) = acc;
+        if (d == 0) a.part_ml[at * a.items + item] = make_float2(m, l);
+      }
+    }
+  }
+  if (!a.cluster) return;
+  // ---- the items, in order: the tile's values are dealt to the cluster's blocks
+  __syncwarp();
+  cluster_sync_all();
+  if (items > 1) {
+    const uint32_t o_at = smem_u32(sm.item), ml_at = smem_u32(sm.item_ml);
+    for (int e = item * kThreads + threadIdx.x; e < rows * (D / 4); e += items * kThreads) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
+      float2 ml[kMostCluster];
+      float4 x[kMostCluster];
+      float m = -INFINITY;
+#pragma unroll
+      for (int i = 0; i < kMostCluster; ++i)
+        if (i < items) {
+          ml[i] = ld_cluster_f32x2(cluster_map(ml_at + r * 8, i));
+          x[i] = ld_cluster_f32x4(cluster_map(o_at + (r * D + d) * 4, i));
+        }
+#pragma unroll
+      for (int i = 0; i < kMostCluster; ++i)
+        if (i < items) m = fmaxf(m, ml[i].x);
+      const float z = finite_max(m);
+      float l = 0.f;
+      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+#pragma unroll
+      for (int i = 0; i < kMostCluster; ++i)
+        if (i < items) add_scaled(acc, l, x[i], ml[i].y, ex2(ml[i].x - z));
+      store_row<BF16, D>(a, row0 + node_of(r), q_head(r), d, m, l, acc);
+    }
+  }
+  __syncwarp();
+  cluster_sync_all();                    // the peers have read this block's part
+}
+
+// Joins a row's items, one query head per block: the items are dealt to the
+// block's thread groups (one thread per four dims) in turn and the groups'
+// sums are added in order, so the result depends on the row's items alone.
+constexpr int kJoinThreads = 256;
+
+template <bool BF16, int D>
+__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a) {
+  constexpr int L = D / 4, NG = kJoinThreads / L;
+  __shared__ float s_max[kJoinThreads / 32];
+  __shared__ float4 s_acc[NG][L];
+  __shared__ float s_l[NG];
+  const int h = blockIdx.x % a.Hq, node = blockIdx.x / a.Hq, tree = blockIdx.y;
+  pdl_wait();      // in every block: the grid ends after the first kernel's
+  const Span sp = find_span(a, tree);
+  const int items = (sp.pages + a.split - 1) / a.split;
+  if (items <= 1 || node >= sp.count) return;
+  const int64_t row = static_cast<int64_t>(tree) * a.nodes + node, at = row * a.Hq + h;
+  const float2* ml = a.part_ml + at * a.items;
+  const float4* po = reinterpret_cast<const float4*>(a.part_o + at * a.items * D);
+  float m = -INFINITY;
+  for (int i = threadIdx.x; i < items; i += kJoinThreads) m = fmaxf(m, ml[i].x);
+#pragma unroll
+  for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, x));
+  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
+  __syncthreads();
+#pragma unroll
+  for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, s_max[w]);
+  const float z = finite_max(m);
+  const int grp = threadIdx.x / L, d = threadIdx.x % L;
+  float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+  float l = 0.f;
+#pragma unroll 4
+  for (int i = grp; i < items; i += NG) {
+    const float2 x = ml[i];
+    add_scaled(acc, l, po[static_cast<int64_t>(i) * L + d], x.y, ex2(x.x - z));
+  }
+  s_acc[grp][d] = acc;
+  if (d == 0) s_l[grp] = l;
+  __syncthreads();
+  if (grp > 0) return;
+  for (int i = 1; i < NG; ++i) add_scaled(acc, l, s_acc[i][d], s_l[i], 1.f);
+  store_row<BF16, D>(a, row, h, 4 * d, m, l, acc);
+}
+
+// Pages of an item when the caller leaves it open: one wave of blocks shares the
+// cache evenly, or eight items that join in a cluster where that is not long; of
+// several trees, which may differ in length, items of at most kMostPages.
+constexpr int64_t wave_of(int head_dim) { return head_dim == 64 ? 320 : 256; }
+constexpr int kMostPages = 12;
+int auto_split(int pages, int trees, int64_t blocks_per_item, int head_dim) {
+  const int64_t wave = wave_of(head_dim) / blocks_per_item;
+  int64_t items = wave < 1 ? 1 : wave;
+  if (items > kMostCluster && pages <= 8 * kMostCluster) items = kMostCluster;
+  int64_t split = (pages + items - 1) / items;
+  if (split < 2) split = 2;
+  if (split > kMostPages && trees > 1) split = kMostPages;
+  return static_cast<int>(split < pages ? split : pages);
+}
+
+// 16-row tiles of a block.
+int row_tiles(int, int) { return 1; }
+
+struct Plan {
+  int mt, tiles, split, items;
+};
+Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window, int split_pages) {
+  Plan p;
+  const int G = n_heads / c.n_kv_heads;
+  p.mt = row_tiles(nodes * G, c.head_dim);
+  p.tiles = (nodes * G + 16 * p.mt - 1) / (16 * p.mt);
+  int pages = c.pt_stride;
+  if (window > 0) {
+    const int64_t most = (static_cast<int64_t>(window) - 1 + nodes + kPageTokens - 2) / kPageTokens + 1;
+    if (most < pages) pages = static_cast<int>(most);
+  }
+  p.split = split_pages > 0 ? std::min(split_pages, c.pt_stride)
+                            : auto_split(pages, trees, static_cast<int64_t>(trees < 1 ? 1 : trees) *
+                                                           c.n_kv_heads * p.tiles,
+                                         c.head_dim);
+  p.items = (pages + p.split - 1) / p.split;
+  return p;
+}
+
+template <bool BF16, int D, int MT>
+cudaError_t launch_tiles(const TreeArgs& a, int trees, cudaStream_t s) {
+  static DeviceOnce once;
+  constexpr size_t smem = sizeof(Smem<D, MT>);
+  auto kernel = tree_attention_kernel<BF16, D, MT>;
+  cudaError_t e = once.run([&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+  });
+  if (e != cudaSuccess) return e;
+  e = launch_ex(kernel, dim3(a.items, a.cache.Hkv * a.tiles, trees), dim3(kThreads), smem, s, false,
+                dim3(a.cluster ? a.items : 1, 1, 1), a);
+  if (e != cudaSuccess || a.items == 1 || a.cluster) return e;
+  return launch_ex(tree_join_kernel<BF16, D>, dim3(a.Hq * a.nodes, trees), dim3(kJoinThreads), 0, s,
+                   true, dim3(1, 1, 1), a);
+}
+
+template <bool BF16, int D>
+cudaError_t launch_tree(const TreeArgs& a, int mt, int trees, cudaStream_t s) {
+  (void)mt;
+  return launch_tiles<BF16, D, 1>(a, trees, s);
+}
+
+size_t up256(size_t x) { return (x + 255) / 256 * 256; }
+
+struct Scratch {
+  size_t o, ml, total;   // offsets of the partial accumulators and of their (max, sum)
+};
+Scratch scratch_of(const gs_cache& c, int64_t rows, int n_heads, size_t items) {
+  const size_t n = static_cast<size_t>(rows) * n_heads * items;
+  const size_t ml = kErrBytes + up256(n * c.head_dim * sizeof(float));
+  return {kErrBytes, ml, ml + up256(n * sizeof(float2))};
+}
+
+// GS_OK, or what is wrong with the sizes of a call.
+int check_sizes(const gs_cache* c, int trees, int nodes, int n_heads, int split_pages) {
+  if (const int rc = check_cache(c)) return rc;
+  if (trees < 0 || nodes < 1 || n_heads < 1 || n_heads % c->n_kv_heads || split_pages < 0)
+    return GS_ERR_INVALID_ARG;
+  // trees and heads' tiles are grid dimensions
+  if (nodes > kMostNodes || trees > 65535 || n_heads >= (1 << 14)) return GS_ERR_UNSUPPORTED;
+  return GS_OK;
+}
+
+}  // namespace
+}  // namespace gs
+
+extern "C" size_t gs_tree_attention_scratch_bytes(const gs_cache* cache, int trees, int nodes,
+                                                  int n_heads, int split_pages) {
+  using namespace gs;
+  if (check_sizes(cache, trees, nodes, n_heads, split_pages) != GS_OK) return 0;
+  const Plan p = plan_tree(*cache, trees, nodes, n_heads, 0, split_pages);
+  // An open split follows the pages that a window leaves: whatever it is, the
+  // items are at most one wave's share, a cluster, or pages / kMostPages, and
+  // the rounding.
+  size_t items = p.items;
+  if (split_pages == 0) {
+    const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * cache->n_kv_heads * p.tiles;
+    const size_t wave = static_cast<size_t>(wave_of(cache->head_dim) / blocks),
+                 cut = cache->pt_stride / kMostPages, cluster = kMostCluster;
+    items = std::max(std::max(wave, cut), cluster) + 2;
+    if (items > static_cast<size_t>(cache->pt_stride)) items = cache->pt_stride;
+  }
+  return scratch_of(*cache, static_cast<int64_t>(trees) * nodes, n_heads, items).total;
+}
+
+extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t ld_q,
+                                 const int32_t* seq, const int32_t* n, const int32_t* count,
+                                 const uint64_t* mask, const int32_t* pos, int trees, int nodes,
+                                 int n_heads, float scale, int window, void* out, int64_t ld_out,
+                                 float* lse, int split_pages, void* scratch, size_t scratch_bytes,
+                                 void* stream) {
+  using namespace gs;
+  if (const int rc = check_sizes(cache, trees, nodes, n_heads, split_pages)) return rc;
+  if (!q || !n || !mask || !out || !scratch || window < 0 || (window > 0 && !pos) ||
+      !(scale > 0.f) || !std::isfinite(scale))
+    return GS_ERR_INVALID_ARG;
+  const int D = cache->head_dim;
+  const int64_t width = static_cast<int64_t>(n_heads) * D;
+  if (ld_q < width || ld_out < width || ld_q % 8 || ld_out % 8 || !aligned16(q) || !aligned16(out) ||
+      (reinterpret_cast<uintptr_t>(scratch) & 255) || (reinterpret_cast<uintptr_t>(mask) & 7))
+    return GS_ERR_INVALID_ARG;
+  if (!aligned4(seq, n, count, pos, lse)) return GS_ERR_INVALID_ARG;
+  if (scratch_bytes < gs_tree_attention_scratch_bytes(cache, trees, nodes, n_heads, split_pages))
+    return GS_ERR_OOM;
+  if (trees == 0) return GS_OK;
+  const Plan p = plan_tree(*cache, trees, nodes, n_heads, window, split_pages);
+  const Scratch sc = scratch_of(*cache, static_cast<int64_t>(trees) * nodes, n_heads, p.items);
+  uint8_t* base = static_cast<uint8_t*>(scratch);
+  TreeArgs a;
+  a.q = static_cast<const uint16_t*>(q);
+  a.ld_q = ld_q;
+  a.seq = seq;
+  a.n = n;
+  a.count = count;
+  a.pos = pos;
+  a.mask = mask;
+  a.out = static_cast<uint16_t*>(out);
+  a.ld_out = ld_out;
+  a.lse = lse;
+  a.Hq = n_heads;
+  a.G = n_heads / cache->n_kv_heads;
+  a.nodes = nodes;
+  a.tiles = p.tiles;
+  a.window = window;
+  a.split = p.split;
+  a.items = p.items;
+  a.cluster = p.items > 1 && p.items <= kMostCluster &&
+              static_cast<int64_t>(p.items) * cache->n_kv_heads * p.tiles * trees <= wave_of(D);
+  a.scale_log2 = scale * kLog2e;
+  a.part_o = reinterpret_cast<float*>(base + sc.o);
+  a.part_ml = reinterpret_cast<float2*>(base + sc.ml);
+  a.err = static_cast<int*>(scratch);
+  a.cache = cache_view(*cache);
+  cudaStream_t s = static_cast<cudaStream_t>(stream);
+  cudaError_t e;
+  if (cache->dtype == GS_BF16)
+    e = D == 64 ? launch_tree<true, 64>(a, p.mt, trees, s) : launch_tree<true, 128>(a, p.mt, trees, s);
+  else
+    e = D == 64 ? launch_tree<false, 64>(a, p.mt, trees, s) : launch_tree<false, 128>(a, p.mt, trees, s);
+  return e == cudaSuccess ? GS_OK : GS_ERR_CUDA;
+}

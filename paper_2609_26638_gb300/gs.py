@@ -89,6 +89,11 @@ class gs_sample_params(ctypes.Structure):
     _fields_ = [(n, ctypes.c_void_p) for n in ("temperature", "top_p", "min_p", "top_k")]
 
 
+class gs_qweight(ctypes.Structure):
+    _fields_ = [("packed", ctypes.c_void_p)] + [
+        (n, ctypes.c_int) for n in ("N", "K", "group", "dtype", "zeros", "gated")]
+
+
 def _load():
     if not os.path.exists(LIB_PATH):
         raise ImportError(f"libgs.so not built at {LIB_PATH}; run __graft_entry__.build()")
@@ -133,6 +138,14 @@ def _load():
         "gs_sample": (i32, [vp, i64, i32, i32, i32, ctypes.POINTER(gs_sample_params), vp, vp, vp,
                             vp, vp]),
         "gs_pages_copy": (i32, [vp, i32, vp, i32, i32, i64, vp, vp, i32, vp, vp]),
+        "gs_tree_attention_scratch_bytes": (sz, [ctypes.POINTER(gs_cache), i32, i32, i32, i32]),
+        "gs_tree_attention": (i32, [ctypes.POINTER(gs_cache), vp, i64, vp, vp, vp, vp, vp, i32, i32,
+                                    i32, ctypes.c_float, i32, vp, i64, vp, i32, vp, sz, vp]),
+        "gs_tree_accept": (i32, [vp, vp, vp, vp, vp, i32, i32, i32, vp, vp, vp, vp, vp]),
+        "gs_tree_commit": (i32, [ctypes.POINTER(gs_cache), i32, vp, vp, vp, vp, i32, i32, vp, vp]),
+        "gs_qweight_bytes": (sz, [ctypes.POINTER(gs_qweight)]),
+        "gs_qweight_pack": (i32, [ctypes.POINTER(gs_qweight), vp, vp, vp, vp]),
+        "gs_qlinear": (i32, [ctypes.POINTER(gs_qweight), vp, i64, vp, i64, i32, i32, vp, vp]),
     }
     for name, (res, args) in sig.items():
         f = getattr(lib, name)
@@ -148,7 +161,8 @@ EXPORTED = ("gs_workspace_bytes", "gs_create", "gs_destroy", "gs_last_error", "g
             "gs_attention_scratch_bytes", "gs_attention", "gs_linear_scratch_bytes", "gs_linear",
             "gs_linear_noalloc", "gs_linear_noalloc_status", "gs_rope_table", "gs_rope_append",
             "gs_decode_attention_scratch_bytes", "gs_decode_attention", "gs_sample",
-            "gs_pages_copy")
+            "gs_pages_copy", "gs_tree_attention_scratch_bytes", "gs_tree_attention", "gs_tree_accept",
+            "gs_tree_commit", "gs_qweight_bytes", "gs_qweight_pack", "gs_qlinear")
 
 
 def lib():
@@ -350,3 +364,55 @@ def gs_pages_copy(src_ptr, src_pages, dst_ptr, dst_pages, n_layers, page_bytes, 
                             src_ids_ptr, dst_ids_ptr, n, err_ptr, stream_ptr)
     if rc != GS_OK:
         raise GsError(rc, "gs_pages_copy")
+
+
+# ------------------------------------------------------------------ drafted trees, 4-bit weights
+def gs_tree_attention_scratch_bytes(cache: gs_cache, trees, nodes, n_heads, split_pages) -> int:
+    return int(_lib.gs_tree_attention_scratch_bytes(cache, trees, nodes, n_heads, split_pages))
+
+
+def gs_tree_attention(cache: gs_cache, q_ptr, ld_q, seq_ptr, n_ptr, count_ptr, mask_ptr, pos_ptr, trees,
+                      nodes, n_heads, scale, window, out_ptr, ld_out, lse_ptr, split_pages, scratch_ptr,
+                      scratch_bytes, stream_ptr) -> None:
+    """Attention of every node of drafted trees over their sequences' pages and their masks' nodes."""
+    rc = _lib.gs_tree_attention(cache, q_ptr, ld_q, seq_ptr, n_ptr, count_ptr, mask_ptr, pos_ptr, trees,
+                                nodes, n_heads, scale, window, out_ptr, ld_out, lse_ptr, split_pages,
+                                scratch_ptr, scratch_bytes, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_tree_attention")
+
+
+def gs_tree_accept(parent_ptr, token_ptr, choice_ptr, count_ptr, most_ptr, eos, trees, nodes, path_ptr,
+                   next_ptr, length_ptr, err_ptr, stream_ptr) -> None:
+    """The path of each tree along the nodes that carry their parent's choice."""
+    rc = _lib.gs_tree_accept(parent_ptr, token_ptr, choice_ptr, count_ptr, most_ptr, eos, trees, nodes,
+                             path_ptr, next_ptr, length_ptr, err_ptr, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_tree_accept")
+
+
+def gs_tree_commit(cache: gs_cache, n_layers, seq_ptr, n_ptr, path_ptr, length_ptr, trees, nodes, err_ptr,
+                   stream_ptr) -> None:
+    """Move the keys and values of accepted paths to consecutive slots, in every layer."""
+    rc = _lib.gs_tree_commit(cache, n_layers, seq_ptr, n_ptr, path_ptr, length_ptr, trees, nodes, err_ptr,
+                             stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_tree_commit")
+
+
+def gs_qweight_bytes(w: gs_qweight) -> int:
+    return int(_lib.gs_qweight_bytes(w))
+
+
+def gs_qweight_pack(w: gs_qweight, q_ptr, scale_ptr, zero_ptr, stream_ptr) -> None:
+    """Lay 4-bit weights out in the order in which gs_qlinear reads them."""
+    rc = _lib.gs_qweight_pack(w, q_ptr, scale_ptr, zero_ptr, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_qweight_pack")
+
+
+def gs_qlinear(w: gs_qweight, x_ptr, ld_x, y_ptr, ld_y, M, epilogue, err_ptr, stream_ptr) -> None:
+    """y = x w^T with 4-bit weights (epilogues EPI_STORE_F16, EPI_RESID_F32, EPI_SWIGLU)."""
+    rc = _lib.gs_qlinear(w, x_ptr, ld_x, y_ptr, ld_y, M, epilogue, err_ptr, stream_ptr)
+    if rc != GS_OK:
+        raise GsError(rc, "gs_qlinear")

@@ -1,0 +1,209 @@
+"""gs_qlinear against products in 64 bits.
+
+Tolerances.  q - z is exact and so are its products with x in fp32 (5 and at
+most 11 bits).  With A = sum_k |w_k x_k| of an output, each tensor instruction
+adds 16 products with an error of at most 2^-22 of the sum so far, which is at most
+A: K / 16 of them, and one product with a scale per group, a sum per slice:
+(K / 8 + 32) 2^-23 A.  Then the output's rounding, u |y| with u = 2^-11 (fp16) or
+2^-8 (bf16), or 2^-24 (|y| + |acc|) for fp32.  A gate's error passes through silu
+with a slope of at most 1.1, and its exponential and quotient add 2^-20 of the result."""
+import numpy as np
+import pytest
+import torch
+
+pytestmark = pytest.mark.gpu
+DEV = "cuda:0"
+TYPES = {"fp16": torch.float16, "bf16": torch.bfloat16}
+UNIT = {"fp16": 2.0 ** -11, "bf16": 2.0 ** -8}
+
+
+@pytest.fixture(scope="module")
+def gs():
+    from paper_2609_26638_gb300 import gs as binding
+    return binding
+
+
+def _weights(gs, dtype, N, K, group, zeros, gated, seed=0, scale=0.05, stream=None):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    q = torch.randint(0, 16, (N, K), device=DEV, generator=g, dtype=torch.uint8)
+    s = (scale * (0.5 + torch.rand(N, K // group, device=DEV, generator=g))).to(TYPES[dtype])
+    z = torch.randint(0, 16, (N, K // group), device=DEV, generator=g, dtype=torch.uint8) if zeros else None
+    w = gs.gs_qweight(0, N, K, group, gs.GS_F16 if dtype == "fp16" else gs.GS_BF16, int(zeros), int(gated))
+    packed = torch.full((gs.gs_qweight_bytes(w) + 64,), 0x7F, dtype=torch.uint8, device=DEV)
+    w.packed = packed.data_ptr()
+    plain = (q[:, 0::2] | (q[:, 1::2] << 4)).contiguous()
+    torch.cuda.synchronize()
+    gs.gs_qweight_pack(w, plain.data_ptr(), s.data_ptr(), z.data_ptr() if zeros else 0,
+                       (stream or torch.cuda.current_stream()).cuda_stream)
+    torch.cuda.synchronize()
+    assert (packed[-64:] == 0x7F).all()
+    w.held = packed                      # the descriptor names the memory, it does not own it
+    zz = 8 if z is None else z.double().repeat_interleave(group, 1)
+    return w, (q.double() - zz) * s.double().repeat_interleave(group, 1)
+
+
+def _run(gs, w, x, epilogue=0, y=None, ld=None, stream=None):
+    outs = w.N // 2 if w.gated else w.N
+    if y is None:
+        y = torch.full((x.shape[0], ld or outs), 7.0, dtype=torch.float32 if epilogue == 1 else x.dtype,
+                       device=DEV)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    torch.cuda.synchronize()
+    gs.gs_qlinear(w, x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), x.shape[0], epilogue,
+                  err.data_ptr(), (stream or torch.cuda.current_stream()).cuda_stream)
+    torch.cuda.synchronize()
+    return y, int(err.item())
+
+
+def _x(dtype, M, K, seed=1, scale=1.0):
+    g = torch.Generator(device=DEV).manual_seed(seed)
+    return (scale * torch.randn(M, K, device=DEV, generator=g)).to(TYPES[dtype])
+
+
+def _bounds(W, x, y_plain=None):
+    K = W.shape[1]
+    return (K / 8 + 32) * 2.0 ** -23 * (x.double().abs() @ W.abs().t())
+
+
+def _check(dtype, y, W, x, gated=False):
+    u = UNIT[dtype]
+    acc, err = x.double() @ W.t(), _bounds(W, x)
+    if gated:
+        half = W.shape[0] // 2
+        (ga, up), (eg, eu) = (t.split(half, dim=1) for t in (acc, err))
+        silu = ga * torch.sigmoid(ga)
+        acc = silu * up
+        err = 1.1 * eg * (up.abs() + eu) + silu.abs() * eu + 2.0 ** -20 * acc.abs()
+    bound = err + u * (acc.abs() + err) + 2.0 ** -25
+    worst = ((y.double() - acc).abs() / bound).max().item()
+    assert worst <= 1.0, worst
+
+
+SHAPES = [(1, 32), (7, 32), (16, 64), (40, 96), (128, 128), (129, 160), (1000, 1024), (130, 2080),
+          (2048, 512), (264, 4096), (5000, 320)]
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("group", [32, 64, 128])
+@pytest.mark.parametrize("zeros", [False, True])
+def test_shapes(gs, dtype, group, zeros):
+    for i, (N, K) in enumerate(SHAPES):
+        K = -(-K // group) * group
+        w, W = _weights(gs, dtype, N, K, group, zeros, False, seed=i)
+        for M in (1, 2, 8, 9, 17, 33):
+            x = _x(dtype, M, K, seed=M)
+            y, err = _run(gs, w, x)
+            assert err == 0
+            _check(dtype, y, W, x)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("F,K,group", [(1, 32, 32), (8, 64, 64), (13, 96, 32), (64, 256, 128),
+                                       (1000, 1024, 64), (4096, 1024, 32)])
+def test_gated(gs, dtype, F, K, group):
+    w, W = _weights(gs, dtype, 2 * F, K, group, True, True, seed=F, scale=0.02)
+    for M in (1, 5, 16, 40):
+        x = _x(dtype, M, K, seed=M)
+        y, err = _run(gs, w, x, epilogue=2)
+        assert err == 0
+        _check(dtype, y, W, x, gated=True)
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+def test_residual(gs, dtype):
+    for N, K in ((7, 64), (1024, 1024), (515, 192)):
+        w, W = _weights(gs, dtype, N, K, 64, True, False)
+        for M in (1, 19, 70):
+            x = _x(dtype, M, K)
+            before = torch.randn(M, N + 3, device=DEV)
+            y, err = _run(gs, w, x, epilogue=1, y=before.clone())
+            assert err == 0 and torch.equal(y[:, N:], before[:, N:])
+            acc, e = x.double() @ W.t(), _bounds(W, x)
+            want = before[:, :N].double() + acc
+            bound = e + 2.0 ** -24 * (want.abs() + acc.abs() + 2 * e) + 2.0 ** -30
+            assert ((y[:, :N].double() - want).abs() <= bound).all()
+
+
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("N,K,gated", [(1024, 1024, False), (264, 4096, False), (2048, 640, True),
+                                       (20000, 256, False)])
+def test_rows_do_not_depend_on_the_batch(gs, dtype, N, K, gated):
+    """A row has the same bits alone and in any batch, at any place of it."""
+    w, W = _weights(gs, dtype, N, K, 64, True, gated, scale=0.02)
+    x = _x(dtype, 150, K)
+    epi = 2 if gated else 0
+    whole, err = _run(gs, w, x, epilogue=epi)
+    assert err == 0
+    _check(dtype, whole, W, x, gated)
+    for a, b in ((0, 1), (3, 4), (77, 78), (5, 13), (20, 36), (64, 96), (100, 150), (1, 66)):
+        y, _ = _run(gs, w, x[a:b], epilogue=epi)
+        assert torch.equal(y, whole[a:b]), (a, b)
+
+
+def test_strides_and_streams(gs):
+    """Rows apart in memory, odd output strides, what lies between is left alone."""
+    for dtype in TYPES:
+        w, W = _weights(gs, dtype, 200, 192, 64, True, False, stream=torch.cuda.Stream())
+        wide = torch.full((21, 192 + 24), float("nan"), dtype=TYPES[dtype], device=DEV)
+        wide[:, :192] = _x(dtype, 21, 192)
+        plain, _ = _run(gs, w, wide[:, :192].contiguous())
+        for ld in (200, 201, 202, 204, 333):
+            y, err = _run(gs, w, wide[:, :192], ld=ld, stream=torch.cuda.Stream())
+            assert err == 0 and torch.equal(y[:, :200], plain) and (y[:, 200:] == 7).all()
+        # an output that starts in the middle of eight bytes
+        room = torch.full((21 * 300,), 7.0, dtype=TYPES[dtype], device=DEV)
+        y, err = _run(gs, w, wide[:, :192], y=room[1: 1 + 21 * 204].view(21, 204))
+        assert torch.equal(y[:, :200], plain) and (room[1 + 21 * 204:] == 7).all() and room[0] == 7
+
+
+def test_values_that_are_not_finite(gs):
+    """A row's infinities and NaN stay in that row."""
+    w, _ = _weights(gs, "bf16", 300, 256, 32, True, False)
+    x = _x("bf16", 12, 256)
+    base, _ = _run(gs, w, x)
+    x[3, 17], x[5, 200] = float("inf"), float("nan")
+    y, _ = _run(gs, w, x)
+    keep = [i for i in range(12) if i not in (3, 5)]
+    assert torch.equal(y[keep], base[keep])
+    assert not torch.isfinite(y[3]).any() and torch.isnan(y[5]).all()
+
+
+def test_range_word(gs):
+    """An fp16 output beyond the type's range is infinite and raises the word."""
+    w, W = _weights(gs, "fp16", 64, 128, 64, False, False, scale=40.0)
+    x = _x("fp16", 3, 128, scale=100.0)
+    x[1] = 0
+    y, err = _run(gs, w, x)
+    assert err == 3 and torch.isinf(y[0]).any() and (y[1] == 0).all()
+    w, W = _weights(gs, "bf16", 64, 128, 64, False, False, scale=40.0)
+    y, err = _run(gs, w, x.bfloat16())
+    assert err == 0 and torch.isfinite(y).all()
+
+
+def test_offsets_past_32_bits(gs):
+    """Rows of inputs and outputs that lie more than 2^31 elements apart."""
+    w, W = _weights(gs, "bf16", 48, 64, 32, False, False)
+    far = 2 ** 31 + 64
+    room = torch.zeros(far + 64, dtype=torch.bfloat16, device=DEV)
+    x = room.as_strided((2, 64), (far, 1))
+    x.copy_(_x("bf16", 2, 64))
+    out = torch.zeros(far + 64, dtype=torch.bfloat16, device=DEV)
+    y, err = _run(gs, w, x, y=out.as_strided((2, 48), (far, 1)))
+    assert err == 0
+    _check("bf16", y, W, x)
+
+
+def test_captured_and_replayed(gs):
+    w, W = _weights(gs, "fp16", 2048, 1024, 64, True, True, scale=0.02)
+    x, y = _x("fp16", 17, 1024), torch.zeros(17, 1024, dtype=torch.float16, device=DEV)
+    err = torch.zeros(1, dtype=torch.int32, device=DEV)
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+        gs.gs_qlinear(w, x.data_ptr(), 1024, y.data_ptr(), 1024, 17, 2, err.data_ptr(),
+                      torch.cuda.current_stream().cuda_stream)
+    for seed in (1, 2):
+        x.copy_(_x("fp16", 17, 1024, seed=seed))
+        graph.replay()
+        torch.cuda.synchronize()
+        want, _ = _run(gs, w, x, epilogue=2)
+        assert torch.equal(y, want)
