@@ -70,6 +70,10 @@ cudaError_t launch_gemm(int bn, int epi, const CUtensorMap& tmW, const CUtensorM
 // or the encode fails.
 bool make_map(CUtensorMap* m, const void* base, uint64_t rows, uint64_t cols, uint32_t box_rows);
 
+// The same for an array of up to five dimensions, innermost first: `strides` in bytes,
+// of all but the innermost; 128-byte swizzle, 16-bit elements of either type.
+bool make_map_nd(CUtensorMap* m, const void* base, int rank, const uint64_t* dims,
+                 const uint64_t* strides, const uint32_t* box);
 
 // Sets the dynamic shared-memory limit of every GEMM instantiation once.
 cudaError_t gemm_init_attributes();

@@ -20,127 +20,11 @@
 #include <algorithm>
 #include <cmath>
 
-#include "attend_common.cuh"
 #include "internal.h"
+#include "tree_wide.cuh"
 
 namespace gs {
 namespace {
-
-constexpr size_t kErrBytes = 256;    // the error word at the scratch's start
-constexpr int kMostNodes = 64;       // bits of a mask
-constexpr int kMostCluster = 8;
-
-struct TreeArgs {
-  const uint16_t* q;
-  int64_t ld_q;
-  const int32_t *seq, *n, *count, *pos;
-  const uint64_t* mask;
-  uint16_t* out;
-  int64_t ld_out;
-  float* lse;
-  int Hq, G, nodes, tiles, window, split, items;
-  int cluster;        // the items of a tile are one cluster, and join there
-  float scale_log2;
-  float* part_o;      // [row][head][item][D]
-  float2* part_ml;    // [row][head][item]
-  int* err;
-  CacheView cache;
-};
-
-// A tree's numbers: cached keys, keys in all, nodes in use, the first key that
-// any node sees, its page and the pages from there on.
-struct Span {
-  int n, keys, count, lo, lo_most, page0, pages;
-  const int32_t* table;
-};
-
-// The first cached key that a node at position `pos` sees; positions below n
-// count as n.
-__device__ __forceinline__ int first_key(int pos, int n, int window) {
-  const long long lo = static_cast<long long>(max(pos, n)) + 1 - window;
-  return lo < 0 ? 0 : lo > n ? n : static_cast<int>(lo);
-}
-
-// The tree's numbers are read by one warp for its block: all threads go through
-// the same pages and barriers whatever happens to the arrays meanwhile.
-__device__ __forceinline__ Span find_span(const TreeArgs& a, int tree) {
-  __shared__ int s_v[6];
-  if (threadIdx.x < 32) {
-    int seq = a.seq ? a.seq[tree] : tree, n = a.n[tree];
-    int count = a.count ? a.count[tree] : a.nodes;
-    const int most = a.cache.pt_stride * kPageTokens;
-    bool bad = count < 0 || count > a.nodes;
-    count = min(max(count, 0), a.nodes);
-    if (n < 0 || n > most - count) {
-      bad = true;
-      n = n < 0 ? 0 : min(n, most);
-    }
-    int keys = min(n + count, most);
-    if (seq < 0 || seq >= a.cache.n_seq) {
-      bad = true;
-      seq = 0;
-      n = keys = 0;
-    }
-    int lo = a.window > 0 ? n : 0, lo_most = 0;
-    if (a.window > 0) {
-      for (int i = threadIdx.x; i < count; i += 32) {
-        const int x = first_key(a.pos[static_cast<int64_t>(tree) * a.nodes + i], n, a.window);
-        lo = min(lo, x);
-        lo_most = max(lo_most, x);
-      }
-      lo = __reduce_min_sync(0xFFFFFFFFu, lo);
-      lo_most = __reduce_max_sync(0xFFFFFFFFu, lo_most);
-    }
-    if (threadIdx.x == 0) {
-      if (bad) atomicExch(a.err, kErrBounds);
-      s_v[0] = seq, s_v[1] = n, s_v[2] = keys, s_v[3] = count, s_v[4] = lo, s_v[5] = lo_most;
-    }
-  }
-  __syncthreads();
-  Span s;
-  s.n = s_v[1];
-  s.keys = s_v[2];
-  s.count = s_v[3];
-  s.lo = s_v[4];
-  s.lo_most = s_v[5];
-  s.page0 = s.lo / kPageTokens;
-  s.pages = max(0, (s.keys + kPageTokens - 1) / kPageTokens - s.page0);
-  s.table = a.cache.page_table + static_cast<int64_t>(s_v[0]) * a.cache.pt_stride;
-  return s;
-}
-
-__device__ __forceinline__ uint32_t bits_below(int x) {
-  return x <= 0 ? 0u : x >= 32 ? 0xFFFFFFFFu : (1u << x) - 1u;
-}
-// Which of the tokens tok0 .. tok0 + 31 a row sees.  `mask` has no bits at or
-// beyond the tree's count.
-__device__ __forceinline__ uint32_t row_view(uint64_t mask, int lo, int n, int tok0) {
-  const int d = n - tok0;
-  uint32_t v = bits_below(d) & ~bits_below(lo - tok0);
-  if (d < 32 && d > -64)
-    v |= d >= 0 ? static_cast<uint32_t>(mask) << d : static_cast<uint32_t>(mask >> -d);
-  return v;
-}
-
-// Which of a register's two 16-bit values are infinite or NaN: all bits of their halves.
-template <bool BF16>
-__device__ __forceinline__ uint32_t not_finite(uint32_t v) {
-  constexpr uint32_t E = BF16 ? 0x7F80u : 0x7C00u;
-  return ((v & E) == E ? 0x0000FFFFu : 0u) | ((v & (E << 16)) == (E << 16) ? 0xFFFF0000u : 0u);
-}
-
-// Four dims of a row's output, and with the first of them its log-sum-exp.
-template <bool BF16, int D>
-__device__ __forceinline__ void store_row(const TreeArgs& a, int64_t row, int head, int d, float m,
-                                          float l, const float4& acc) {
-  const float inv = l != 0.f ? 1.f / l : 0.f;
-  *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(head) * D + d) =
-      make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-  if (d == 0 && a.lse)     // (the 15 go out of m and l first, without a rounding)
-    a.lse[row * a.Hq + head] =
-        l != 0.f ? (finite_max(m) + kHeld<BF16> + log2f(l * (BF16 ? 1.f : 0x1p-15f))) * kLn2
-                 : -INFINITY;
-}
 
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kStep = 32;            // tokens of a warp's step: half a page
@@ -561,6 +445,12 @@ __global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs 
 // several trees, which may differ in length, items of at most kMostPages.
 constexpr int64_t wave_of(int head_dim) { return head_dim == 64 ? 320 : 256; }
 constexpr int kMostPages = 12;
+// The wide kernel: one wave of two blocks per SM; whole steps of two pages.
+int wide_split(int pages, int64_t blocks_per_item) {
+  const int64_t items = std::max<int64_t>(1, 2 * kNumSMs / blocks_per_item);
+  const int64_t split = ((pages + items - 1) / items + 1) / 2 * 2;
+  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(split, 2), std::max(pages, 1)));
+}
 int auto_split(int pages, int trees, int64_t blocks_per_item, int head_dim) {
   const int64_t wave = wave_of(head_dim) / blocks_per_item;
   int64_t items = wave < 1 ? 1 : wave;
@@ -571,50 +461,61 @@ int auto_split(int pages, int trees, int64_t blocks_per_item, int head_dim) {
   return static_cast<int>(split < pages ? split : pages);
 }
 
-// 16-row tiles of a block.
-int row_tiles(int, int) { return 1; }
+// Rows of a KV head from which the wide kernel takes over.
+bool is_wide(int rows, int) { return rows > 48; }
 
 struct Plan {
-  int mt, tiles, split, items;
+  bool wide;
+  int tiles, split, items;
 };
 Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window, int split_pages) {
   Plan p;
   const int G = n_heads / c.n_kv_heads;
-  p.mt = row_tiles(nodes * G, c.head_dim);
-  p.tiles = (nodes * G + 16 * p.mt - 1) / (16 * p.mt);
+  p.wide = is_wide(nodes * G, c.head_dim);
+  const int tile_rows = p.wide ? kWideRows : 16;
+  p.tiles = (nodes * G + tile_rows - 1) / tile_rows;
   int pages = c.pt_stride;
   if (window > 0) {
     const int64_t most = (static_cast<int64_t>(window) - 1 + nodes + kPageTokens - 2) / kPageTokens + 1;
     if (most < pages) pages = static_cast<int>(most);
   }
+  const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * c.n_kv_heads * p.tiles;
   p.split = split_pages > 0 ? std::min(split_pages, c.pt_stride)
-                            : auto_split(pages, trees, static_cast<int64_t>(trees < 1 ? 1 : trees) *
-                                                           c.n_kv_heads * p.tiles,
-                                         c.head_dim);
+            : p.wide        ? wide_split(pages, blocks)
+                            : auto_split(pages, trees, blocks, c.head_dim);
   p.items = (pages + p.split - 1) / p.split;
   return p;
 }
 
-template <bool BF16, int D, int MT>
-cudaError_t launch_tiles(const TreeArgs& a, int trees, cudaStream_t s) {
-  static DeviceOnce once;
-  constexpr size_t smem = sizeof(Smem<D, MT>);
-  auto kernel = tree_attention_kernel<BF16, D, MT>;
-  cudaError_t e = once.run([&] {
-    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
-  });
-  if (e != cudaSuccess) return e;
-  e = launch_ex(kernel, dim3(a.items, a.cache.Hkv * a.tiles, trees), dim3(kThreads), smem, s, false,
-                dim3(a.cluster ? a.items : 1, 1, 1), a);
-  if (e != cudaSuccess || a.items == 1 || a.cluster) return e;
+template <bool BF16, int D>
+cudaError_t launch_join(const TreeArgs& a, int trees, cudaStream_t s) {
   return launch_ex(tree_join_kernel<BF16, D>, dim3(a.Hq * a.nodes, trees), dim3(kJoinThreads), 0, s,
                    true, dim3(1, 1, 1), a);
 }
 
 template <bool BF16, int D>
-cudaError_t launch_tree(const TreeArgs& a, int mt, int trees, cudaStream_t s) {
-  (void)mt;
-  return launch_tiles<BF16, D, 1>(a, trees, s);
+cudaError_t launch_tree(const gs_cache& c, const TreeArgs& a, bool wide, int trees, cudaStream_t s) {
+  static DeviceOnce once;
+  auto narrow = tree_attention_kernel<BF16, D, 1>;
+  auto broad = tree_wide_kernel<BF16, D>;
+  constexpr size_t smem = sizeof(Smem<D, 1>), wide_smem = WideSmem<D>::total;
+  cudaError_t e = once.run([&] {
+    cudaError_t r = cudaFuncSetAttribute(narrow, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    return r != cudaSuccess ? r
+                            : cudaFuncSetAttribute(broad, cudaFuncAttributeMaxDynamicSharedMemorySize,
+                                                   wide_smem);
+  });
+  if (e != cudaSuccess) return e;
+  const dim3 grid(a.items, a.cache.Hkv * a.tiles, trees);
+  if (wide) {
+    CUtensorMap k, v;
+    if (!pool_maps(c, &k, &v)) return cudaErrorUnknown;
+    e = launch_ex(broad, grid, dim3(kWideThreads), wide_smem, s, false, dim3(1, 1, 1), k, v, a);
+  } else {
+    e = launch_ex(narrow, grid, dim3(kThreads), smem, s, false, dim3(a.cluster ? a.items : 1, 1, 1), a);
+  }
+  if (e != cudaSuccess || a.items == 1 || a.cluster) return e;
+  return launch_join<BF16, D>(a, trees, s);
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -652,8 +553,8 @@ extern "C" size_t gs_tree_attention_scratch_bytes(const gs_cache* cache, int tre
   size_t items = p.items;
   if (split_pages == 0) {
     const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * cache->n_kv_heads * p.tiles;
-    const size_t wave = static_cast<size_t>(wave_of(cache->head_dim) / blocks),
-                 cut = cache->pt_stride / kMostPages, cluster = kMostCluster;
+    const size_t wave = static_cast<size_t>((p.wide ? 2 * kNumSMs : wave_of(cache->head_dim)) / blocks),
+                 cut = p.wide ? 0 : cache->pt_stride / kMostPages, cluster = kMostCluster;
     items = std::max(std::max(wave, cut), cluster) + 2;
     if (items > static_cast<size_t>(cache->pt_stride)) items = cache->pt_stride;
   }
@@ -701,7 +602,7 @@ extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t l
   a.window = window;
   a.split = p.split;
   a.items = p.items;
-  a.cluster = p.items > 1 && p.items <= kMostCluster &&
+  a.cluster = !p.wide && p.items > 1 && p.items <= kMostCluster &&
               static_cast<int64_t>(p.items) * cache->n_kv_heads * p.tiles * trees <= wave_of(D);
   a.scale_log2 = scale * kLog2e;
   a.part_o = reinterpret_cast<float*>(base + sc.o);
@@ -711,8 +612,10 @@ extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t l
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (cache->dtype == GS_BF16)
-    e = D == 64 ? launch_tree<true, 64>(a, p.mt, trees, s) : launch_tree<true, 128>(a, p.mt, trees, s);
+    e = D == 64 ? launch_tree<true, 64>(*cache, a, p.wide, trees, s)
+                : launch_tree<true, 128>(*cache, a, p.wide, trees, s);
   else
-    e = D == 64 ? launch_tree<false, 64>(a, p.mt, trees, s) : launch_tree<false, 128>(a, p.mt, trees, s);
+    e = D == 64 ? launch_tree<false, 64>(*cache, a, p.wide, trees, s)
+                : launch_tree<false, 128>(*cache, a, p.wide, trees, s);
   return e == cudaSuccess ? GS_OK : GS_ERR_CUDA;
 }
