@@ -53,6 +53,8 @@ tree_attention_kernel(const TreeArgs a) {
   const Span sp = find_span(a, tree);
   const int items = (sp.pages + a.split - 1) / a.split;
   const int rows = min(R, sp.count * a.G - tile * R);     // query rows of this tile
+  if (item == 0 && blockIdx.y == 0 && threadIdx.x == 0)
+    a.part_n[tree] = make_int2(sp.pages, sp.count);
   if (rows <= 0 || (item >= items && item > 0)) {
     if (a.cluster) {                     // the barriers below want every block
       cluster_sync_all();
@@ -396,48 +398,68 @@ tree_attention_kernel(const TreeArgs a) {
   cluster_sync_all();                    // the peers have read this block's part
 }
 
-// Joins a row's items, one query head per block: the items are dealt to the
-// block's thread groups (one thread per four dims) in turn and the groups'
-// sums are added in order, so the result depends on the row's items alone.
+// Joins the items of each row and head, a thread per four dims.  Eight items
+// in order make a chunk, the chunks are added in order: however many thread groups
+// share a row's chunks, the sums are the same.  (A cluster's items are one chunk.)
 constexpr int kJoinThreads = 256;
 
 template <bool BF16, int D>
-__global__ void __launch_bounds__(kJoinThreads) tree_join_kernel(const TreeArgs a) {
+__global__ void __launch_bounds__(kJoinThreads, 4)
+tree_join_kernel(const TreeArgs a, int groups, int64_t rows) {
   constexpr int L = D / 4, NG = kJoinThreads / L;
-  __shared__ float s_max[kJoinThreads / 32];
   __shared__ float4 s_acc[NG][L];
   __shared__ float s_l[NG];
-  const int h = blockIdx.x % a.Hq, node = blockIdx.x / a.Hq, tree = blockIdx.y;
+  const int grp = threadIdx.x / L, d = threadIdx.x % L, sub = grp % groups;
+  const int64_t at = static_cast<int64_t>(blockIdx.x) * (NG / groups) + grp / groups;   // row, head
+  const bool in = at < rows * a.Hq;
+  const int64_t row = in ? at / a.Hq : 0;
+  const int tree = static_cast<int>(row / a.nodes), node = static_cast<int>(row % a.nodes);
+  const float2* ml = a.part_ml + (in ? at : 0) * a.items;
+  const float4* po = reinterpret_cast<const float4*>(a.part_o + (in ? at : 0) * a.items * D);
   pdl_wait();      // in every block: the grid ends after the first kernel's
-  const Span sp = find_span(a, tree);
-  const int items = (sp.pages + a.split - 1) / a.split;
-  if (items <= 1 || node >= sp.count) return;
-  const int64_t row = static_cast<int64_t>(tree) * a.nodes + node, at = row * a.Hq + h;
-  const float2* ml = a.part_ml + at * a.items;
-  const float4* po = reinterpret_cast<const float4*>(a.part_o + at * a.items * D);
+  const int2 have = a.part_n[tree];
+  const int items = in && node < have.y ? (have.x + a.split - 1) / a.split : 0;
   float m = -INFINITY;
-  for (int i = threadIdx.x; i < items; i += kJoinThreads) m = fmaxf(m, ml[i].x);
+  for (int i = d; i < a.items; i += L) {
+    const float x = ml[i].x;             // (beyond this row's items: anything)
+    if (i < items) m = fmaxf(m, x);
+  }
 #pragma unroll
-  for (int x = 16; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, x));
-  if ((threadIdx.x & 31) == 0) s_max[threadIdx.x >> 5] = m;
-  __syncthreads();
-#pragma unroll
-  for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, s_max[w]);
+  for (int x = L / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, x));
   const float z = finite_max(m);
-  const int grp = threadIdx.x / L, d = threadIdx.x % L;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
-#pragma unroll 4
-  for (int i = grp; i < items; i += NG) {
-    const float2 x = ml[i];
-    add_scaled(acc, l, po[static_cast<int64_t>(i) * L + d], x.y, ex2(x.x - z));
+  const int rounds = groups > 1 ? ((a.items + 7) / 8 + groups - 1) / groups : (items + 7) / 8;
+  for (int round = 0; round < rounds; ++round) {
+    const int first = (round * groups + sub) * 8;
+    float4 part = make_float4(0.f, 0.f, 0.f, 0.f);
+    float pl = 0.f;
+#pragma unroll
+    for (int h = 0; h < 8; h += 4) {
+      float4 v[4];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (first + h + i < items) v[i] = po[static_cast<int64_t>(first + h + i) * L + d];
+#pragma unroll
+      for (int i = 0; i < 4; ++i)
+        if (first + h + i < items) {
+          const float2 x = ml[first + h + i];
+          add_scaled(part, pl, v[i], x.y, ex2(x.x - z));
+        }
+    }
+    if (groups == 1) {
+      add_scaled(acc, l, part, pl, 1.f);
+      continue;
+    }
+    s_acc[grp][d] = part;
+    if (d == 0) s_l[grp] = pl;
+    __syncthreads();
+    if (sub == 0)
+      for (int i = 0; i < groups && first + 8 * i < items; ++i)
+        add_scaled(acc, l, s_acc[grp + i][d], s_l[grp + i], 1.f);
+    __syncthreads();
   }
-  s_acc[grp][d] = acc;
-  if (d == 0) s_l[grp] = l;
-  __syncthreads();
-  if (grp > 0) return;
-  for (int i = 1; i < NG; ++i) add_scaled(acc, l, s_acc[i][d], s_l[i], 1.f);
-  store_row<BF16, D>(a, row, h, 4 * d, m, l, acc);
+  if (sub == 0 && items > 1) store_row<BF16, D>(a, row, static_cast<int>(at % a.Hq), 4 * d, m, l, acc);
 }
 
 // Pages of an item when the caller leaves it open: one wave of blocks shares the
@@ -489,8 +511,14 @@ Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window,
 
 template <bool BF16, int D>
 cudaError_t launch_join(const TreeArgs& a, int trees, cudaStream_t s) {
-  return launch_ex(tree_join_kernel<BF16, D>, dim3(a.Hq * a.nodes, trees), dim3(kJoinThreads), 0, s,
-                   true, dim3(1, 1, 1), a);
+  // a row's chunks are shared by as many groups as the GPU has room for
+  constexpr int NG = kJoinThreads / (D / 4);
+  const int64_t rows = static_cast<int64_t>(trees) * a.nodes, chunks = (a.items + 7) / 8;
+  int groups = 1;
+  while (groups < NG && groups < chunks && rows * a.Hq * groups < kNumSMs * 4 * NG) groups *= 2;
+  const int64_t blocks = (rows * a.Hq * groups + NG - 1) / NG;
+  return launch_ex(tree_join_kernel<BF16, D>, dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads),
+                   0, s, true, dim3(1, 1, 1), a, groups, rows);
 }
 
 template <bool BF16, int D>
@@ -520,13 +548,17 @@ cudaError_t launch_tree(const gs_cache& c, const TreeArgs& a, bool wide, int tre
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 
-struct Scratch {
-  size_t o, ml, total;   // offsets of the partial accumulators and of their (max, sum)
+struct Scratch {         // offsets of the trees' sizes, the partial accumulators, their (max, sum)
+  size_t n, o, ml, total;
 };
-Scratch scratch_of(const gs_cache& c, int64_t rows, int n_heads, size_t items) {
-  const size_t n = static_cast<size_t>(rows) * n_heads * items;
-  const size_t ml = kErrBytes + up256(n * c.head_dim * sizeof(float));
-  return {kErrBytes, ml, ml + up256(n * sizeof(float2))};
+Scratch scratch_of(const gs_cache& c, int trees, int nodes, int n_heads, size_t items) {
+  const size_t rows = static_cast<size_t>(trees) * nodes * n_heads * items;
+  Scratch s;
+  s.n = kErrBytes;
+  s.o = s.n + up256(trees * sizeof(int2));
+  s.ml = s.o + up256(rows * c.head_dim * sizeof(float));
+  s.total = s.ml + up256(rows * sizeof(float2));
+  return s;
 }
 
 // GS_OK, or what is wrong with the sizes of a call.
@@ -558,7 +590,7 @@ extern "C" size_t gs_tree_attention_scratch_bytes(const gs_cache* cache, int tre
     items = std::max(std::max(wave, cut), cluster) + 2;
     if (items > static_cast<size_t>(cache->pt_stride)) items = cache->pt_stride;
   }
-  return scratch_of(*cache, static_cast<int64_t>(trees) * nodes, n_heads, items).total;
+  return scratch_of(*cache, trees, nodes, n_heads, items).total;
 }
 
 extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t ld_q,
@@ -582,7 +614,7 @@ extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t l
     return GS_ERR_OOM;
   if (trees == 0) return GS_OK;
   const Plan p = plan_tree(*cache, trees, nodes, n_heads, window, split_pages);
-  const Scratch sc = scratch_of(*cache, static_cast<int64_t>(trees) * nodes, n_heads, p.items);
+  const Scratch sc = scratch_of(*cache, trees, nodes, n_heads, p.items);
   uint8_t* base = static_cast<uint8_t*>(scratch);
   TreeArgs a;
   a.q = static_cast<const uint16_t*>(q);
@@ -607,6 +639,7 @@ extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t l
   a.scale_log2 = scale * kLog2e;
   a.part_o = reinterpret_cast<float*>(base + sc.o);
   a.part_ml = reinterpret_cast<float2*>(base + sc.ml);
+  a.part_n = reinterpret_cast<int2*>(base + sc.n);
   a.err = static_cast<int*>(scratch);
   a.cache = cache_view(*cache);
   cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -23,6 +23,7 @@ struct TreeArgs {
   float scale_log2;
   float* part_o;      // [row][head][item][D]
   float2* part_ml;    // [row][head][item]
+  int2* part_n;       // [tree]: pages, nodes in use
   int* err;
   CacheView cache;
 };
