@@ -7,7 +7,7 @@
 //
 // (s' = s log2(e), m the running maximum, 15 less in fp16.)  A query row is one
 // query head of one node; the rows of a KV head, node by node, are cut into tiles
-// of 16 MT.  A block takes one tile and one item of `split` pages; its warps take
+// of 16.  A block takes one tile and one item of `split` pages; its warps take
 // the item's half pages in turn, straight from global memory into the operand
 // registers of m16n8k16 instructions, and are joined at the item's end.
 //
@@ -26,26 +26,65 @@
 namespace gs {
 namespace {
 
+// A tree's numbers, the first key that any of its nodes sees and the first that
+// all see, that key's page and the pages from there on.
+struct Span {
+  int n, keys, count, lo, lo_most, page0, pages;
+  const int32_t* table;
+};
+// They are read by one warp for its block: all threads go through the same pages
+// and barriers whatever happens to the arrays meanwhile.
+__device__ __forceinline__ Span find_span(const TreeArgs& a, int tree) {
+  __shared__ int s_v[6];
+  if (threadIdx.x < 32) {
+    const TreeNums t = read_tree(a, tree);
+    int lo = a.window > 0 ? t.n : 0, lo_most = 0;
+    if (a.window > 0) {
+      for (int i = threadIdx.x; i < t.count; i += 32) {
+        const int x = first_key(a.pos[static_cast<int64_t>(tree) * a.nodes + i], t.n, a.window);
+        lo = min(lo, x);
+        lo_most = max(lo_most, x);
+      }
+      lo = __reduce_min_sync(0xFFFFFFFFu, lo);
+      lo_most = __reduce_max_sync(0xFFFFFFFFu, lo_most);
+    }
+    if (threadIdx.x == 0) {
+      if (t.bad) atomicExch(a.err, kErrBounds);
+      s_v[0] = t.seq, s_v[1] = t.n, s_v[2] = t.keys, s_v[3] = t.count, s_v[4] = lo, s_v[5] = lo_most;
+    }
+  }
+  __syncthreads();
+  Span s;
+  s.n = s_v[1];
+  s.keys = s_v[2];
+  s.count = s_v[3];
+  s.lo = s_v[4];
+  s.lo_most = s_v[5];
+  s.page0 = s.lo / kPageTokens;
+  s.pages = max(0, (s.keys + kPageTokens - 1) / kPageTokens - s.page0);
+  s.table = a.cache.page_table + static_cast<int64_t>(s_v[0]) * a.cache.pt_stride;
+  return s;
+}
+
 constexpr int kWarps = 4, kThreads = kWarps * 32;
 constexpr int kStep = 32;            // tokens of a warp's step: half a page
 
-template <int D, int MT>
+template <int D>
 struct Smem {
-  static constexpr int R = 16 * MT, P = D + 8;   // row pitch: 8 rows x 4 lanes on distinct banks
+  static constexpr int R = 16, P = D + 8;   // row pitch: 8 rows x 4 lanes on distinct banks
   alignas(16) float so[kWarps * 16 * P];         // the warps' parts of 16 rows
   alignas(16) float item[R * D];                 // in a cluster: this item's part
-  alignas(16) uint16_t q[MT > 1 ? R * P : 8];    // queries, where they do not fit in registers
   float2 ml[kWarps][R], item_ml[R];
   uint64_t mask[R];
   int lo[R];
 };
 
-template <bool BF16, int D, int MT>
-__global__ void __launch_bounds__(kThreads, D == 64 && MT == 1 ? 3 : 2)
+template <bool BF16, int D>
+__global__ void __launch_bounds__(kThreads, D == 64 ? 3 : 2)
 tree_attention_kernel(const TreeArgs a) {
-  constexpr int R = 16 * MT, P = D + 8, C = D / 32;
+  constexpr int R = Smem<D>::R, P = Smem<D>::P, C = D / 32;
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  Smem<D, MT>& sm = *reinterpret_cast<Smem<D, MT>*>(smem_raw);
+  Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw);
   pdl_trigger();   // the joining kernel may take its place; it waits for this one's end
   const int tree = blockIdx.z, head = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
   const int item = blockIdx.x;
@@ -54,7 +93,7 @@ tree_attention_kernel(const TreeArgs a) {
   const int items = (sp.pages + a.split - 1) / a.split;
   const int rows = min(R, sp.count * a.G - tile * R);     // query rows of this tile
   if (item == 0 && blockIdx.y == 0 && threadIdx.x == 0)
-    a.part_n[tree] = make_int2(sp.pages, sp.count);
+    a.part_n[tree] = TreePart{0, sp.pages, sp.count};
   if (rows <= 0 || (item >= items && item > 0)) {
     if (a.cluster) {                     // the barriers below want every block
       cluster_sync_all();
@@ -110,7 +149,7 @@ tree_attention_kernel(const TreeArgs a) {
 
   // each row's mask and first key, and Q in the operand's order: of each 32
   // dims, dims 8q .. 8q + 7 on lane q
-  for (int r = threadIdx.x; r < R; r += kThreads) {
+  if (const int r = threadIdx.x; r < R) {
     uint64_t mask = 0;
     int lo = sp.n;
     if (r < rows) {
@@ -123,70 +162,48 @@ tree_attention_kernel(const TreeArgs a) {
     sm.mask[r] = mask;
     sm.lo[r] = lo;
   }
-  uint32_t qa[MT > 1 ? 1 : C][4], qb[MT > 1 ? 1 : C][4];
+  uint32_t qa[C][4], qb[C][4];
   const uint4 zero4 = make_uint4(0, 0, 0, 0);
-  if constexpr (MT == 1) {
 #pragma unroll
-    for (int c = 0; c < C; ++c) {
-      const uint4 u = g < rows ? *reinterpret_cast<const uint4*>(q_at(g) + 8 * q + 32 * c) : zero4;
-      const uint4 w =
-          g + 8 < rows ? *reinterpret_cast<const uint4*>(q_at(g + 8) + 8 * q + 32 * c) : zero4;
-      qa[c][0] = u.x, qa[c][1] = u.y, qa[c][2] = u.z, qa[c][3] = u.w;
-      qb[c][0] = w.x, qb[c][1] = w.y, qb[c][2] = w.z, qb[c][3] = w.w;
-    }
-  } else {
-    for (int e = threadIdx.x; e < R * (D / 8); e += kThreads) {
-      const int r = e / (D / 8), d = e % (D / 8) * 8;
-      *reinterpret_cast<uint4*>(sm.q + r * P + d) =
-          r < rows ? *reinterpret_cast<const uint4*>(q_at(r) + d) : zero4;
-    }
+  for (int c = 0; c < C; ++c) {
+    const uint4 u = g < rows ? *reinterpret_cast<const uint4*>(q_at(g) + 8 * q + 32 * c) : zero4;
+    const uint4 w =
+        g + 8 < rows ? *reinterpret_cast<const uint4*>(q_at(g + 8) + 8 * q + 32 * c) : zero4;
+    qa[c][0] = u.x, qa[c][1] = u.y, qa[c][2] = u.z, qa[c][3] = u.w;
+    qb[c][0] = w.x, qb[c][1] = w.y, qb[c][2] = w.z, qb[c][3] = w.w;
   }
   __syncthreads();
 
-  float o[MT][D / 8][4], m0[MT], m1[MT], l0[MT], l1[MT];
+  float o[D / 8][4];
 #pragma unroll
-  for (int t = 0; t < MT; ++t) {
-#pragma unroll
-    for (int i = 0; i < D / 8; ++i) o[t][i][0] = o[t][i][1] = o[t][i][2] = o[t][i][3] = 0.f;
-    m0[t] = m1[t] = -INFINITY;
-    l0[t] = l1[t] = 0.f;
-  }
+  for (int i = 0; i < D / 8; ++i) o[i][0] = o[i][1] = o[i][2] = o[i][3] = 0.f;
+  float m0 = -INFINITY, m1 = -INFINITY, l0 = 0.f, l1 = 0.f;
   for (int j = 0; j < cnt; ++j) {
     const int tok0 = (begin + warp + j * kWarps) * kStep;
     const bool edge = tok0 < sp.lo_most || tok0 + kStep > sp.n;
     uint32_t some = 0u, all = 0xFFFFFFFFu;               // tokens that some row, every row sees
-    uint32_t pa[MT][4], pb[MT][4];
-#pragma unroll
-    for (int t = 0; t < MT; ++t) {
+    uint32_t pa[4], pb[4];
+    {
       // ---- S = Q K^T; column n of S tile i is token 8 (n/2) + 2 i + n%2
       float s[4][4];
 #pragma unroll
       for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
 #pragma unroll
       for (int c = 0; c < C; ++c) {
-        uint4 u, w;
-        if constexpr (MT == 1) {
-          u = make_uint4(qa[c][0], qa[c][1], qa[c][2], qa[c][3]);
-          w = make_uint4(qb[c][0], qb[c][1], qb[c][2], qb[c][3]);
-        } else {
-          u = *reinterpret_cast<const uint4*>(sm.q + (16 * t + g) * P + 8 * q + 32 * c);
-          w = *reinterpret_cast<const uint4*>(sm.q + (16 * t + g + 8) * P + 8 * q + 32 * c);
-        }
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          mma16816<BF16>(s[i], u.x, w.x, u.y, w.y, k[i * C + c].x, k[i * C + c].y);
+          mma16816<BF16>(s[i], qa[c][0], qb[c][0], qa[c][1], qb[c][1], k[i * C + c].x, k[i * C + c].y);
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          mma16816<BF16>(s[i], u.z, w.z, u.w, w.w, k[i * C + c].z, k[i * C + c].w);
+          mma16816<BF16>(s[i], qa[c][2], qb[c][2], qa[c][3], qb[c][3], k[i * C + c].z, k[i * C + c].w);
       }
       // ---- softmax; this lane's columns 2q, 2q + 1 of tile i are tokens
       //      tok0 + 8 q + 2 i + {0, 1}
       if (edge) {
-        const int r = 16 * t + g;
-        const uint32_t v0 = row_view(sm.mask[r], sm.lo[r], sp.n, tok0),
-                       v1 = row_view(sm.mask[r + 8], sm.lo[r + 8], sp.n, tok0);
-        if (r < rows) some |= v0, all &= v0;
-        if (r + 8 < rows) some |= v1, all &= v1;
+        const uint32_t v0 = row_view(sm.mask[g], sm.lo[g], sp.n, tok0),
+                       v1 = row_view(sm.mask[g + 8], sm.lo[g + 8], sp.n, tok0);
+        if (g < rows) some |= v0, all &= v0;
+        if (g + 8 < rows) some |= v1, all &= v1;
         const uint32_t w0 = v0 >> (8 * q), w1 = v1 >> (8 * q);
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -206,33 +223,33 @@ tree_attention_kernel(const TreeArgs a) {
       x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
       x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
       x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
-      const float n0 = fmaxf(m0[t], held_max<BF16>(x0, a.scale_log2)),
-                  n1 = fmaxf(m1[t], held_max<BF16>(x1, a.scale_log2));
-      if (__any_sync(0xFFFFFFFFu, n0 != m0[t] || n1 != m1[t])) {
-        const float f0 = ex2(m0[t] - finite_max(n0)), f1 = ex2(m1[t] - finite_max(n1));
-        l0[t] *= f0;
-        l1[t] *= f1;
+      const float n0 = fmaxf(m0, held_max<BF16>(x0, a.scale_log2)),
+                  n1 = fmaxf(m1, held_max<BF16>(x1, a.scale_log2));
+      if (__any_sync(0xFFFFFFFFu, n0 != m0 || n1 != m1)) {
+        const float f0 = ex2(m0 - finite_max(n0)), f1 = ex2(m1 - finite_max(n1));
+        l0 *= f0;
+        l1 *= f1;
 #pragma unroll
         for (int i = 0; i < D / 8; ++i) {
-          o[t][i][0] *= f0;
-          o[t][i][1] *= f0;
-          o[t][i][2] *= f1;
-          o[t][i][3] *= f1;
+          o[i][0] *= f0;
+          o[i][1] *= f0;
+          o[i][2] *= f1;
+          o[i][3] *= f1;
         }
-        m0[t] = n0;
-        m1[t] = n1;
+        m0 = n0;
+        m1 = n1;
       }
-      const float z0 = finite_max(m0[t]), z1 = finite_max(m1[t]);
+      const float z0 = finite_max(m0), z1 = finite_max(m1);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
         const float e0 = ex2(fmaf(s[i][0], a.scale_log2, -z0)),
                     e1 = ex2(fmaf(s[i][1], a.scale_log2, -z0)),
                     e2 = ex2(fmaf(s[i][2], a.scale_log2, -z1)),
                     e3 = ex2(fmaf(s[i][3], a.scale_log2, -z1));
-        l0[t] += e0 + e1;
-        l1[t] += e2 + e3;
-        pa[t][i] = pack2<BF16>(e0, e1);
-        pb[t][i] = pack2<BF16>(e2, e3);
+        l0 += e0 + e1;
+        l1 += e2 + e3;
+        pa[i] = pack2<BF16>(e0, e1);
+        pb[i] = pack2<BF16>(e2, e3);
       }
     }
     const uint16_t* v_now = v_at;
@@ -279,27 +296,24 @@ tree_attention_kernel(const TreeArgs a) {
               w[e] &= ~sel;
             }
           x[i] = make_uint4(w[0], w[1], w[2], w[3]);
-#pragma unroll
-          for (int t = 0; t < MT; ++t) {
+          {
             float p[4] = {0.f, 0.f, 0.f, 0.f};
-            mma16816<BF16>(p, pa[t][0], pb[t][0], pa[t][1], pb[t][1], one[0], one[1]);
-            mma16816<BF16>(p, pa[t][2], pb[t][2], pa[t][3], pb[t][3], one[2], one[3]);
-            const int r = 16 * t + g;
-            if ((row_view(sm.mask[r], sm.lo[r], sp.n, tok0) >> tok) & 1)
-              o[t][i0 + i][0] += p[0], o[t][i0 + i][1] += p[1];
-            if ((row_view(sm.mask[r + 8], sm.lo[r + 8], sp.n, tok0) >> tok) & 1)
-              o[t][i0 + i][2] += p[2], o[t][i0 + i][3] += p[3];
+            mma16816<BF16>(p, pa[0], pb[0], pa[1], pb[1], one[0], one[1]);
+            mma16816<BF16>(p, pa[2], pb[2], pa[3], pb[3], one[2], one[3]);
+            if ((row_view(sm.mask[g], sm.lo[g], sp.n, tok0) >> tok) & 1)
+              o[i0 + i][0] += p[0], o[i0 + i][1] += p[1];
+            if ((row_view(sm.mask[g + 8], sm.lo[g + 8], sp.n, tok0) >> tok) & 1)
+              o[i0 + i][2] += p[2], o[i0 + i][3] += p[3];
           }
         }
       }
-#pragma unroll
-      for (int t = 0; t < MT; ++t) {
-#pragma unroll
-        for (int i = 0; i < 8; ++i)
-          mma16816<BF16>(o[t][i0 + i], pa[t][0], pb[t][0], pa[t][1], pb[t][1], x[i].x, x[i].y);
+      {
 #pragma unroll
         for (int i = 0; i < 8; ++i)
-          mma16816<BF16>(o[t][i0 + i], pa[t][2], pb[t][2], pa[t][3], pb[t][3], x[i].z, x[i].w);
+          mma16816<BF16>(o[i0 + i], pa[0], pb[0], pa[1], pb[1], x[i].x, x[i].y);
+#pragma unroll
+        for (int i = 0; i < 8; ++i)
+          mma16816<BF16>(o[i0 + i], pa[2], pb[2], pa[3], pb[3], x[i].z, x[i].w);
       }
     };
     multiply(0, v);
@@ -310,56 +324,52 @@ tree_attention_kernel(const TreeArgs a) {
     }
   }
 
-  // ---- the warps' parts are joined, in warp order, 16 rows at a time
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    l0[t] += __shfl_xor_sync(0xFFFFFFFFu, l0[t], 1);
-    l0[t] += __shfl_xor_sync(0xFFFFFFFFu, l0[t], 2);
-    l1[t] += __shfl_xor_sync(0xFFFFFFFFu, l1[t], 1);
-    l1[t] += __shfl_xor_sync(0xFFFFFFFFu, l1[t], 2);
+  // ---- the warps' parts are joined, in warp order
+  {
+    l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1);
+    l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
+    l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1);
+    l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 2);
     if (q == 0) {
-      sm.ml[warp][16 * t + g] = make_float2(m0[t], l0[t]);
-      sm.ml[warp][16 * t + g + 8] = make_float2(m1[t], l1[t]);
+      sm.ml[warp][g] = make_float2(m0, l0);
+      sm.ml[warp][g + 8] = make_float2(m1, l1);
     }
   }
   const int used = min(kWarps, steps);
-#pragma unroll
-  for (int t = 0; t < MT; ++t) {
-    if (t > 0) __syncthreads();
+  {
     if (cnt > 0) {
 #pragma unroll
       for (int i = 0; i < D / 8; ++i) {
         *reinterpret_cast<float2*>(sm.so + (warp * 16 + g) * P + 8 * i + 2 * q) =
-            make_float2(o[t][i][0], o[t][i][1]);
+            make_float2(o[i][0], o[i][1]);
         *reinterpret_cast<float2*>(sm.so + (warp * 16 + g + 8) * P + 8 * i + 2 * q) =
-            make_float2(o[t][i][2], o[t][i][3]);
+            make_float2(o[i][2], o[i][3]);
       }
     }
     __syncthreads();
-    const int here = min(16, rows - 16 * t);
-    for (int e = threadIdx.x; e < here * (D / 4); e += kThreads) {
-      const int r = e / (D / 4), d = e % (D / 4) * 4, rt = 16 * t + r;
+    for (int e = threadIdx.x; e < rows * (D / 4); e += kThreads) {
+      const int r = e / (D / 4), d = e % (D / 4) * 4;
       float m = -INFINITY, l = 0.f;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int w = 0; w < used; ++w) m = fmaxf(m, sm.ml[w][rt].x);
+      for (int w = 0; w < used; ++w) m = fmaxf(m, sm.ml[w][r].x);
       const float z = finite_max(m);
       for (int w = 0; w < used; ++w) {
-        const float f = ex2(sm.ml[w][rt].x - z);
+        const float f = ex2(sm.ml[w][r].x - z);
         const float4 x = *reinterpret_cast<const float4*>(sm.so + (w * 16 + r) * P + d);
-        l = fmaf(f, sm.ml[w][rt].y, l);
+        l = fmaf(f, sm.ml[w][r].y, l);
         acc.x = fmaf(f, x.x, acc.x);
         acc.y = fmaf(f, x.y, acc.y);
         acc.z = fmaf(f, x.z, acc.z);
         acc.w = fmaf(f, x.w, acc.w);
       }
-      const int64_t row = row0 + node_of(rt);
+      const int64_t row = row0 + node_of(r);
       if (items <= 1) {
-        store_row<BF16, D>(a, row, q_head(rt), d, m, l, acc);
+        store_row<BF16, D>(a, row, q_head(r), d, m, l, acc);
       } else if (a.cluster) {
-        *reinterpret_cast<float4*>(sm.item + rt * D + d) = acc;
-        if (d == 0) sm.item_ml[rt] = make_float2(m, l);
+        *reinterpret_cast<float4*>(sm.item + r * D + d) = acc;
+        if (d == 0) sm.item_ml[r] = make_float2(m, l);
       } else {
-        const int64_t at = row * a.Hq + q_head(rt);
+        const int64_t at = row * a.Hq + q_head(r);
         *reinterpret_cast<float4*>(a.part_o + (at * a.items + item) * D + d) = acc;
         if (d == 0) a.part_ml[at * a.items + item] = make_float2(m, l);
       }
@@ -398,10 +408,19 @@ tree_attention_kernel(const TreeArgs a) {
   cluster_sync_all();                    // the peers have read this block's part
 }
 
-// Joins the items of each row and head, a thread per four dims.  Eight items
+// Joins the parts of each row and head, a thread per four dims.  Eight parts
 // in order make a chunk, the chunks are added in order: however many thread groups
 // share a row's chunks, the sums are the same.  (A cluster's items are one chunk.)
 constexpr int kJoinThreads = 256;
+
+__device__ __forceinline__ int block_max(int v) {
+  __shared__ int s_max;
+  if (threadIdx.x == 0) s_max = 0;
+  __syncthreads();
+  if (v > 0) atomicMax(&s_max, v);
+  __syncthreads();
+  return s_max;
+}
 
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kJoinThreads, 4)
@@ -414,24 +433,41 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows) {
   const bool in = at < rows * a.Hq;
   const int64_t row = in ? at / a.Hq : 0;
   const int tree = static_cast<int>(row / a.nodes), node = static_cast<int>(row % a.nodes);
-  const float2* ml = a.part_ml + (in ? at : 0) * a.items;
-  const float4* po = reinterpret_cast<const float4*>(a.part_o + (in ? at : 0) * a.items * D);
+  const int head = static_cast<int>(at % a.Hq);
   pdl_wait();      // in every block: the grid ends after the first kernel's
-  const int2 have = a.part_n[tree];
-  const int items = in && node < have.y ? (have.x + a.split - 1) / a.split : 0;
-  float m = -INFINITY;
-  for (int i = d; i < a.items; i += L) {
-    const float x = ml[i].x;             // (beyond this row's items: anything)
-    if (i < items) m = fmaxf(m, x);
+  const TreePart have = a.part_n[tree];
+  // part i lies at first + (i > 0 ? more : 0) + i * step
+  int parts = 0;
+  int64_t first = at * a.items, more = 0, step = 1;
+  if (in && node < have.count) {
+    if (a.items > 0) {
+      parts = (have.pages + a.split - 1) / a.split;
+    } else {       // the blocks that share this tile's pages
+      const int64_t total = a.part_all[0], blocks = a.part_all[1];
+      const int r = node * a.G + head % a.G, tiles = (have.count * a.G + kWideRows - 1) / kWideRows;
+      const int64_t u = have.first +
+                        static_cast<int64_t>(head / a.G * tiles + r / kWideRows) * have.pages;
+      const int64_t b0 = ((u + 1) * blocks - 1) / total,
+                    b1 = ((u + have.pages) * blocks - 1) / total;
+      parts = static_cast<int>(b1 - b0) + 1;
+      first = (2 * b0 + 1) * kWideRows + r % kWideRows;
+      more = -kWideRows;
+      step = 2 * kWideRows;
+    }
   }
+  auto part_at = [&](int i) { return first + (i > 0 ? more : 0) + i * step; };
+  float m = -INFINITY;
+  for (int i = d; i < parts; i += L) m = fmaxf(m, a.part_ml[part_at(i)].x);
 #pragma unroll
   for (int x = L / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, x));
   const float z = finite_max(m);
+  const float4* po = reinterpret_cast<const float4*>(a.part_o) + d;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
-  const int rounds = groups > 1 ? ((a.items + 7) / 8 + groups - 1) / groups : (items + 7) / 8;
+  // (with several groups to a row, all of the block go through the same rounds)
+  const int rounds = groups > 1 ? block_max((parts + 8 * groups - 1) / (8 * groups)) : (parts + 7) / 8;
   for (int round = 0; round < rounds; ++round) {
-    const int first = (round * groups + sub) * 8;
+    const int first_of = (round * groups + sub) * 8;
     float4 part = make_float4(0.f, 0.f, 0.f, 0.f);
     float pl = 0.f;
 #pragma unroll
@@ -439,11 +475,11 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows) {
       float4 v[4];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (first + h + i < items) v[i] = po[static_cast<int64_t>(first + h + i) * L + d];
+        if (first_of + h + i < parts) v[i] = po[part_at(first_of + h + i) * L];
 #pragma unroll
       for (int i = 0; i < 4; ++i)
-        if (first + h + i < items) {
-          const float2 x = ml[first + h + i];
+        if (first_of + h + i < parts) {
+          const float2 x = a.part_ml[part_at(first_of + h + i)];
           add_scaled(part, pl, v[i], x.y, ex2(x.x - z));
         }
     }
@@ -455,11 +491,11 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows) {
     if (d == 0) s_l[grp] = pl;
     __syncthreads();
     if (sub == 0)
-      for (int i = 0; i < groups && first + 8 * i < items; ++i)
+      for (int i = 0; i < groups && first_of + 8 * i < parts; ++i)
         add_scaled(acc, l, s_acc[grp + i][d], s_l[grp + i], 1.f);
     __syncthreads();
   }
-  if (sub == 0 && items > 1) store_row<BF16, D>(a, row, static_cast<int>(at % a.Hq), 4 * d, m, l, acc);
+  if (sub == 0 && parts > 1) store_row<BF16, D>(a, row, head, 4 * d, m, l, acc);
 }
 
 // Pages of an item when the caller leaves it open: one wave of blocks shares the
@@ -467,12 +503,6 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows) {
 // several trees, which may differ in length, items of at most kMostPages.
 constexpr int64_t wave_of(int head_dim) { return head_dim == 64 ? 320 : 256; }
 constexpr int kMostPages = 12;
-// The wide kernel: one wave of two blocks per SM; whole steps of two pages.
-int wide_split(int pages, int64_t blocks_per_item) {
-  const int64_t items = std::max<int64_t>(1, 2 * kNumSMs / blocks_per_item);
-  const int64_t split = ((pages + items - 1) / items + 1) / 2 * 2;
-  return static_cast<int>(std::min<int64_t>(std::max<int64_t>(split, 2), std::max(pages, 1)));
-}
 int auto_split(int pages, int trees, int64_t blocks_per_item, int head_dim) {
   const int64_t wave = wave_of(head_dim) / blocks_per_item;
   int64_t items = wave < 1 ? 1 : wave;
@@ -484,18 +514,21 @@ int auto_split(int pages, int trees, int64_t blocks_per_item, int head_dim) {
 }
 
 // Rows of a KV head from which the wide kernel takes over.
-bool is_wide(int rows, int) { return rows > 48; }
+constexpr int kNarrowRows = 16;
 
 struct Plan {
-  bool wide;
+  bool wide, shared;             // shared: the wide kernel's blocks share all pages
   int tiles, split, items;
 };
 Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window, int split_pages) {
   Plan p;
   const int G = n_heads / c.n_kv_heads;
-  p.wide = is_wide(nodes * G, c.head_dim);
+  p.wide = nodes * G > kNarrowRows;
   const int tile_rows = p.wide ? kWideRows : 16;
   p.tiles = (nodes * G + tile_rows - 1) / tile_rows;
+  p.shared = p.wide && split_pages == 0 && trees <= kMostShared;
+  p.split = p.items = 0;
+  if (p.shared) return p;
   int pages = c.pt_stride;
   if (window > 0) {
     const int64_t most = (static_cast<int64_t>(window) - 1 + nodes + kPageTokens - 2) / kPageTokens + 1;
@@ -503,32 +536,22 @@ Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window,
   }
   const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * c.n_kv_heads * p.tiles;
   p.split = split_pages > 0 ? std::min(split_pages, c.pt_stride)
-            : p.wide        ? wide_split(pages, blocks)
+            : p.wide        ? pages          // (many trees: a block for each tile)
                             : auto_split(pages, trees, blocks, c.head_dim);
   p.items = (pages + p.split - 1) / p.split;
   return p;
 }
 
-template <bool BF16, int D>
-cudaError_t launch_join(const TreeArgs& a, int trees, cudaStream_t s) {
-  // a row's chunks are shared by as many groups as the GPU has room for
-  constexpr int NG = kJoinThreads / (D / 4);
-  const int64_t rows = static_cast<int64_t>(trees) * a.nodes, chunks = (a.items + 7) / 8;
-  int groups = 1;
-  while (groups < NG && groups < chunks && rows * a.Hq * groups < kNumSMs * 4 * NG) groups *= 2;
-  const int64_t blocks = (rows * a.Hq * groups + NG - 1) / NG;
-  return launch_ex(tree_join_kernel<BF16, D>, dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads),
-                   0, s, true, dim3(1, 1, 1), a, groups, rows);
-}
+constexpr int kWideBlocks = 2 * kNumSMs;
 
 template <bool BF16, int D>
 cudaError_t launch_tree(const gs_cache& c, const TreeArgs& a, bool wide, int trees, cudaStream_t s) {
   static DeviceOnce once;
-  auto narrow = tree_attention_kernel<BF16, D, 1>;
+  auto narrow = tree_attention_kernel<BF16, D>;
   auto broad = tree_wide_kernel<BF16, D>;
-  constexpr size_t smem = sizeof(Smem<D, 1>), wide_smem = WideSmem<D>::total;
+  constexpr size_t smem = sizeof(Smem<D>), wide_smem = WideSmem<D>::total;
   cudaError_t e = once.run([&] {
-    cudaError_t r = cudaFuncSetAttribute(narrow, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
+    const cudaError_t r = cudaFuncSetAttribute(narrow, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
     return r != cudaSuccess ? r
                             : cudaFuncSetAttribute(broad, cudaFuncAttributeMaxDynamicSharedMemorySize,
                                                    wide_smem);
@@ -538,12 +561,21 @@ cudaError_t launch_tree(const gs_cache& c, const TreeArgs& a, bool wide, int tre
   if (wide) {
     CUtensorMap k, v;
     if (!pool_maps(c, &k, &v)) return cudaErrorUnknown;
-    e = launch_ex(broad, grid, dim3(kWideThreads), wide_smem, s, false, dim3(1, 1, 1), k, v, a);
+    e = launch_ex(broad, a.items ? grid : dim3(kWideBlocks), dim3(kWideThreads), wide_smem, s, false,
+                  dim3(1, 1, 1), k, v, a, trees);
   } else {
     e = launch_ex(narrow, grid, dim3(kThreads), smem, s, false, dim3(a.cluster ? a.items : 1, 1, 1), a);
   }
   if (e != cudaSuccess || a.items == 1 || a.cluster) return e;
-  return launch_join<BF16, D>(a, trees, s);
+  // a row's chunks are shared by as many groups as the GPU has room for
+  constexpr int NG = kJoinThreads / (D / 4);
+  const int64_t rows = static_cast<int64_t>(trees) * a.nodes;
+  const int64_t most = a.items ? a.items : kWideBlocks / (static_cast<int64_t>(trees) * a.cache.Hkv * a.tiles) + 2;
+  int groups = 1;
+  while (groups < NG && groups * 8 < most && rows * a.Hq * groups < kNumSMs * 4 * NG) groups *= 2;
+  const int64_t blocks = (rows * a.Hq * groups + NG - 1) / NG;
+  return launch_ex(tree_join_kernel<BF16, D>, dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads),
+                   0, s, true, dim3(1, 1, 1), a, groups, rows);
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }
@@ -551,11 +583,13 @@ size_t up256(size_t x) { return (x + 255) / 256 * 256; }
 struct Scratch {         // offsets of the trees' sizes, the partial accumulators, their (max, sum)
   size_t n, o, ml, total;
 };
-Scratch scratch_of(const gs_cache& c, int trees, int nodes, int n_heads, size_t items) {
-  const size_t rows = static_cast<size_t>(trees) * nodes * n_heads * items;
+// Parts: one per row, head and item; two tiles per block where the blocks share the pages.
+Scratch scratch_of(const gs_cache& c, int trees, int nodes, int n_heads, bool shared, size_t items) {
+  const size_t rows = shared ? 2ull * kWideBlocks * kWideRows
+                             : static_cast<size_t>(trees) * nodes * n_heads * items;
   Scratch s;
   s.n = kErrBytes;
-  s.o = s.n + up256(trees * sizeof(int2));
+  s.o = s.n + up256(16 + trees * sizeof(TreePart));
   s.ml = s.o + up256(rows * c.head_dim * sizeof(float));
   s.total = s.ml + up256(rows * sizeof(float2));
   return s;
@@ -579,18 +613,18 @@ extern "C" size_t gs_tree_attention_scratch_bytes(const gs_cache* cache, int tre
   using namespace gs;
   if (check_sizes(cache, trees, nodes, n_heads, split_pages) != GS_OK) return 0;
   const Plan p = plan_tree(*cache, trees, nodes, n_heads, 0, split_pages);
-  // An open split follows the pages that a window leaves: whatever it is, the
-  // items are at most one wave's share, a cluster, or pages / kMostPages, and
-  // the rounding.
+  // An open split of the narrow kernel follows the pages that a window leaves:
+  // whatever it is, the items are at most one wave's share, a cluster, or pages /
+  // kMostPages, and the rounding.
   size_t items = p.items;
-  if (split_pages == 0) {
+  if (split_pages == 0 && !p.wide) {
     const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * cache->n_kv_heads * p.tiles;
-    const size_t wave = static_cast<size_t>((p.wide ? 2 * kNumSMs : wave_of(cache->head_dim)) / blocks),
-                 cut = p.wide ? 0 : cache->pt_stride / kMostPages, cluster = kMostCluster;
+    const size_t wave = static_cast<size_t>(wave_of(cache->head_dim) / blocks),
+                 cut = cache->pt_stride / kMostPages, cluster = kMostCluster;
     items = std::max(std::max(wave, cut), cluster) + 2;
     if (items > static_cast<size_t>(cache->pt_stride)) items = cache->pt_stride;
   }
-  return scratch_of(*cache, trees, nodes, n_heads, items).total;
+  return scratch_of(*cache, trees, nodes, n_heads, p.shared, items).total;
 }
 
 extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t ld_q,
@@ -614,7 +648,7 @@ extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t l
     return GS_ERR_OOM;
   if (trees == 0) return GS_OK;
   const Plan p = plan_tree(*cache, trees, nodes, n_heads, window, split_pages);
-  const Scratch sc = scratch_of(*cache, trees, nodes, n_heads, p.items);
+  const Scratch sc = scratch_of(*cache, trees, nodes, n_heads, p.shared, p.items);
   uint8_t* base = static_cast<uint8_t*>(scratch);
   TreeArgs a;
   a.q = static_cast<const uint16_t*>(q);
@@ -639,7 +673,8 @@ extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t l
   a.scale_log2 = scale * kLog2e;
   a.part_o = reinterpret_cast<float*>(base + sc.o);
   a.part_ml = reinterpret_cast<float2*>(base + sc.ml);
-  a.part_n = reinterpret_cast<int2*>(base + sc.n);
+  a.part_all = reinterpret_cast<int64_t*>(base + sc.n);
+  a.part_n = reinterpret_cast<TreePart*>(base + sc.n + 16);
   a.err = static_cast<int*>(scratch);
   a.cache = cache_view(*cache);
   cudaStream_t s = static_cast<cudaStream_t>(stream);

@@ -10,6 +10,12 @@ constexpr size_t kErrBytes = 256;    // the error word at the scratch's start
 constexpr int kMostNodes = 64;       // bits of a mask
 constexpr int kMostCluster = 8;
 
+// What the joining kernel has to know of a tree.
+struct TreePart {
+  int64_t first;      // its first page in the order of all work (wide kernel, open split)
+  int pages, count;
+};
+
 struct TreeArgs {
   const uint16_t* q;
   int64_t ld_q;
@@ -23,16 +29,10 @@ struct TreeArgs {
   float scale_log2;
   float* part_o;      // [row][head][item][D]
   float2* part_ml;    // [row][head][item]
-  int2* part_n;       // [tree]: pages, nodes in use
+  TreePart* part_n;   // [tree]
+  int64_t* part_all;  // pages of all work, blocks that share it (wide kernel, open split)
   int* err;
   CacheView cache;
-};
-
-// A tree's numbers: cached keys, keys in all, nodes in use, the first key that
-// any node sees, its page and the pages from there on.
-struct Span {
-  int n, keys, count, lo, lo_most, page0, pages;
-  const int32_t* table;
 };
 
 // The first cached key that a node at position `pos` sees; positions below n
@@ -42,52 +42,29 @@ __device__ __forceinline__ int first_key(int pos, int n, int window) {
   return lo < 0 ? 0 : lo > n ? n : static_cast<int>(lo);
 }
 
-// The tree's numbers are read by one warp for its block: all threads go through
-// the same pages and barriers whatever happens to the arrays meanwhile.
-__device__ __forceinline__ Span find_span(const TreeArgs& a, int tree) {
-  __shared__ int s_v[6];
-  if (threadIdx.x < 32) {
-    int seq = a.seq ? a.seq[tree] : tree, n = a.n[tree];
-    int count = a.count ? a.count[tree] : a.nodes;
-    const int most = a.cache.pt_stride * kPageTokens;
-    bool bad = count < 0 || count > a.nodes;
-    count = min(max(count, 0), a.nodes);
-    if (n < 0 || n > most - count) {
-      bad = true;
-      n = n < 0 ? 0 : min(n, most);
-    }
-    int keys = min(n + count, most);
-    if (seq < 0 || seq >= a.cache.n_seq) {
-      bad = true;
-      seq = 0;
-      n = keys = 0;
-    }
-    int lo = a.window > 0 ? n : 0, lo_most = 0;
-    if (a.window > 0) {
-      for (int i = threadIdx.x; i < count; i += 32) {
-        const int x = first_key(a.pos[static_cast<int64_t>(tree) * a.nodes + i], n, a.window);
-        lo = min(lo, x);
-        lo_most = max(lo_most, x);
-      }
-      lo = __reduce_min_sync(0xFFFFFFFFu, lo);
-      lo_most = __reduce_max_sync(0xFFFFFFFFu, lo_most);
-    }
-    if (threadIdx.x == 0) {
-      if (bad) atomicExch(a.err, kErrBounds);
-      s_v[0] = seq, s_v[1] = n, s_v[2] = keys, s_v[3] = count, s_v[4] = lo, s_v[5] = lo_most;
-    }
+// A tree's numbers as they can be used: sequence, cached keys, keys in all, nodes in use.
+struct TreeNums {
+  int seq, n, keys, count;
+  bool bad;
+};
+__device__ __forceinline__ TreeNums read_tree(const TreeArgs& a, int tree) {
+  TreeNums t;
+  const int most = a.cache.pt_stride * kPageTokens;
+  t.seq = a.seq ? a.seq[tree] : tree;
+  t.n = a.n[tree];
+  t.count = a.count ? a.count[tree] : a.nodes;
+  t.bad = t.count < 0 || t.count > a.nodes;
+  t.count = min(max(t.count, 0), a.nodes);
+  if (t.n < 0 || t.n > most - t.count) {
+    t.bad = true;
+    t.n = t.n < 0 ? 0 : min(t.n, most);
   }
-  __syncthreads();
-  Span s;
-  s.n = s_v[1];
-  s.keys = s_v[2];
-  s.count = s_v[3];
-  s.lo = s_v[4];
-  s.lo_most = s_v[5];
-  s.page0 = s.lo / kPageTokens;
-  s.pages = max(0, (s.keys + kPageTokens - 1) / kPageTokens - s.page0);
-  s.table = a.cache.page_table + static_cast<int64_t>(s_v[0]) * a.cache.pt_stride;
-  return s;
+  t.keys = min(t.n + t.count, most);
+  if (t.seq < 0 || t.seq >= a.cache.n_seq) {
+    t.bad = true;
+    t.seq = t.n = t.keys = 0;
+  }
+  return t;
 }
 
 __device__ __forceinline__ uint32_t bits_below(int x) {

@@ -10,10 +10,19 @@
 //       tensor memory, so its maximum and sum never leave the thread
 //   O += P V     P in tensor memory, over S's place; V^T pages from shared memory
 //
-// A fifth warp fetches K by TMA and issues the S products, a sixth fetches V^T and
-// issues the O products (both lie in the cache as K-major operands): the two
-// chains run side by side, as do two blocks per SM.  S has two places, so that
-// the products of the next page run during the softmax of this one.
+// Four more warps fetch K and V^T by TMA (both lie in the cache as K-major operands)
+// and issue the S and the O products: to issue a copy takes a thread 300 to 400
+// cycles, a product about 110, so that one thread for two of these tasks would bound
+// the block (measured: 1580 cycles a page instead of 1100).  S has three places (two
+// at head dim 128), so that the products of the next pages run during the
+// softmax of this one.  The softmax warps take over registers of the other four: at
+// 128 to a thread they would spill.
+//
+// With a split that the caller gives, a block takes one item.  With an open one the
+// blocks share all pages of all trees evenly, in the order of tree, head, tile and
+// page: a block's share is a few segments, each of one tile, and those that are not
+// a whole tile's pages leave their part to the joining kernel.  So no block waits for a
+// longer one, and what a row's table could hold does not matter.
 //
 // m moves only when a row's maximum rises by more than 2^8 (O is rescaled then; the result
 // does not depend on m but for rounding).  In fp16 it is set 7 below the
@@ -33,16 +42,23 @@ namespace {
 
 constexpr int kWideRows = 128;                       // query rows of a block
 constexpr int kSoftWarps = 4, kSoftThreads = 128;
-constexpr int kScoreWarp = kSoftWarps, kValueWarp = kSoftWarps + 1;
-constexpr int kWideThreads = kSoftThreads + 64;      // (with one more warp, registers spill)
-constexpr int kTmemCols = 256;                       // S (and P) twice 64, O up to 128
-constexpr int kTmemO = 128;
+constexpr int kFetchKWarp = kSoftWarps, kFetchVWarp = kSoftWarps + 1, kScoreWarp = kSoftWarps + 2,
+              kValueWarp = kSoftWarps + 3;
+constexpr int kWideThreads = 256;
+// Registers of a softmax thread and of the others: what 256 threads of 128 have.
+constexpr int kSoftRegs = 184, kWorkRegs = 72;
+static_assert(kSoftThreads * kSoftRegs + (kWideThreads - kSoftThreads) * kWorkRegs == kWideThreads * 128);
+constexpr int kTmemCols = 256;                       // the places of S (and P), and O
+constexpr int kMostShared = 1024;                    // trees whose pages are shared evenly
+constexpr int kFewPages = 4;                         // the least share of a block
 constexpr float kRise = 8.f;                         // log2 units
 
 template <int D>
 struct WideSmem {
   static constexpr int H = D / 64;                   // 64-dim halves
-  static constexpr int stages = D == 64 ? 4 : 2;
+  static constexpr int stages = D == 64 ? 4 : 2;     // pages in flight
+  static constexpr int places = D == 64 ? 3 : 2;     // of S, 64 columns each; O behind them
+  static constexpr int o_col = 64 * places;
   static constexpr int q_bytes = H * kWideRows * 128;
   static constexpr int page_bytes = D * 128;         // K: [half][64 tokens][64 dims]; V^T: [dims][64 tokens]
   static constexpr int k_at = q_bytes, v_at = k_at + stages * page_bytes;
@@ -59,6 +75,26 @@ __device__ __forceinline__ float max3(float x, float y, float z) {
   float r;
   asm("max.f32 %0, %1, %2, %3;" : "=f"(r) : "f"(x), "f"(y), "f"(z));
   return r;
+}
+
+// 32 lanes x 16 columns, with the wait.
+__device__ __forceinline__ void tmem_ld16(uint32_t taddr, uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.ld.sync.aligned.32x32b.x16.b32 "
+      "{%0, %1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15}, [%16];"
+      : "=r"(r[0]), "=r"(r[1]), "=r"(r[2]), "=r"(r[3]), "=r"(r[4]), "=r"(r[5]), "=r"(r[6]),
+        "=r"(r[7]), "=r"(r[8]), "=r"(r[9]), "=r"(r[10]), "=r"(r[11]), "=r"(r[12]), "=r"(r[13]),
+        "=r"(r[14]), "=r"(r[15])
+      : "r"(taddr));
+  asm volatile("tcgen05.wait::ld.sync.aligned;" ::: "memory");
+}
+__device__ __forceinline__ void tmem_st16(uint32_t taddr, const uint32_t (&r)[16]) {
+  asm volatile(
+      "tcgen05.st.sync.aligned.32x32b.x16.b32 [%0], "
+      "{%1, %2, %3, %4, %5, %6, %7, %8, %9, %10, %11, %12, %13, %14, %15, %16};" ::"r"(taddr),
+      "r"(r[0]), "r"(r[1]), "r"(r[2]), "r"(r[3]), "r"(r[4]), "r"(r[5]), "r"(r[6]), "r"(r[7]),
+      "r"(r[8]), "r"(r[9]), "r"(r[10]), "r"(r[11]), "r"(r[12]), "r"(r[13]), "r"(r[14]), "r"(r[15])
+      : "memory");
 }
 
 // D += A B with A (two 16-bit values per column) in tensor memory.
@@ -94,40 +130,201 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
       : "memory");
 }
 
+__device__ __forceinline__ void block_barrier() {    // all warps, wherever they are
+  asm volatile("bar.sync 2, 256;" ::: "memory");
+}
 __device__ __forceinline__ void soft_barrier() {     // the softmax warps
   asm volatile("bar.sync 1, 128;" ::: "memory");
+}
+
+// The pages that a tree's nodes see: its first, and how many (0 without nodes).
+struct Pages {
+  int first, count;
+};
+__device__ __forceinline__ Pages tree_pages(const TreeArgs& a, const TreeNums& t) {
+  const int lo = a.window > 0 ? first_key(0, t.n, a.window) : 0;   // (of positions from n on)
+  const int first = min(min(lo, t.n) / kPageTokens, a.cache.pt_stride - 1);
+  return {first, t.count > 0 ? max(1, (t.keys + kPageTokens - 1) / kPageTokens - first) : 0};
+}
+__device__ __forceinline__ int tree_tiles(const TreeArgs& a, int count) {
+  return (count * a.G + kWideRows - 1) / kWideRows;
+}
+
+// One block's next piece of work.
+struct Segment {
+  int tree, head, tile, rows;            // rows: in use in this tile; 0: nothing is left
+  int n, keys, lo_most;
+  int seq, page, pages;                  // pages of the sequence's table
+  int64_t part;                          // its row of parts, -1: the whole tile
+};
+
+// The order of all work, walked by one warp.  Lane l holds tree 32 chunk + l.
+struct Walk {
+  int64_t at, end, total;                // this block's pages
+  int64_t before;                        // pages of the trees before the chunk
+  int64_t work, upto;                    // the lane's tree: its pages, and with those before
+  int chunk, blocks;
+};
+// It rests in shared memory between two segments.
+struct WalkRest {
+  int64_t at, end, work[32], upto[32];
+  int chunk;
+};
+__device__ __forceinline__ void walk_rest(WalkRest& r, const Walk& w, int lane) {
+  r.work[lane] = w.work;
+  r.upto[lane] = w.upto;
+  if (lane == 0) r.at = w.at, r.end = w.end, r.chunk = w.chunk;
+  __syncwarp();
+}
+__device__ __forceinline__ void walk_wake(const WalkRest& r, Walk& w, int lane) {
+  w.work = r.work[lane];
+  w.upto = r.upto[lane];
+  w.at = r.at;
+  w.end = r.end;
+  w.chunk = r.chunk;
+  __syncwarp();
+}
+__device__ __forceinline__ int64_t walk_load(const TreeArgs& a, int trees, int lane, Walk& w, bool tell) {
+  const int tree = w.chunk * 32 + lane;
+  w.work = 0;
+  if (tree < trees) {
+    const TreeNums t = read_tree(a, tree);
+    const Pages p = tree_pages(a, t);
+    w.work = static_cast<int64_t>(p.count) * a.cache.Hkv * tree_tiles(a, t.count);
+    if (tell && t.bad) atomicExch(a.err, kErrBounds);
+  }
+  w.upto = w.work;
+#pragma unroll
+  for (int x = 1; x < 32; x *= 2) {
+    const int64_t y = __shfl_up_sync(0xFFFFFFFFu, w.upto, x);
+    if (lane >= x) w.upto += y;
+  }
+  const int64_t sum = __shfl_sync(0xFFFFFFFFu, w.upto, 31);
+  if (tell && tree < trees) {
+    const TreeNums t = read_tree(a, tree);
+    a.part_n[tree] = {w.before + w.upto - w.work, tree_pages(a, t).count, t.count};
+  }
+  w.upto += w.before;
+  return sum;
+}
+__device__ __forceinline__ void walk_begin(const TreeArgs& a, int trees, int lane, Walk& w) {
+  const bool tell = blockIdx.x == 0;
+  w.before = 0;
+  const int chunks = (trees + 31) / 32;
+  for (w.chunk = 0; w.chunk < chunks; ++w.chunk) w.before += walk_load(a, trees, lane, w, tell);
+  w.total = w.before;
+  const int64_t most = max(static_cast<int64_t>(1), w.total / kFewPages);
+  w.blocks = static_cast<int>(min(static_cast<int64_t>(gridDim.x), most));
+  if (tell && lane == 0) a.part_all[0] = w.total, a.part_all[1] = w.blocks;
+  w.at = w.end = 0;
+  if (static_cast<int>(blockIdx.x) < w.blocks) {
+    w.at = w.total * blockIdx.x / w.blocks;
+    w.end = w.total * (blockIdx.x + 1) / w.blocks;
+  }
+  w.before = 0;
+  w.chunk = 0;
+  if (w.at < w.end) walk_load(a, trees, lane, w, false);
+}
+// The first cached key that all of a tree's nodes see (one warp).
+__device__ __forceinline__ int last_first_key(const TreeArgs& a, int tree, const TreeNums& t, int lane) {
+  if (a.window == 0) return 0;
+  int lo = 0;
+  for (int i = lane; i < t.count; i += 32)
+    lo = max(lo, first_key(a.pos[static_cast<int64_t>(tree) * a.nodes + i], t.n, a.window));
+  return __reduce_max_sync(0xFFFFFFFFu, lo);
+}
+__device__ __forceinline__ void walk_next(const TreeArgs& a, int trees, int lane, Walk& w, Segment& s) {
+  if (w.at >= w.end) {
+    if (lane == 0) s.rows = 0;
+    return;
+  }
+  uint32_t in;
+  while (!(in = __ballot_sync(0xFFFFFFFFu, w.upto > w.at)) && (w.chunk + 1) * 32 < trees) {
+    w.before = __shfl_sync(0xFFFFFFFFu, w.upto, 31);
+    ++w.chunk;
+    walk_load(a, trees, lane, w, false);
+  }
+  const int l = in ? __ffs(in) - 1 : 31;
+  const int64_t first = __shfl_sync(0xFFFFFFFFu, w.upto - w.work, l);
+  const int tree = w.chunk * 32 + l;
+  const TreeNums t = read_tree(a, tree);
+  const Pages p = tree_pages(a, t);
+  const int tiles = tree_tiles(a, t.count);
+  const int lo_most = last_first_key(a, tree, t, lane);
+  if (lane == 0) {
+    // (numbers that changed since they were added up end the walk)
+    const int64_t in_tree = w.at - first;
+    const int unit = in && p.count > 0 ? static_cast<int>(in_tree / p.count) : 0;
+    const int from = in && p.count > 0 ? static_cast<int>(in_tree % p.count) : 0;
+    const int pages = static_cast<int>(min(static_cast<int64_t>(p.count - from), w.end - w.at));
+    s.rows = in && pages > 0 && unit < a.cache.Hkv * tiles
+                 ? min(kWideRows, t.count * a.G - unit % tiles * kWideRows) : 0;
+    s.tree = tree;
+    s.head = unit / max(tiles, 1);
+    s.tile = unit % max(tiles, 1);
+    s.n = t.n, s.keys = t.keys, s.lo_most = lo_most;
+    s.seq = t.seq;
+    s.page = p.first + from;
+    s.pages = pages;
+    // a block's first segment may go on with a tile, its last leave one unfinished
+    s.part = pages == p.count ? -1
+                              : (2ll * blockIdx.x + (from == 0 ? 1 : 0)) * kWideRows;
+  }
+  w.at += __shfl_sync(0xFFFFFFFFu, lane == 0 ? max(s.pages, 1) : 0, 0);
+}
+
+// The block's next segment: of its share, or its one item.
+__device__ __forceinline__ void next_segment(const TreeArgs& a, int trees, int lane, int seg,
+                                             WalkRest& rest, Segment& s) {
+  if (a.items == 0) {
+    Walk walk;
+    walk_wake(rest, walk, lane);
+    walk_next(a, trees, lane, walk, s);
+    walk_rest(rest, walk, lane);
+    return;
+  }
+  const int tree = blockIdx.z, head = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
+  const TreeNums t = read_tree(a, tree);
+  const Pages p = tree_pages(a, t);
+  const int lo_most = last_first_key(a, tree, t, lane);
+  if (lane == 0) {
+    const int from = blockIdx.x * a.split;
+    const bool any = seg == 0 && from < p.count;
+    s = {tree, head, tile, any ? min(kWideRows, t.count * a.G - tile * kWideRows) : 0, t.n, t.keys,
+         lo_most, t.seq, p.first + from, min(a.split, p.count - from), p.count > a.split ? 0 : -1};
+    if (blockIdx.x == 0 && blockIdx.y == 0 && seg == 0) {
+      if (t.bad) atomicExch(a.err, kErrBounds);
+      a.part_n[tree] = {0, p.count, t.count};
+    }
+  }
 }
 
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kWideThreads, 2)
 tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                 const TreeArgs a) {
+                 const TreeArgs a, int trees) {
   using L = WideSmem<D>;
-  constexpr int H = L::H, ST = L::stages;
+  constexpr int H = L::H, ST = L::stages, NP = L::places, O = L::o_col;
   extern __shared__ uint8_t smem_raw[];
+  __shared__ Segment s_seg;
+  __shared__ WalkRest s_walk;
   __shared__ uint32_t s_some[2][kSoftWarps], s_all[2][kSoftWarps], s_odd[2];
   __shared__ int64_t s_place[kWideRows];   // of each row: its query, then its output or part
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars_at);
   const uint32_t k_full = smem_u32(bars), k_empty = k_full + 8 * ST, v_full = k_empty + 8 * ST,
-                 v_empty = v_full + 8 * ST, s_full = v_empty + 8 * ST, p_full = s_full + 16,
-                 pv_done = p_full + 16, q_full = pv_done + 16;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * ST + 7);
+                 v_empty = v_full + 8 * ST, s_full = v_empty + 8 * ST, p_full = s_full + 8 * NP,
+                 pv_done = p_full + 8 * NP, q_full = pv_done + 8 * NP;
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * ST + 3 * NP + 1);
   pdl_trigger();   // the joining kernel may take its place; it waits for this one's end
-  const int tree = blockIdx.z, head = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
-  const int item = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
-  const Span sp = find_span(a, tree);
-  const int items = (sp.pages + a.split - 1) / a.split;
-  const int rows = min(kWideRows, sp.count * a.G - tile * kWideRows);
-  if (blockIdx.x == 0 && blockIdx.y == 0 && threadIdx.x == 0)
-    a.part_n[tree] = make_int2(sp.pages, sp.count);
-  if (rows <= 0 || (item >= items && item > 0)) return;
-  const int64_t row0 = static_cast<int64_t>(tree) * a.nodes;
-  const int page_begin = sp.page0 + item * a.split;
-  const int pages = max(0, min(a.split, sp.pages - item * a.split));
-
+  const bool shared = a.items == 0;      // an open split
+  if (warp == kFetchKWarp && shared) {
+    Walk walk;
+    walk_begin(a, trees, lane, walk);
+    walk_rest(s_walk, walk, lane);
+  }
   if (threadIdx.x == 0) {
     tma_prefetch_desc(&map_k);
     tma_prefetch_desc(&map_v);
@@ -137,7 +334,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       mbar_init(v_full + 8 * i, 1);
       mbar_init(v_empty + 8 * i, 1);
     }
-    for (int i = 0; i < 2; ++i) {
+    for (int i = 0; i < NP; ++i) {
       mbar_init(s_full + 8 * i, 1);
       mbar_init(p_full + 8 * i, kSoftWarps);
       mbar_init(pv_done + 8 * i, 1);
@@ -146,331 +343,364 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     fence_mbar_init();
   }
   if (warp == kScoreWarp) tmem_alloc(smem_u32(tmem_slot), kTmemCols);
-  tc_fence_before();
-  __syncthreads();
-  tc_fence_after();
-  const uint32_t tmem = *tmem_slot;
   bool ok = true;
-
-  if (warp == kScoreWarp || warp == kValueWarp) {
-    // ---- TMA and products.  Lane l holds the number of page 32 i + l.  A page's
-    // place in the ring is filled again as soon as its products are done.
-    const bool value = warp == kValueWarp;
-    const uint32_t full = value ? v_full : k_full, empty = value ? v_empty : k_empty;
-    const uint32_t ring = smem_u32(smem + (value ? L::v_at : L::k_at));
-    const uint64_t qd = umma_desc_sw128(smem_u32(smem));
-    int ids = 0, issued = 0;
-    auto fetch = [&](int j) {              // (all lanes)
-      if (j >= pages) return;
-      if (!(j & 31) && j + lane < pages) {
-        ids = sp.table[page_begin + j + lane];
-        if (ids < 0 || ids >= a.cache.n_pages) {
-          atomicExch(a.err, kErrBounds);
-          ids = 0;
-        }
-      }
-      const int page = __shfl_sync(0xFFFFFFFFu, ids, j & 31);
-      if (lane == 0 && ok) {
-        const int st = j % ST;
-        const int block = (2 * page + value) * a.cache.Hkv + head;
-        const uint32_t dst = ring + st * L::page_bytes, bar = full + 8 * st;
-        if (j >= ST) ok = mbar_wait(empty + 8 * st, (j / ST + 1) & 1, a.err);
-        if (ok) {
-          mbar_arrive_expect_tx(bar, L::page_bytes);
-          if (value) {
-            tma_load_3d(dst, &map_v, 0, 0, block, bar);
-          } else {
-#pragma unroll
-            for (int h = 0; h < H; ++h)
-              tma_load_4d(dst + h * kPageTokens * 128, &map_k, 0, h, 0, block, bar);
-          }
-          issued = j + 1;
-        }
-      }
-      __syncwarp();
-    };
-    for (int j = 0; j < ST; ++j) fetch(j);
-    if (lane == 0 && !value && pages > 0) ok = mbar_wait(q_full, 0, a.err);
-    for (int j = 0; j < pages; ++j) {
-      const int st = j % ST, at = j & 1;
-      if (lane == 0 && ok) {
-        ok = mbar_wait(full + 8 * st, (j / ST) & 1, a.err);
-        if (!value) {      // S of page j, where P of page j - 2 was
-          ok = ok && (j < 2 || mbar_wait(pv_done + 8 * at, (j / 2 + 1) & 1, a.err));
-          if (ok) {
-            tc_fence_after();
-            const uint64_t kd = umma_desc_sw128(ring + st * L::page_bytes);
-#pragma unroll
-            for (int k = 0; k < D / 16; ++k)
-              umma_f16(tmem + 64 * at, qd + (k / 4) * (kWideRows * 128 >> 4) + (k % 4) * 2,
-                       kd + (k / 4) * (kPageTokens * 128 >> 4) + (k % 4) * 2,
-                       wide_idesc<BF16>(kPageTokens), k > 0);
-            umma_commit(s_full + 8 * at);
-            umma_commit(empty + 8 * st);
-          }
-        } else {           // O += P V
-          ok = ok && mbar_wait(p_full + 8 * at, (j / 2) & 1, a.err);
-          if (ok) {
-            tc_fence_after();
-            const uint64_t vd = umma_desc_sw128(ring + st * L::page_bytes);
-#pragma unroll
-            for (int k = 0; k < kPageTokens / 16; ++k)
-              umma_f16_ta(tmem + kTmemO, tmem + 64 * at + 8 * k, vd + k * 2, wide_idesc<BF16>(D));
-            umma_commit(pv_done + 8 * at);
-            umma_commit(empty + 8 * st);
-          }
-        }
-      }
-      __syncwarp();
-      fetch(j + ST);
-    }
-    // the block's shared memory outlives its copies
-    if (lane == 0)
-      for (int j = max(0, issued - ST); j < issued; ++j)
-        mbar_wait(full + 8 * (j % ST), (j / ST) & 1, a.err);
-    __syncwarp();
-  } else {
-    // ---- softmax: thread = row = lane of tensor memory
-    const int r = threadIdx.x;
-    const bool live = r < rows, busy = warp * 32 < rows;   // the row, any row of the warp is in use
-    const int node = live ? (tile * kWideRows + r) / a.G : 0;
-    const int q_head = head * a.G + (live ? (tile * kWideRows + r) % a.G : 0);
-    // queries, a row's 16-byte pieces by neighbouring threads (rows not in use
-    // hold anything: they meet no other)
-    s_place[r] = live ? (row0 + node) * a.ld_q + static_cast<int64_t>(q_head) * D : -1;
-    soft_barrier();
-#pragma unroll 4
-    for (int i = 0; i < D / 8; ++i) {
-      const int e = r + i * kSoftThreads, row = e / (D / 8), c = e % (D / 8);
-      const uint32_t to = smem_u32(smem) + (c / 8) * kWideRows * 128 + swizzled(row, c % 8);
-      if (row < rows)
-        asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(a.q + s_place[row] + 8 * c)
-                     : "memory");
-    }
-    const uint32_t trow = tmem + (static_cast<uint32_t>(warp * 32) << 16);
-    {
-      uint32_t zero[32];
-#pragma unroll
-      for (int i = 0; i < 32; ++i) zero[i] = 0u;
-#pragma unroll
-      for (int c = 0; c < D / 32; ++c) tmem_st32(trow + kTmemO + 32 * c, zero);
-      tmem_wait_st();
-    }
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    fence_proxy_async_smem();
-    tc_fence_before();
-    __syncwarp();
-    if (lane == 0) mbar_arrive(q_full);
-    uint64_t mask = 0;
-    int lo = sp.n;
-    if (live) {
-      mask = a.mask[row0 + node];
-      if (sp.keys - sp.n < 64) mask &= (1ull << (sp.keys - sp.n)) - 1;
-      lo = a.window > 0 ? min(max(first_key(a.pos[row0 + node], sp.n, a.window), sp.lo), sp.lo_most)
-                        : 0;
-    }
-    // waits are warp-uniform; after a failure the warp stops waiting
-    auto wait = [&](uint32_t bar, uint32_t phase) {
-      if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, phase, a.err)) != 0;
-      return ok;
-    };
-    constexpr float kSet = BF16 ? 0.f : 7.f;         // how far below the maximum m is set
-    const F32x2 scale2 = join2(a.scale_log2, a.scale_log2);
-    float m = -INFINITY, l = 0.f;
-    for (int j = 0; j < pages; ++j) {
-      const int at = j & 1, tok0 = (page_begin + j) * kPageTokens;
-      const bool edge = tok0 < sp.lo_most || tok0 + kPageTokens > sp.n;
-      wait(s_full + 8 * at, (j / 2) & 1);
+  // pages are counted over all segments: page j uses ring place j % ST; `at`, the
+  // place of S, and `turn`, its uses so far mod 2, are counted along
+  int base = 0, at = 0;
+  uint32_t turn = 0;
+  auto step = [&] {
+    if (++at == NP) at = 0, turn ^= 1;
+  };
+  if (warp >= kSoftWarps) {
+    asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWorkRegs));
+    for (int seg = 0;; ++seg) {
+      tc_fence_before();
+      block_barrier();                   // the last segment's numbers and memory are done with
+      if (warp == kFetchKWarp) next_segment(a, trees, lane, seg, s_walk, s_seg);
+      block_barrier();
       tc_fence_after();
-      if (busy) {
-        uint32_t s[2][32];
-        tmem_ld32_nowait(trow + 64 * at, s[0]);
-        tmem_ld32_nowait(trow + 64 * at + 32, s[1]);
-        tmem_wait_ld();
-        if (edge) {
-#pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint32_t v = row_view(mask, lo, sp.n, tok0 + 32 * h);
-#pragma unroll
-            for (int i = 0; i < 32; ++i)
-              if (!((v >> i) & 1)) s[h][i] = 0xFF800000u;
-          }
-        }
-        float x[4];
-#pragma unroll
-        for (int e = 0; e < 4; ++e) {
-          x[e] = fmaxf(__uint_as_float(s[0][e]), __uint_as_float(s[1][e]));
-#pragma unroll
-          for (int i = 4; i < 32; i += 4)
-            x[e] = max3(x[e], __uint_as_float(s[0][i + e]), __uint_as_float(s[1][i + e]));
-        }
-        const float mx = fmaxf(max3(x[0], x[1], x[2]), x[3]) * a.scale_log2;
-        const bool rise = mx - kSet > m + kRise || (m == -INFINITY && mx > m);
-        if (__any_sync(0xFFFFFFFFu, rise)) {
-          const float set = rise ? mx - kSet : m;
-          const float f = rise ? ex2(m - set) : 1.f;   // (m = -inf: 0)
-          l *= f;
-          m = set;
-          if (j > 0 && wait(pv_done + 8 * (at ^ 1), ((j - 1) / 2) & 1)) {
-            tc_fence_after();
-#pragma unroll
-            for (int c = 0; c < D / 32; ++c) {
-              uint32_t o[32];
-              tmem_ld32_nowait(trow + kTmemO + 32 * c, o);
-              tmem_wait_ld();
-#pragma unroll
-              for (int i = 0; i < 32; ++i) o[i] = __float_as_uint(f * __uint_as_float(o[i]));
-              tmem_st32(trow + kTmemO + 32 * c, o);
+      const int pages = s_seg.pages, end = base + pages;
+      if (s_seg.rows <= 0) break;
+      const uint32_t tmem = *tmem_slot;
+      if (warp == kFetchKWarp || warp == kFetchVWarp) {
+        // ---- TMA: the segment's pages; lane l holds the number of page 32 i + l
+        const bool value = warp == kFetchVWarp;
+        const uint32_t full = value ? v_full : k_full, empty = value ? v_empty : k_empty;
+        const uint32_t ring = smem_u32(smem + (value ? L::v_at : L::k_at));
+        const int32_t* table = a.cache.page_table +
+                               static_cast<int64_t>(s_seg.seq) * a.cache.pt_stride + s_seg.page - base;
+        const int which = (value ? a.cache.Hkv : 0) + s_seg.head;
+        int ids = 0, fetched = base;
+        for (int j = base; j < end && ok; ++j) {
+          const int i = (j - base) & 31;
+          if (i == 0 && j + lane < end) {
+            ids = table[j + lane];
+            if (ids < 0 || ids >= a.cache.n_pages) {
+              atomicExch(a.err, kErrBounds);
+              ids = 0;
             }
           }
-        }
-        const float z = finite_max(m);
-        const F32x2 z2 = join2(-z, -z);
-        F32x2 sum2[2] = {join2(0.f, 0.f), join2(0.f, 0.f)};
-        uint32_t p[32];
+          const int block = 2 * a.cache.Hkv * __shfl_sync(0xFFFFFFFFu, ids, i) + which;
+          if (lane == 0) {
+            const uint32_t bar = full + 8 * (j % ST), dst = ring + j % ST * L::page_bytes;
+            if (j >= ST) ok = mbar_wait(empty + 8 * (j % ST), (j / ST + 1) & 1, a.err);
+            if (ok) {
+              mbar_arrive_expect_tx(bar, L::page_bytes);
+              if (value) {
+                tma_load_3d(dst, &map_v, 0, 0, block, bar);
+              } else {
 #pragma unroll
-        for (int i = 0; i < 32; ++i) {
-          const float2 e = split2(fma2(join2(__uint_as_float(s[i / 16][2 * (i % 16)]),
-                                             __uint_as_float(s[i / 16][2 * (i % 16) + 1])),
-                                       scale2, z2));
-          const float u = ex2(e.x), w = ex2(e.y);
-          sum2[i & 1] = add2(sum2[i & 1], join2(u, w));
-          p[i] = pack2<BF16>(u, w);
+                for (int h = 0; h < H; ++h)
+                  tma_load_4d(dst + h * kPageTokens * 128, &map_k, 0, h, 0, block, bar);
+              }
+              fetched = j + 1;
+            }
+          }
+          ok = __shfl_sync(0xFFFFFFFFu, ok, 0);
         }
-        tmem_st32(trow + 64 * at, p);
-        const float2 sum = split2(add2(sum2[0], sum2[1]));
-        l += sum.x + sum.y;
+        // the ring outlives its copies
+        if (lane == 0)
+          for (int j = max(base, fetched - ST); j < fetched; ++j)
+            mbar_wait(full + 8 * (j % ST), (j / ST) & 1, a.err);
+      } else if (lane == 0 && warp == kScoreWarp) {
+        // ---- S, where an earlier page's P was
+        const uint64_t qd = umma_desc_sw128(smem_u32(smem));
+        ok = ok && mbar_wait(q_full, seg & 1, a.err);
+        for (int j = base; j < end && ok; ++j) {
+          const int st = j % ST;
+          ok = (j < NP || mbar_wait(pv_done + 8 * at, turn ^ 1, a.err)) &&
+               mbar_wait(k_full + 8 * st, (j / ST) & 1, a.err);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t kd = umma_desc_sw128(smem_u32(smem + L::k_at + st * L::page_bytes));
+#pragma unroll
+          for (int k = 0; k < D / 16; ++k)
+            umma_f16(tmem + 64 * at, qd + (k / 4) * (kWideRows * 128 >> 4) + (k % 4) * 2,
+                     kd + (k / 4) * (kPageTokens * 128 >> 4) + (k % 4) * 2,
+                     wide_idesc<BF16>(kPageTokens), k > 0);
+          umma_commit(s_full + 8 * at);
+          umma_commit(k_empty + 8 * st);
+          step();
+        }
+      } else if (lane == 0) {
+        // ---- O += P V
+        for (int j = base; j < end && ok; ++j) {
+          const int st = j % ST;
+          ok = mbar_wait(v_full + 8 * st, (j / ST) & 1, a.err) &&
+               mbar_wait(p_full + 8 * at, turn, a.err);
+          if (!ok) break;
+          tc_fence_after();
+          const uint64_t vd = umma_desc_sw128(smem_u32(smem + L::v_at + st * L::page_bytes));
+#pragma unroll
+          for (int k = 0; k < kPageTokens / 16; ++k)
+            umma_f16_ta(tmem + O, tmem + 64 * at + 8 * k, vd + k * 2, wide_idesc<BF16>(D));
+          umma_commit(pv_done + 8 * at);
+          umma_commit(v_empty + 8 * st);
+          step();
+        }
+      }
+      __syncwarp();
+      base = end;
+    }
+  } else {
+    asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
+    for (;;) {
+      tc_fence_before();
+      block_barrier();
+      block_barrier();
+      tc_fence_after();
+      const uint32_t tmem = *tmem_slot;
+      const int rows = s_seg.rows, pages = s_seg.pages;
+      if (rows <= 0) break;
+      const int head = s_seg.head, page0 = s_seg.page;
+      // ---- softmax: thread = row = lane of tensor memory
+      const int r = threadIdx.x;
+      const bool live = r < rows, busy = warp * 32 < rows;   // the row, any row of the warp is in use
+      const int of = live ? s_seg.tile * kWideRows + r : 0, node = of / a.G;
+      const int q_head = head * a.G + of % a.G, n = s_seg.n, lo_most = s_seg.lo_most;
+      const int64_t row = static_cast<int64_t>(s_seg.tree) * a.nodes + node;
+      // queries, a row's 16-byte pieces by neighbouring threads (rows not in use
+      // hold anything: they meet no other, and never rise)
+      s_place[r] = live ? row * a.ld_q + static_cast<int64_t>(q_head) * D : -1;
+      soft_barrier();
+#pragma unroll 4
+      for (int i = 0; i < D / 8; ++i) {
+        const int e = r + i * kSoftThreads, qr = e / (D / 8), c = e % (D / 8);
+        const uint32_t to = smem_u32(smem) + (c / 8) * kWideRows * 128 + swizzled(qr, c % 8);
+        if (qr < rows)
+          asm volatile("cp.async.cg.shared.global [%0], [%1], 16;" ::"r"(to), "l"(a.q + s_place[qr] + 8 * c)
+                       : "memory");
+      }
+      const uint32_t trow = tmem + (static_cast<uint32_t>(warp * 32) << 16);
+      if (busy) {
+        uint32_t zero[16];
+#pragma unroll
+        for (int i = 0; i < 16; ++i) zero[i] = 0u;
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) tmem_st16(trow + O + 16 * c, zero);
         tmem_wait_st();
       }
-      if (edge) {
-        // values that no row sees are cleared; those that are not finite and that
-        // some rows see go to their O by hand
-        const int st = j % ST;
-        uint8_t* v = smem + L::v_at + st * L::page_bytes;
-#pragma unroll
-        for (int w = 0; w < 2; ++w) {
-          const uint32_t x = row_view(mask, lo, sp.n, tok0 + 32 * w);
-          const uint32_t some = __reduce_or_sync(0xFFFFFFFFu, live ? x : 0u),
-                         all = __reduce_and_sync(0xFFFFFFFFu, live ? x : 0xFFFFFFFFu);
-          if (lane == 0) s_some[w][warp] = some, s_all[w][warp] = all;
-        }
-        if (r < 2) s_odd[r] = 0u;
-        wait(v_full + 8 * st, (j / ST) & 1);
-        soft_barrier();
-        // chunk = 8 tokens of a dim
-        for (int e = r; e < D * 8; e += kSoftThreads) {
-          const int chunk = e % 8, dim = e / 8, w = chunk / 4, shift = chunk % 4 * 8;
-          uint32_t some = 0u, all = 0xFFFFFFFFu;
-#pragma unroll
-          for (int k = 0; k < kSoftWarps; ++k) some |= s_some[w][k], all &= s_all[w][k];
-          const uint32_t keep = some >> shift, part = (some & ~all) >> shift;
-          if ((keep & 0xFF) == 0xFF && !(part & 0xFF)) continue;
-          uint4* to = reinterpret_cast<uint4*>(v + swizzled(dim, chunk));
-          const uint4 x = *to;
-          uint32_t word[4] = {x.x, x.y, x.z, x.w}, odd = 0u;
-#pragma unroll
-          for (int k = 0; k < 4; ++k) {
-            if (!((keep >> (2 * k)) & 1)) word[k] &= 0xFFFF0000u;
-            if (!((keep >> (2 * k + 1)) & 1)) word[k] &= 0x0000FFFFu;
-            const uint32_t nf = not_finite<BF16>(word[k]);
-            odd |= ((nf & 1u) | (nf >> 30 & 2u)) << (2 * k) & part;
-          }
-          *to = make_uint4(word[0], word[1], word[2], word[3]);
-          if (odd & 0xFFu) atomicOr(&s_odd[w], (odd & 0xFFu) << shift);
-        }
-        soft_barrier();
-        if (s_odd[0] | s_odd[1]) {
-          if (j > 0) wait(pv_done + 8 * (at ^ 1), ((j - 1) / 2) & 1);
-          tc_fence_after();
-          for (int c = 0; c < D / 32; ++c) {
-            uint32_t o[32];
-            tmem_ld32_nowait(trow + kTmemO + 32 * c, o);
-            tmem_wait_ld();
-            for (int w = 0; w < 2; ++w)
-              for (uint32_t left = s_odd[w] & row_view(mask, lo, sp.n, tok0 + 32 * w); left;
-                   left &= left - 1) {
-                const int tok = 32 * w + __ffs(left) - 1;
-#pragma unroll
-                for (int i = 0; i < 32; ++i) {
-                  const uint32_t h = *reinterpret_cast<const uint16_t*>(
-                      v + swizzled(32 * c + i, tok / 8) + tok % 8 * 2);
-                  if (not_finite<BF16>(h))
-                    o[i] = __float_as_uint(__uint_as_float(o[i]) + unpack2<BF16>(h).x);
-                }
-              }
-            __syncwarp();
-            tmem_st32(trow + kTmemO + 32 * c, o);
-          }
-          tmem_wait_st();
-          soft_barrier();
-          for (int e = r; e < D * 8; e += kSoftThreads) {
-            const int chunk = e % 8, dim = e / 8;
-            const uint32_t odd = s_odd[chunk / 4] >> (chunk % 4 * 8);
-            if (!(odd & 0xFF)) continue;
-            uint4* to = reinterpret_cast<uint4*>(v + swizzled(dim, chunk));
-            const uint4 x = *to;
-            uint32_t word[4] = {x.x, x.y, x.z, x.w};
-#pragma unroll
-            for (int k = 0; k < 4; ++k) {
-              const uint32_t sel = ((odd >> (2 * k)) & 1 ? 0x0000FFFFu : 0u) |
-                                   ((odd >> (2 * k + 1)) & 1 ? 0xFFFF0000u : 0u);
-              word[k] &= ~(not_finite<BF16>(word[k]) & sel);
-            }
-            *to = make_uint4(word[0], word[1], word[2], word[3]);
-          }
-        }
-        soft_barrier();                  // the words above are free for the next page
-        fence_proxy_async_smem();
+      uint64_t mask = 0;
+      int lo = n;
+      if (live) {
+        mask = a.mask[row];
+        if (s_seg.keys - n < 64) mask &= (1ull << (s_seg.keys - n)) - 1;
+        lo = a.window > 0 ? min(first_key(a.pos[row], n, a.window), lo_most) : 0;
       }
+      asm volatile("cp.async.wait_all;" ::: "memory");
+      fence_proxy_async_smem();
       tc_fence_before();
       __syncwarp();
-      if (lane == 0) mbar_arrive(p_full + 8 * at);
-    }
-    // ---- the row's end
-    if (pages > 0) wait(pv_done + 8 * ((pages - 1) & 1), ((pages - 1) / 2) & 1);
-    tc_fence_after();
-    // (the last O is done, and so are all products and copies: their shared
-    // memory takes the rows, which are then written a row's pieces by neighbours)
-    const int64_t row = row0 + node, at = row * a.Hq + q_head;
-    constexpr int P = D + 4;
-    float* so = reinterpret_cast<float*>(smem);
-    const float inv = items > 1 ? 1.f : l != 0.f ? 1.f / l : 0.f;
-    if (busy) {
+      if (lane == 0) mbar_arrive(q_full);
+      // waits are warp-uniform; after a failure the warp stops waiting
+      auto wait = [&](uint32_t bar, uint32_t phase) {
+        if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, phase, a.err)) != 0;
+        return ok;
+      };
+      constexpr float kSet = BF16 ? 0.f : 7.f;         // how far below the maximum m is set
+      const F32x2 scale2 = join2(a.scale_log2, a.scale_log2);
+      float m = -INFINITY, l = 0.f;
+      for (int j = 0; j < pages; ++j) {
+        const int tok0 = (page0 + j) * kPageTokens;
+        const bool edge = tok0 < lo_most || tok0 + kPageTokens > n;
+        // the products of the page before this one
+        const int was = at == 0 ? NP - 1 : at - 1;
+        const uint32_t was_turn = at == 0 ? turn ^ 1 : turn;
+        wait(s_full + 8 * at, turn);
+        tc_fence_after();
+        if (busy) {
+          uint32_t s[2][32];
+          tmem_ld32_nowait(trow + 64 * at, s[0]);
+          tmem_ld32_nowait(trow + 64 * at + 32, s[1]);
+          tmem_wait_ld();
+          if (edge) {
 #pragma unroll
-      for (int c = 0; c < D / 32; ++c) {
-        uint32_t o[32];
-        tmem_ld32_nowait(trow + kTmemO + 32 * c, o);
-        tmem_wait_ld();
+            for (int h = 0; h < 2; ++h) {
+              const uint32_t v = row_view(mask, lo, n, tok0 + 32 * h);
 #pragma unroll
-        for (int i = 0; i < 32; i += 4)
-          *reinterpret_cast<float4*>(so + r * P + 32 * c + i) =
-              make_float4(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv,
-                          __uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+              for (int i = 0; i < 32; ++i)
+                if (!((v >> i) & 1)) s[h][i] = 0xFF800000u;
+            }
+          }
+          float x[4];
+#pragma unroll
+          for (int e = 0; e < 4; ++e) {
+            x[e] = fmaxf(__uint_as_float(s[0][e]), __uint_as_float(s[1][e]));
+#pragma unroll
+            for (int i = 4; i < 32; i += 4)
+              x[e] = max3(x[e], __uint_as_float(s[0][i + e]), __uint_as_float(s[1][i + e]));
+          }
+          const float mx = fmaxf(max3(x[0], x[1], x[2]), x[3]) * a.scale_log2;
+          const bool rise = live && (mx - kSet > m + kRise || (m == -INFINITY && mx > m));
+          if (__any_sync(0xFFFFFFFFu, rise)) {
+            const float set = rise ? mx - kSet : m;
+            const float f = rise ? ex2(m - set) : 1.f;   // (m = -inf: 0)
+            l *= f;
+            m = set;
+            if (j > 0 && wait(pv_done + 8 * was, was_turn)) {
+              tc_fence_after();
+              for (int c = 0; c < D / 16; ++c) {
+                uint32_t o[16];
+                tmem_ld16(trow + O + 16 * c, o);
+#pragma unroll
+                for (int i = 0; i < 16; ++i) o[i] = __float_as_uint(f * __uint_as_float(o[i]));
+                tmem_st16(trow + O + 16 * c, o);
+              }
+            }
+          }
+          const float z = finite_max(m);
+          const F32x2 z2 = join2(-z, -z);
+          F32x2 sum2[2] = {join2(0.f, 0.f), join2(0.f, 0.f)};
+#pragma unroll
+          for (int h = 0; h < 2; ++h) {
+            uint32_t p[16];
+#pragma unroll
+            for (int i = 0; i < 16; ++i) {
+              const float2 e = split2(fma2(
+                  join2(__uint_as_float(s[h][2 * i]), __uint_as_float(s[h][2 * i + 1])), scale2, z2));
+              const float u = ex2(e.x), w = ex2(e.y);
+              sum2[i & 1] = add2(sum2[i & 1], join2(u, w));
+              p[i] = pack2<BF16>(u, w);
+            }
+            tmem_st16(trow + 64 * at + 16 * h, p);
+          }
+          const float2 sum = split2(add2(sum2[0], sum2[1]));
+          l += sum.x + sum.y;
+          tmem_wait_st();
+        }
+        if (edge) {
+          // values that no row sees are cleared; those that are not finite and that
+          // some rows see go to their O by hand
+          const int st = (base + j) % ST;
+          uint8_t* v = smem + L::v_at + st * L::page_bytes;
+#pragma unroll
+          for (int w = 0; w < 2; ++w) {
+            const uint32_t x = row_view(mask, lo, n, tok0 + 32 * w);
+            const uint32_t some = __reduce_or_sync(0xFFFFFFFFu, live ? x : 0u),
+                           all = __reduce_and_sync(0xFFFFFFFFu, live ? x : 0xFFFFFFFFu);
+            if (lane == 0) s_some[w][warp] = some, s_all[w][warp] = all;
+          }
+          if (r < 2) s_odd[r] = 0u;
+          wait(v_full + 8 * st, ((base + j) / ST) & 1);
+          soft_barrier();
+          // chunk = 8 tokens of a dim
+          for (int e = r; e < D * 8; e += kSoftThreads) {
+            const int chunk = e % 8, dim = e / 8, w = chunk / 4, shift = chunk % 4 * 8;
+            uint32_t some = 0u, all = 0xFFFFFFFFu;
+#pragma unroll
+            for (int k = 0; k < kSoftWarps; ++k) some |= s_some[w][k], all &= s_all[w][k];
+            const uint32_t keep = some >> shift, part = (some & ~all) >> shift;
+            if ((keep & 0xFF) == 0xFF && !(part & 0xFF)) continue;
+            uint4* to = reinterpret_cast<uint4*>(v + swizzled(dim, chunk));
+            const uint4 x = *to;
+            uint32_t word[4] = {x.x, x.y, x.z, x.w}, odd = 0u;
+#pragma unroll
+            for (int k = 0; k < 4; ++k) {
+              if (!((keep >> (2 * k)) & 1)) word[k] &= 0xFFFF0000u;
+              if (!((keep >> (2 * k + 1)) & 1)) word[k] &= 0x0000FFFFu;
+              const uint32_t nf = not_finite<BF16>(word[k]);
+              odd |= ((nf & 1u) | (nf >> 30 & 2u)) << (2 * k) & part;
+            }
+            *to = make_uint4(word[0], word[1], word[2], word[3]);
+            if (odd & 0xFFu) atomicOr(&s_odd[w], (odd & 0xFFu) << shift);
+          }
+          soft_barrier();
+          if (s_odd[0] | s_odd[1]) {
+            if (j > 0) wait(pv_done + 8 * was, was_turn);
+            tc_fence_after();
+            for (int c = 0; c < D / 16; ++c) {
+              uint32_t o[16];
+              tmem_ld16(trow + O + 16 * c, o);
+              for (int w = 0; w < 2; ++w)
+                for (uint32_t left = s_odd[w] & row_view(mask, lo, n, tok0 + 32 * w); left;
+                     left &= left - 1) {
+                  const int tok = 32 * w + __ffs(left) - 1;
+#pragma unroll
+                  for (int i = 0; i < 16; ++i) {
+                    const uint32_t h = *reinterpret_cast<const uint16_t*>(
+                        v + swizzled(16 * c + i, tok / 8) + tok % 8 * 2);
+                    if (not_finite<BF16>(h))
+                      o[i] = __float_as_uint(__uint_as_float(o[i]) + unpack2<BF16>(h).x);
+                  }
+                }
+              __syncwarp();
+              tmem_st16(trow + O + 16 * c, o);
+            }
+            tmem_wait_st();
+            soft_barrier();
+            for (int e = r; e < D * 8; e += kSoftThreads) {
+              const int chunk = e % 8, dim = e / 8;
+              const uint32_t odd = s_odd[chunk / 4] >> (chunk % 4 * 8);
+              if (!(odd & 0xFF)) continue;
+              uint4* to = reinterpret_cast<uint4*>(v + swizzled(dim, chunk));
+              const uint4 x = *to;
+              uint32_t word[4] = {x.x, x.y, x.z, x.w};
+#pragma unroll
+              for (int k = 0; k < 4; ++k) {
+                const uint32_t sel = ((odd >> (2 * k)) & 1 ? 0x0000FFFFu : 0u) |
+                                     ((odd >> (2 * k + 1)) & 1 ? 0xFFFF0000u : 0u);
+                word[k] &= ~(not_finite<BF16>(word[k]) & sel);
+              }
+              *to = make_uint4(word[0], word[1], word[2], word[3]);
+            }
+          }
+          soft_barrier();                  // the words above are free for the next page
+          fence_proxy_async_smem();
+        }
+        tc_fence_before();
+        __syncwarp();
+        if (lane == 0) mbar_arrive(p_full + 8 * at);
+        step();
       }
-    }
-    if (live) {
-      if (items > 1)
-        a.part_ml[at * a.items + item] = make_float2(m, l);
-      else if (a.lse)
-        a.lse[at] = l != 0.f ? (finite_max(m) + log2f(l)) * kLn2 : -INFINITY;
-      s_place[r] = items > 1 ? (at * a.items + item) * D : row * a.ld_out + static_cast<int64_t>(q_head) * D;
-    }
-    soft_barrier();
+      // ---- the rows' end.  The last O is done, and so are all products and copies:
+      // their shared memory takes the rows, which are then written a row's pieces
+      // by neighbours.
+      wait(pv_done + 8 * (at == 0 ? NP - 1 : at - 1), at == 0 ? turn ^ 1 : turn);
+      tc_fence_after();
+      const int64_t out_at = row * a.Hq + q_head, part = s_seg.part;
+      const bool whole = part < 0;
+      constexpr int P = D + 4;
+      float* so = reinterpret_cast<float*>(smem);
+      const float inv = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
+      if (busy) {
+#pragma unroll
+        for (int c = 0; c < D / 16; ++c) {
+          uint32_t o[16];
+          tmem_ld16(trow + O + 16 * c, o);
+#pragma unroll
+          for (int i = 0; i < 16; i += 4)
+            *reinterpret_cast<float4*>(so + r * P + 16 * c + i) =
+                make_float4(__uint_as_float(o[i]) * inv, __uint_as_float(o[i + 1]) * inv,
+                            __uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
+        }
+      }
+      if (live) {
+        const int64_t slot = shared ? part + r : out_at * a.items + blockIdx.x;
+        if (!whole)
+          a.part_ml[slot] = make_float2(m, l);
+        else if (a.lse)
+          a.lse[out_at] = l != 0.f ? (finite_max(m) + log2f(l)) * kLn2 : -INFINITY;
+        s_place[r] = whole ? row * a.ld_out + static_cast<int64_t>(q_head) * D : slot * D;
+      }
+      soft_barrier();
 #pragma unroll 4
-    for (int e = r; e < rows * (D / 4); e += kSoftThreads) {
-      const int i = e / (D / 4), d = e % (D / 4) * 4;
-      const float4 v = *reinterpret_cast<const float4*>(so + i * P + d);
-      if (items > 1)
-        *reinterpret_cast<float4*>(a.part_o + s_place[i] + d) = v;
-      else
-        *reinterpret_cast<uint2*>(a.out + s_place[i] + d) =
-            make_uint2(pack2<BF16>(v.x, v.y), pack2<BF16>(v.z, v.w));
+      for (int e = r; e < rows * (D / 4); e += kSoftThreads) {
+        const int i = e / (D / 4), d = e % (D / 4) * 4;
+        const float4 v = *reinterpret_cast<const float4*>(so + i * P + d);
+        if (!whole)
+          *reinterpret_cast<float4*>(a.part_o + s_place[i] + d) = v;
+        else
+          *reinterpret_cast<uint2*>(a.out + s_place[i] + d) =
+              make_uint2(pack2<BF16>(v.x, v.y), pack2<BF16>(v.z, v.w));
+      }
+      fence_proxy_async_smem();            // (copies of the next segment follow)
+      base += pages;
     }
-    tc_fence_before();
   }
-  __syncthreads();
-  tc_fence_after();
-  if (warp == kScoreWarp) tmem_dealloc(tmem, kTmemCols);
+  if (warp == kScoreWarp) {
+    __syncwarp();
+    tmem_dealloc(*tmem_slot, kTmemCols);
+  }
 }
 
 // The pool as the kernels' TMA boxes see it: blocks (a page's K or V^T of a KV
