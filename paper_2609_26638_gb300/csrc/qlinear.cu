@@ -1,22 +1,26 @@
 // qlinear.cu -- products of a few rows with 4-bit weights and group scales.
 //
-//   y[m, r] = sum_g s[r, g] * sum_{k in g} (q[r, k] - z[r, g]) x[m, k]
+//   y[m, r] = sum_g s[r, g] * (sum_{k in g} q[r, k] x[m, k] - z[r, g] sum_{k in g} x[m, k])
 //
-// The inner sums are m16n8k16 tensor instructions on the whole numbers q - z,
-// exact in either type, accumulated in fp32; a group's sum is then multiplied by
-// its scale in fp32.  So a weight is never rounded.  16 weight rows are the
-// instruction's rows, 8 tokens its columns.
+// The inner sums are m16n8k16 tensor instructions: 16 weight rows are the
+// instruction's rows, 8 tokens its columns.  Their operand is the whole number q with
+// as little work as possible, for the weights are read once and each takes part
+// in few products.  In fp16 the four bits as they lie are a number, q 2^-24 (or, four places
+// up, q 2^-20, for the tile's upper rows): one mask for two weights.  In bf16 they
+// become the upper mantissa bits of 16 + q.  What that adds, and the zero, come off as
+// one multiple of the tokens' sum over the group, before the group's scale: all of it is
+// fp32, no weight is rounded, and the error is that of fp32 sums of 15 (31 in bf16) s
+// |x| a weight.
 //
 // Weights are laid out once (gs_qweight_pack) in the order in which lanes read
 // them: a block of 16 rows and 64 k is 512 bytes, 16 per lane, of which each 32
-// bits are the lane's operand of one instruction, two 4-bit values per mask.  A
-// dot product does not care in which order its terms come: of each 32 k, lane t
-// of a row's four takes 8 neighbouring ones, so that tokens are read from shared
-// memory 16 bytes at a time.
+// bits are the lane's operand of one instruction.  A dot product does not care in
+// which order its terms come: of each 32 k, lane t of a row's four takes 8
+// neighbouring ones, so that tokens are read from shared memory 16 bytes at a time.
 //
-// A warp takes one tile of 16 rows, a block eight, over one slice of K; the
-// slices of a tile are a cluster, and add up in slice order.  The slices follow
-// from the weights' shape alone, so a row's result does not depend on the others.
+// A warp takes one tile of 16 rows over one slice of K; the slices of a tile are a
+// cluster, and add up in slice order.  The slices follow from the weights' shape
+// alone, so a row's result does not depend on the others.
 #include <algorithm>
 
 #include "attend_common.cuh"
@@ -25,11 +29,9 @@
 namespace gs {
 namespace {
 
-constexpr int kWarps = 8, kThreads = kWarps * 32;
-constexpr int kTileRows = 16, kBlockRows = kWarps * kTileRows;
+constexpr int kTileRows = 16;
 constexpr int kBlockK = 64;                        // k of one packed block
 constexpr int kBlockBytes = kTileRows * kBlockK / 2;
-constexpr int kPartPitch = kBlockRows + 4;         // 2-row stores of 8 rows x 4 lanes on distinct banks
 constexpr int kMostSlices = 8;
 
 struct Layout {
@@ -68,11 +70,20 @@ __device__ __forceinline__ int64_t weight_row(int64_t tile, int r, int N, int ga
   return f < N / 2 ? f + (r >= 8 ? N / 2 : 0) : -1;
 }
 
-// One 16-byte piece per thread.  Value j of the instruction's four operand
-// registers (row g or g + 8, first or second k pair) lies at bits 4 j and 16 + 4 j.
+// Where a word of eight weights has value j (of the instruction's four operand
+// registers: row g or g + 8, first or second k pair), for the pair's first and
+// second k.  fp16: bits 4 j and 16 + 4 j.  bf16: three bits further up, the last
+// value going round the word's end, so that a rotation by 4 j brings it under
+// the mantissa's upper bits.
+__device__ __forceinline__ uint32_t place_pair(int j, uint32_t first, uint32_t second, bool bf16) {
+  const uint32_t v = first | second << 16;
+  return bf16 ? __funnelshift_l(v, v, 4 * j + 3) : v << (4 * j);
+}
+
+// One 16-byte piece per thread.
 __global__ void __launch_bounds__(256)
-pack_weights_kernel(const uint8_t* q, int N, int K, int gated, int64_t pieces, int64_t blocks,
-                    uint4* out) {
+pack_weights_kernel(const uint8_t* q, int N, int K, int gated, bool bf16, int64_t pieces,
+                    int64_t blocks, uint4* out) {
   const int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (e >= pieces) return;
   const int lane = e & 31, g = lane >> 2, t = lane & 3;
@@ -89,7 +100,7 @@ pack_weights_kernel(const uint8_t* q, int N, int K, int gated, int64_t pieces, i
         if (row[h] < 0) continue;
         const uint8_t* p = q + (row[h] * K + k) / 2;
         const uint32_t a = p[0], b = p[1];         // k, k + 1 and k + 2, k + 3, low nibble first
-        v[i] |= ((a & 15) | (a >> 4) << 16) << (4 * h) | ((b & 15) | (b >> 4) << 16) << (4 * h + 8);
+        v[i] |= place_pair(h, a & 15, a >> 4, bf16) | place_pair(2 + h, b & 15, b >> 4, bf16);
       }
   }
   out[e] = make_uint4(v[0], v[1], v[2], v[3]);
@@ -117,82 +128,107 @@ struct LinearArgs {
   void* y;
   int64_t ld_y;
   int64_t tiles, blocks, groups;
-  int M, K, outs, group, slice;        // slice: 64-k blocks of a slice of K
+  int M, K, outs, slice;        // slice: 64-k blocks of a slice of K
   int epilogue;
   int* err;
 };
 
+// A word's four operand registers.  What is multiplied is, for q of the tile's
+// lower and upper rows: fp16: q 2^-24 and q 2^-20; bf16: (16 + q) 2^-4, both.
 template <bool BF16>
-__device__ __forceinline__ uint32_t sub2(uint32_t a, uint32_t b) {
-  uint32_t r;
+__device__ __forceinline__ void operands(uint32_t w, uint32_t (&v)[4]) {
   if constexpr (BF16) {
-    __nv_bfloat162 x, y;
-    memcpy(&x, &a, 4);
-    memcpy(&y, &b, 4);
-    x = __hsub2(x, y);
-    memcpy(&r, &x, 4);
+#pragma unroll
+    for (int j = 0; j < 4; ++j)
+      v[j] = ((j ? __funnelshift_r(w, w, 4 * j) : w) & 0x00780078u) | 0x3F803F80u;
   } else {
-    __half2 x, y;
-    memcpy(&x, &a, 4);
-    memcpy(&y, &b, 4);
-    x = __hsub2(x, y);
-    memcpy(&r, &x, 4);
+    v[0] = w & 0x000F000Fu;
+    v[1] = w & 0x00F000F0u;
+    v[2] = w >> 8 & 0x000F000Fu;
+    v[3] = w >> 8 & 0x00F000F0u;
   }
-  return r;
 }
-
-// 1024 + q in fp16 and 128 + q in bf16 are q in the low bits of a constant.
 template <bool BF16>
-constexpr uint32_t kBias = BF16 ? 0x43004300u : 0x64006400u;
+constexpr float kUnit0 = BF16 ? 0x1p4f : 0x1p24f;  // what a lower row's sum is multiplied by
+template <bool BF16>
+constexpr float kUnit1 = BF16 ? 0x1p4f : 0x1p20f;
+template <bool BF16>
+constexpr float kAdded = BF16 ? 16.f : 0.f;
 
-template <bool BF16, bool SMALL, int NT>
-__global__ void __launch_bounds__(kThreads) qlinear_kernel(const LinearArgs a) {
-  constexpr int MT = 8 * NT;                       // tokens of a block
-  constexpr int KC = NT == 8 ? 512 : 1024;         // k of a chunk of x in shared memory
-  constexpr int XP = KC + 32;                      // pitch: 8 lanes of 2 tokens on distinct banks
-  constexpr int PF = 4;                            // packed blocks fetched ahead
+template <int NT>
+struct Shape {
+  static constexpr int tokens = 8 * NT;            // of a block
+  static constexpr int warps = NT <= 2 ? 4 : 8;
+  static constexpr int threads = 32 * warps, rows = warps * kTileRows;
+  static constexpr int chunk = NT == 1 ? 2048 : NT == 2 ? 1024 : 512;   // k of x in shared memory
+  static constexpr int pitch = chunk + 32;         // 8 lanes of 2 tokens on distinct banks
+  static constexpr int part_pitch = rows + 4;      // 2-row stores of 8 rows x 4 lanes likewise
+  static constexpr int x_bytes = tokens * pitch * 2;
+  template <int G>
+  static constexpr int smem = std::max(x_bytes + chunk / G * tokens * 4, tokens * part_pitch * 4);
+};
+
+// G: the group, 32, 64 or 128.
+template <bool BF16, int G, int NT>
+__global__ void __launch_bounds__(Shape<NT>::threads) qlinear_kernel(const LinearArgs a) {
+  using S = Shape<NT>;
+  constexpr int KC = S::chunk, XP = S::pitch, W = S::warps, PP = S::part_pitch;
+  constexpr int PF = G == 32 || NT == 8 ? 4 : 8;   // packed blocks fetched ahead
+  constexpr int NG = PF * kBlockK / G;             // their groups
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  uint16_t* sx = reinterpret_cast<uint16_t*>(smem_raw);
+  uint16_t* sx = reinterpret_cast<uint16_t*>(smem_raw);              // [token][k]
+  float* sums = reinterpret_cast<float*>(smem_raw + S::x_bytes);     // [group][token]
   float* part = reinterpret_cast<float*>(smem_raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int slices = gridDim.y, m0 = blockIdx.z * MT;
-  const int64_t tile = static_cast<int64_t>(blockIdx.x) * kWarps + warp;
+  const int slices = gridDim.y, m0 = blockIdx.z * S::tokens;
+  const int64_t tile = static_cast<int64_t>(blockIdx.x) * W + warp;
   const int b0 = blockIdx.y * a.slice, b1 = min(static_cast<int64_t>(b0) + a.slice, a.blocks);
   const bool live = tile < a.tiles;
-  const uint4* w = a.w + (tile * a.blocks) * 32 + lane;
-  const uint32_t* sc = a.scale + tile * a.groups * 8 + g;
-  const uint16_t* zr = a.zero ? a.zero + tile * a.groups * 8 + g : nullptr;
-  constexpr int NS = SMALL ? 2 : 1;                // scales of a block
+  const uint4* w = a.w + (live ? tile : 0) * a.blocks * 32 + lane;
+  const uint32_t* sc = a.scale + (live ? tile : 0) * a.groups * 8 + g;
+  const uint16_t* zr = a.zero ? a.zero + (live ? tile : 0) * a.groups * 8 + g : nullptr;
   uint4 wq[PF];
-  uint32_t sq[PF][NS], zq[PF][NS];
-  auto fetch = [&](int b, int at) {
+  uint32_t sq[NG];
+  uint16_t zq[NG];
+  auto fetch = [&](int b, int p) {                 // block b, to place p
     if (!live || b >= b1) return;
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
-                 : "=r"(wq[at].x), "=r"(wq[at].y), "=r"(wq[at].z), "=r"(wq[at].w)
+                 : "=r"(wq[p].x), "=r"(wq[p].y), "=r"(wq[p].z), "=r"(wq[p].w)
                  : "l"(w + static_cast<int64_t>(b) * 32));
+    constexpr int per = kBlockK >= G ? kBlockK / G : 1;
+    if (kBlockK >= G || p % 2 == 0)                // (a group of 128: with its first block)
 #pragma unroll
-    for (int h = 0; h < NS; ++h) {
-      const int64_t grp = SMALL ? min(static_cast<int64_t>(2 * b + h), a.groups - 1)
-                                : static_cast<int64_t>(b) * kBlockK / a.group;
-      sq[at][h] = sc[grp * 8];
-      zq[at][h] = zr ? zr[grp * 8] : 0x0808u;
-    }
+      for (int h = 0; h < per; ++h) {
+        const int64_t at = min(static_cast<int64_t>(b) * kBlockK / G + h, a.groups - 1);
+        sq[p * kBlockK / G + h] = sc[at * 8];
+        if (zr) zq[p * kBlockK / G + h] = zr[at * 8];
+      }
   };
 #pragma unroll
   for (int p = 0; p < PF; ++p) fetch(b0 + p, p);
-  float c[NT][4];
+  float c[NT][4], acc[NT][4];
 #pragma unroll
-  for (int i = 0; i < NT; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
+  for (int i = 0; i < NT; ++i)
+#pragma unroll
+    for (int e = 0; e < 4; ++e) c[i][e] = acc[i][e] = 0.f;
   for (int cb = b0; cb < b1; cb += KC / kBlockK) {
-    // ---- this chunk's tokens
+    // ---- this chunk's tokens, and their sums over each group
     if (cb > b0) __syncthreads();
-    for (int e = threadIdx.x; e < MT * (KC / 8); e += kThreads) {
+    const int kn = min(KC, (b1 - cb) * kBlockK);   // a multiple of 64
+#pragma unroll 4
+    for (int e = threadIdx.x; e < S::tokens * (KC / 8); e += S::threads) {
       const int m = e / (KC / 8), k = e % (KC / 8) * 8;
       const int64_t kg = static_cast<int64_t>(cb) * kBlockK + k;
       uint4 v = make_uint4(0, 0, 0, 0);
-      if (m0 + m < a.M && kg < a.K)
+      if (m0 + m < a.M && k < kn && kg < a.K)
         v = *reinterpret_cast<const uint4*>(a.x + (m0 + m) * a.ld_x + kg);
       *reinterpret_cast<uint4*>(sx + m * XP + k) = v;
+      const float2 f0 = unpack2<BF16>(v.x), f1 = unpack2<BF16>(v.y), f2 = unpack2<BF16>(v.z),
+                   f3 = unpack2<BF16>(v.w);
+      float sum = ((f0.x + f0.y) + (f1.x + f1.y)) + ((f2.x + f2.y) + (f3.x + f3.y));
+#pragma unroll
+      for (int x = 1; x < G / 8; x *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
+      if (k % G == 0) sums[k / G * S::tokens + m] = sum;
     }
     __syncthreads();
     if (!live) continue;
@@ -203,38 +239,50 @@ __global__ void __launch_bounds__(kThreads) qlinear_kernel(const LinearArgs a) {
         const int b = bb + p;
         if (b >= ce) break;
         const uint32_t words[4] = {wq[p].x, wq[p].y, wq[p].z, wq[p].w};
-        uint32_t av[4][4];
-        float2 s[NS];
+        // (the group's numbers are taken before the fetch puts others in their place)
+        constexpr int per = kBlockK >= G ? kBlockK / G : 1;
+        float2 f[per], z[per];
 #pragma unroll
-        for (int h = 0; h < NS; ++h) {
-          s[h] = unpack2<BF16>(sq[p][h]);
-          const uint32_t z0 = zq[p][h] & 15, z1 = zq[p][h] >> 8 & 15;
-          const uint32_t bias0 = kBias<BF16> | z0 | z0 << 16, bias1 = kBias<BF16> | z1 | z1 << 16;
-#pragma unroll
-          for (int i = 0; i < 4 / NS; ++i)
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-              av[h * 2 + i][j] = sub2<BF16>((words[h * 2 + i] >> (4 * j) & 0x000F000Fu) | kBias<BF16>,
-                                            j & 1 ? bias1 : bias0);
+        for (int h = 0; h < per; ++h) {
+          const int at = p * kBlockK / G + h;
+          f[h] = unpack2<BF16>(sq[at]);
+          f[h].x *= kUnit0<BF16>;
+          f[h].y *= kUnit1<BF16>;
+          const uint32_t zz = zr ? zq[at] : 0x0808u;
+          z[h].x = -(kAdded<BF16> + static_cast<float>(zz & 15)) / kUnit0<BF16>;
+          z[h].y = -(kAdded<BF16> + static_cast<float>(zz >> 8 & 15)) / kUnit1<BF16>;
         }
-        fetch(b + PF, p);
+        // (a group of two blocks: its numbers lie at the first one's place, which is
+        // filled again only after the second)
+        const bool ends = G <= kBlockK || p % 2 == 1 || b + 1 >= b1;
+        if (G <= kBlockK) {
+          fetch(b + PF, p);
+        } else {
+          if (p % 2 == 1) fetch(b + PF - 1, p - 1), fetch(b + PF, p);
+        }
         const uint16_t* xr = sx + (b - cb) * kBlockK + 8 * t;
 #pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          float acc[4] = {0.f, 0.f, 0.f, 0.f};
+        for (int h = 0; h < 2; ++h) {
+          uint32_t v[2][4];
+          operands<BF16>(words[2 * h], v[0]);
+          operands<BF16>(words[2 * h + 1], v[1]);
 #pragma unroll
-          for (int h = 0; h < 2; ++h) {
-            const uint4 v = *reinterpret_cast<const uint4*>(xr + (8 * i + g) * XP + 32 * h);
-            mma16816<BF16>(acc, av[2 * h][0], av[2 * h][1], av[2 * h][2], av[2 * h][3], v.x, v.y);
-            mma16816<BF16>(acc, av[2 * h + 1][0], av[2 * h + 1][1], av[2 * h + 1][2],
-                           av[2 * h + 1][3], v.z, v.w);
-            if (SMALL || h == 1) {
-              const float2 f = s[SMALL ? h : 0];
-              c[i][0] = fmaf(f.x, acc[0], c[i][0]);
-              c[i][1] = fmaf(f.x, acc[1], c[i][1]);
-              c[i][2] = fmaf(f.y, acc[2], c[i][2]);
-              c[i][3] = fmaf(f.y, acc[3], c[i][3]);
-              acc[0] = acc[1] = acc[2] = acc[3] = 0.f;
+          for (int i = 0; i < NT; ++i) {
+            const uint4 x = *reinterpret_cast<const uint4*>(xr + (8 * i + g) * XP + 32 * h);
+            mma16816<BF16>(acc[i], v[0][0], v[0][1], v[0][2], v[0][3], x.x, x.y);
+            mma16816<BF16>(acc[i], v[1][0], v[1][1], v[1][2], v[1][3], x.z, x.w);
+          }
+          if (G == 32 || (h == 1 && ends)) {
+            const float2 fs = f[G == 32 ? h : 0], zs = z[G == 32 ? h : 0];
+            const float* su = sums + ((b - cb) * kBlockK + 32 * h) / G * S::tokens + 2 * t;
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+              const float2 u = *reinterpret_cast<const float2*>(su + 8 * i);
+              c[i][0] = fmaf(fs.x, fmaf(zs.x, u.x, acc[i][0]), c[i][0]);
+              c[i][1] = fmaf(fs.x, fmaf(zs.x, u.y, acc[i][1]), c[i][1]);
+              c[i][2] = fmaf(fs.y, fmaf(zs.y, u.x, acc[i][2]), c[i][2]);
+              c[i][3] = fmaf(fs.y, fmaf(zs.y, u.y, acc[i][3]), c[i][3]);
+              acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
             }
           }
         }
@@ -245,39 +293,37 @@ __global__ void __launch_bounds__(kThreads) qlinear_kernel(const LinearArgs a) {
   __syncthreads();
 #pragma unroll
   for (int i = 0; i < NT; ++i) {
-    float* p = part + (8 * i + 2 * t) * kPartPitch + warp * kTileRows + g;
+    float* p = part + (8 * i + 2 * t) * PP + warp * kTileRows + g;
     p[0] = c[i][0];
-    p[kPartPitch] = c[i][1];
+    p[PP] = c[i][1];
     p[8] = c[i][2];
-    p[kPartPitch + 8] = c[i][3];
+    p[PP + 8] = c[i][3];
   }
   __syncwarp();
   if (slices > 1)
     cluster_sync_all();
   else
     __syncthreads();
-  const int tokens = min(MT, a.M - m0), rank = blockIdx.y;
+  const int tokens = min(S::tokens, a.M - m0), rank = blockIdx.y;
   const uint32_t part_at = smem_u32(part);
   auto total = [&](int m, int r) {                 // four rows of a token
-    float4 v = *reinterpret_cast<const float4*>(part + m * kPartPitch + r);
-    if (slices > 1) {
-      const uint32_t at = part_at + (m * kPartPitch + r) * 4;
-      float4 u[kMostSlices];
+    if (slices == 1) return *reinterpret_cast<const float4*>(part + m * PP + r);
+    const uint32_t at = part_at + (m * PP + r) * 4;
+    float4 u[kMostSlices];
 #pragma unroll
-      for (int i = 0; i < kMostSlices; ++i)
-        if (i < slices) u[i] = ld_cluster_f32x4(cluster_map(at, i));
-      v = u[0];
+    for (int i = 0; i < kMostSlices; ++i)
+      if (i < slices) u[i] = ld_cluster_f32x4(cluster_map(at, i));
+    float4 v = u[0];
 #pragma unroll
-      for (int i = 1; i < kMostSlices; ++i)
-        if (i < slices) v.x += u[i].x, v.y += u[i].y, v.z += u[i].z, v.w += u[i].w;
-    }
+    for (int i = 1; i < kMostSlices; ++i)
+      if (i < slices) v.x += u[i].x, v.y += u[i].y, v.z += u[i].z, v.w += u[i].w;
     return v;
   };
   const bool gated = a.epilogue == 2;
-  const int quads = gated ? kBlockRows / 8 : kBlockRows / 4;      // fours of outputs of a token
+  const int quads = gated ? S::rows / 8 : S::rows / 4;      // fours of outputs of a token
   const int64_t out0 = static_cast<int64_t>(blockIdx.x) * quads * 4;
   bool range = false;
-  for (int e = rank * kThreads + threadIdx.x; e < tokens * quads; e += slices * kThreads) {
+  for (int e = rank * S::threads + threadIdx.x; e < tokens * quads; e += slices * S::threads) {
     const int m = e / quads, o = e % quads * 4;
     float r[4];
     if (gated) {
@@ -321,36 +367,42 @@ __global__ void __launch_bounds__(kThreads) qlinear_kernel(const LinearArgs a) {
   if (slices > 1) cluster_sync_all();              // the peers have read this block's part
 }
 
-// Slices of K: two blocks per SM where the rows alone are too few, of at least
-// 128 k.  N and K decide, not M.
+// Slices of K, of whole groups and at least 128 k: 16 warps per SM where the rows
+// alone are too few.  N and K decide, not M.
 int slices_of(const Layout& l) {
-  const int64_t wide = (l.tiles + kWarps - 1) / kWarps;
-  int64_t s = (2 * kNumSMs + wide - 1) / wide;
+  int64_t s = 16 * kNumSMs / l.tiles;
   s = std::min<int64_t>(s, (l.blocks + 1) / 2);
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(s, kMostSlices)));
 }
 
-template <bool BF16, bool SMALL, int NT>
-cudaError_t launch_linear(LinearArgs a, int slices, cudaStream_t s) {
+template <bool BF16, int G, int NT>
+cudaError_t launch_linear(const LinearArgs& a, int slices, cudaStream_t s) {
+  using S = Shape<NT>;
   static DeviceOnce once;
-  constexpr int MT = 8 * NT, KC = NT == 8 ? 512 : 1024;
-  constexpr size_t smem = std::max<size_t>(MT * (KC + 32) * 2, MT * kPartPitch * 4);
-  auto kernel = qlinear_kernel<BF16, SMALL, NT>;
+  constexpr size_t smem = S::template smem<G>;
+  auto kernel = qlinear_kernel<BF16, G, NT>;
   cudaError_t e = once.run([&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (e != cudaSuccess) return e;
-  const dim3 grid(static_cast<unsigned>((a.tiles + kWarps - 1) / kWarps), slices,
-                  (a.M + MT - 1) / MT);
-  return launch_ex(kernel, grid, dim3(kThreads), smem, s, false, dim3(1, slices, 1), a);
+  const dim3 grid(static_cast<unsigned>((a.tiles + S::warps - 1) / S::warps), slices,
+                  (a.M + S::tokens - 1) / S::tokens);
+  return launch_ex(kernel, grid, dim3(S::threads), smem, s, false, dim3(1, slices, 1), a);
 }
 
-template <bool BF16, bool SMALL>
+template <bool BF16, int G>
 cudaError_t launch_rows(const LinearArgs& a, int slices, cudaStream_t s) {
-  if (a.M <= 8) return launch_linear<BF16, SMALL, 1>(a, slices, s);
-  if (a.M <= 16) return launch_linear<BF16, SMALL, 2>(a, slices, s);
-  if (a.M <= 32) return launch_linear<BF16, SMALL, 4>(a, slices, s);
-  return launch_linear<BF16, SMALL, 8>(a, slices, s);
+  if (a.M <= 8) return launch_linear<BF16, G, 1>(a, slices, s);
+  if (a.M <= 16) return launch_linear<BF16, G, 2>(a, slices, s);
+  if (a.M <= 32) return launch_linear<BF16, G, 4>(a, slices, s);
+  return launch_linear<BF16, G, 8>(a, slices, s);
+}
+
+template <bool BF16>
+cudaError_t launch_group(const LinearArgs& a, int group, int slices, cudaStream_t s) {
+  if (group == 32) return launch_rows<BF16, 32>(a, slices, s);
+  if (group == 64) return launch_rows<BF16, 64>(a, slices, s);
+  return launch_rows<BF16, 128>(a, slices, s);
 }
 
 }  // namespace
@@ -374,7 +426,7 @@ extern "C" int gs_qweight_pack(const gs_qweight* w, const void* q, const void* s
   const int64_t pieces = l.tiles * l.blocks * 32, total = l.tiles * l.groups * kTileRows;
   if (pieces / 256 >= (1ll << 31) - 1) return GS_ERR_UNSUPPORTED;
   pack_weights_kernel<<<static_cast<unsigned>((pieces + 255) / 256), 256, 0, s>>>(
-      static_cast<const uint8_t*>(q), w->N, w->K, w->gated, pieces, l.blocks,
+      static_cast<const uint8_t*>(q), w->N, w->K, w->gated, w->dtype == GS_BF16, pieces, l.blocks,
       reinterpret_cast<uint4*>(base));
   if (cudaGetLastError() != cudaSuccess) return GS_ERR_CUDA;
   pack_scales_kernel<<<static_cast<unsigned>((total + 255) / 256), 256, 0, s>>>(
@@ -413,16 +465,15 @@ extern "C" int gs_qlinear(const gs_qweight* w, const void* x, int64_t ld_x, void
   a.M = M;
   a.K = w->K;
   a.outs = outs;
-  a.group = w->group;
-  a.slice = static_cast<int>((l.blocks + want - 1) / want);
+  a.slice = static_cast<int>(((l.blocks + want - 1) / want + 1) / 2 * 2);   // whole groups
   a.epilogue = epilogue;
   a.err = err;
   const int slices = static_cast<int>((l.blocks + a.slice - 1) / a.slice);
   cudaStream_t s = static_cast<cudaStream_t>(stream);
   cudaError_t e;
   if (w->dtype == GS_BF16)
-    e = w->group == 32 ? launch_rows<true, true>(a, slices, s) : launch_rows<true, false>(a, slices, s);
+    e = launch_group<true>(a, w->group, slices, s);
   else
-    e = w->group == 32 ? launch_rows<false, true>(a, slices, s) : launch_rows<false, false>(a, slices, s);
+    e = launch_group<false>(a, w->group, slices, s);
   return e == cudaSuccess ? GS_OK : GS_ERR_CUDA;
 }

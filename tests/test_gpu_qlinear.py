@@ -1,12 +1,18 @@
 """gs_qlinear against products in 64 bits.
 
-Tolerances.  q - z is exact and so are its products with x in fp32 (5 and at
-most 11 bits).  With A = sum_k |w_k x_k| of an output, each tensor instruction
-adds 16 products with an error of at most 2^-22 of the sum so far, which is at most
-A: K / 16 of them, and one product with a scale per group, a sum per slice:
-(K / 8 + 32) 2^-23 A.  Then the output's rounding, u |y| with u = 2^-11 (fp16) or
-2^-8 (bf16), or 2^-24 (|y| + |acc|) for fp32.  A gate's error passes through silu
-with a slope of at most 1.1, and its exponential and quotient add 2^-20 of the result."""
+Tolerances.  The kernel adds q x (in bf16 (16 + q) x) and takes the zero's part off
+as a multiple of the sum of x.  With B = sum_k c s |x_k|, c = 15 in fp16 and 31 in
+bf16, every partial sum is at most B.  A tensor instruction adds 16 products with an
+error of at most 2^-22 of the sum so far: K / 16 of them; then come a sum of x, two
+products and two sums per group, a sum per slice: (K / 8 + 32) 2^-23 B.  Then the
+output's rounding, u |y| with u = 2^-11 (fp16) or 2^-8 (bf16), or 2^-24 (|y| + |acc|)
+for fp32.  A gate's error passes through silu with a slope of at most 1.1, and its
+exponential and quotient add 2^-20 of the result.
+
+That bound is for the worst signs.  For random ones the sums' errors are far below the
+output's rounding, which is evenly spread over at most u |y|: over many outputs the
+mean square of the error is at most (u |y|)^2 / 3, of which 0.6 u leaves 4 per cent for
+the rest."""
 import numpy as np
 import pytest
 import torch
@@ -38,6 +44,8 @@ def _weights(gs, dtype, N, K, group, zeros, gated, seed=0, scale=0.05, stream=No
     torch.cuda.synchronize()
     assert (packed[-64:] == 0x7F).all()
     w.held = packed                      # the descriptor names the memory, it does not own it
+    w.sums = 15.0 if dtype == "fp16" else 31.0
+    w.scales = s.double().repeat_interleave(group, 1)
     zz = 8 if z is None else z.double().repeat_interleave(group, 1)
     return w, (q.double() - zz) * s.double().repeat_interleave(group, 1)
 
@@ -60,14 +68,13 @@ def _x(dtype, M, K, seed=1, scale=1.0):
     return (scale * torch.randn(M, K, device=DEV, generator=g)).to(TYPES[dtype])
 
 
-def _bounds(W, x, y_plain=None):
-    K = W.shape[1]
-    return (K / 8 + 32) * 2.0 ** -23 * (x.double().abs() @ W.abs().t())
+def _bounds(w, x):
+    return (w.K / 8 + 32) * 2.0 ** -23 * w.sums * (x.double().abs() @ w.scales.t())
 
 
-def _check(dtype, y, W, x, gated=False):
+def _check(dtype, y, W, x, w, gated=False):
     u = UNIT[dtype]
-    acc, err = x.double() @ W.t(), _bounds(W, x)
+    acc, err = x.double() @ W.t(), _bounds(w, x)
     if gated:
         half = W.shape[0] // 2
         (ga, up), (eg, eu) = (t.split(half, dim=1) for t in (acc, err))
@@ -75,8 +82,10 @@ def _check(dtype, y, W, x, gated=False):
         acc = silu * up
         err = 1.1 * eg * (up.abs() + eu) + silu.abs() * eu + 2.0 ** -20 * acc.abs()
     bound = err + u * (acc.abs() + err) + 2.0 ** -25
-    worst = ((y.double() - acc).abs() / bound).max().item()
-    assert worst <= 1.0, worst
+    off = (y.double() - acc).abs()
+    assert (off / bound).max().item() <= 1.0
+    if acc.numel() >= 1000:
+        assert off.square().mean().sqrt() <= 0.6 * u * acc.square().mean().sqrt()
 
 
 SHAPES = [(1, 32), (7, 32), (16, 64), (40, 96), (128, 128), (129, 160), (1000, 1024), (130, 2080),
@@ -94,7 +103,7 @@ def test_shapes(gs, dtype, group, zeros):
             x = _x(dtype, M, K, seed=M)
             y, err = _run(gs, w, x)
             assert err == 0
-            _check(dtype, y, W, x)
+            _check(dtype, y, W, x, w)
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
@@ -106,7 +115,7 @@ def test_gated(gs, dtype, F, K, group):
         x = _x(dtype, M, K, seed=M)
         y, err = _run(gs, w, x, epilogue=2)
         assert err == 0
-        _check(dtype, y, W, x, gated=True)
+        _check(dtype, y, W, x, w, gated=True)
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
@@ -118,7 +127,7 @@ def test_residual(gs, dtype):
             before = torch.randn(M, N + 3, device=DEV)
             y, err = _run(gs, w, x, epilogue=1, y=before.clone())
             assert err == 0 and torch.equal(y[:, N:], before[:, N:])
-            acc, e = x.double() @ W.t(), _bounds(W, x)
+            acc, e = x.double() @ W.t(), _bounds(w, x)
             want = before[:, :N].double() + acc
             bound = e + 2.0 ** -24 * (want.abs() + acc.abs() + 2 * e) + 2.0 ** -30
             assert ((y[:, :N].double() - want).abs() <= bound).all()
@@ -134,7 +143,7 @@ def test_rows_do_not_depend_on_the_batch(gs, dtype, N, K, gated):
     epi = 2 if gated else 0
     whole, err = _run(gs, w, x, epilogue=epi)
     assert err == 0
-    _check(dtype, whole, W, x, gated)
+    _check(dtype, whole, W, x, w, gated)
     for a, b in ((0, 1), (3, 4), (77, 78), (5, 13), (20, 36), (64, 96), (100, 150), (1, 66)):
         y, _ = _run(gs, w, x[a:b], epilogue=epi)
         assert torch.equal(y, whole[a:b]), (a, b)
@@ -190,7 +199,7 @@ def test_offsets_past_32_bits(gs):
     out = torch.zeros(far + 64, dtype=torch.bfloat16, device=DEV)
     y, err = _run(gs, w, x, y=out.as_strided((2, 48), (far, 1)))
     assert err == 0
-    _check("bf16", y, W, x)
+    _check("bf16", y, W, x, w)
 
 
 def test_captured_and_replayed(gs):
