@@ -35,7 +35,7 @@ constexpr int kBlockBytes = kTileRows * kBlockK / 2;
 constexpr int kMostSlices = 8;
 
 struct Layout {
-  int64_t tiles, blocks, groups;                   // row tiles; 64-k blocks and groups of a row
+  int64_t tiles, blocks, groups;                   // row tiles; 64-k blocks and their groups
   int64_t scale_at, zero_at, total;                // byte offsets
 };
 inline Layout layout_of(const gs_qweight& w) {
@@ -43,7 +43,7 @@ inline Layout layout_of(const gs_qweight& w) {
   const int per = w.gated ? 8 : kTileRows;         // outputs of a tile
   l.tiles = ((w.gated ? w.N / 2 : w.N) + per - 1) / per;
   l.blocks = (w.K + kBlockK - 1) / kBlockK;
-  l.groups = w.K / w.group;
+  l.groups = (l.blocks * kBlockK + w.group - 1) / w.group;
   l.scale_at = l.tiles * l.blocks * kBlockBytes;
   l.zero_at = l.scale_at + l.tiles * l.groups * kTileRows * 2;
   l.total = l.zero_at + (w.zeros ? l.tiles * l.groups * kTileRows : 0);
@@ -109,14 +109,15 @@ pack_weights_kernel(const uint8_t* q, int N, int K, int gated, bool bf16, int64_
 // Scales and zeros as [tile][group][8][2]: rows g and g + 8 side by side.
 __global__ void __launch_bounds__(256)
 pack_scales_kernel(const uint16_t* scale, const uint8_t* zero, int N, int gated, int64_t total,
-                   int64_t groups, uint16_t* scale_out, uint8_t* zero_out) {
+                   int64_t groups, int64_t have, uint16_t* scale_out, uint8_t* zero_out) {
   const int64_t e = static_cast<int64_t>(blockIdx.x) * 256 + threadIdx.x;
   if (e >= total) return;
   const int r = static_cast<int>(e & 15);
   const int64_t group = (e >> 4) % groups, tile = (e >> 4) / groups;
   const int64_t row = weight_row(tile, (r >> 1) + 8 * (r & 1), N, gated);
-  scale_out[e] = row >= 0 ? scale[row * groups + group] : 0;
-  if (zero) zero_out[e] = row >= 0 ? zero[row * groups + group] & 15 : 0;
+  const bool in = row >= 0 && group < have;        // (the last block may be half a block)
+  scale_out[e] = in ? scale[row * have + group] : 0;
+  if (zero) zero_out[e] = in ? zero[row * have + group] & 15 : 0;
 }
 
 struct LinearArgs {
@@ -160,133 +161,171 @@ struct Shape {
   static constexpr int tokens = 8 * NT;            // of a block
   static constexpr int warps = NT <= 2 ? 4 : 8;
   static constexpr int threads = 32 * warps, rows = warps * kTileRows;
-  static constexpr int chunk = NT == 1 ? 2048 : NT == 2 ? 1024 : 512;   // k of x in shared memory
+  static constexpr int chunk = NT == 1 ? 1024 : NT <= 4 ? 512 : 256;   // k of x in shared memory, twice
   static constexpr int pitch = chunk + 32;         // 8 lanes of 2 tokens on distinct banks
   static constexpr int part_pitch = rows + 4;      // 2-row stores of 8 rows x 4 lanes likewise
   static constexpr int x_bytes = tokens * pitch * 2;
   template <int G>
-  static constexpr int smem = std::max(x_bytes + chunk / G * tokens * 4, tokens * part_pitch * 4);
+  static constexpr int smem = std::max(2 * x_bytes + chunk / G * tokens * 4, tokens * part_pitch * 4);
 };
+
+// A group's scales and zeros as the sums want them: c += f (z u + acc) for the tile's
+// lower and upper row, u the tokens' sum.
+template <bool BF16>
+__device__ __forceinline__ void group_factors(uint32_t scale, uint32_t zero, float2& f, float2& z) {
+  f = unpack2<BF16>(scale);
+  f.x *= kUnit0<BF16>;
+  f.y *= kUnit1<BF16>;
+  // a byte as the last one of 2^23 is a number; the products and sums are exact
+  const float z0 = __uint_as_float(__byte_perm(zero, 0x4B000000u, 0x7650)),
+              z1 = __uint_as_float(__byte_perm(zero, 0x4B000000u, 0x7651));
+  z.x = fmaf(z0, -1.f / kUnit0<BF16>, (8388608.f - kAdded<BF16>) / kUnit0<BF16>);
+  z.y = fmaf(z1, -1.f / kUnit1<BF16>, (8388608.f - kAdded<BF16>) / kUnit1<BF16>);
+}
 
 // G: the group, 32, 64 or 128.
 template <bool BF16, int G, int NT>
-__global__ void __launch_bounds__(Shape<NT>::threads) qlinear_kernel(const LinearArgs a) {
+__global__ void __launch_bounds__(Shape<NT>::threads, NT <= 2 ? 4 : 2) qlinear_kernel(const LinearArgs a) {
   using S = Shape<NT>;
   constexpr int KC = S::chunk, XP = S::pitch, W = S::warps, PP = S::part_pitch;
   constexpr int PF = G == 32 || NT == 8 ? 4 : 8;   // packed blocks fetched ahead
   constexpr int NG = PF * kBlockK / G;             // their groups
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  uint16_t* sx = reinterpret_cast<uint16_t*>(smem_raw);              // [token][k]
-  float* sums = reinterpret_cast<float*>(smem_raw + S::x_bytes);     // [group][token]
+  uint16_t* sx = reinterpret_cast<uint16_t*>(smem_raw);                  // [2][token][k]
+  float* sums = reinterpret_cast<float*>(smem_raw + 2 * S::x_bytes);     // [group][token]
   float* part = reinterpret_cast<float*>(smem_raw);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
   const int slices = gridDim.y, m0 = blockIdx.z * S::tokens;
+  const int tokens = min(S::tokens, a.M - m0);     // (the others' columns hold anything)
   const int64_t tile = static_cast<int64_t>(blockIdx.x) * W + warp;
   const int b0 = blockIdx.y * a.slice, b1 = min(static_cast<int64_t>(b0) + a.slice, a.blocks);
   const bool live = tile < a.tiles;
-  const uint4* w = a.w + (live ? tile : 0) * a.blocks * 32 + lane;
-  const uint32_t* sc = a.scale + (live ? tile : 0) * a.groups * 8 + g;
-  const uint16_t* zr = a.zero ? a.zero + (live ? tile : 0) * a.groups * 8 + g : nullptr;
+  const int64_t of = live ? tile : 0;
+  // this lane's place in the block after the one it works on, and its groups' there
+  const uint4* w = a.w + (of * a.blocks + b0) * 32 + lane;
+  const uint32_t* sc = a.scale + (of * a.groups + static_cast<int64_t>(b0) * kBlockK / G) * 8 + g;
+  const uint16_t* zr = a.zero ? a.zero + (sc - a.scale) : nullptr;
   uint4 wq[PF];
   uint32_t sq[NG];
   uint16_t zq[NG];
-  auto fetch = [&](int b, int p) {                 // block b, to place p
-    if (!live || b >= b1) return;
+  auto fetch = [&](int at, int p) {                // the block `at` blocks on, to place p
     asm volatile("ld.global.nc.L1::no_allocate.v4.u32 {%0,%1,%2,%3}, [%4];"
                  : "=r"(wq[p].x), "=r"(wq[p].y), "=r"(wq[p].z), "=r"(wq[p].w)
-                 : "l"(w + static_cast<int64_t>(b) * 32));
-    constexpr int per = kBlockK >= G ? kBlockK / G : 1;
+                 : "l"(w + at * 32));
     if (kBlockK >= G || p % 2 == 0)                // (a group of 128: with its first block)
 #pragma unroll
-      for (int h = 0; h < per; ++h) {
-        const int64_t at = min(static_cast<int64_t>(b) * kBlockK / G + h, a.groups - 1);
-        sq[p * kBlockK / G + h] = sc[at * 8];
-        if (zr) zq[p * kBlockK / G + h] = zr[at * 8];
+      for (int h = 0; h < (kBlockK >= G ? kBlockK / G : 1); ++h) {
+        sq[p * kBlockK / G + h] = sc[(at * kBlockK / G + h) * 8];
+        zq[p * kBlockK / G + h] = zr ? zr[(at * kBlockK / G + h) * 8] : 0x0808;
       }
   };
+  auto copy = [&](int cb, int to) {                // a chunk's tokens
+    const int kn = min(KC, (b1 - cb) * kBlockK);   // a multiple of 64
+    const int64_t k0 = static_cast<int64_t>(cb) * kBlockK;
+    for (int e = threadIdx.x; e < tokens * (KC / 8); e += S::threads) {
+      const int m = e / (KC / 8), k = e % (KC / 8) * 8;
+      if (k >= kn) continue;
+      const bool in = k0 + k < a.K;                // (else zeros)
+      asm volatile("cp.async.ca.shared.global [%0], [%1], 16, %2;" ::"r"(
+                       smem_u32(sx + to * (S::x_bytes / 2) + m * XP + k)),
+                   "l"(a.x + (m0 + m) * a.ld_x + (in ? k0 + k : 0)), "r"(in ? 16 : 0)
+                   : "memory");
+    }
+  };
+  copy(b0, 0);
 #pragma unroll
-  for (int p = 0; p < PF; ++p) fetch(b0 + p, p);
+  for (int p = 0; p < PF; ++p)
+    if (live && b0 + p < b1) fetch(p, p);
   float c[NT][4], acc[NT][4];
 #pragma unroll
   for (int i = 0; i < NT; ++i)
 #pragma unroll
     for (int e = 0; e < 4; ++e) c[i][e] = acc[i][e] = 0.f;
-  for (int cb = b0; cb < b1; cb += KC / kBlockK) {
-    // ---- this chunk's tokens, and their sums over each group
-    if (cb > b0) __syncthreads();
-    const int kn = min(KC, (b1 - cb) * kBlockK);   // a multiple of 64
-#pragma unroll 4
-    for (int e = threadIdx.x; e < S::tokens * (KC / 8); e += S::threads) {
-      const int m = e / (KC / 8), k = e % (KC / 8) * 8;
-      const int64_t kg = static_cast<int64_t>(cb) * kBlockK + k;
-      uint4 v = make_uint4(0, 0, 0, 0);
-      if (m0 + m < a.M && k < kn && kg < a.K)
-        v = *reinterpret_cast<const uint4*>(a.x + (m0 + m) * a.ld_x + kg);
-      *reinterpret_cast<uint4*>(sx + m * XP + k) = v;
-      const float2 f0 = unpack2<BF16>(v.x), f1 = unpack2<BF16>(v.y), f2 = unpack2<BF16>(v.z),
-                   f3 = unpack2<BF16>(v.w);
-      float sum = ((f0.x + f0.y) + (f1.x + f1.y)) + ((f2.x + f2.y) + (f3.x + f3.y));
+  int buf = 0;
+  for (int cb = b0; cb < b1; cb += KC / kBlockK, buf ^= 1) {
+    asm volatile("cp.async.wait_all;" ::: "memory");
+    __syncthreads();                               // the chunk is there, the last one done with
+    if (cb + KC / kBlockK < b1) copy(cb + KC / kBlockK, buf ^ 1);
+    const uint16_t* x0 = sx + buf * (S::x_bytes / 2) + g * XP + 8 * t;
+    const int ce = min(cb + KC / kBlockK, b1);
+    // ---- the tokens' sums over each group: a product with ones, shared by the warps
+    constexpr uint32_t one = BF16 ? 0x3F803F80u : 0x3C003C00u;
+    const int jobs = ((ce - cb) * kBlockK + G - 1) / G * NT;
+    for (int e = warp; e < jobs; e += W) {
+      const int i = e % NT, grp = e / NT;
+      float u[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int x = 1; x < G / 8; x *= 2) sum += __shfl_xor_sync(0xFFFFFFFFu, sum, x);
-      if (k % G == 0) sums[k / G * S::tokens + m] = sum;
+      for (int h = 0; h < G / 32; ++h) {
+        const uint4 v = *reinterpret_cast<const uint4*>(x0 + 8 * i * XP + grp * G + 32 * h);
+        mma16816<BF16>(u, one, one, one, one, v.x, v.y);
+        mma16816<BF16>(u, one, one, one, one, v.z, v.w);
+      }
+      if (g == 0)
+        *reinterpret_cast<float2*>(sums + grp * S::tokens + 8 * i + 2 * t) = make_float2(u[0], u[1]);
     }
     __syncthreads();
     if (!live) continue;
-    const int ce = min(cb + KC / kBlockK, b1);
-    for (int bb = cb; bb < ce; bb += PF) {
+    // one block: its products, and at a group's end its factors
+    auto work = [&](int b, int p, bool ahead) {
+      const uint32_t words[4] = {wq[p].x, wq[p].y, wq[p].z, wq[p].w};
+      const uint16_t* xr = x0 + (b - cb) * kBlockK;
+      const float* su = sums + (b - cb) * kBlockK / G * S::tokens + 2 * t;
 #pragma unroll
-      for (int p = 0; p < PF; ++p) {
-        const int b = bb + p;
-        if (b >= ce) break;
-        const uint32_t words[4] = {wq[p].x, wq[p].y, wq[p].z, wq[p].w};
-        // (the group's numbers are taken before the fetch puts others in their place)
-        constexpr int per = kBlockK >= G ? kBlockK / G : 1;
-        float2 f[per], z[per];
+      for (int h = 0; h < 2; ++h) {
+        uint32_t v[2][4];
+        operands<BF16>(words[2 * h], v[0]);
+        operands<BF16>(words[2 * h + 1], v[1]);
 #pragma unroll
-        for (int h = 0; h < per; ++h) {
-          const int at = p * kBlockK / G + h;
-          f[h] = unpack2<BF16>(sq[at]);
-          f[h].x *= kUnit0<BF16>;
-          f[h].y *= kUnit1<BF16>;
-          const uint32_t zz = zr ? zq[at] : 0x0808u;
-          z[h].x = -(kAdded<BF16> + static_cast<float>(zz & 15)) / kUnit0<BF16>;
-          z[h].y = -(kAdded<BF16> + static_cast<float>(zz >> 8 & 15)) / kUnit1<BF16>;
+        for (int i = 0; i < NT; ++i) {
+          const uint4 x = *reinterpret_cast<const uint4*>(xr + 8 * i * XP + 32 * h);
+          mma16816<BF16>(acc[i], v[0][0], v[0][1], v[0][2], v[0][3], x.x, x.y);
+          mma16816<BF16>(acc[i], v[1][0], v[1][1], v[1][2], v[1][3], x.z, x.w);
         }
-        // (a group of two blocks: its numbers lie at the first one's place, which is
-        // filled again only after the second)
-        const bool ends = G <= kBlockK || p % 2 == 1 || b + 1 >= b1;
-        if (G <= kBlockK) {
-          fetch(b + PF, p);
-        } else {
-          if (p % 2 == 1) fetch(b + PF - 1, p - 1), fetch(b + PF, p);
-        }
-        const uint16_t* xr = sx + (b - cb) * kBlockK + 8 * t;
-#pragma unroll
-        for (int h = 0; h < 2; ++h) {
-          uint32_t v[2][4];
-          operands<BF16>(words[2 * h], v[0]);
-          operands<BF16>(words[2 * h + 1], v[1]);
+        if (G == 32 || (h == 1 && (G == 64 || p % 2 == 1))) {
+          const int at = p * kBlockK / G + (G == 32 ? h : 0);
+          float2 f, z;
+          group_factors<BF16>(sq[at], zq[at], f, z);
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
-            const uint4 x = *reinterpret_cast<const uint4*>(xr + (8 * i + g) * XP + 32 * h);
-            mma16816<BF16>(acc[i], v[0][0], v[0][1], v[0][2], v[0][3], x.x, x.y);
-            mma16816<BF16>(acc[i], v[1][0], v[1][1], v[1][2], v[1][3], x.z, x.w);
-          }
-          if (G == 32 || (h == 1 && ends)) {
-            const float2 fs = f[G == 32 ? h : 0], zs = z[G == 32 ? h : 0];
-            const float* su = sums + ((b - cb) * kBlockK + 32 * h) / G * S::tokens + 2 * t;
-#pragma unroll
-            for (int i = 0; i < NT; ++i) {
-              const float2 u = *reinterpret_cast<const float2*>(su + 8 * i);
-              c[i][0] = fmaf(fs.x, fmaf(zs.x, u.x, acc[i][0]), c[i][0]);
-              c[i][1] = fmaf(fs.x, fmaf(zs.x, u.y, acc[i][1]), c[i][1]);
-              c[i][2] = fmaf(fs.y, fmaf(zs.y, u.x, acc[i][2]), c[i][2]);
-              c[i][3] = fmaf(fs.y, fmaf(zs.y, u.y, acc[i][3]), c[i][3]);
-              acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
-            }
+            const float2 u = *reinterpret_cast<const float2*>(su + (G == 32 ? h * S::tokens : 0) + 8 * i);
+            c[i][0] = fmaf(f.x, fmaf(z.x, u.x, acc[i][0]), c[i][0]);
+            c[i][1] = fmaf(f.x, fmaf(z.x, u.y, acc[i][1]), c[i][1]);
+            c[i][2] = fmaf(f.y, fmaf(z.y, u.x, acc[i][2]), c[i][2]);
+            c[i][3] = fmaf(f.y, fmaf(z.y, u.y, acc[i][3]), c[i][3]);
+            acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
           }
         }
       }
+      if (!ahead) return;
+      // (a group of two blocks keeps its numbers until its second one is done)
+      if (G <= kBlockK) {
+        fetch(PF + p, p);
+      } else if (p % 2 == 1) {
+        fetch(PF + p - 1, p - 1);
+        fetch(PF + p, p);
+      }
+    };
+    int b = cb;
+    for (; b + PF <= ce && b + 2 * PF <= b1; b += PF) {      // with PF more blocks to fetch
+#pragma unroll
+      for (int p = 0; p < PF; ++p) work(b + p, p, true);
+      w += PF * 32;
+      sc += NG * 8;
+      if (zr) zr += NG * 8;
+    }
+    for (; b < ce; b += PF) {
+#pragma unroll
+      for (int p = 0; p < PF; ++p) {
+        if (b + p >= ce) break;
+        work(b + p, p, false);
+      }
+      // the next ones, as many as there are
+#pragma unroll
+      for (int p = 0; p < PF; ++p)
+        if (b + PF + p < b1) fetch(PF + p, p);
+      w += PF * 32;
+      sc += NG * 8;
+      if (zr) zr += NG * 8;
     }
   }
   // ---- the block's rows as [token][row], then the slices are added in order
@@ -304,7 +343,7 @@ __global__ void __launch_bounds__(Shape<NT>::threads) qlinear_kernel(const Linea
     cluster_sync_all();
   else
     __syncthreads();
-  const int tokens = min(S::tokens, a.M - m0), rank = blockIdx.y;
+  const int rank = blockIdx.y;
   const uint32_t part_at = smem_u32(part);
   auto total = [&](int m, int r) {                 // four rows of a token
     if (slices == 1) return *reinterpret_cast<const float4*>(part + m * PP + r);
@@ -431,7 +470,7 @@ extern "C" int gs_qweight_pack(const gs_qweight* w, const void* q, const void* s
   if (cudaGetLastError() != cudaSuccess) return GS_ERR_CUDA;
   pack_scales_kernel<<<static_cast<unsigned>((total + 255) / 256), 256, 0, s>>>(
       static_cast<const uint16_t*>(scale), static_cast<const uint8_t*>(zero), w->N, w->gated, total,
-      l.groups, reinterpret_cast<uint16_t*>(base + l.scale_at), base + l.zero_at);
+      l.groups, w->K / w->group, reinterpret_cast<uint16_t*>(base + l.scale_at), base + l.zero_at);
   return cudaGetLastError() == cudaSuccess ? GS_OK : GS_ERR_CUDA;
 }
 
