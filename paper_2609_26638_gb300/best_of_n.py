@@ -6,7 +6,8 @@ from the library's operators: projections by ``gs_linear``, heads into the cache
 by ``gs_rope_append``, one-token attention by ``gs_decode_attention``, tokens by
 ``gs_sample``.  The prompt is run once; its pages are then shared by all
 continuations (``PagePool.fork``), each of which copies only the page that it
-goes on writing.
+goes on writing.  Matrices may be 4-bit (``qweight.QWeight``, by ``gs_qlinear``), and
+``feed_trees`` runs the nodes of drafted trees (``tree_decode.py`` decodes with them).
 
     python -m paper_2609_26638_gb300.best_of_n --n 8 --new 32
 """
@@ -20,7 +21,9 @@ import torch
 
 from . import gs
 from .cache import PAGE_TOKENS, PagePool
+from .qweight import QWeight
 
+MAX_NODES = 64               # nodes of a drafted tree: bits of a mask
 EPS = 1e-6
 
 
@@ -63,8 +66,8 @@ def random_weights(shape: Shape, seed: int = 0, device: str = "cuda:0") -> Dict[
 
 
 def check_weights(shape: Shape, weights: Dict[str, object], device) -> None:
-    """Refuses weights that are not what ``random_weights`` makes for this shape:
-    the kernels read them through pointers."""
+    """Refuses weights that are not what ``random_weights`` makes for this shape, or
+    4-bit matrices of the same sizes: the kernels read them through pointers."""
     s = shape
     q, f, d = s.n_heads * s.head_dim, s.d_ffn, s.d_model
     layer = dict(norm1=(d,), qkv=(s.qkv_dim, d), q_gain=(s.head_dim,), k_gain=(s.head_dim,), o=(d, q),
@@ -76,6 +79,12 @@ def check_weights(shape: Shape, weights: Dict[str, object], device) -> None:
     for held, shapes in want + [(w, layer) for w in layers]:
         for name, size in shapes.items():
             t = held.get(name)
+            if isinstance(t, QWeight) and len(size) == 2 and name != "embed":
+                if (t.shape != size or t.dtype != torch.float16 or t.device != device
+                        or t.gated != (name == "gate_up")):
+                    raise gs.GsError(gs.GS_ERR_INVALID_ARG,
+                                     f"{name}: a 4-bit matrix {list(size)} with fp16 scales on {device} needed")
+                continue
             if (not isinstance(t, torch.Tensor) or t.shape != size or not t.is_contiguous()
                     or t.dtype != (torch.float16 if len(size) == 2 else torch.bfloat16)
                     or t.device != device or t.data_ptr() % 16):
@@ -105,6 +114,33 @@ def check_runs(runs, max_rows: int) -> int:
     if any(a[0] == b[0] and b[1] < a[2] for a, b in zip(spans, spans[1:])):
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "two runs name one slot")
     return rows
+
+
+def check_trees(trees, max_rows: int, max_seqs: int):
+    """(nodes of the widest tree, masks, depths) of (sequence, first slot, tokens,
+    parents) trees; refuses trees that are empty, too wide, not in order, or of one
+    sequence.  A mask has a bit for each ancestor and for the node itself."""
+    trees = list(trees)
+    if not trees or any(len(t) == 0 for _, _, t, _ in trees):
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "no nodes")
+    nodes = max(len(t) for _, _, t, _ in trees)
+    if nodes > MAX_NODES or nodes * len(trees) > max_rows or len(trees) > max_seqs:
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "more nodes than a tree or the decoder's max_rows has")
+    if len({s for s, _, _, _ in trees}) < len(trees):
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "two trees of one sequence")
+    masks, depths = [], []
+    for _, _, t, parents in trees:
+        if len(parents) != len(t):
+            raise gs.GsError(gs.GS_ERR_INVALID_ARG, "a parent for every node needed")
+        mask, depth = [], []
+        for i, p in enumerate(parents):
+            if i and not 0 <= p < i:
+                raise gs.GsError(gs.GS_ERR_INVALID_ARG, "a node's parent must come before it")
+            mask.append(1 << i | (mask[p] if i else 0))
+            depth.append(depth[p] + 1 if i else 0)
+        masks.append(mask + [0] * (nodes - len(t)))
+        depths.append(depth + [0] * (nodes - len(t)))
+    return nodes, masks, depths
 
 
 class StepDecoder:
@@ -141,6 +177,8 @@ class StepDecoder:
             need = max(gs.gs_decode_attention_scratch_bytes(self.pool.layer(0), r, shape.n_heads, 0)
                        for r in range(1, max_rows + 1))
             self.attn_scratch = torch.zeros(need, dtype=torch.uint8, device=self.device)
+            self.tree_scratch = None           # made by the first tree
+            self.q_err = torch.zeros(1, dtype=torch.int32, device=self.device)
             wide = max(shape.qkv_dim, shape.d_model, 2 * shape.d_ffn, shape.vocab)
             need = max(gs.gs_linear_scratch_bytes(r, wide, 1) for r in range(1, max_rows + 1))
             # a scratch, and so an error word, for each product of a step: a call
@@ -152,6 +190,10 @@ class StepDecoder:
 
     def _linear(self, x, w, y, n_out: int, epilogue: int, at: int) -> None:
         """y = x w^T as the step's ``at``-th product."""
+        if isinstance(w, QWeight):
+            gs.gs_qlinear(w.desc, x.data_ptr(), x.stride(0), y.data_ptr(), y.stride(0), x.shape[0],
+                          epilogue, self.q_err.data_ptr(), self.stream.cuda_stream)
+            return
         scratch = self.gemm_scratch[at]
         gs.gs_linear(x.data_ptr(), w.data_ptr(), y.data_ptr(), x.shape[0], n_out, x.shape[1], epilogue,
                      1, scratch.data_ptr(), scratch.numel(), self.stream.cuda_stream)
@@ -179,8 +221,7 @@ class StepDecoder:
         return logits
 
     def _feed(self, runs, rows):
-        s, st = self.shape, self.stream.cuda_stream
-        dev = self.device
+        s, st, dev = self.shape, self.stream.cuda_stream, self.device
 
         def ids(values):
             return torch.tensor(values, dtype=torch.int32).to(dev)
@@ -188,35 +229,132 @@ class StepDecoder:
         slot = ids([first + i for _, first, t in runs for i in range(len(t))])
         n = slot + 1                       # a token sees itself and what lies before it
         token = torch.cat([torch.as_tensor(t, dtype=torch.int64, device=dev) for _, _, t in runs])
+        width = s.n_heads * s.head_dim
+
+        def attend(cache, qkv, out):
+            gs.gs_decode_attention(cache, qkv.data_ptr(), s.qkv_dim, seq.data_ptr(), n.data_ptr(), rows,
+                                   s.n_heads, s.head_dim ** -0.5, 0, out.data_ptr(), width, 0, 0,
+                                   self.attn_scratch.data_ptr(), self.attn_scratch.numel(), st)
+        last = torch.tensor([len(t) for _, _, t in runs]).cumsum(0).to(dev) - 1
+        return self._layers(token, seq, slot, slot, attend, last)
+
+    def _layers(self, token, seq, slot, pos, attend, last):
+        """fp16 logits of rows ``last`` (None: all) after the tokens' rows have gone
+        through every layer; ``attend`` runs a layer's attention from qkv to out."""
+        s, st, dev, rows = self.shape, self.stream.cuda_stream, self.device, token.shape[0]
         inside = token.clamp(0, s.vocab - 1)
         self.pool.err.logical_or_((inside != token).any())
         h = self.w["embed"][inside].float()
         qkv = torch.empty(rows, s.qkv_dim, dtype=torch.float16, device=dev)
-        out = torch.empty(rows, s.n_heads * s.head_dim, dtype=torch.float16, device=dev)
+        # (rows beyond a tree's nodes are left as they are by its attention)
+        out = torch.zeros(rows, s.n_heads * s.head_dim, dtype=torch.float16, device=dev)
         act = torch.empty(rows, s.d_ffn, dtype=torch.float16, device=dev)
-        width = s.n_heads * s.head_dim
         for i, w in enumerate(self.w["layers"]):
             cache = self.pool.layer(i)
             self._linear(self._norm(h, w["norm1"]), w["qkv"], qkv, s.qkv_dim, gs.EPI_STORE_F16, 4 * i)
             # queries in place: the key and value parts of qkv are read by the same call
             gs.gs_rope_append(cache, self.rope, qkv.data_ptr(), s.qkv_dim, rows, s.n_heads,
                               w["q_gain"].data_ptr(), w["k_gain"].data_ptr(), EPS, seq.data_ptr(),
-                              slot.data_ptr(), slot.data_ptr(), qkv.data_ptr(), s.qkv_dim,
+                              slot.data_ptr(), pos.data_ptr(), qkv.data_ptr(), s.qkv_dim,
                               self.pool.err.data_ptr(), st)
-            gs.gs_decode_attention(cache, qkv.data_ptr(), s.qkv_dim, seq.data_ptr(), n.data_ptr(), rows,
-                                   s.n_heads, s.head_dim ** -0.5, 0, out.data_ptr(), width, 0, 0,
-                                   self.attn_scratch.data_ptr(), self.attn_scratch.numel(), st)
+            attend(cache, qkv, out)
             self._linear(out, w["o"], h, s.d_model, gs.EPI_RESID_F32, 4 * i + 1)
             self._linear(self._norm(h, w["norm2"]), w["gate_up"], act, s.d_ffn, gs.EPI_SWIGLU,
                          4 * i + 2)
             self._linear(act, w["down"], h, s.d_model, gs.EPI_RESID_F32, 4 * i + 3)
-        last = torch.tensor([len(t) for _, _, t in runs]).cumsum(0).to(dev) - 1
-        x = self._norm(h[last], self.w["norm"])
-        logits = torch.empty(len(runs), s.vocab, dtype=torch.float16, device=dev)
+        x = self._norm(h if last is None else h[last], self.w["norm"])
+        logits = torch.empty(x.shape[0], s.vocab, dtype=torch.float16, device=dev)
         self._linear(x, self.w["lm_head"], logits, s.vocab, gs.EPI_STORE_F16, 4 * s.n_layers)
         words = self.gemm_scratch[:, :4].view(torch.int32)
         torch.maximum(self.gemm_err, words.amax(), out=self.gemm_err)
         return logits
+
+    def feed_trees(self, trees) -> torch.Tensor:
+        """fp16 logits [trees, nodes, vocab] after every node of drafted trees.
+
+        trees: (sequence, first slot n, tokens, parents), one for a sequence, each of up
+        to 64 nodes; node 0 is the root, the token that follows the n cached ones, and
+        a parent comes before its children (the root's is not looked at).  Node i lies at
+        slot n + i, at position n + its depth, and sees the cached tokens and its
+        ancestors.  What is kept of a tree is ``keep``'s to say; until then the
+        sequence has n tokens.  Rows of ``logits`` beyond a tree's nodes hold anything."""
+        trees = list(trees)
+        nodes, masks, depths = check_trees(trees, self.max_rows, self.pool.table.rows.shape[0])
+        for _, _, t, _ in trees:
+            check_tokens(t, self.shape.vocab)
+        caller = torch.cuda.current_stream(self.device)
+        self.stream.wait_stream(caller)
+        self.pool.prepare([(s, n, len(t)) for s, n, t, _ in trees])
+        with torch.cuda.stream(self.stream):
+            logits = self._feed_trees(trees, nodes, masks, depths)
+        caller.wait_stream(self.stream)
+        logits.record_stream(caller)
+        return logits
+
+    def _feed_trees(self, trees, nodes, masks, depths):
+        s, st, dev, b = self.shape, self.stream.cuda_stream, self.device, len(trees)
+
+        def ids(values, dtype=torch.int32):
+            return torch.tensor(values, dtype=dtype).to(dev)
+        pad = [[0] * (nodes - len(t)) for _, _, t, _ in trees]
+        token = torch.cat([torch.as_tensor(list(t) + p, dtype=torch.int64) for (_, _, t, _), p in
+                           zip(trees, pad)]).to(dev)
+        seq = ids([q for q, _, _, _ in trees])
+        n, count = ids([first for _, first, _, _ in trees]), ids([len(t) for _, _, t, _ in trees])
+        # a row beyond its tree writes nothing
+        slot = ids([[first + i for i in range(len(t))] + [-1] * len(p)
+                    for (_, first, t, _), p in zip(trees, pad)]).view(-1)
+        pos = ids([[first + d for d in depth] for (_, first, _, _), depth in zip(trees, depths)]).view(-1)
+        mask = ids([[m - (1 << 64) if m >> 63 else m for m in row] for row in masks], torch.int64)
+        width = s.n_heads * s.head_dim
+        need = gs.gs_tree_attention_scratch_bytes(self.pool.layer(0), b, nodes, s.n_heads, 0)
+        if self.tree_scratch is None or self.tree_scratch.numel() < need:
+            word = self.tree_scratch[:4].clone() if self.tree_scratch is not None else None
+            self.tree_scratch = torch.zeros(need, dtype=torch.uint8, device=dev)
+            if word is not None:
+                self.tree_scratch[:4] = word
+
+        def attend(cache, qkv, out):
+            gs.gs_tree_attention(cache, qkv.data_ptr(), s.qkv_dim, seq.data_ptr(), n.data_ptr(),
+                                 count.data_ptr(), mask.data_ptr(), 0, b, nodes, s.n_heads,
+                                 s.head_dim ** -0.5, 0, out.data_ptr(), width, 0, 0,
+                                 self.tree_scratch.data_ptr(), self.tree_scratch.numel(), st)
+        row_seq = seq[:, None].expand(b, nodes).contiguous().view(-1)
+        return self._layers(token, row_seq, slot, pos, attend, None).view(b, nodes, s.vocab)
+
+    def keep(self, trees, choice: torch.Tensor, most: Optional[List[int]] = None, eos: int = -1):
+        """Keep the path of each tree (as given to ``feed_trees``) that its choices name.
+
+        choice: int32 [trees, nodes] on the decoder's device, the token chosen after each node;
+        most: the longest path of each tree.  Returns lists of each tree's new tokens:
+        after them the sequence has n plus as many cached tokens, and the last one is the
+        next root.  (Synchronises.)"""
+        trees = list(trees)
+        nodes, _, _ = check_trees(trees, self.max_rows, self.pool.table.rows.shape[0])
+        b = len(trees)
+        if (choice.dtype != torch.int32 or choice.shape != (b, nodes) or not choice.is_contiguous()
+                or choice.device != self.device or (most is not None and len(most) != b)):
+            raise gs.GsError(gs.GS_ERR_INVALID_ARG, "choices or limits do not fit the trees")
+        self.stream.wait_stream(torch.cuda.current_stream(self.device))
+        choice.record_stream(self.stream)
+        with torch.cuda.stream(self.stream):
+            def ids(values):
+                return torch.tensor(values, dtype=torch.int32).to(self.device)
+            parent = ids([[max(p, 0) for p in up] + [0] * (nodes - len(up)) for _, _, _, up in trees])
+            token = ids([[int(x) for x in t] + [0] * (nodes - len(t)) for _, _, t, _ in trees])
+            seq, n = ids([q for q, _, _, _ in trees]), ids([first for _, first, _, _ in trees])
+            count = ids([len(t) for _, _, t, _ in trees])
+            limit = ids(list(most)) if most is not None else None
+            path, new = torch.empty_like(choice), torch.empty_like(choice)
+            length = torch.empty_like(n)
+            err, st = self.pool.err.data_ptr(), self.stream.cuda_stream
+            gs.gs_tree_accept(parent.data_ptr(), token.data_ptr(), choice.data_ptr(), count.data_ptr(),
+                              limit.data_ptr() if limit is not None else 0, eos, b, nodes, path.data_ptr(),
+                              new.data_ptr(), length.data_ptr(), err, st)
+            gs.gs_tree_commit(self.pool.layer(0), self.shape.n_layers, seq.data_ptr(), n.data_ptr(),
+                              path.data_ptr(), length.data_ptr(), b, nodes, err, st)
+            rows, lengths = new.tolist(), length.tolist()
+        return [row[:m] for row, m in zip(rows, lengths)]
 
     def check(self) -> None:
         """Synchronise and raise if a kernel met an index out of range, or a
@@ -224,14 +362,23 @@ class StepDecoder:
         self.stream.synchronize()
         with torch.cuda.stream(self.stream):
             attn = self.attn_scratch[:4].view(torch.int32)
-            attend, linear = int(attn.item()), int(self.gemm_err.item())
+            attend, linear = int(attn.item()), max(int(self.gemm_err.item()), int(self.q_err.item()))
             attn.zero_()
             self.gemm_err.zero_()
+            self.q_err.zero_()
+            tree = 0
+            if self.tree_scratch is not None:
+                word = self.tree_scratch[:4].view(torch.int32)
+                tree = int(word.item())
+                word.zero_()
         self.pool.check()
         if attend:
             raise gs.GsError(gs.GS_ERR_DEVICE_CHECK, "gs_decode_attention")
+        if tree:
+            raise gs.GsError(gs.GS_ERR_TIMEOUT if tree == 2 else gs.GS_ERR_DEVICE_CHECK, "gs_tree_attention")
         if linear:
-            raise gs.GsError(gs.GS_ERR_TIMEOUT if linear == 2 else gs.GS_ERR_DEVICE_CHECK, "gs_linear")
+            raise gs.GsError(gs.GS_ERR_TIMEOUT if linear == 2 else gs.GS_ERR_DEVICE_CHECK,
+                             "gs_linear or gs_qlinear")
 
 
 LOGIT_TYPES = {torch.float16: gs.GS_F16, torch.bfloat16: gs.GS_BF16, torch.float32: gs.GS_F32}
