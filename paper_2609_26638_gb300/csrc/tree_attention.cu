@@ -424,7 +424,7 @@ __device__ __forceinline__ int block_max(int v) {
 
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kJoinThreads, 4)
-tree_join_kernel(const TreeArgs a, int groups, int64_t rows) {
+tree_join_kernel(const TreeArgs a, int groups, int64_t rows, int team) {
   constexpr int L = D / 4, NG = kJoinThreads / L;
   __shared__ float4 s_acc[NG][L];
   __shared__ float s_l[NG];
@@ -444,15 +444,16 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows) {
       parts = (have.pages + a.split - 1) / a.split;
     } else {       // the blocks that share this tile's pages
       const int64_t total = a.part_all[0], blocks = a.part_all[1];
-      const int r = node * a.G + head % a.G, tiles = (have.count * a.G + kWideRows - 1) / kWideRows;
-      const int64_t u = have.first +
-                        static_cast<int64_t>(head / a.G * tiles + r / kWideRows) * have.pages;
+      const int r = node * a.G + head % a.G, tile = r / kWideRows;
+      const int tiles = (have.count * a.G + kWideRows - 1) / kWideRows;
+      const int64_t u = have.first + static_cast<int64_t>(head / a.G * ((tiles + team - 1) / team) +
+                                                          tile / team) * have.pages;
       const int64_t b0 = ((u + 1) * blocks - 1) / total,
                     b1 = ((u + have.pages) * blocks - 1) / total;
       parts = static_cast<int>(b1 - b0) + 1;
-      first = (2 * b0 + 1) * kWideRows + r % kWideRows;
-      more = -kWideRows;
-      step = 2 * kWideRows;
+      first = ((2 * b0 + 1) * team + tile % team) * kWideRows + r % kWideRows;
+      more = -static_cast<int64_t>(team) * kWideRows;
+      step = 2ll * team * kWideRows;
     }
   }
   auto part_at = [&](int i) { return first + (i > 0 ? more : 0) + i * step; };
@@ -543,6 +544,7 @@ Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window,
 }
 
 constexpr int kWideBlocks = 2 * kNumSMs;
+constexpr int kMostTeam = 8;
 
 template <bool BF16, int D>
 cudaError_t launch_tree(const gs_cache& c, const TreeArgs& a, bool wide, int trees, cudaStream_t s) {
@@ -558,11 +560,13 @@ cudaError_t launch_tree(const gs_cache& c, const TreeArgs& a, bool wide, int tre
   });
   if (e != cudaSuccess) return e;
   const dim3 grid(a.items, a.cache.Hkv * a.tiles, trees);
+  // blocks of a team: as even a division of the tiles as kMostTeam allows
+  const int teams = (a.tiles + kMostTeam - 1) / kMostTeam, team = (a.tiles + teams - 1) / teams;
   if (wide) {
     CUtensorMap k, v;
     if (!pool_maps(c, &k, &v)) return cudaErrorUnknown;
-    e = launch_ex(broad, a.items ? grid : dim3(kWideBlocks), dim3(kWideThreads), wide_smem, s, false,
-                  dim3(1, 1, 1), k, v, a, trees);
+    e = launch_ex(broad, a.items ? grid : dim3(kWideBlocks / team * team), dim3(kWideThreads), wide_smem,
+                  s, false, dim3(1, 1, 1), k, v, a, trees, team);
   } else {
     e = launch_ex(narrow, grid, dim3(kThreads), smem, s, false, dim3(a.cluster ? a.items : 1, 1, 1), a);
   }
@@ -570,12 +574,12 @@ cudaError_t launch_tree(const gs_cache& c, const TreeArgs& a, bool wide, int tre
   // a row's chunks are shared by as many groups as the GPU has room for
   constexpr int NG = kJoinThreads / (D / 4);
   const int64_t rows = static_cast<int64_t>(trees) * a.nodes;
-  const int64_t most = a.items ? a.items : kWideBlocks / (static_cast<int64_t>(trees) * a.cache.Hkv * a.tiles) + 2;
+  const int64_t most = a.items ? a.items : kWideBlocks / (static_cast<int64_t>(trees) * a.cache.Hkv * teams * team) + 2;
   int groups = 1;
   while (groups < NG && groups * 8 < most && rows * a.Hq * groups < kNumSMs * 4 * NG) groups *= 2;
   const int64_t blocks = (rows * a.Hq * groups + NG - 1) / NG;
   return launch_ex(tree_join_kernel<BF16, D>, dim3(static_cast<unsigned>(blocks)), dim3(kJoinThreads),
-                   0, s, true, dim3(1, 1, 1), a, groups, rows);
+                   0, s, true, dim3(1, 1, 1), a, groups, rows, team);
 }
 
 size_t up256(size_t x) { return (x + 255) / 256 * 256; }

@@ -22,7 +22,11 @@
 // blocks share all pages of all trees evenly, in the order of tree, head, tile and
 // page: a block's share is a few segments, each of one tile, and those that are not
 // a whole tile's pages leave their part to the joining kernel.  So no block waits for a
-// longer one, and what a row's table could hold does not matter.
+// longer one, and what a row's table could hold does not matter.  The tiles of one head
+// read the same pages: they go to as many neighbouring blocks (a team), which share the
+// pages as one block would, and so read them at the same time, from L2.  (As clusters that
+// multicast each page the teams were slower, one document of 65,001 tokens and 264 rows
+// 97 us: fewer blocks fit, and each waits for the others at every page.)
 //
 // m moves only when a row's maximum rises by more than 2^8 (O is rescaled then; the result
 // does not depend on m but for rounding).  In fp16 it is set 7 below the
@@ -131,9 +135,11 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
 }
 
 __device__ __forceinline__ void block_barrier() {    // all warps, wherever they are
+  __syncwarp();
   asm volatile("bar.sync 2, 256;" ::: "memory");
 }
 __device__ __forceinline__ void soft_barrier() {     // the softmax warps
+  __syncwarp();
   asm volatile("bar.sync 1, 128;" ::: "memory");
 }
 
@@ -158,40 +164,53 @@ struct Segment {
   int64_t part;                          // its row of parts, -1: the whole tile
 };
 
+// Blocks that take the tiles of one head, this block's place among them.
+struct Team {
+  int size, rank;
+};
+
 // The order of all work, walked by one warp.  Lane l holds tree 32 chunk + l.
 struct Walk {
   int64_t at, end, total;                // this block's pages
   int64_t before;                        // pages of the trees before the chunk
   int64_t work, upto;                    // the lane's tree: its pages, and with those before
+  TreeNums nums;                         // its numbers
   int chunk, blocks;
 };
 // It rests in shared memory between two segments.
 struct WalkRest {
   int64_t at, end, work[32], upto[32];
+  TreeNums nums[32];
   int chunk;
 };
 __device__ __forceinline__ void walk_rest(WalkRest& r, const Walk& w, int lane) {
   r.work[lane] = w.work;
   r.upto[lane] = w.upto;
+  r.nums[lane] = w.nums;
   if (lane == 0) r.at = w.at, r.end = w.end, r.chunk = w.chunk;
   __syncwarp();
 }
 __device__ __forceinline__ void walk_wake(const WalkRest& r, Walk& w, int lane) {
   w.work = r.work[lane];
   w.upto = r.upto[lane];
+  w.nums = r.nums[lane];
   w.at = r.at;
   w.end = r.end;
   w.chunk = r.chunk;
   __syncwarp();
 }
-__device__ __forceinline__ int64_t walk_load(const TreeArgs& a, int trees, int lane, Walk& w, bool tell) {
+__device__ __forceinline__ int64_t walk_load(const TreeArgs& a, int trees, int lane, Team team, Walk& w,
+                                             bool tell) {
   const int tree = w.chunk * 32 + lane;
   w.work = 0;
+  w.nums = {0, 0, 0, 0, false};
+  int pages = 0;
   if (tree < trees) {
-    const TreeNums t = read_tree(a, tree);
-    const Pages p = tree_pages(a, t);
-    w.work = static_cast<int64_t>(p.count) * a.cache.Hkv * tree_tiles(a, t.count);
-    if (tell && t.bad) atomicExch(a.err, kErrBounds);
+    w.nums = read_tree(a, tree);
+    pages = tree_pages(a, w.nums).count;
+    w.work = static_cast<int64_t>(pages) * a.cache.Hkv *
+             ((tree_tiles(a, w.nums.count) + team.size - 1) / team.size);
+    if (tell && w.nums.bad) atomicExch(a.err, kErrBounds);
   }
   w.upto = w.work;
 #pragma unroll
@@ -200,30 +219,28 @@ __device__ __forceinline__ int64_t walk_load(const TreeArgs& a, int trees, int l
     if (lane >= x) w.upto += y;
   }
   const int64_t sum = __shfl_sync(0xFFFFFFFFu, w.upto, 31);
-  if (tell && tree < trees) {
-    const TreeNums t = read_tree(a, tree);
-    a.part_n[tree] = {w.before + w.upto - w.work, tree_pages(a, t).count, t.count};
-  }
   w.upto += w.before;
+  if (tell && tree < trees) a.part_n[tree] = {w.upto - w.work, pages, w.nums.count};
   return sum;
 }
-__device__ __forceinline__ void walk_begin(const TreeArgs& a, int trees, int lane, Walk& w) {
+__device__ __forceinline__ void walk_begin(const TreeArgs& a, int trees, int lane, Team team, Walk& w) {
   const bool tell = blockIdx.x == 0;
   w.before = 0;
   const int chunks = (trees + 31) / 32;
-  for (w.chunk = 0; w.chunk < chunks; ++w.chunk) w.before += walk_load(a, trees, lane, w, tell);
+  for (w.chunk = 0; w.chunk < chunks; ++w.chunk) w.before += walk_load(a, trees, lane, team, w, tell);
   w.total = w.before;
   const int64_t most = max(static_cast<int64_t>(1), w.total / kFewPages);
-  w.blocks = static_cast<int>(min(static_cast<int64_t>(gridDim.x), most));
+  const int64_t mine = blockIdx.x / team.size;       // the team's number
+  w.blocks = static_cast<int>(min(static_cast<int64_t>(gridDim.x / team.size), most));
   if (tell && lane == 0) a.part_all[0] = w.total, a.part_all[1] = w.blocks;
   w.at = w.end = 0;
-  if (static_cast<int>(blockIdx.x) < w.blocks) {
-    w.at = w.total * blockIdx.x / w.blocks;
-    w.end = w.total * (blockIdx.x + 1) / w.blocks;
+  if (mine < w.blocks) {
+    w.at = w.total * mine / w.blocks;
+    w.end = w.total * (mine + 1) / w.blocks;
   }
   w.before = 0;
   w.chunk = 0;
-  if (w.at < w.end) walk_load(a, trees, lane, w, false);
+  if (chunks > 1 && w.at < w.end) walk_load(a, trees, lane, team, w, false);   // (the only one is there)
 }
 // The first cached key that all of a tree's nodes see (one warp).
 __device__ __forceinline__ int last_first_key(const TreeArgs& a, int tree, const TreeNums& t, int lane) {
@@ -233,7 +250,8 @@ __device__ __forceinline__ int last_first_key(const TreeArgs& a, int tree, const
     lo = max(lo, first_key(a.pos[static_cast<int64_t>(tree) * a.nodes + i], t.n, a.window));
   return __reduce_max_sync(0xFFFFFFFFu, lo);
 }
-__device__ __forceinline__ void walk_next(const TreeArgs& a, int trees, int lane, Walk& w, Segment& s) {
+__device__ __forceinline__ void walk_next(const TreeArgs& a, int trees, int lane, Team team, Walk& w,
+                                          Segment& s) {
   if (w.at >= w.end) {
     if (lane == 0) s.rows = 0;
     return;
@@ -242,44 +260,52 @@ __device__ __forceinline__ void walk_next(const TreeArgs& a, int trees, int lane
   while (!(in = __ballot_sync(0xFFFFFFFFu, w.upto > w.at)) && (w.chunk + 1) * 32 < trees) {
     w.before = __shfl_sync(0xFFFFFFFFu, w.upto, 31);
     ++w.chunk;
-    walk_load(a, trees, lane, w, false);
+    walk_load(a, trees, lane, team, w, false);
   }
   const int l = in ? __ffs(in) - 1 : 31;
   const int64_t first = __shfl_sync(0xFFFFFFFFu, w.upto - w.work, l);
   const int tree = w.chunk * 32 + l;
-  const TreeNums t = read_tree(a, tree);
+  const TreeNums t = {__shfl_sync(0xFFFFFFFFu, w.nums.seq, l), __shfl_sync(0xFFFFFFFFu, w.nums.n, l),
+                      __shfl_sync(0xFFFFFFFFu, w.nums.keys, l), __shfl_sync(0xFFFFFFFFu, w.nums.count, l),
+                      false};
   const Pages p = tree_pages(a, t);
   const int tiles = tree_tiles(a, t.count);
   const int lo_most = last_first_key(a, tree, t, lane);
   if (lane == 0) {
-    // (numbers that changed since they were added up end the walk)
     const int64_t in_tree = w.at - first;
+    const int groups = max((tiles + team.size - 1) / team.size, 1);
     const int unit = in && p.count > 0 ? static_cast<int>(in_tree / p.count) : 0;
     const int from = in && p.count > 0 ? static_cast<int>(in_tree % p.count) : 0;
     const int pages = static_cast<int>(min(static_cast<int64_t>(p.count - from), w.end - w.at));
-    s.rows = in && pages > 0 && unit < a.cache.Hkv * tiles
-                 ? min(kWideRows, t.count * a.G - unit % tiles * kWideRows) : 0;
     s.tree = tree;
-    s.head = unit / max(tiles, 1);
-    s.tile = unit % max(tiles, 1);
+    s.head = unit / groups;
+    s.tile = unit % groups * team.size + team.rank;
+    s.rows = in && pages > 0 && unit < a.cache.Hkv * groups
+                 ? (s.tile < tiles ? min(kWideRows, t.count * a.G - s.tile * kWideRows) : -1)
+                 : 0;
     s.n = t.n, s.keys = t.keys, s.lo_most = lo_most;
     s.seq = t.seq;
     s.page = p.first + from;
     s.pages = pages;
-    // a block's first segment may go on with a tile, its last leave one unfinished
+    // a team's first segment may go on with a tile, its last leave one unfinished
+    const int64_t mine = blockIdx.x / team.size;
     s.part = pages == p.count ? -1
-                              : (2ll * blockIdx.x + (from == 0 ? 1 : 0)) * kWideRows;
+                              : ((2 * mine + (from == 0 ? 1 : 0)) * team.size + team.rank) * kWideRows;
   }
   w.at += __shfl_sync(0xFFFFFFFFu, lane == 0 ? max(s.pages, 1) : 0, 0);
 }
 
 // The block's next segment: of its share, or its one item.
-__device__ __forceinline__ void next_segment(const TreeArgs& a, int trees, int lane, int seg,
-                                             WalkRest& rest, Segment& s) {
+__device__ __forceinline__ void next_segment(const TreeArgs& a, int trees, int lane, Team team,
+                                             int seg, WalkRest& rest, Segment& s) {
   if (a.items == 0) {
     Walk walk;
     walk_wake(rest, walk, lane);
-    walk_next(a, trees, lane, walk, s);
+    int rows;
+    do {                                 // (a tree may have fewer tiles than the team blocks)
+      walk_next(a, trees, lane, team, walk, s);
+      rows = __shfl_sync(0xFFFFFFFFu, lane == 0 ? s.rows : 0, 0);
+    } while (rows < 0);
     walk_rest(rest, walk, lane);
     return;
   }
@@ -302,7 +328,7 @@ __device__ __forceinline__ void next_segment(const TreeArgs& a, int trees, int l
 template <bool BF16, int D>
 __global__ void __launch_bounds__(kWideThreads, 2)
 tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constant__ CUtensorMap map_v,
-                 const TreeArgs a, int trees) {
+                 const TreeArgs a, int trees, int team_size) {
   using L = WideSmem<D>;
   constexpr int H = L::H, ST = L::stages, NP = L::places, O = L::o_col;
   extern __shared__ uint8_t smem_raw[];
@@ -320,9 +346,10 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   pdl_trigger();   // the joining kernel may take its place; it waits for this one's end
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const bool shared = a.items == 0;      // an open split
+  const Team team = {team_size, static_cast<int>(blockIdx.x % team_size)};
   if (warp == kFetchKWarp && shared) {
     Walk walk;
-    walk_begin(a, trees, lane, walk);
+    walk_begin(a, trees, lane, team, walk);
     walk_rest(s_walk, walk, lane);
   }
   if (threadIdx.x == 0) {
@@ -356,7 +383,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     for (int seg = 0;; ++seg) {
       tc_fence_before();
       block_barrier();                   // the last segment's numbers and memory are done with
-      if (warp == kFetchKWarp) next_segment(a, trees, lane, seg, s_walk, s_seg);
+      if (warp == kFetchKWarp) next_segment(a, trees, lane, team, seg, s_walk, s_seg);
       block_barrier();
       tc_fence_after();
       const int pages = s_seg.pages, end = base + pages;

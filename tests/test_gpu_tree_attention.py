@@ -154,7 +154,7 @@ NS = [0, 1, 31, 32, 47, 63, 64, 65, 130, 511, 700]
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
 @pytest.mark.parametrize("D", [64, 128])
 @pytest.mark.parametrize("nodes,Hq,Hkv", [(1, 4, 4), (2, 16, 2), (5, 16, 8), (17, 4, 2), (17, 3, 1),
-                                          (33, 8, 1), (63, 5, 1), (64, 4, 4), (64, 16, 2), (9, 40, 1)])
+                                          (33, 8, 1), (63, 5, 1), (64, 4, 4), (64, 16, 2), (9, 40, 1), (64, 12, 1)])
 def test_lengths_nodes_and_groups(gs, dtype, D, nodes, Hq, Hkv):
     c = _case(dtype, NS, nodes, Hq, Hkv, D, seed=nodes + Hq + D)
     out, lse, err = _run(gs, c, all_nodes=True)
@@ -163,7 +163,7 @@ def test_lengths_nodes_and_groups(gs, dtype, D, nodes, Hq, Hkv):
 
 
 @pytest.mark.parametrize("dtype,D", [("fp16", 64), ("bf16", 128)])
-@pytest.mark.parametrize("nodes,Hq,Hkv", [(7, 4, 2), (40, 8, 4), (64, 2, 1)])
+@pytest.mark.parametrize("nodes,Hq,Hkv", [(7, 4, 2), (40, 8, 4), (64, 2, 1), (64, 8, 1), (60, 10, 1)])
 def test_any_mask_and_counts(gs, dtype, D, nodes, Hq, Hkv):
     """Any pattern of bits, nodes that see nothing, trees of fewer nodes, of none."""
     counts = [nodes, 0, 1, nodes // 2, nodes - 1, nodes, nodes, 3, nodes, 0, nodes // 3]
