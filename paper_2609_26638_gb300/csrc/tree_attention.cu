@@ -6,10 +6,15 @@
 //   o_i = sum_j 2^(s'_ij - m_i) v_j / l_i,  l_i = sum_j 2^(s'_ij - m_i)
 //
 // (s' = s log2(e), m the running maximum, 15 less in fp16.)  A query row is one
-// query head of one node; the rows of a KV head, node by node, are cut into tiles
-// of 16.  A block takes one tile and one item of `split` pages; its warps take
+// query head of one node.  Up to 16 rows of a KV head, node by node, are one tile of the
+// narrow kernel below, more are tiles of 128 for the one in tree_wide.cuh (fp16, 16 / 8
+// heads of 64, 32 trees of 1024 to 6144 tokens: 16 rows 50 us here; 32 and 48 rows 77 and
+// 104 us with two and three tiles to a warp here, for want of registers, 62 and 68 there).
+//
+// A narrow block takes one KV head and one item of `split` pages; its warps take
 // the item's half pages in turn, straight from global memory into the operand
-// registers of m16n8k16 instructions, and are joined at the item's end.
+// registers of m16n8k16 instructions, and are joined at the item's end.  Every byte of
+// the cache is read once, and bounds it.
 //
 // Only steps that reach the tree's nodes, or a window's start, look at masks: a row's
 // view of the step's 32 tokens is one word, the cached range or'ed with its
@@ -86,12 +91,11 @@ tree_attention_kernel(const TreeArgs a) {
   extern __shared__ __align__(16) uint8_t smem_raw[];
   Smem<D>& sm = *reinterpret_cast<Smem<D>*>(smem_raw);
   pdl_trigger();   // the joining kernel may take its place; it waits for this one's end
-  const int tree = blockIdx.z, head = blockIdx.y / a.tiles, tile = blockIdx.y % a.tiles;
-  const int item = blockIdx.x;
+  const int tree = blockIdx.z, head = blockIdx.y, item = blockIdx.x;
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, q = lane & 3;
   const Span sp = find_span(a, tree);
   const int items = (sp.pages + a.split - 1) / a.split;
-  const int rows = min(R, sp.count * a.G - tile * R);     // query rows of this tile
+  const int rows = sp.count * a.G;       // query rows, at most R
   if (item == 0 && blockIdx.y == 0 && threadIdx.x == 0)
     a.part_n[tree] = TreePart{0, sp.pages, sp.count};
   if (rows <= 0 || (item >= items && item > 0)) {
@@ -102,8 +106,8 @@ tree_attention_kernel(const TreeArgs a) {
     return;
   }
   const int64_t row0 = static_cast<int64_t>(tree) * a.nodes;   // the tree's first row
-  auto node_of = [&](int r) { return (tile * R + r) / a.G; };
-  auto q_head = [&](int r) { return head * a.G + (tile * R + r) % a.G; };
+  auto node_of = [&](int r) { return r / a.G; };
+  auto q_head = [&](int r) { return head * a.G + r % a.G; };
   auto q_at = [&](int r) {
     return a.q + (row0 + node_of(r)) * a.ld_q + static_cast<int64_t>(q_head(r)) * D;
   };
@@ -183,74 +187,72 @@ tree_attention_kernel(const TreeArgs a) {
     const bool edge = tok0 < sp.lo_most || tok0 + kStep > sp.n;
     uint32_t some = 0u, all = 0xFFFFFFFFu;               // tokens that some row, every row sees
     uint32_t pa[4], pb[4];
-    {
-      // ---- S = Q K^T; column n of S tile i is token 8 (n/2) + 2 i + n%2
-      float s[4][4];
+    // ---- S = Q K^T; column n of S tile i is token 8 (n/2) + 2 i + n%2
+    float s[4][4];
 #pragma unroll
-      for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
+    for (int i = 0; i < 4; ++i) s[i][0] = s[i][1] = s[i][2] = s[i][3] = 0.f;
 #pragma unroll
-      for (int c = 0; c < C; ++c) {
+    for (int c = 0; c < C; ++c) {
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          mma16816<BF16>(s[i], qa[c][0], qb[c][0], qa[c][1], qb[c][1], k[i * C + c].x, k[i * C + c].y);
+      for (int i = 0; i < 4; ++i)
+        mma16816<BF16>(s[i], qa[c][0], qb[c][0], qa[c][1], qb[c][1], k[i * C + c].x, k[i * C + c].y);
 #pragma unroll
-        for (int i = 0; i < 4; ++i)
-          mma16816<BF16>(s[i], qa[c][2], qb[c][2], qa[c][3], qb[c][3], k[i * C + c].z, k[i * C + c].w);
-      }
-      // ---- softmax; this lane's columns 2q, 2q + 1 of tile i are tokens
-      //      tok0 + 8 q + 2 i + {0, 1}
-      if (edge) {
-        const uint32_t v0 = row_view(sm.mask[g], sm.lo[g], sp.n, tok0),
-                       v1 = row_view(sm.mask[g + 8], sm.lo[g + 8], sp.n, tok0);
-        if (g < rows) some |= v0, all &= v0;
-        if (g + 8 < rows) some |= v1, all &= v1;
-        const uint32_t w0 = v0 >> (8 * q), w1 = v1 >> (8 * q);
-#pragma unroll
-        for (int i = 0; i < 4; ++i) {
-          if (!((w0 >> (2 * i)) & 1)) s[i][0] = -INFINITY;
-          if (!((w0 >> (2 * i + 1)) & 1)) s[i][1] = -INFINITY;
-          if (!((w1 >> (2 * i)) & 1)) s[i][2] = -INFINITY;
-          if (!((w1 >> (2 * i + 1)) & 1)) s[i][3] = -INFINITY;
-        }
-      }
-      float x0 = -INFINITY, x1 = -INFINITY;
+      for (int i = 0; i < 4; ++i)
+        mma16816<BF16>(s[i], qa[c][2], qb[c][2], qa[c][3], qb[c][3], k[i * C + c].z, k[i * C + c].w);
+    }
+    // ---- softmax; this lane's columns 2q, 2q + 1 of tile i are tokens
+    //      tok0 + 8 q + 2 i + {0, 1}
+    if (edge) {
+      const uint32_t v0 = row_view(sm.mask[g], sm.lo[g], sp.n, tok0),
+                     v1 = row_view(sm.mask[g + 8], sm.lo[g + 8], sp.n, tok0);
+      if (g < rows) some |= v0, all &= v0;
+      if (g + 8 < rows) some |= v1, all &= v1;
+      const uint32_t w0 = v0 >> (8 * q), w1 = v1 >> (8 * q);
 #pragma unroll
       for (int i = 0; i < 4; ++i) {
-        x0 = fmaxf(x0, fmaxf(s[i][0], s[i][1]));
-        x1 = fmaxf(x1, fmaxf(s[i][2], s[i][3]));
+        if (!((w0 >> (2 * i)) & 1)) s[i][0] = -INFINITY;
+        if (!((w0 >> (2 * i + 1)) & 1)) s[i][1] = -INFINITY;
+        if (!((w1 >> (2 * i)) & 1)) s[i][2] = -INFINITY;
+        if (!((w1 >> (2 * i + 1)) & 1)) s[i][3] = -INFINITY;
       }
-      x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1));
-      x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
-      x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
-      x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
-      const float n0 = fmaxf(m0, held_max<BF16>(x0, a.scale_log2)),
-                  n1 = fmaxf(m1, held_max<BF16>(x1, a.scale_log2));
-      if (__any_sync(0xFFFFFFFFu, n0 != m0 || n1 != m1)) {
-        const float f0 = ex2(m0 - finite_max(n0)), f1 = ex2(m1 - finite_max(n1));
-        l0 *= f0;
-        l1 *= f1;
+    }
+    float x0 = -INFINITY, x1 = -INFINITY;
 #pragma unroll
-        for (int i = 0; i < D / 8; ++i) {
-          o[i][0] *= f0;
-          o[i][1] *= f0;
-          o[i][2] *= f1;
-          o[i][3] *= f1;
-        }
-        m0 = n0;
-        m1 = n1;
-      }
-      const float z0 = finite_max(m0), z1 = finite_max(m1);
+    for (int i = 0; i < 4; ++i) {
+      x0 = fmaxf(x0, fmaxf(s[i][0], s[i][1]));
+      x1 = fmaxf(x1, fmaxf(s[i][2], s[i][3]));
+    }
+    x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 1));
+    x0 = fmaxf(x0, __shfl_xor_sync(0xFFFFFFFFu, x0, 2));
+    x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
+    x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
+    const float n0 = fmaxf(m0, held_max<BF16>(x0, a.scale_log2)),
+                n1 = fmaxf(m1, held_max<BF16>(x1, a.scale_log2));
+    if (__any_sync(0xFFFFFFFFu, n0 != m0 || n1 != m1)) {
+      const float f0 = ex2(m0 - finite_max(n0)), f1 = ex2(m1 - finite_max(n1));
+      l0 *= f0;
+      l1 *= f1;
 #pragma unroll
-      for (int i = 0; i < 4; ++i) {
-        const float e0 = ex2(fmaf(s[i][0], a.scale_log2, -z0)),
-                    e1 = ex2(fmaf(s[i][1], a.scale_log2, -z0)),
-                    e2 = ex2(fmaf(s[i][2], a.scale_log2, -z1)),
-                    e3 = ex2(fmaf(s[i][3], a.scale_log2, -z1));
-        l0 += e0 + e1;
-        l1 += e2 + e3;
-        pa[i] = pack2<BF16>(e0, e1);
-        pb[i] = pack2<BF16>(e2, e3);
+      for (int i = 0; i < D / 8; ++i) {
+        o[i][0] *= f0;
+        o[i][1] *= f0;
+        o[i][2] *= f1;
+        o[i][3] *= f1;
       }
+      m0 = n0;
+      m1 = n1;
+    }
+    const float z0 = finite_max(m0), z1 = finite_max(m1);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+      const float e0 = ex2(fmaf(s[i][0], a.scale_log2, -z0)),
+                  e1 = ex2(fmaf(s[i][1], a.scale_log2, -z0)),
+                  e2 = ex2(fmaf(s[i][2], a.scale_log2, -z1)),
+                  e3 = ex2(fmaf(s[i][3], a.scale_log2, -z1));
+      l0 += e0 + e1;
+      l1 += e2 + e3;
+      pa[i] = pack2<BF16>(e0, e1);
+      pb[i] = pack2<BF16>(e2, e3);
     }
     const uint16_t* v_now = v_at;
     find_step(j + 1);
@@ -296,25 +298,21 @@ tree_attention_kernel(const TreeArgs a) {
               w[e] &= ~sel;
             }
           x[i] = make_uint4(w[0], w[1], w[2], w[3]);
-          {
-            float p[4] = {0.f, 0.f, 0.f, 0.f};
-            mma16816<BF16>(p, pa[0], pb[0], pa[1], pb[1], one[0], one[1]);
-            mma16816<BF16>(p, pa[2], pb[2], pa[3], pb[3], one[2], one[3]);
-            if ((row_view(sm.mask[g], sm.lo[g], sp.n, tok0) >> tok) & 1)
-              o[i0 + i][0] += p[0], o[i0 + i][1] += p[1];
-            if ((row_view(sm.mask[g + 8], sm.lo[g + 8], sp.n, tok0) >> tok) & 1)
-              o[i0 + i][2] += p[2], o[i0 + i][3] += p[3];
-          }
+          float p[4] = {0.f, 0.f, 0.f, 0.f};
+          mma16816<BF16>(p, pa[0], pb[0], pa[1], pb[1], one[0], one[1]);
+          mma16816<BF16>(p, pa[2], pb[2], pa[3], pb[3], one[2], one[3]);
+          if ((row_view(sm.mask[g], sm.lo[g], sp.n, tok0) >> tok) & 1)
+            o[i0 + i][0] += p[0], o[i0 + i][1] += p[1];
+          if ((row_view(sm.mask[g + 8], sm.lo[g + 8], sp.n, tok0) >> tok) & 1)
+            o[i0 + i][2] += p[2], o[i0 + i][3] += p[3];
         }
       }
-      {
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          mma16816<BF16>(o[i0 + i], pa[0], pb[0], pa[1], pb[1], x[i].x, x[i].y);
+      for (int i = 0; i < 8; ++i)
+        mma16816<BF16>(o[i0 + i], pa[0], pb[0], pa[1], pb[1], x[i].x, x[i].y);
 #pragma unroll
-        for (int i = 0; i < 8; ++i)
-          mma16816<BF16>(o[i0 + i], pa[2], pb[2], pa[3], pb[3], x[i].z, x[i].w);
-      }
+      for (int i = 0; i < 8; ++i)
+        mma16816<BF16>(o[i0 + i], pa[2], pb[2], pa[3], pb[3], x[i].z, x[i].w);
     };
     multiply(0, v);
     load_v(j + 1);
@@ -325,54 +323,50 @@ tree_attention_kernel(const TreeArgs a) {
   }
 
   // ---- the warps' parts are joined, in warp order
-  {
-    l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1);
-    l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
-    l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1);
-    l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 2);
-    if (q == 0) {
-      sm.ml[warp][g] = make_float2(m0, l0);
-      sm.ml[warp][g + 8] = make_float2(m1, l1);
-    }
+  l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 1);
+  l0 += __shfl_xor_sync(0xFFFFFFFFu, l0, 2);
+  l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 1);
+  l1 += __shfl_xor_sync(0xFFFFFFFFu, l1, 2);
+  if (q == 0) {
+    sm.ml[warp][g] = make_float2(m0, l0);
+    sm.ml[warp][g + 8] = make_float2(m1, l1);
   }
   const int used = min(kWarps, steps);
-  {
-    if (cnt > 0) {
+  if (cnt > 0) {
 #pragma unroll
-      for (int i = 0; i < D / 8; ++i) {
-        *reinterpret_cast<float2*>(sm.so + (warp * 16 + g) * P + 8 * i + 2 * q) =
-            make_float2(o[i][0], o[i][1]);
-        *reinterpret_cast<float2*>(sm.so + (warp * 16 + g + 8) * P + 8 * i + 2 * q) =
-            make_float2(o[i][2], o[i][3]);
-      }
+    for (int i = 0; i < D / 8; ++i) {
+      *reinterpret_cast<float2*>(sm.so + (warp * 16 + g) * P + 8 * i + 2 * q) =
+          make_float2(o[i][0], o[i][1]);
+      *reinterpret_cast<float2*>(sm.so + (warp * 16 + g + 8) * P + 8 * i + 2 * q) =
+          make_float2(o[i][2], o[i][3]);
     }
-    __syncthreads();
-    for (int e = threadIdx.x; e < rows * (D / 4); e += kThreads) {
-      const int r = e / (D / 4), d = e % (D / 4) * 4;
-      float m = -INFINITY, l = 0.f;
-      float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
-      for (int w = 0; w < used; ++w) m = fmaxf(m, sm.ml[w][r].x);
-      const float z = finite_max(m);
-      for (int w = 0; w < used; ++w) {
-        const float f = ex2(sm.ml[w][r].x - z);
-        const float4 x = *reinterpret_cast<const float4*>(sm.so + (w * 16 + r) * P + d);
-        l = fmaf(f, sm.ml[w][r].y, l);
-        acc.x = fmaf(f, x.x, acc.x);
-        acc.y = fmaf(f, x.y, acc.y);
-        acc.z = fmaf(f, x.z, acc.z);
-        acc.w = fmaf(f, x.w, acc.w);
-      }
-      const int64_t row = row0 + node_of(r);
-      if (items <= 1) {
-        store_row<BF16, D>(a, row, q_head(r), d, m, l, acc);
-      } else if (a.cluster) {
-        *reinterpret_cast<float4*>(sm.item + r * D + d) = acc;
-        if (d == 0) sm.item_ml[r] = make_float2(m, l);
-      } else {
-        const int64_t at = row * a.Hq + q_head(r);
-        *reinterpret_cast<float4*>(a.part_o + (at * a.items + item) * D + d) = acc;
-        if (d == 0) a.part_ml[at * a.items + item] = make_float2(m, l);
-      }
+  }
+  __syncthreads();
+  for (int e = threadIdx.x; e < rows * (D / 4); e += kThreads) {
+    const int r = e / (D / 4), d = e % (D / 4) * 4;
+    float m = -INFINITY, l = 0.f;
+    float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
+    for (int w = 0; w < used; ++w) m = fmaxf(m, sm.ml[w][r].x);
+    const float z = finite_max(m);
+    for (int w = 0; w < used; ++w) {
+      const float f = ex2(sm.ml[w][r].x - z);
+      const float4 x = *reinterpret_cast<const float4*>(sm.so + (w * 16 + r) * P + d);
+      l = fmaf(f, sm.ml[w][r].y, l);
+      acc.x = fmaf(f, x.x, acc.x);
+      acc.y = fmaf(f, x.y, acc.y);
+      acc.z = fmaf(f, x.z, acc.z);
+      acc.w = fmaf(f, x.w, acc.w);
+    }
+    const int64_t row = row0 + node_of(r);
+    if (items <= 1) {
+      store_row<BF16, D>(a, row, q_head(r), d, m, l, acc);
+    } else if (a.cluster) {
+      *reinterpret_cast<float4*>(sm.item + r * D + d) = acc;
+      if (d == 0) sm.item_ml[r] = make_float2(m, l);
+    } else {
+      const int64_t at = row * a.Hq + q_head(r);
+      *reinterpret_cast<float4*>(a.part_o + (at * a.items + item) * D + d) = acc;
+      if (d == 0) a.part_ml[at * a.items + item] = make_float2(m, l);
     }
   }
   if (!a.cluster) return;
@@ -499,23 +493,26 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows, int team) {
   if (sub == 0 && parts > 1) store_row<BF16, D>(a, row, head, 4 * d, m, l, acc);
 }
 
-// Pages of an item when the caller leaves it open: one wave of blocks shares the
-// cache evenly, or eight items that join in a cluster where that is not long; of
-// several trees, which may differ in length, items of at most kMostPages.
+// Pages of an item of the narrow kernel when the caller leaves it open.  One tree: one
+// wave of blocks shares the cache evenly, or eight items that join in a cluster where that is
+// not long.  Several trees, which may differ in length: items of at most 16 pages, so
+// that the tail behind the longest is short, or 32 where the trees' heads alone fill the
+// GPU, as every part of 16 rows is written and read again (fp16, 16 / 8 heads of 64, 8
+// nodes: 64 trees of 8192 tokens 171 us with 33 pages, 184 with 16, 191 with 12; four
+// of 20,000 25 with 16, 30 with 32; 32 of 1024 to 6144 49 with 12 to 24).
 constexpr int64_t wave_of(int head_dim) { return head_dim == 64 ? 320 : 256; }
-constexpr int kMostPages = 12;
+constexpr int kMostPages = 16;
 int auto_split(int pages, int trees, int64_t blocks_per_item, int head_dim) {
   const int64_t wave = wave_of(head_dim) / blocks_per_item;
   int64_t items = wave < 1 ? 1 : wave;
   if (items > kMostCluster && pages <= 8 * kMostCluster) items = kMostCluster;
   int64_t split = (pages + items - 1) / items;
   if (split < 2) split = 2;
-  if (split > kMostPages && trees > 1) split = kMostPages;
+  if (trees > 1) split = std::min<int64_t>(split, wave < 1 ? 2 * kMostPages : kMostPages);
   return static_cast<int>(split < pages ? split : pages);
 }
 
-// Rows of a KV head from which the wide kernel takes over.
-constexpr int kNarrowRows = 16;
+constexpr int kNarrowRows = 16;    // of a KV head; more are the wide kernel's
 
 struct Plan {
   bool wide, shared;             // shared: the wide kernel's blocks share all pages
@@ -525,8 +522,7 @@ Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window,
   Plan p;
   const int G = n_heads / c.n_kv_heads;
   p.wide = nodes * G > kNarrowRows;
-  const int tile_rows = p.wide ? kWideRows : 16;
-  p.tiles = (nodes * G + tile_rows - 1) / tile_rows;
+  p.tiles = p.wide ? (nodes * G + kWideRows - 1) / kWideRows : 1;
   p.shared = p.wide && split_pages == 0 && trees <= kMostShared;
   p.split = p.items = 0;
   if (p.shared) return p;
@@ -535,7 +531,7 @@ Plan plan_tree(const gs_cache& c, int trees, int nodes, int n_heads, int window,
     const int64_t most = (static_cast<int64_t>(window) - 1 + nodes + kPageTokens - 2) / kPageTokens + 1;
     if (most < pages) pages = static_cast<int>(most);
   }
-  const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * c.n_kv_heads * p.tiles;
+  const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * c.n_kv_heads;
   p.split = split_pages > 0 ? std::min(split_pages, c.pt_stride)
             : p.wide        ? pages          // (many trees: a block for each tile)
                             : auto_split(pages, trees, blocks, c.head_dim);
@@ -622,7 +618,7 @@ extern "C" size_t gs_tree_attention_scratch_bytes(const gs_cache* cache, int tre
   // kMostPages, and the rounding.
   size_t items = p.items;
   if (split_pages == 0 && !p.wide) {
-    const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * cache->n_kv_heads * p.tiles;
+    const int64_t blocks = static_cast<int64_t>(trees < 1 ? 1 : trees) * cache->n_kv_heads;
     const size_t wave = static_cast<size_t>(wave_of(cache->head_dim) / blocks),
                  cut = cache->pt_stride / kMostPages, cluster = kMostCluster;
     items = std::max(std::max(wave, cut), cluster) + 2;
@@ -673,7 +669,7 @@ extern "C" int gs_tree_attention(const gs_cache* cache, const void* q, int64_t l
   a.split = p.split;
   a.items = p.items;
   a.cluster = !p.wide && p.items > 1 && p.items <= kMostCluster &&
-              static_cast<int64_t>(p.items) * cache->n_kv_heads * p.tiles * trees <= wave_of(D);
+              static_cast<int64_t>(p.items) * cache->n_kv_heads * trees <= wave_of(D);
   a.scale_log2 = scale * kLog2e;
   a.part_o = reinterpret_cast<float*>(base + sc.o);
   a.part_ml = reinterpret_cast<float2*>(base + sc.ml);
