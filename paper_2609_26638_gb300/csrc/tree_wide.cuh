@@ -134,6 +134,22 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
       : "memory");
 }
 
+// mbar_wait, in as little code as it takes.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* err) {
+  uint64_t start = 0;
+#pragma unroll 1
+  for (uint32_t i = 1; !mbar_try_wait(bar, parity); ++i) {
+    if (i & 255) continue;
+    const uint64_t now = global_timer_ns();
+    if (start == 0) start = now;
+    if (now - start > kWaitLimitNs) {
+      atomicExch(err, kErrTimeout);
+      return false;
+    }
+  }
+  return true;
+}
+
 __device__ __forceinline__ void block_barrier() {    // all warps, wherever they are
   __syncwarp();
   asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -410,7 +426,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           const int block = 2 * a.cache.Hkv * __shfl_sync(0xFFFFFFFFu, ids, i) + which;
           if (lane == 0) {
             const uint32_t bar = full + 8 * (j % ST), dst = ring + j % ST * L::page_bytes;
-            if (j >= ST) ok = mbar_wait(empty + 8 * (j % ST), (j / ST + 1) & 1, a.err);
+            if (j >= ST) ok = wait_for(empty + 8 * (j % ST), (j / ST + 1) & 1, a.err);
             if (ok) {
               mbar_arrive_expect_tx(bar, L::page_bytes);
               if (value) {
@@ -428,15 +444,15 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         // the ring outlives its copies
         if (lane == 0)
           for (int j = max(base, fetched - ST); j < fetched; ++j)
-            mbar_wait(full + 8 * (j % ST), (j / ST) & 1, a.err);
+            wait_for(full + 8 * (j % ST), (j / ST) & 1, a.err);
       } else if (lane == 0 && warp == kScoreWarp) {
         // ---- S, where an earlier page's P was
         const uint64_t qd = umma_desc_sw128(smem_u32(smem));
-        ok = ok && mbar_wait(q_full, seg & 1, a.err);
+        ok = ok && wait_for(q_full, seg & 1, a.err);
         for (int j = base; j < end && ok; ++j) {
           const int st = j % ST;
-          ok = (j < NP || mbar_wait(pv_done + 8 * at, turn ^ 1, a.err)) &&
-               mbar_wait(k_full + 8 * st, (j / ST) & 1, a.err);
+          ok = (j < NP || wait_for(pv_done + 8 * at, turn ^ 1, a.err)) &&
+               wait_for(k_full + 8 * st, (j / ST) & 1, a.err);
           if (!ok) break;
           tc_fence_after();
           const uint64_t kd = umma_desc_sw128(smem_u32(smem + L::k_at + st * L::page_bytes));
@@ -453,8 +469,8 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         // ---- O += P V
         for (int j = base; j < end && ok; ++j) {
           const int st = j % ST;
-          ok = mbar_wait(v_full + 8 * st, (j / ST) & 1, a.err) &&
-               mbar_wait(p_full + 8 * at, turn, a.err);
+          ok = wait_for(v_full + 8 * st, (j / ST) & 1, a.err) &&
+               wait_for(p_full + 8 * at, turn, a.err);
           if (!ok) break;
           tc_fence_after();
           const uint64_t vd = umma_desc_sw128(smem_u32(smem + L::v_at + st * L::page_bytes));
@@ -521,7 +537,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       if (lane == 0) mbar_arrive(q_full);
       // waits are warp-uniform; after a failure the warp stops waiting
       auto wait = [&](uint32_t bar, uint32_t phase) {
-        if (ok) ok = __all_sync(0xFFFFFFFFu, mbar_wait(bar, phase, a.err)) != 0;
+        if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(bar, phase, a.err)) != 0;
         return ok;
       };
       constexpr float kSet = BF16 ? 0.f : 7.f;         // how far below the maximum m is set
