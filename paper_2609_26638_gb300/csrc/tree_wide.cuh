@@ -582,6 +582,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             m = set;
             if (j > 0 && wait(pv_done + 8 * was, was_turn)) {
               tc_fence_after();
+#pragma unroll 1
               for (int c = 0; c < D / 16; ++c) {
                 uint32_t o[16];
                 tmem_ld16(trow + O + 16 * c, o);
@@ -627,6 +628,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           wait(v_full + 8 * st, ((base + j) / ST) & 1);
           soft_barrier();
           // chunk = 8 tokens of a dim
+#pragma unroll 1
           for (int e = r; e < D * 8; e += kSoftThreads) {
             const int chunk = e % 8, dim = e / 8, w = chunk / 4, shift = chunk % 4 * 8;
             uint32_t some = 0u, all = 0xFFFFFFFFu;
@@ -651,10 +653,13 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           if (s_odd[0] | s_odd[1]) {
             if (j > 0) wait(pv_done + 8 * was, was_turn);
             tc_fence_after();
+#pragma unroll 1
             for (int c = 0; c < D / 16; ++c) {
               uint32_t o[16];
               tmem_ld16(trow + O + 16 * c, o);
+#pragma unroll 1
               for (int w = 0; w < 2; ++w)
+#pragma unroll 1
                 for (uint32_t left = s_odd[w] & row_view(mask, lo, n, tok0 + 32 * w); left;
                      left &= left - 1) {
                   const int tok = 32 * w + __ffs(left) - 1;
@@ -671,6 +676,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             }
             tmem_wait_st();
             soft_barrier();
+#pragma unroll 1
             for (int e = r; e < D * 8; e += kSoftThreads) {
               const int chunk = e % 8, dim = e / 8;
               const uint32_t odd = s_odd[chunk / 4] >> (chunk % 4 * 8);
@@ -706,7 +712,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
       float* so = reinterpret_cast<float*>(smem);
       const float inv = !whole ? 1.f : l != 0.f ? 1.f / l : 0.f;
       if (busy) {
-#pragma unroll
+#pragma unroll 1
         for (int c = 0; c < D / 16; ++c) {
           uint32_t o[16];
           tmem_ld16(trow + O + 16 * c, o);
