@@ -348,7 +348,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   using L = WideSmem<D>;
   constexpr int H = L::H, ST = L::stages, NP = L::places, O = L::o_col;
   extern __shared__ uint8_t smem_raw[];
-  __shared__ Segment s_seg;
+  __shared__ Segment s_segs[2];            // this one, the next
   __shared__ WalkRest s_walk;
   __shared__ uint32_t s_some[2][kSoftWarps], s_all[2][kSoftWarps], s_odd[2];
   __shared__ int64_t s_place[kWideRows];   // of each row: its query, then its output or part
@@ -397,11 +397,12 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWorkRegs));
     for (int seg = 0;; ++seg) {
+      // (found while the last one's pages are still at work)
+      if (warp == kFetchKWarp) next_segment(a, trees, lane, team, seg, s_walk, s_segs[seg & 1]);
       tc_fence_before();
-      block_barrier();                   // the last segment's numbers and memory are done with
-      if (warp == kFetchKWarp) next_segment(a, trees, lane, team, seg, s_walk, s_seg);
-      block_barrier();
+      block_barrier();                   // the last segment's memory is done with, this one is known
       tc_fence_after();
+      const Segment& s_seg = s_segs[seg & 1];
       const int pages = s_seg.pages, end = base + pages;
       if (s_seg.rows <= 0) break;
       const uint32_t tmem = *tmem_slot;
@@ -487,11 +488,11 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
     }
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
-    for (;;) {
+    for (int seg = 0;; ++seg) {
       tc_fence_before();
       block_barrier();
-      block_barrier();
       tc_fence_after();
+      const Segment& s_seg = s_segs[seg & 1];
       const uint32_t tmem = *tmem_slot;
       const int rows = s_seg.rows, pages = s_seg.pages;
       if (rows <= 0) break;
