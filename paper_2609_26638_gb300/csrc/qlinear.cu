@@ -21,6 +21,15 @@
 // A warp takes one tile of 16 rows over one slice of K; the slices of a tile are a
 // cluster, and add up in slice order.  The slices follow from the weights' shape
 // alone, so a row's result does not depend on the others.
+//
+// What bounds it: 28,672 x 8192 and one token 28 us, 4.4 TB/s of weights and near one
+// instruction for two weights of a warp's lanes; 8192 x 8192, 11 us for one token, 12 for 8, 15.7
+// for 16, 25 for 32, 43 for 64: from 16 on the issue of products and of the loads of
+// tokens (for 32, the tensor pipes are 35 per cent busy, the issue slots 37); with
+// fewer weights the start of a block: a first weight, the tokens and their sums, 4 us in all
+// (1024 x 1024 and one token 3.3 us).  Two tiles to a warp read the tokens half as often but
+// leave half the warps (28 us for 32); with the weights unpacked to shared memory for
+// 128-row tensor memory products it took 24 to 39, the issue of small products again.
 #include <algorithm>
 
 #include "attend_common.cuh"
@@ -130,6 +139,7 @@ struct LinearArgs {
   int64_t ld_y;
   int64_t tiles, blocks, groups;
   int M, K, outs, slice;        // slice: 64-k blocks of a slice of K
+  int rounds;                   // thread blocks' rows; with ON one takes every gridDim.x-th
   int epilogue;
   int* err;
 };
@@ -156,17 +166,27 @@ constexpr float kUnit1 = BF16 ? 0x1p4f : 0x1p20f;
 template <bool BF16>
 constexpr float kAdded = BF16 ? 16.f : 0.f;
 
-template <int NT>
+// ON: a wave of blocks that keep the tokens in shared memory and go on from tile to tile.
+template <int NT, bool ON>
 struct Shape {
   static constexpr int tokens = 8 * NT;            // of a block
   static constexpr int warps = NT <= 2 ? 4 : 8;
   static constexpr int threads = 32 * warps, rows = warps * kTileRows;
-  static constexpr int chunk = NT == 1 ? 1024 : NT <= 4 ? 512 : 256;   // k of x in shared memory, twice
+  static constexpr int resident = warps == 4 ? 4 : 2;    // blocks of an SM
+  // k of x in shared memory: twice, or all of them
+  static constexpr int chunk = (NT == 1 ? 1024 : NT <= 4 ? 512 : 256) * (ON ? 2 : 1);
   static constexpr int pitch = chunk + 32;         // 8 lanes of 2 tokens on distinct banks
   static constexpr int part_pitch = rows + 4;      // 2-row stores of 8 rows x 4 lanes likewise
-  static constexpr int x_bytes = tokens * pitch * 2;
+  static constexpr int x_bytes = tokens * pitch * 2, part_bytes = tokens * part_pitch * 4;
   template <int G>
-  static constexpr int smem = std::max(2 * x_bytes + chunk / G * tokens * 4, tokens * part_pitch * 4);
+  static constexpr int ahead = G == 32 || NT == 8 ? 4 : 8;          // packed blocks fetched ahead
+  template <int G>
+  static constexpr int sum_bytes = chunk / G * tokens * 4;
+  static constexpr int sum_at = x_bytes * (ON ? 1 : 2);
+  template <int G>
+  static constexpr int part_at = ON ? sum_at + sum_bytes<G> : 0;
+  template <int G>
+  static constexpr int smem = std::max(sum_at + sum_bytes<G>, part_at<G> + part_bytes);
 };
 
 // A group's scales and zeros as the sums want them: c += f (z u + acc) for the tile's
@@ -184,22 +204,22 @@ __device__ __forceinline__ void group_factors(uint32_t scale, uint32_t zero, flo
 }
 
 // G: the group, 32, 64 or 128.
-template <bool BF16, int G, int NT>
-__global__ void __launch_bounds__(Shape<NT>::threads, NT <= 2 ? 4 : 2) qlinear_kernel(const LinearArgs a) {
-  using S = Shape<NT>;
+template <bool BF16, int G, int NT, bool ON>
+__global__ void __launch_bounds__(Shape<NT, ON>::threads, Shape<NT, ON>::resident)
+qlinear_kernel(const LinearArgs a) {
+  using S = Shape<NT, ON>;
   constexpr int KC = S::chunk, XP = S::pitch, W = S::warps, PP = S::part_pitch;
-  constexpr int PF = G == 32 || NT == 8 ? 4 : 8;   // packed blocks fetched ahead
-  constexpr int NG = PF * kBlockK / G;             // their groups
+  constexpr int PF = S::template ahead<G>, NG = PF * kBlockK / G;   // their groups
   extern __shared__ __align__(16) uint8_t smem_raw[];
-  uint16_t* sx = reinterpret_cast<uint16_t*>(smem_raw);                  // [2][token][k]
-  float* sums = reinterpret_cast<float*>(smem_raw + 2 * S::x_bytes);     // [group][token]
-  float* part = reinterpret_cast<float*>(smem_raw);
+  uint16_t* sx = reinterpret_cast<uint16_t*>(smem_raw);                  // [buffer][token][k]
+  float* sums = reinterpret_cast<float*>(smem_raw + S::sum_at);          // [group][token]
+  float* part = reinterpret_cast<float*>(smem_raw + S::template part_at<G>);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31, g = lane >> 2, t = lane & 3;
-  const int slices = gridDim.y, m0 = blockIdx.z * S::tokens;
+  const int slices = ON ? 1 : gridDim.y, m0 = blockIdx.z * S::tokens;
   const int tokens = min(S::tokens, a.M - m0);     // (the others' columns hold anything)
-  const int64_t tile = static_cast<int64_t>(blockIdx.x) * W + warp;
+  int64_t tile = static_cast<int64_t>(blockIdx.x) * W + warp;
   const int b0 = blockIdx.y * a.slice, b1 = min(static_cast<int64_t>(b0) + a.slice, a.blocks);
-  const bool live = tile < a.tiles;
+  bool live = tile < a.tiles;
   const int64_t of = live ? tile : 0;
   // this lane's place in the block after the one it works on, and its groups' there
   const uint4* w = a.w + (of * a.blocks + b0) * 32 + lane;
@@ -242,168 +262,188 @@ __global__ void __launch_bounds__(Shape<NT>::threads, NT <= 2 ? 4 : 2) qlinear_k
 #pragma unroll
     for (int e = 0; e < 4; ++e) c[i][e] = acc[i][e] = 0.f;
   int buf = 0;
-  for (int cb = b0; cb < b1; cb += KC / kBlockK, buf ^= 1) {
-    asm volatile("cp.async.wait_all;" ::: "memory");
-    __syncthreads();                               // the chunk is there, the last one done with
-    if (cb + KC / kBlockK < b1) copy(cb + KC / kBlockK, buf ^ 1);
-    const uint16_t* x0 = sx + buf * (S::x_bytes / 2) + g * XP + 8 * t;
-    const int ce = min(cb + KC / kBlockK, b1);
-    // ---- the tokens' sums over each group: a product with ones, shared by the warps
-    constexpr uint32_t one = BF16 ? 0x3F803F80u : 0x3C003C00u;
-    const int jobs = ((ce - cb) * kBlockK + G - 1) / G * NT;
-    for (int e = warp; e < jobs; e += W) {
-      const int i = e % NT, grp = e / NT;
-      float u[4] = {0.f, 0.f, 0.f, 0.f};
-#pragma unroll
-      for (int h = 0; h < G / 32; ++h) {
-        const uint4 v = *reinterpret_cast<const uint4*>(x0 + 8 * i * XP + grp * G + 32 * h);
-        mma16816<BF16>(u, one, one, one, one, v.x, v.y);
-        mma16816<BF16>(u, one, one, one, one, v.z, v.w);
+  for (int round = blockIdx.x;;) {
+    const bool first = !ON || round == static_cast<int>(blockIdx.x);
+    const bool again = ON && tile + gridDim.x * W < a.tiles;         // this warp has another tile
+    for (int cb = b0; cb < b1; cb += KC / kBlockK, buf ^= ON ? 0 : 1) {
+      if (first) {
+        asm volatile("cp.async.wait_all;" ::: "memory");
+        __syncthreads();                             // the chunk is there, the last one done with
+        if (!ON && cb + KC / kBlockK < b1) copy(cb + KC / kBlockK, buf ^ 1);
       }
-      if (g == 0)
-        *reinterpret_cast<float2*>(sums + grp * S::tokens + 8 * i + 2 * t) = make_float2(u[0], u[1]);
-    }
-    __syncthreads();
-    if (!live) continue;
-    // one block: its products, and at a group's end its factors
-    auto work = [&](int b, int p, bool ahead) {
-      const uint32_t words[4] = {wq[p].x, wq[p].y, wq[p].z, wq[p].w};
-      const uint16_t* xr = x0 + (b - cb) * kBlockK;
-      const float* su = sums + (b - cb) * kBlockK / G * S::tokens + 2 * t;
+      const uint16_t* x0 = sx + buf * (S::x_bytes / 2) + g * XP + 8 * t;
+      const int ce = min(cb + KC / kBlockK, b1);
+      // ---- the tokens' sums over each group: a product with ones, shared by the warps
+      constexpr uint32_t one = BF16 ? 0x3F803F80u : 0x3C003C00u;
+      const int jobs = first ? ((ce - cb) * kBlockK + G - 1) / G * NT : 0;
+      for (int e = warp; e < jobs; e += W) {
+        const int i = e % NT, grp = e / NT;
+        float u[4] = {0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-      for (int h = 0; h < 2; ++h) {
-        uint32_t v[2][4];
-        operands<BF16>(words[2 * h], v[0]);
-        operands<BF16>(words[2 * h + 1], v[1]);
-#pragma unroll
-        for (int i = 0; i < NT; ++i) {
-          const uint4 x = *reinterpret_cast<const uint4*>(xr + 8 * i * XP + 32 * h);
-          mma16816<BF16>(acc[i], v[0][0], v[0][1], v[0][2], v[0][3], x.x, x.y);
-          mma16816<BF16>(acc[i], v[1][0], v[1][1], v[1][2], v[1][3], x.z, x.w);
+        for (int h = 0; h < G / 32; ++h) {
+          const uint4 v = *reinterpret_cast<const uint4*>(x0 + 8 * i * XP + grp * G + 32 * h);
+          mma16816<BF16>(u, one, one, one, one, v.x, v.y);
+          mma16816<BF16>(u, one, one, one, one, v.z, v.w);
         }
-        if (G == 32 || (h == 1 && (G == 64 || p % 2 == 1))) {
-          const int at = p * kBlockK / G + (G == 32 ? h : 0);
-          float2 f, z;
-          group_factors<BF16>(sq[at], zq[at], f, z);
+        if (g == 0)
+          *reinterpret_cast<float2*>(sums + grp * S::tokens + 8 * i + 2 * t) = make_float2(u[0], u[1]);
+      }
+      if (first) __syncthreads();
+      if (!live) continue;
+      // one block: its products, and at a group's end its factors
+      auto work = [&](int b, int p, bool ahead) {
+        const uint32_t words[4] = {wq[p].x, wq[p].y, wq[p].z, wq[p].w};
+        const uint16_t* xr = x0 + (b - cb) * kBlockK;
+        const float* su = sums + (b - cb) * kBlockK / G * S::tokens + 2 * t;
+#pragma unroll
+        for (int h = 0; h < 2; ++h) {
+          uint32_t v[2][4];
+          operands<BF16>(words[2 * h], v[0]);
+          operands<BF16>(words[2 * h + 1], v[1]);
 #pragma unroll
           for (int i = 0; i < NT; ++i) {
-            const float2 u = *reinterpret_cast<const float2*>(su + (G == 32 ? h * S::tokens : 0) + 8 * i);
-            c[i][0] = fmaf(f.x, fmaf(z.x, u.x, acc[i][0]), c[i][0]);
-            c[i][1] = fmaf(f.x, fmaf(z.x, u.y, acc[i][1]), c[i][1]);
-            c[i][2] = fmaf(f.y, fmaf(z.y, u.x, acc[i][2]), c[i][2]);
-            c[i][3] = fmaf(f.y, fmaf(z.y, u.y, acc[i][3]), c[i][3]);
-            acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+            const uint4 x = *reinterpret_cast<const uint4*>(xr + 8 * i * XP + 32 * h);
+            mma16816<BF16>(acc[i], v[0][0], v[0][1], v[0][2], v[0][3], x.x, x.y);
+            mma16816<BF16>(acc[i], v[1][0], v[1][1], v[1][2], v[1][3], x.z, x.w);
+          }
+          if (G == 32 || (h == 1 && (G == 64 || p % 2 == 1))) {
+            const int at = p * kBlockK / G + (G == 32 ? h : 0);
+            float2 f, z;
+            group_factors<BF16>(sq[at], zq[at], f, z);
+#pragma unroll
+            for (int i = 0; i < NT; ++i) {
+              const float2 u = *reinterpret_cast<const float2*>(su + (G == 32 ? h * S::tokens : 0) + 8 * i);
+              c[i][0] = fmaf(f.x, fmaf(z.x, u.x, acc[i][0]), c[i][0]);
+              c[i][1] = fmaf(f.x, fmaf(z.x, u.y, acc[i][1]), c[i][1]);
+              c[i][2] = fmaf(f.y, fmaf(z.y, u.x, acc[i][2]), c[i][2]);
+              c[i][3] = fmaf(f.y, fmaf(z.y, u.y, acc[i][3]), c[i][3]);
+              acc[i][0] = acc[i][1] = acc[i][2] = acc[i][3] = 0.f;
+            }
           }
         }
-      }
-      if (!ahead) return;
-      // (a group of two blocks keeps its numbers until its second one is done)
-      if (G <= kBlockK) {
-        fetch(PF + p, p);
-      } else if (p % 2 == 1) {
-        fetch(PF + p - 1, p - 1);
-        fetch(PF + p, p);
-      }
-    };
-    int b = cb;
-    for (; b + PF <= ce && b + 2 * PF <= b1; b += PF) {      // with PF more blocks to fetch
+        if (!ahead) return;
+        // (a group of two blocks keeps its numbers until its second one is done)
+        if (G <= kBlockK) {
+          fetch(PF + p, p);
+        } else if (p % 2 == 1) {
+          fetch(PF + p - 1, p - 1);
+          fetch(PF + p, p);
+        }
+      };
+      int b = cb;
+      // with PF more blocks to fetch, of the next tile at last
+      for (; b + PF <= ce && (b + 2 * PF <= b1 || (again && b + PF == b1)); b += PF) {
+        if (ON && b + PF == b1) {
+          const int64_t skip = gridDim.x * W - 1;
+          w += skip * a.blocks * 32;
+          sc += skip * a.groups * 8;
+          if (zr) zr += skip * a.groups * 8;
+        }
 #pragma unroll
-      for (int p = 0; p < PF; ++p) work(b + p, p, true);
-      w += PF * 32;
-      sc += NG * 8;
-      if (zr) zr += NG * 8;
+        for (int p = 0; p < PF; ++p) work(b + p, p, true);
+        w += PF * 32;
+        sc += NG * 8;
+        if (zr) zr += NG * 8;
+      }
+      for (; b < ce; b += PF) {
+#pragma unroll
+        for (int p = 0; p < PF; ++p) {
+          if (b + p >= ce) break;
+          work(b + p, p, false);
+        }
+        // the next ones, as many as there are
+#pragma unroll
+        for (int p = 0; p < PF; ++p)
+          if (b + PF + p < b1) fetch(PF + p, p);
+        w += PF * 32;
+        sc += NG * 8;
+        if (zr) zr += NG * 8;
+      }
     }
-    for (; b < ce; b += PF) {
-#pragma unroll
-      for (int p = 0; p < PF; ++p) {
-        if (b + p >= ce) break;
-        work(b + p, p, false);
-      }
-      // the next ones, as many as there are
-#pragma unroll
-      for (int p = 0; p < PF; ++p)
-        if (b + PF + p < b1) fetch(PF + p, p);
-      w += PF * 32;
-      sc += NG * 8;
-      if (zr) zr += NG * 8;
-    }
-  }
-  // ---- the block's rows as [token][row], then the slices are added in order
-  __syncthreads();
-#pragma unroll
-  for (int i = 0; i < NT; ++i) {
-    float* p = part + (8 * i + 2 * t) * PP + warp * kTileRows + g;
-    p[0] = c[i][0];
-    p[PP] = c[i][1];
-    p[8] = c[i][2];
-    p[PP + 8] = c[i][3];
-  }
-  __syncwarp();
-  if (slices > 1)
-    cluster_sync_all();
-  else
+    // ---- the block's rows as [token][row], then the slices are added in order
     __syncthreads();
-  const int rank = blockIdx.y;
-  const uint32_t part_at = smem_u32(part);
-  auto total = [&](int m, int r) {                 // four rows of a token
-    if (slices == 1) return *reinterpret_cast<const float4*>(part + m * PP + r);
-    const uint32_t at = part_at + (m * PP + r) * 4;
-    float4 u[kMostSlices];
 #pragma unroll
-    for (int i = 0; i < kMostSlices; ++i)
-      if (i < slices) u[i] = ld_cluster_f32x4(cluster_map(at, i));
-    float4 v = u[0];
-#pragma unroll
-    for (int i = 1; i < kMostSlices; ++i)
-      if (i < slices) v.x += u[i].x, v.y += u[i].y, v.z += u[i].z, v.w += u[i].w;
-    return v;
-  };
-  const bool gated = a.epilogue == 2;
-  const int quads = gated ? S::rows / 8 : S::rows / 4;      // fours of outputs of a token
-  const int64_t out0 = static_cast<int64_t>(blockIdx.x) * quads * 4;
-  bool range = false;
-  for (int e = rank * S::threads + threadIdx.x; e < tokens * quads; e += slices * S::threads) {
-    const int m = e / quads, o = e % quads * 4;
-    float r[4];
-    if (gated) {
-      const int at = o / 8 * kTileRows + o % 8;
-      const float4 ga = total(m, at), up = total(m, at + 8);
-      r[0] = ga.x / (1.f + expf(-ga.x)) * up.x;
-      r[1] = ga.y / (1.f + expf(-ga.y)) * up.y;
-      r[2] = ga.z / (1.f + expf(-ga.z)) * up.z;
-      r[3] = ga.w / (1.f + expf(-ga.w)) * up.w;
-    } else {
-      const float4 v = total(m, o);
-      r[0] = v.x, r[1] = v.y, r[2] = v.z, r[3] = v.w;
+    for (int i = 0; i < NT; ++i) {
+      float* p = part + (8 * i + 2 * t) * PP + warp * kTileRows + g;
+      p[0] = c[i][0];
+      p[PP] = c[i][1];
+      p[8] = c[i][2];
+      p[PP + 8] = c[i][3];
     }
-    const int64_t at = (m0 + m) * a.ld_y + out0 + o;
-    const int left = static_cast<int>(min(static_cast<int64_t>(4), a.outs - (out0 + o)));
-    if (left <= 0) continue;
-    if (a.epilogue == 1) {
-      float* y = static_cast<float*>(a.y) + at;
+    __syncwarp();
+    if (slices > 1)
+      cluster_sync_all();
+    else
+      __syncthreads();
+    const int rank = ON ? 0 : blockIdx.y;
+    const uint32_t part_at = smem_u32(part);
+    auto total = [&](int m, int r) {                 // four rows of a token
+      if (slices == 1) return *reinterpret_cast<const float4*>(part + m * PP + r);
+      const uint32_t at = part_at + (m * PP + r) * 4;
+      float4 u[kMostSlices];
 #pragma unroll
-      for (int i = 0; i < 4; ++i)
-        if (i < left) y[i] += r[i];
-    } else {
-      uint16_t* y = static_cast<uint16_t*>(a.y) + at;
-      const uint32_t lo = pack2<BF16>(r[0], r[1]), hi = pack2<BF16>(r[2], r[3]);
-      if (!BF16)
+      for (int i = 0; i < kMostSlices; ++i)
+        if (i < slices) u[i] = ld_cluster_f32x4(cluster_map(at, i));
+      float4 v = u[0];
 #pragma unroll
-        for (int i = 0; i < 4; ++i) range |= i < left && !(fabsf(r[i]) <= 65504.f);
-      if (left == 4 && !(reinterpret_cast<uintptr_t>(y) & 7)) {
-        *reinterpret_cast<uint2*>(y) = make_uint2(lo, hi);
+      for (int i = 1; i < kMostSlices; ++i)
+        if (i < slices) v.x += u[i].x, v.y += u[i].y, v.z += u[i].z, v.w += u[i].w;
+      return v;
+    };
+    const bool gated = a.epilogue == 2;
+    const int quads = gated ? S::rows / 8 : S::rows / 4;      // fours of outputs of a token
+    const int64_t out0 = static_cast<int64_t>(round) * quads * 4;
+    bool range = false;
+    for (int e = rank * S::threads + threadIdx.x; e < tokens * quads; e += slices * S::threads) {
+      const int m = e / quads, o = e % quads * 4;
+      float r[4];
+      if (gated) {
+        const int at = o / 8 * kTileRows + o % 8;
+        const float4 ga = total(m, at), up = total(m, at + 8);
+        r[0] = ga.x / (1.f + expf(-ga.x)) * up.x;
+        r[1] = ga.y / (1.f + expf(-ga.y)) * up.y;
+        r[2] = ga.z / (1.f + expf(-ga.z)) * up.z;
+        r[3] = ga.w / (1.f + expf(-ga.w)) * up.w;
       } else {
-        const uint16_t h[4] = {static_cast<uint16_t>(lo), static_cast<uint16_t>(lo >> 16),
-                               static_cast<uint16_t>(hi), static_cast<uint16_t>(hi >> 16)};
+        const float4 v = total(m, o);
+        r[0] = v.x, r[1] = v.y, r[2] = v.z, r[3] = v.w;
+      }
+      const int64_t at = (m0 + m) * a.ld_y + out0 + o;
+      const int left = static_cast<int>(min(static_cast<int64_t>(4), a.outs - (out0 + o)));
+      if (left <= 0) continue;
+      if (a.epilogue == 1) {
+        float* y = static_cast<float*>(a.y) + at;
 #pragma unroll
         for (int i = 0; i < 4; ++i)
-          if (i < left) y[i] = h[i];
+          if (i < left) y[i] += r[i];
+      } else {
+        uint16_t* y = static_cast<uint16_t*>(a.y) + at;
+        const uint32_t lo = pack2<BF16>(r[0], r[1]), hi = pack2<BF16>(r[2], r[3]);
+        if (!BF16)
+#pragma unroll
+          for (int i = 0; i < 4; ++i) range |= i < left && !(fabsf(r[i]) <= 65504.f);
+        if (left == 4 && !(reinterpret_cast<uintptr_t>(y) & 7)) {
+          *reinterpret_cast<uint2*>(y) = make_uint2(lo, hi);
+        } else {
+          const uint16_t h[4] = {static_cast<uint16_t>(lo), static_cast<uint16_t>(lo >> 16),
+                                 static_cast<uint16_t>(hi), static_cast<uint16_t>(hi >> 16)};
+#pragma unroll
+          for (int i = 0; i < 4; ++i)
+            if (i < left) y[i] = h[i];
+        }
       }
     }
+    if (range) atomicExch(a.err, kErrRange);
+    __syncwarp();
+    if (slices > 1) cluster_sync_all();            // the peers have read this block's part
+    if (!ON) return;
+    round += gridDim.x;
+    if (round >= a.rounds) return;
+    tile += gridDim.x * W;
+    live = tile < a.tiles;
+#pragma unroll
+    for (int i = 0; i < NT; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
   }
-  if (range) atomicExch(a.err, kErrRange);
-  __syncwarp();
-  if (slices > 1) cluster_sync_all();              // the peers have read this block's part
 }
 
 // Slices of K, of whole groups and at least 128 k: 16 warps per SM where the rows
@@ -414,27 +454,41 @@ int slices_of(const Layout& l) {
   return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(s, kMostSlices)));
 }
 
-template <bool BF16, int G, int NT>
-cudaError_t launch_linear(const LinearArgs& a, int slices, cudaStream_t s) {
-  using S = Shape<NT>;
+template <bool BF16, int G, int NT, bool ON>
+cudaError_t launch_linear(const LinearArgs& args, int slices, cudaStream_t s) {
+  using S = Shape<NT, ON>;
   static DeviceOnce once;
   constexpr size_t smem = S::template smem<G>;
-  auto kernel = qlinear_kernel<BF16, G, NT>;
+  auto kernel = qlinear_kernel<BF16, G, NT, ON>;
   cudaError_t e = once.run([&] {
     return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, smem);
   });
   if (e != cudaSuccess) return e;
-  const dim3 grid(static_cast<unsigned>((a.tiles + S::warps - 1) / S::warps), slices,
+  LinearArgs a = args;
+  a.rounds = static_cast<int>((a.tiles + S::warps - 1) / S::warps);
+  const dim3 grid(ON ? std::min(a.rounds, S::resident * kNumSMs) : a.rounds, slices,
                   (a.M + S::tokens - 1) / S::tokens);
   return launch_ex(kernel, grid, dim3(S::threads), smem, s, false, dim3(1, slices, 1), a);
 }
 
+// With one slice and few enough k, a wave of blocks goes on from tile to tile: 59,392 rows, K
+// 1024, bf16, 5 tokens 11.7 us, 13.0 with a block for each 64 rows, which waits for its first
+// weights and tokens every time (K 2048, one token 19.5 and 21.6; 16 tokens 13.9 and 15.9; a
+// wave or less, 20,480 rows, 7.0 either way).
+template <bool BF16, int G, int NT>
+cudaError_t launch_on(const LinearArgs& a, int slices, cudaStream_t s) {
+  using S = Shape<NT, true>;
+  if (slices == 1 && a.blocks <= S::chunk / kBlockK && a.blocks % S::template ahead<G> == 0)
+    return launch_linear<BF16, G, NT, true>(a, slices, s);
+  return launch_linear<BF16, G, NT, false>(a, slices, s);
+}
+
 template <bool BF16, int G>
 cudaError_t launch_rows(const LinearArgs& a, int slices, cudaStream_t s) {
-  if (a.M <= 8) return launch_linear<BF16, G, 1>(a, slices, s);
-  if (a.M <= 16) return launch_linear<BF16, G, 2>(a, slices, s);
-  if (a.M <= 32) return launch_linear<BF16, G, 4>(a, slices, s);
-  return launch_linear<BF16, G, 8>(a, slices, s);
+  if (a.M <= 8) return launch_on<BF16, G, 1>(a, slices, s);
+  if (a.M <= 16) return launch_on<BF16, G, 2>(a, slices, s);
+  if (a.M <= 32) return launch_linear<BF16, G, 4, false>(a, slices, s);
+  return launch_linear<BF16, G, 8, false>(a, slices, s);
 }
 
 template <bool BF16>

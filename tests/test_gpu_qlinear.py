@@ -149,6 +149,24 @@ def test_rows_do_not_depend_on_the_batch(gs, dtype, N, K, gated):
         assert torch.equal(y, whole[a:b]), (a, b)
 
 
+@pytest.mark.parametrize("dtype", ["fp16", "bf16"])
+@pytest.mark.parametrize("N,K,group,zeros,gated", [
+    (39991, 1024, 128, True, False), (24573, 2048, 64, False, False), (60000, 512, 32, True, False),
+    (40002, 1024, 32, True, True), (19473, 512, 128, False, False)])
+def test_many_outputs(gs, dtype, N, K, group, zeros, gated):
+    """More tiles than a wave of blocks has warps: what goes on from tile to tile, the last tile
+    cut short, what lies behind it left alone."""
+    w, W = _weights(gs, dtype, N, K, group, zeros, gated, scale=0.02)
+    epi, outs = 2 if gated else 0, N // 2 if gated else N
+    x = _x(dtype, 40, K)
+    whole, err = _run(gs, w, x, epilogue=epi)
+    assert err == 0
+    _check(dtype, whole, W, x, w, gated)
+    for a, b in ((0, 1), (3, 8), (8, 16), (9, 25), (23, 40)):
+        y, err = _run(gs, w, x[a:b], epilogue=epi, ld=outs + 5)
+        assert err == 0 and torch.equal(y[:, :outs], whole[a:b]) and (y[:, outs:] == 7).all(), (a, b)
+
+
 def test_strides_and_streams(gs):
     """Rows apart in memory, odd output strides, what lies between is left alone."""
     for dtype in TYPES:
