@@ -603,10 +603,23 @@ int gs_pages_copy(const void *src, int src_pages, void *dst, int dst_pages, int 
  *           without a window (0).
  *   lse     device fp32 [trees * nodes, n_heads] or NULL: ln of the sum of exp of
  *           the scores
- *   split_pages, scratch  as in gs_decode_attention
+ *   split_pages  pages per work item: items are reduced independently and joined in
+ *           a fixed order, and a row's result depends on its own keys, the split and
+ *           `nodes` only.  0: chosen; with more than 16 query rows of a KV head (nodes *
+ *           n_heads / n_kv_heads) and at most 1024 trees the pages of all trees are
+ *           then shared evenly, and how a row's sums are rounded depends on the other
+ *           trees of the call (never on the order of execution: a repeated call
+ *           gives the same bits).
+ *   scratch device, 256-byte aligned, at least gs_tree_attention_scratch_bytes(...)
+ *           bytes (0 on a bad argument); its first int32 is the error word: raised by
+ *           a sequence, page, count or n out of range (n + count beyond the table, or
+ *           a negative one), or 2 where a wait within the kernel ran out.  The rest
+ *           may hold anything.  Calls that may run at the same time need scratch of
+ *           their own; graphs that are replayed one after another may share it.
  * What the cache holds where a node does not see it has no influence on that node,
  * infinities and NaN included.  Scores, maxima, sums and accumulators are fp32;
- * the probabilities are rounded to the cache's type for the product with V.
+ * the probabilities are rounded to the cache's type for the product with V (those
+ * below 2^-29 of the largest lose bits in fp16, below 2^-21 with more than 16 rows).
  * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (head_dim, nodes > 64, trees >
  * 65535, n_heads > 16383), GS_ERR_OOM (scratch too small), GS_ERR_CUDA. */
 size_t gs_tree_attention_scratch_bytes(const gs_cache *cache, int trees, int nodes, int n_heads,
@@ -685,8 +698,12 @@ int gs_qweight_pack(const gs_qweight *w, const void *q, const void *scale, const
  *   y   device [M, N], row stride ld_y.  epilogue 0: dtype, y = acc; 1: fp32, y +=
  *       acc; 2: dtype [M, N / 2], silu(gate) * up (gated weights, and only they)
  *   err device int32: 3 is stored where an fp16 output is beyond the type's range
- * q - z is exact, sums and the products with s are fp32: the output's rounding is
- * the only one.  A row's result is the same for any M.
+ * No weight is rounded: sums of q x and of x over each group are fp32, z times the
+ * latter is taken off, and s multiplies in fp32; the error before the output's
+ * rounding is that of fp32 sums of terms up to 15 s |x| (31 s |x| in bf16).  A row's
+ * result is the same for any M.  A row of x that holds an infinity or a NaN, or
+ * (bf16) values beyond 2^110, may give NaN where the sum would be infinite or finite;
+ * other rows are not touched by it.
  * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (as above, M > 2^21), GS_ERR_CUDA. */
 int gs_qlinear(const gs_qweight *w, const void *x, int64_t ld_x, void *y, int64_t ld_y, int M,
                int epilogue, int32_t *err, void *stream);
