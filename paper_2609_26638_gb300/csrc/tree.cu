@@ -144,10 +144,10 @@ __global__ void __launch_bounds__(kCommitThreads) tree_commit_kernel(const Commi
   __syncthreads();
   const int length = s_length, n = s_n, seq = s_seq;
   if (length == 0) return;
-  bool bad = length < 0 || length > a.nodes || seq < 0 || seq >= a.cache.n_seq || n < 0 ||
-             n > a.cache.pt_stride * kPageTokens - a.nodes;
+  bool bad = length < 0 || length > a.nodes || seq < 0 || seq >= a.cache.n_seq || n < 0;
   if (!bad && tid < length) {
-    bad = path < 0 || path >= a.nodes || (tid > 0 && path <= s_path[tid - 1]);
+    bad = path < 0 || path >= a.nodes || path >= a.cache.pt_stride * kPageTokens - n ||
+          (tid > 0 && path <= s_path[tid - 1]);
     if (!bad && path != tid) {
       atomicMin(&s_first, tid);
       const int32_t* table = a.cache.page_table + static_cast<int64_t>(seq) * a.cache.pt_stride;
@@ -240,7 +240,6 @@ extern "C" int gs_tree_commit(const gs_cache* cache, int n_layers, const int32_t
   if (!aligned4(seq, n, path, length, err)) return GS_ERR_INVALID_ARG;
   // layers and trees are grid dimensions
   if (nodes > kMostNodes || n_layers > 65535 || trees > 65535) return GS_ERR_UNSUPPORTED;
-  if (nodes > cache->pt_stride * kPageTokens) return GS_ERR_INVALID_ARG;
   if (trees == 0) return GS_OK;
   CommitArgs a;
   a.cache = cache_view(*cache);

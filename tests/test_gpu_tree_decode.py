@@ -157,6 +157,20 @@ def test_right_drafts_are_kept(bn, td):
     assert again == text and steps == 4
 
 
+def test_texts_that_fill_the_context(bn, td):
+    """Trees at the end of a table, cut to the room there, beside wide ones."""
+    from paper_2609_26638_gb300 import gs
+    shape = bn.Shape(vocab=128)
+    weights = bn.random_weights(shape, 8)
+    dec = bn.StepDecoder(shape, weights, n_pages=12, max_seqs=2, max_ctx=128)
+    rng = np.random.default_rng(6)
+    prompts = [rng.integers(0, 3, n).tolist() for n in (108, 60)]
+    out, _ = td.tree_decode(dec, prompts, 20, max_nodes=40, ngram=1, temperature=0.0)
+    assert [len(t) for t in out] == [20, 20]
+    for p, t in zip(prompts, out):
+        _greedy_or_near(bn, shape, weights, p, t, gs)
+
+
 def test_sampled_text_does_not_depend_on_the_drafts(bn, td):
     """With the numbers of each position given, drafts change nothing; and an eos ends a text."""
     shape = bn.Shape()

@@ -226,6 +226,20 @@ def test_other_sequences_and_offsets_past_32_bits(gs):
     assert torch.equal(pool[:, small], want)
 
 
+@pytest.mark.parametrize("room", [1, 5, 16])
+def test_paths_that_end_with_the_table(gs, room):
+    """A tree of few nodes at the end of its table, beside a wider one."""
+    rng = np.random.default_rng(room)
+    pool, table = _pool(rng, 2, [100, 100], 20, 2, 64)
+    ns = [64 * table.shape[1] - room, 30]
+    path, length = _paths(rng, 2, 20)
+    path[0], length[0] = -1, (room + 1) // 2
+    path[0, : length[0]] = np.arange(room)[room % 2 == 0:: 2]      # its last node is the table's last
+    want = _moved(pool, table, ns, path, length, 2, 64)
+    assert _commit(gs, pool, table, ns, path, length, 2, 64) == 0
+    assert torch.equal(pool, want)
+
+
 def test_commit_error_word(gs):
     """What is out of range raises the word; nothing of that tree moves, the others do."""
     rng = np.random.default_rng(4)
