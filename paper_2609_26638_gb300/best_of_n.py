@@ -246,8 +246,9 @@ class StepDecoder:
         self.pool.err.logical_or_((inside != token).any())
         h = self.w["embed"][inside].float()
         qkv = torch.empty(rows, s.qkv_dim, dtype=torch.float16, device=dev)
-        # (rows beyond a tree's nodes are left as they are by its attention)
-        out = torch.zeros(rows, s.n_heads * s.head_dim, dtype=torch.float16, device=dev)
+        out = torch.empty(rows, s.n_heads * s.head_dim, dtype=torch.float16, device=dev)
+        if last is None:           # rows beyond a tree's nodes are left as they are by its attention
+            out.zero_()
         act = torch.empty(rows, s.d_ffn, dtype=torch.float16, device=dev)
         for i, w in enumerate(self.w["layers"]):
             cache = self.pool.layer(i)

@@ -24,6 +24,8 @@ def quantize(w: torch.Tensor, group: int = 64, zeros: bool = False
     or 7; with them its least weight is 0 or below it, its largest 15."""
     if w.dim() != 2 or w.dtype not in TYPES or group not in (32, 64, 128) or w.shape[1] % group:
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "a 16-bit [N, K] matrix with K a multiple of the group needed")
+    if not torch.isfinite(w).all():
+        raise gs.GsError(gs.GS_ERR_INVALID_ARG, "an infinite or NaN weight")
     x = w.float().view(w.shape[0], -1, group)
     lo, hi = x.amin(-1).clamp(max=0), x.amax(-1).clamp(min=0)
     scale = ((hi - lo) / 15 if zeros else torch.maximum(-lo / 8, hi / 7)).to(w.dtype)
@@ -41,7 +43,7 @@ class QWeight:
 
     def __init__(self, q: torch.Tensor, scale: torch.Tensor, zero: Optional[torch.Tensor] = None, *,
                  group: int, gated: bool = False):
-        n, k = q.shape[0], 2 * q.shape[1] if q.dim() == 2 else 0
+        n, k = (q.shape[0], 2 * q.shape[1]) if q.dim() == 2 else (0, 0)
         want = (n, k // group if group > 0 else 0)
         held = [t for t in (q, scale, zero) if t is not None]
         if (q.dim() != 2 or q.dtype != torch.uint8 or scale.dtype not in TYPES or scale.shape != want

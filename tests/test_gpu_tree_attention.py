@@ -365,6 +365,52 @@ def test_offsets_past_32_bits(gs, nodes):
     _check(c, out, lse)
 
 
+@pytest.mark.parametrize("nodes,trees", [(2, 1500), (20, 1024), (20, 1025), (33, 1300)])
+def test_many_trees(gs, nodes, trees):
+    """More trees than the wide kernel shares out, and as many; short, of a few sequences."""
+    c = _case("bf16", [3, 0, 70, 129, 64, 31, 200], nodes, 4, 2, 64, seed=trees)
+    pick = np.random.default_rng(trees).integers(0, 7, trees).tolist()
+    out, lse, err = _run(gs, c, only=pick)
+    assert err == 0
+    first = {}
+    for i, b in enumerate(pick):
+        first.setdefault(b, i)
+    rows = torch.tensor([first[b] for b in range(7)], device=DEV)
+    o, l = out.view(trees, nodes, -1), lse.view(trees, nodes, -1)
+    _check(c, o[rows].reshape(7 * nodes, -1), l[rows].reshape(7 * nodes, -1))
+    # trees of the same sequence are the same tree: other shares of its pages round otherwise,
+    # and both are within the bound above of A, at most the largest value
+    same = torch.tensor([first[b] for b in pick], device=DEV)
+    most = max(v.abs().max().item() for v in c["v"])
+    assert ((o.double() - o[same].double()).abs() <= 2 * (2.1 * UNIT["bf16"] + 1e-4) * most).all()
+    if trees > 1024 or nodes == 2:
+        assert torch.equal(o, o[same]) and torch.equal(l, l[same])
+
+
+@pytest.mark.parametrize("nodes", [4, 40])
+def test_two_calls_at_once(gs, nodes):
+    """Calls on two streams, each with scratch of its own, over one cache."""
+    c = _case("fp16", [2000, 70, 900, 1500], nodes, 8, 2, 64, seed=3)
+    cache = _cache(gs, c["pool"], c["table"], 2, 64, "fp16")
+    n, mask = _dev(np.array(c["ns"])), _dev(c["mask"].view(np.int64), torch.int64)
+    qs = [c["q"].reshape(4 * nodes, -1).contiguous(), c["q"].flip(1).reshape(4 * nodes, -1).contiguous()]
+    want = [_run(gs, c, q=q, all_nodes=True)[0] for q in qs]
+    nb = gs.gs_tree_attention_scratch_bytes(cache, 4, nodes, 8, 0)
+    scratch = torch.zeros(2, -(-nb // 256) * 256, dtype=torch.uint8, device=DEV)
+    outs = torch.zeros(2, 20, 4 * nodes, 512, dtype=torch.float16, device=DEV)
+    streams = [torch.cuda.Stream() for _ in qs]
+    torch.cuda.synchronize()
+    for i in range(20):
+        for j, st in enumerate(streams):
+            gs.gs_tree_attention(cache, qs[j].data_ptr(), 512, 0, n.data_ptr(), 0, mask.data_ptr(), 0, 4, nodes,
+                                 8, 0.125, 0, outs[j, i].data_ptr(), 512, 0, 0, scratch[j].data_ptr(), nb,
+                                 st.cuda_stream)
+    torch.cuda.synchronize()
+    for j in range(2):
+        assert (outs[j] == want[j]).all()
+    assert (scratch[:, :4] == 0).all()
+
+
 @pytest.mark.parametrize("nodes", [4, 40])
 def test_error_word(gs, nodes):
     """A bad sequence, length, count or page raises the word; the other trees are right."""

@@ -80,9 +80,14 @@ def test_quantize_refuses(mods):
     w = torch.zeros(4, 128, dtype=torch.float16)
     for bad in ((w.float(), 64), (w[0], 64), (w, 16), (w, 0), (w[:, :96], 64), (w[None], 64)):
         _refused(qw.gs, qw.quantize, *bad)
+    for bad in (float("nan"), float("inf"), float("-inf")):
+        broken = w.clone()
+        broken[2, 100] = bad
+        _refused(qw.gs, qw.quantize, broken, 64)
     q, s, _ = qw.quantize(w)
     _refused(qw.gs, qw.QWeight, q, s, group=64)                  # not on a device
     _refused(qw.gs, qw.QWeight, q[0], s, group=64)
+    _refused(qw.gs, qw.QWeight, q[0, 0], s, group=64)
 
 
 def test_tree_decode_refuses(mods):
