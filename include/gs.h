@@ -693,17 +693,18 @@ size_t gs_qweight_bytes(const gs_qweight *w);
 int gs_qweight_pack(const gs_qweight *w, const void *q, const void *scale, const void *zero,
                     void *stream);
 
-/* Y = X . W^T with 4-bit weights, made for the few rows of a decoding step.
+/* Y = X . W^T with 4-bit weights, made for the rows of a decoding step.
  *   x   device [M, K] of dtype, row stride ld_x (a multiple of 8), 16-byte aligned
  *   y   device [M, N], row stride ld_y.  epilogue 0: dtype, y = acc; 1: fp32, y +=
  *       acc; 2: dtype [M, N / 2], silu(gate) * up (gated weights, and only they)
- *   err device int32: 3 is stored where an fp16 output is beyond the type's range
+ *   err device int32: 3 is stored where an fp16 output is beyond the type's range, 2
+ *       where a wait within the kernel ran out (M > 32)
  * No weight is rounded: sums of q x and of x over each group are fp32, z times the
  * latter is taken off, and s multiplies in fp32; the error before the output's
  * rounding is that of fp32 sums of terms up to 15 s |x| (31 s |x| in bf16).  A row's
- * result is the same for any M.  A row of x that holds an infinity or a NaN, or
- * (bf16) values beyond 2^110, may give NaN where the sum would be infinite or finite;
- * other rows are not touched by it.
+ * result is the same for any M up to 32, and for any M beyond.  A row of x that holds an
+ * infinity or a NaN, or (bf16) values beyond 2^110, may give NaN where the sum would be
+ * infinite or finite; other rows are not touched by it.
  * Errors: GS_ERR_INVALID_ARG, GS_ERR_UNSUPPORTED (as above, M > 2^21), GS_ERR_CUDA. */
 int gs_qlinear(const gs_qweight *w, const void *x, int64_t ld_x, void *y, int64_t ld_y, int M,
                int epilogue, int32_t *err, void *stream);

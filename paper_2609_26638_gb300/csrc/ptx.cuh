@@ -72,6 +72,22 @@ __device__ __forceinline__ bool mbar_wait(uint32_t bar, uint32_t parity, int* er
   }
 }
 
+// mbar_wait in as little code as it takes, for kernels whose loops it would swell.
+__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* err) {
+  uint64_t start = 0;
+#pragma unroll 1
+  for (uint32_t i = 1; !mbar_try_wait(bar, parity); ++i) {
+    if (i & 255) continue;
+    const uint64_t now = global_timer_ns();
+    if (start == 0) start = now;
+    if (now - start > kWaitLimitNs) {
+      atomicExch(err, kErrTimeout);
+      return false;
+    }
+  }
+  return true;
+}
+
 // ---------------------------------------------------------------- TMA
 __device__ __forceinline__ void tma_prefetch_desc(const CUtensorMap* m) {
   asm volatile("prefetch.tensormap [%0];" ::"l"(reinterpret_cast<uint64_t>(m)) : "memory");

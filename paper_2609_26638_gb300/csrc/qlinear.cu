@@ -1,4 +1,5 @@
-// qlinear.cu -- products of a few rows with 4-bit weights and group scales.
+// qlinear.cu -- products with 4-bit weights and group scales: few tokens here, more than 32 in
+// qlinear_wide.cuh.
 //
 //   y[m, r] = sum_g s[r, g] * (sum_{k in g} q[r, k] x[m, k] - z[r, g] sum_{k in g} x[m, k])
 //
@@ -24,40 +25,17 @@
 //
 // What bounds it: 28,672 x 8192 and one token 28 us, 4.4 TB/s of weights and near one
 // instruction for two weights of a warp's lanes; 8192 x 8192, 11 us for one token, 12 for 8, 15.7
-// for 16, 25 for 32, 43 for 64: from 16 on the issue of products and of the loads of
-// tokens (for 32, the tensor pipes are 35 per cent busy, the issue slots 37); with
-// fewer weights the start of a block: a first weight, the tokens and their sums, 4 us in all
-// (1024 x 1024 and one token 3.3 us).  Two tiles to a warp read the tokens half as often but
-// leave half the warps (28 us for 32); with the weights unpacked to shared memory for
-// 128-row tensor memory products it took 24 to 39, the issue of small products again.
+// for 16, 26 for 32: from 16 on the issue of products and of the loads of tokens
+// (for 32, the tensor pipes are 35 per cent busy, the issue slots 37); with fewer weights
+// the start of a block: a first weight, the tokens and their sums, 4 us in all (1024 x
+// 1024 and one token 3.3 us).  Two tiles to a warp read the tokens half as often but leave
+// half the warps (28 us for 32).
 #include <algorithm>
 
-#include "attend_common.cuh"
-#include "internal.h"
+#include "qlinear_wide.cuh"
 
 namespace gs {
 namespace {
-
-constexpr int kTileRows = 16;
-constexpr int kBlockK = 64;                        // k of one packed block
-constexpr int kBlockBytes = kTileRows * kBlockK / 2;
-constexpr int kMostSlices = 8;
-
-struct Layout {
-  int64_t tiles, blocks, groups;                   // row tiles; 64-k blocks and their groups
-  int64_t scale_at, zero_at, total;                // byte offsets
-};
-inline Layout layout_of(const gs_qweight& w) {
-  Layout l;
-  const int per = w.gated ? 8 : kTileRows;         // outputs of a tile
-  l.tiles = ((w.gated ? w.N / 2 : w.N) + per - 1) / per;
-  l.blocks = (w.K + kBlockK - 1) / kBlockK;
-  l.groups = (l.blocks * kBlockK + w.group - 1) / w.group;
-  l.scale_at = l.tiles * l.blocks * kBlockBytes;
-  l.zero_at = l.scale_at + l.tiles * l.groups * kTileRows * 2;
-  l.total = l.zero_at + (w.zeros ? l.tiles * l.groups * kTileRows : 0);
-  return l;
-}
 
 inline int check_weight(const gs_qweight* w) {
   if (!w || w->N < 1 || w->K < 32 || (w->dtype != GS_F16 && w->dtype != GS_BF16) || w->zeros < 0 ||
@@ -129,43 +107,6 @@ pack_scales_kernel(const uint16_t* scale, const uint8_t* zero, int N, int gated,
   if (zero) zero_out[e] = in ? zero[row * have + group] & 15 : 0;
 }
 
-struct LinearArgs {
-  const uint4* w;
-  const uint32_t* scale;      // [tile][group][8] pairs
-  const uint16_t* zero;       // the same, pairs of bytes; NULL: 8
-  const uint16_t* x;
-  int64_t ld_x;
-  void* y;
-  int64_t ld_y;
-  int64_t tiles, blocks, groups;
-  int M, K, outs, slice;        // slice: 64-k blocks of a slice of K
-  int rounds;                   // thread blocks' rows; with ON one takes every gridDim.x-th
-  int epilogue;
-  int* err;
-};
-
-// A word's four operand registers.  What is multiplied is, for q of the tile's
-// lower and upper rows: fp16: q 2^-24 and q 2^-20; bf16: (16 + q) 2^-4, both.
-template <bool BF16>
-__device__ __forceinline__ void operands(uint32_t w, uint32_t (&v)[4]) {
-  if constexpr (BF16) {
-#pragma unroll
-    for (int j = 0; j < 4; ++j)
-      v[j] = ((j ? __funnelshift_r(w, w, 4 * j) : w) & 0x00780078u) | 0x3F803F80u;
-  } else {
-    v[0] = w & 0x000F000Fu;
-    v[1] = w & 0x00F000F0u;
-    v[2] = w >> 8 & 0x000F000Fu;
-    v[3] = w >> 8 & 0x00F000F0u;
-  }
-}
-template <bool BF16>
-constexpr float kUnit0 = BF16 ? 0x1p4f : 0x1p24f;  // what a lower row's sum is multiplied by
-template <bool BF16>
-constexpr float kUnit1 = BF16 ? 0x1p4f : 0x1p20f;
-template <bool BF16>
-constexpr float kAdded = BF16 ? 16.f : 0.f;
-
 // ON: a wave of blocks that keep the tokens in shared memory and go on from tile to tile.
 template <int NT, bool ON>
 struct Shape {
@@ -174,12 +115,12 @@ struct Shape {
   static constexpr int threads = 32 * warps, rows = warps * kTileRows;
   static constexpr int resident = warps == 4 ? 4 : 2;    // blocks of an SM
   // k of x in shared memory: twice, or all of them
-  static constexpr int chunk = (NT == 1 ? 1024 : NT <= 4 ? 512 : 256) * (ON ? 2 : 1);
+  static constexpr int chunk = (NT == 1 ? 1024 : 512) * (ON ? 2 : 1);
   static constexpr int pitch = chunk + 32;         // 8 lanes of 2 tokens on distinct banks
   static constexpr int part_pitch = rows + 4;      // 2-row stores of 8 rows x 4 lanes likewise
   static constexpr int x_bytes = tokens * pitch * 2, part_bytes = tokens * part_pitch * 4;
   template <int G>
-  static constexpr int ahead = G == 32 || NT == 8 ? 4 : 8;          // packed blocks fetched ahead
+  static constexpr int ahead = G == 32 ? 4 : 8;          // packed blocks fetched ahead
   template <int G>
   static constexpr int sum_bytes = chunk / G * tokens * 4;
   static constexpr int sum_at = x_bytes * (ON ? 1 : 2);
@@ -375,65 +316,8 @@ qlinear_kernel(const LinearArgs a) {
       cluster_sync_all();
     else
       __syncthreads();
-    const int rank = ON ? 0 : blockIdx.y;
-    const uint32_t part_at = smem_u32(part);
-    auto total = [&](int m, int r) {                 // four rows of a token
-      if (slices == 1) return *reinterpret_cast<const float4*>(part + m * PP + r);
-      const uint32_t at = part_at + (m * PP + r) * 4;
-      float4 u[kMostSlices];
-#pragma unroll
-      for (int i = 0; i < kMostSlices; ++i)
-        if (i < slices) u[i] = ld_cluster_f32x4(cluster_map(at, i));
-      float4 v = u[0];
-#pragma unroll
-      for (int i = 1; i < kMostSlices; ++i)
-        if (i < slices) v.x += u[i].x, v.y += u[i].y, v.z += u[i].z, v.w += u[i].w;
-      return v;
-    };
-    const bool gated = a.epilogue == 2;
-    const int quads = gated ? S::rows / 8 : S::rows / 4;      // fours of outputs of a token
-    const int64_t out0 = static_cast<int64_t>(round) * quads * 4;
-    bool range = false;
-    for (int e = rank * S::threads + threadIdx.x; e < tokens * quads; e += slices * S::threads) {
-      const int m = e / quads, o = e % quads * 4;
-      float r[4];
-      if (gated) {
-        const int at = o / 8 * kTileRows + o % 8;
-        const float4 ga = total(m, at), up = total(m, at + 8);
-        r[0] = ga.x / (1.f + expf(-ga.x)) * up.x;
-        r[1] = ga.y / (1.f + expf(-ga.y)) * up.y;
-        r[2] = ga.z / (1.f + expf(-ga.z)) * up.z;
-        r[3] = ga.w / (1.f + expf(-ga.w)) * up.w;
-      } else {
-        const float4 v = total(m, o);
-        r[0] = v.x, r[1] = v.y, r[2] = v.z, r[3] = v.w;
-      }
-      const int64_t at = (m0 + m) * a.ld_y + out0 + o;
-      const int left = static_cast<int>(min(static_cast<int64_t>(4), a.outs - (out0 + o)));
-      if (left <= 0) continue;
-      if (a.epilogue == 1) {
-        float* y = static_cast<float*>(a.y) + at;
-#pragma unroll
-        for (int i = 0; i < 4; ++i)
-          if (i < left) y[i] += r[i];
-      } else {
-        uint16_t* y = static_cast<uint16_t*>(a.y) + at;
-        const uint32_t lo = pack2<BF16>(r[0], r[1]), hi = pack2<BF16>(r[2], r[3]);
-        if (!BF16)
-#pragma unroll
-          for (int i = 0; i < 4; ++i) range |= i < left && !(fabsf(r[i]) <= 65504.f);
-        if (left == 4 && !(reinterpret_cast<uintptr_t>(y) & 7)) {
-          *reinterpret_cast<uint2*>(y) = make_uint2(lo, hi);
-        } else {
-          const uint16_t h[4] = {static_cast<uint16_t>(lo), static_cast<uint16_t>(lo >> 16),
-                                 static_cast<uint16_t>(hi), static_cast<uint16_t>(hi >> 16)};
-#pragma unroll
-          for (int i = 0; i < 4; ++i)
-            if (i < left) y[i] = h[i];
-        }
-      }
-    }
-    if (range) atomicExch(a.err, kErrRange);
+    finish_rows<BF16, S::rows, S::threads, PP>(a, part, m0, tokens, slices, ON ? 0 : blockIdx.y, round,
+                                              threadIdx.x);
     __syncwarp();
     if (slices > 1) cluster_sync_all();            // the peers have read this block's part
     if (!ON) return;
@@ -445,6 +329,11 @@ qlinear_kernel(const LinearArgs a) {
     for (int i = 0; i < NT; ++i) c[i][0] = c[i][1] = c[i][2] = c[i][3] = 0.f;
   }
 }
+
+// Tokens beyond which the kernel of qlinear_wide.cuh takes over: bf16, 8192 x 8192, 32 tokens
+// 25.9 us here and 31.1 there, 33 to 64 40.5 to 43.1 and 31.4 to 32.5, 128 83.9 and 34.4;
+// 1024 x 1024, fp16, groups of 64, 64 tokens 6.4 and 6.7, 1024 x 4096 11.7 and 9.4.
+constexpr int kFewTokens = 32;
 
 // Slices of K, of whole groups and at least 128 k: 16 warps per SM where the rows
 // alone are too few.  N and K decide, not M.
@@ -483,12 +372,38 @@ cudaError_t launch_on(const LinearArgs& a, int slices, cudaStream_t s) {
   return launch_linear<BF16, G, NT, false>(a, slices, s);
 }
 
+// Many tokens: a wave of blocks of 128 rows and a slice of K, by N and K alone.
+int wide_slices_of(const Layout& l) {
+  const int64_t rows = (l.tiles + kWideTiles - 1) / kWideTiles;
+  int64_t s = kNumSMs / rows;
+  s = std::min<int64_t>(s, (l.blocks + 1) / 2);
+  return static_cast<int>(std::max<int64_t>(1, std::min<int64_t>(s, kMostSlices)));
+}
+
+template <bool BF16, int G>
+cudaError_t launch_wide(const LinearArgs& a, int slices, cudaStream_t s) {
+  static DeviceOnce once;
+  auto kernel = qlinear_wide_kernel<BF16, G>;
+  cudaError_t e = once.run([&] {
+    return cudaFuncSetAttribute(kernel, cudaFuncAttributeMaxDynamicSharedMemorySize, WideShape::total);
+  });
+  if (e != cudaSuccess) return e;
+  CUtensorMap x;
+  const uint64_t dims[2] = {static_cast<uint64_t>(a.K), static_cast<uint64_t>(a.M)},
+                 strides[1] = {static_cast<uint64_t>(a.ld_x) * 2};
+  const uint32_t box[2] = {kBlockK, kWideTokens};
+  if (!make_map_nd(&x, a.x, 2, dims, strides, box)) return cudaErrorUnknown;
+  const dim3 grid(static_cast<unsigned>((a.tiles + kWideTiles - 1) / kWideTiles), slices,
+                  (a.M + kWideTokens - 1) / kWideTokens);
+  return launch_ex(kernel, grid, dim3(kWideBlockThreads), WideShape::total, s, false, dim3(1, slices, 1), x, a);
+}
+
 template <bool BF16, int G>
 cudaError_t launch_rows(const LinearArgs& a, int slices, cudaStream_t s) {
+  if (a.M > kFewTokens) return launch_wide<BF16, G>(a, slices, s);
   if (a.M <= 8) return launch_on<BF16, G, 1>(a, slices, s);
   if (a.M <= 16) return launch_on<BF16, G, 2>(a, slices, s);
-  if (a.M <= 32) return launch_linear<BF16, G, 4, false>(a, slices, s);
-  return launch_linear<BF16, G, 8, false>(a, slices, s);
+  return launch_linear<BF16, G, 4, false>(a, slices, s);
 }
 
 template <bool BF16>
@@ -543,7 +458,7 @@ extern "C" int gs_qlinear(const gs_qweight* w, const void* x, int64_t ld_x, void
   if (M == 0) return GS_OK;
   const Layout l = layout_of(*w);
   const uint8_t* base = static_cast<const uint8_t*>(w->packed);
-  const int want = slices_of(l);
+  const int want = M > kFewTokens ? wide_slices_of(l) : slices_of(l);
   LinearArgs a;
   a.w = reinterpret_cast<const uint4*>(base);
   a.scale = reinterpret_cast<const uint32_t*>(base + l.scale_at);

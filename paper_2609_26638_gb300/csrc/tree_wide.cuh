@@ -144,22 +144,6 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
       : "memory");
 }
 
-// mbar_wait, in as little code as it takes.
-__device__ __forceinline__ bool wait_for(uint32_t bar, uint32_t parity, int* err) {
-  uint64_t start = 0;
-#pragma unroll 1
-  for (uint32_t i = 1; !mbar_try_wait(bar, parity); ++i) {
-    if (i & 255) continue;
-    const uint64_t now = global_timer_ns();
-    if (start == 0) start = now;
-    if (now - start > kWaitLimitNs) {
-      atomicExch(err, kErrTimeout);
-      return false;
-    }
-  }
-  return true;
-}
-
 __device__ __forceinline__ void block_barrier() {    // all warps, wherever they are
   __syncwarp();
   asm volatile("bar.sync 2, 256;" ::: "memory");

@@ -99,7 +99,7 @@ def test_shapes(gs, dtype, group, zeros):
     for i, (N, K) in enumerate(SHAPES):
         K = -(-K // group) * group
         w, W = _weights(gs, dtype, N, K, group, zeros, False, seed=i)
-        for M in (1, 2, 8, 9, 17, 33):
+        for M in (1, 2, 8, 9, 17, 33, 129):
             x = _x(dtype, M, K, seed=M)
             y, err = _run(gs, w, x)
             assert err == 0
@@ -111,7 +111,7 @@ def test_shapes(gs, dtype, group, zeros):
                                        (1000, 1024, 64), (4096, 1024, 32)])
 def test_gated(gs, dtype, F, K, group):
     w, W = _weights(gs, dtype, 2 * F, K, group, True, True, seed=F, scale=0.02)
-    for M in (1, 5, 16, 40):
+    for M in (1, 5, 16, 40, 130):
         x = _x(dtype, M, K, seed=M)
         y, err = _run(gs, w, x, epilogue=2)
         assert err == 0
@@ -137,16 +137,22 @@ def test_residual(gs, dtype):
 @pytest.mark.parametrize("N,K,gated", [(1024, 1024, False), (264, 4096, False), (2048, 640, True),
                                        (20000, 256, False)])
 def test_rows_do_not_depend_on_the_batch(gs, dtype, N, K, gated):
-    """A row has the same bits alone and in any batch, at any place of it."""
+    """A row has the same bits alone and in any batch of up to 32, and in any larger one, at any
+    place of it."""
     w, W = _weights(gs, dtype, N, K, 64, True, gated, scale=0.02)
-    x = _x(dtype, 150, K)
+    x = _x(dtype, 300, K)
     epi = 2 if gated else 0
-    whole, err = _run(gs, w, x, epilogue=epi)
+    many, err = _run(gs, w, x, epilogue=epi)
     assert err == 0
-    _check(dtype, whole, W, x, w, gated)
-    for a, b in ((0, 1), (3, 4), (77, 78), (5, 13), (20, 36), (64, 96), (100, 150), (1, 66)):
+    few = torch.cat([_run(gs, w, x[a: a + 32], epilogue=epi)[0] for a in range(0, 300, 32)])
+    for y in (many, few):
+        _check(dtype, y, W, x, w, gated)
+    for a, b in ((0, 1), (3, 4), (77, 78), (5, 13), (20, 36), (64, 96), (290, 299)):
         y, _ = _run(gs, w, x[a:b], epilogue=epi)
-        assert torch.equal(y, whole[a:b]), (a, b)
+        assert torch.equal(y, few[a:b]), (a, b)
+    for a, b in ((0, 33), (100, 150), (1, 66), (20, 148), (5, 134), (33, 290)):
+        y, _ = _run(gs, w, x[a:b], epilogue=epi)
+        assert torch.equal(y, many[a:b]), (a, b)
 
 
 @pytest.mark.parametrize("dtype", ["fp16", "bf16"])
@@ -158,11 +164,15 @@ def test_many_outputs(gs, dtype, N, K, group, zeros, gated):
     cut short, what lies behind it left alone."""
     w, W = _weights(gs, dtype, N, K, group, zeros, gated, scale=0.02)
     epi, outs = 2 if gated else 0, N // 2 if gated else N
-    x = _x(dtype, 40, K)
+    x = _x(dtype, 130, K)
+    many, err = _run(gs, w, x, epilogue=epi, ld=outs + 3)
+    assert err == 0 and (many[:, outs:] == 7).all()
+    _check(dtype, many[:, :outs], W, x, w, gated)
+    x = x[:32]
     whole, err = _run(gs, w, x, epilogue=epi)
     assert err == 0
     _check(dtype, whole, W, x, w, gated)
-    for a, b in ((0, 1), (3, 8), (8, 16), (9, 25), (23, 40)):
+    for a, b in ((0, 1), (3, 8), (8, 16), (9, 25), (15, 32)):
         y, err = _run(gs, w, x[a:b], epilogue=epi, ld=outs + 5)
         assert err == 0 and torch.equal(y[:, :outs], whole[a:b]) and (y[:, outs:] == 7).all(), (a, b)
 
@@ -177,6 +187,13 @@ def test_strides_and_streams(gs):
         for ld in (200, 201, 202, 204, 333):
             y, err = _run(gs, w, wide[:, :192], ld=ld, stream=torch.cuda.Stream())
             assert err == 0 and torch.equal(y[:, :200], plain) and (y[:, 200:] == 7).all()
+        wide = torch.full((70, 192 + 24), float("nan"), dtype=TYPES[dtype], device=DEV)
+        wide[:, :192] = _x(dtype, 70, 192)
+        many, _ = _run(gs, w, wide[:, :192].contiguous())
+        for ld in (200, 201, 333):
+            y, err = _run(gs, w, wide[:, :192], ld=ld, stream=torch.cuda.Stream())
+            assert err == 0 and torch.equal(y[:, :200], many) and (y[:, 200:] == 7).all()
+        wide = wide[:21]
         # an output that starts in the middle of eight bytes
         room = torch.full((21 * 300,), 7.0, dtype=TYPES[dtype], device=DEV)
         y, err = _run(gs, w, wide[:, :192], y=room[1: 1 + 21 * 204].view(21, 204))
@@ -186,13 +203,15 @@ def test_strides_and_streams(gs):
 def test_values_that_are_not_finite(gs):
     """A row's infinities and NaN stay in that row."""
     w, _ = _weights(gs, "bf16", 300, 256, 32, True, False)
-    x = _x("bf16", 12, 256)
-    base, _ = _run(gs, w, x)
-    x[3, 17], x[5, 200] = float("inf"), float("nan")
-    y, _ = _run(gs, w, x)
-    keep = [i for i in range(12) if i not in (3, 5)]
-    assert torch.equal(y[keep], base[keep])
-    assert not torch.isfinite(y[3]).any() and torch.isnan(y[5]).all()
+    for M in (12, 45):
+        x = _x("bf16", M, 256)
+        base, _ = _run(gs, w, x)
+        x[3, 17], x[5, 200] = float("inf"), float("nan")
+        y, _ = _run(gs, w, x)
+        keep = [i for i in range(M) if i not in (3, 5)]
+        assert torch.equal(y[keep], base[keep])
+        # (an infinity times a weight of zero is NaN, times another one infinite)
+        assert not torch.isfinite(y[3]).any() and torch.isnan(y[5]).all()
 
 
 def test_range_word(gs):
@@ -211,26 +230,33 @@ def test_offsets_past_32_bits(gs):
     """Rows of inputs and outputs that lie more than 2^31 elements apart."""
     w, W = _weights(gs, "bf16", 48, 64, 32, False, False)
     far = 2 ** 31 + 64
-    room = torch.zeros(far + 64, dtype=torch.bfloat16, device=DEV)
+    room = torch.zeros(far + 1024, dtype=torch.bfloat16, device=DEV)
     x = room.as_strided((2, 64), (far, 1))
     x.copy_(_x("bf16", 2, 64))
-    out = torch.zeros(far + 64, dtype=torch.bfloat16, device=DEV)
+    out = torch.zeros(far + 1024, dtype=torch.bfloat16, device=DEV)
     y, err = _run(gs, w, x, y=out.as_strided((2, 48), (far, 1)))
+    assert err == 0
+    _check("bf16", y, W, x, w)
+    far = 2 ** 26 + 8                    # (its row 32 lies beyond 2^31 elements)
+    x = room.as_strided((33, 64), (far, 1))
+    x.copy_(_x("bf16", 33, 64))
+    y, err = _run(gs, w, x, y=out.as_strided((33, 48), (far, 1)))
     assert err == 0
     _check("bf16", y, W, x, w)
 
 
 def test_captured_and_replayed(gs):
     w, W = _weights(gs, "fp16", 2048, 1024, 64, True, True, scale=0.02)
-    x, y = _x("fp16", 17, 1024), torch.zeros(17, 1024, dtype=torch.float16, device=DEV)
-    err = torch.zeros(1, dtype=torch.int32, device=DEV)
-    graph = torch.cuda.CUDAGraph()
-    with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
-        gs.gs_qlinear(w, x.data_ptr(), 1024, y.data_ptr(), 1024, 17, 2, err.data_ptr(),
-                      torch.cuda.current_stream().cuda_stream)
-    for seed in (1, 2):
-        x.copy_(_x("fp16", 17, 1024, seed=seed))
-        graph.replay()
-        torch.cuda.synchronize()
-        want, _ = _run(gs, w, x, epilogue=2)
-        assert torch.equal(y, want)
+    for M in (17, 150):
+        x, y = _x("fp16", M, 1024), torch.zeros(M, 1024, dtype=torch.float16, device=DEV)
+        err = torch.zeros(1, dtype=torch.int32, device=DEV)
+        graph = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(graph, stream=torch.cuda.Stream()):
+            gs.gs_qlinear(w, x.data_ptr(), 1024, y.data_ptr(), 1024, M, 2, err.data_ptr(),
+                          torch.cuda.current_stream().cuda_stream)
+        for seed in (1, 2):
+            x.copy_(_x("fp16", M, 1024, seed=seed))
+            graph.replay()
+            torch.cuda.synchronize()
+            want, _ = _run(gs, w, x, epilogue=2)
+            assert torch.equal(y, want)
