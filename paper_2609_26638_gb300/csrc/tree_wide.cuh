@@ -144,6 +144,16 @@ __device__ __forceinline__ void tma_load_4d(uint32_t dst, const CUtensorMap* m, 
       : "memory");
 }
 
+// A row of shared memory to global memory, with the wait.
+__device__ __forceinline__ void store_bulk(void* to, uint32_t from, uint32_t bytes) {
+  asm volatile(
+      "cp.async.bulk.global.shared::cta.bulk_group [%0], [%1], %2;\n\t"
+      "cp.async.bulk.commit_group;\n\t"
+      "cp.async.bulk.wait_group 0;" ::"l"(to),
+      "r"(from), "r"(bytes)
+      : "memory");
+}
+
 __device__ __forceinline__ void block_barrier() {    // all warps, wherever they are
   __syncwarp();
   asm volatile("bar.sync 2, 256;" ::: "memory");
@@ -697,8 +707,8 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         step();
       }
       // ---- the rows' end.  The last O is done, and so are all products and copies:
-      // their shared memory takes the rows, which are then written a row's pieces
-      // by neighbours.
+      // their shared memory takes the rows.  A part's row is copied from there in one piece,
+      // an output's is written a row's pieces by neighbours.
       wait(pv_done + 8 * (at == 0 ? NP - 1 : at - 1), at == 0 ? turn ^ 1 : turn);
       tc_fence_after();
       const int64_t out_at = row * a.Hq + q_head, part = s_seg.part;
@@ -718,26 +728,28 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                             __uint_as_float(o[i + 2]) * inv, __uint_as_float(o[i + 3]) * inv);
         }
       }
-      if (live) {
-        const int64_t slot = shared ? part + r : out_at * a.items + blockIdx.x;
-        if (!whole)
+      fence_proxy_async_smem();            // (bulk copies follow, and those of the next segment)
+      if (!whole) {
+        if (live) {
+          const int64_t slot = shared ? part + r : out_at * a.items + blockIdx.x;
           a.part_ml[slot] = make_float2(m, l);
-        else if (a.lse)
-          a.lse[out_at] = l != 0.f ? (finite_max(m) + log2f(l)) * kLn2 : -INFINITY;
-        s_place[r] = whole ? row * a.ld_out + static_cast<int64_t>(q_head) * D : slot * D;
-      }
-      soft_barrier();
+          store_bulk(a.part_o + slot * D, smem_u32(so + r * P), D * 4);
+        }
+      } else {
+        if (live) {
+          if (a.lse) a.lse[out_at] = l != 0.f ? (finite_max(m) + log2f(l)) * kLn2 : -INFINITY;
+          s_place[r] = row * a.ld_out + static_cast<int64_t>(q_head) * D;
+        }
+        soft_barrier();
 #pragma unroll 4
-      for (int e = r; e < rows * (D / 4); e += kSoftThreads) {
-        const int i = e / (D / 4), d = e % (D / 4) * 4;
-        const float4 v = *reinterpret_cast<const float4*>(so + i * P + d);
-        if (!whole)
-          *reinterpret_cast<float4*>(a.part_o + s_place[i] + d) = v;
-        else
+        for (int e = r; e < rows * (D / 4); e += kSoftThreads) {
+          const int i = e / (D / 4), d = e % (D / 4) * 4;
+          const float4 v = *reinterpret_cast<const float4*>(so + i * P + d);
           *reinterpret_cast<uint2*>(a.out + s_place[i] + d) =
               make_uint2(pack2<BF16>(v.x, v.y), pack2<BF16>(v.z, v.w));
+        }
+        fence_proxy_async_smem();
       }
-      fence_proxy_async_smem();            // (copies of the next segment follow)
       base += pages;
     }
   }
