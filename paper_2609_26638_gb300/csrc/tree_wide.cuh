@@ -39,9 +39,10 @@
 // those rows' O by hand.
 //
 // Measured: fp16, 16 / 8 heads of 64, 32 trees of 17 nodes over 1024 to 6144 tokens 55 us (a
-// floor of 35 by the cache's bytes); bf16, 32 / 4 heads of 128, one tree over 65,001 tokens 40
-// us with 4 nodes (32 rows), 44 with 16, 59 with 33, 73 with 64 (floors of 20, and of 36 by the
-// products for the last).  A page takes a block 1200 to 1500 cycles, most of them the softmax
+// floor of 35 by the cache's bytes); bf16, 32 / 4 heads of 128, one tree over 65,001 tokens 39
+// us with 4 nodes (32 rows), 42 with 16, 57 with 33, 70 with 64 (floors of 20, and of 36 by the
+// products for the last).  With 16 nodes the pages come in at 90 per cent of the memory's rate,
+// for 22 of the 42 us; the rest is a block's start, its end and the joining.  With 17 a page takes a block 1200 to 1500 cycles, most of them the softmax
 // warps' chain: wait 180, scores 100, maximum 220, powers 430, the rest to pass P on and to go
 // round; a block's start takes 5000, a change of segment 5500.  What shortened the chain was
 // less code (waits written out in a few instructions, 61 to 57 us; the next segment found
