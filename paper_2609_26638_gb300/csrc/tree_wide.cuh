@@ -356,7 +356,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   __shared__ Segment s_segs[2];            // this one, the next
   __shared__ WalkRest s_walk;
   __shared__ uint32_t s_some[2][kSoftWarps], s_all[2][kSoftWarps], s_odd[2];
-  __shared__ int64_t s_place[kWideRows];   // of each row: its query, then its output or part
+  __shared__ int64_t s_place[kWideRows];   // of each row: its query, then its output
   uint8_t* smem = reinterpret_cast<uint8_t*>((reinterpret_cast<uintptr_t>(smem_raw) + 1023) &
                                              ~static_cast<uintptr_t>(1023));
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + L::bars_at);
