@@ -20,6 +20,7 @@
 // registers, 41.
 #pragma once
 #include "qlinear_common.cuh"
+#include "qlinear_places.h"
 
 namespace gs {
 namespace {
@@ -44,7 +45,8 @@ struct WideShape {
   static constexpr int z_at = w_at + kWideTiles * ahead * w_bytes;
   static constexpr int bars_at = z_at + kWideTiles * ahead * z_bytes;
   static constexpr int total = bars_at + 256 + 1024; // (1024: the start is aligned by hand)
-  static_assert(kWideTokens * pitch * 4 <= w_at && total <= 227 * 1024);
+  static constexpr int barriers = 4 * stages + 3 * sums;   // and behind them tensor memory's address
+  static_assert(kWideTokens * pitch * 4 <= w_at && total <= 227 * 1024 && 8 * barriers + 4 <= 256);
 };
 
 // q - z of a word's pairs, in the operands' units.
@@ -85,7 +87,7 @@ qlinear_wide_kernel(const __grid_constant__ CUtensorMap map_x, const LinearArgs 
   uint64_t* bars = reinterpret_cast<uint64_t*>(smem + S::bars_at);
   const uint32_t a_full = smem_u32(bars), a_empty = a_full + 8 * ST, x_full = a_empty + 8 * ST,
                  x_empty = x_full + 8 * ST, s_full = x_empty + 8 * ST, s_empty = s_full + 8 * NB;
-  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + 4 * ST + 2 * NB);
+  uint32_t* tmem_slot = reinterpret_cast<uint32_t*>(bars + S::barriers);
   const int warp = threadIdx.x >> 5, lane = threadIdx.x & 31;
   const int slices = gridDim.y, m0 = blockIdx.z * NTOK, tokens = min(NTOK, a.M - m0);
   const int b0 = blockIdx.y * a.slice;
@@ -101,7 +103,8 @@ qlinear_wide_kernel(const __grid_constant__ CUtensorMap map_x, const LinearArgs 
       mbar_init(x_full + 8 * i, 1);
       mbar_init(x_empty + 8 * i, 1);
     }
-    for (int i = 0; i < NB; ++i) mbar_init(s_full + 8 * i, 1), mbar_init(s_empty + 8 * i, kAddThreads / 32);
+    for (int i = 0; i < NB; ++i) mbar_init(s_full + 8 * i, 1);
+    for (int i = 0; i < 2 * NB; ++i) mbar_init(s_empty + 8 * i, kAddThreads / 32);
     fence_mbar_init();
   }
   if (warp == kAddWarp) tmem_alloc(smem_u32(tmem_slot), 512);
@@ -215,8 +218,8 @@ qlinear_wide_kernel(const __grid_constant__ CUtensorMap map_x, const LinearArgs 
           if (k >= steps) break;
           const int q = s * PG + k * 16 / G;         // the group
           const bool first = k * 16 % G == 0, full = (k + 1) * 16 % G == 0;
-          if (first && q >= NB && ok) {
-            ok = wait_for(s_empty + 8 * (q % NB), (q / NB + 1) & 1, a.err);
+          if (first && q >= NB && ok) {              // the place's last group is added
+            ok = wait_for(s_empty + 8 * place_barrier(q - NB, NB), place_phase(q - NB, NB), a.err);
             tc_fence_after();
           }
           umma_f16(tmem + q % NB * NTOK, ad + (k / 4) * (kWideRowsOut * 128 >> 4) + (k % 4) * 2,
@@ -266,7 +269,7 @@ qlinear_wide_kernel(const __grid_constant__ CUtensorMap map_x, const LinearArgs 
         }
         tc_fence_before();
         __syncwarp();
-        if (lane == 0) mbar_arrive(s_empty + 8 * i);
+        if (lane == 0) mbar_arrive(s_empty + 8 * place_barrier(q, NB));
       }
     }
     // ---- all products are done: the operand's memory takes the rows as [token][row]
