@@ -401,6 +401,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
   };
   if (warp >= kSoftWarps) {
     asm volatile("setmaxnreg.dec.sync.aligned.u32 %0;" ::"n"(kWorkRegs));
+    int issued = 0;                      // pages whose products this warp has issued
     for (int seg = 0;; ++seg) {
       // (found while the last one's pages are still at work)
       if (warp == kFetchKWarp) next_segment(a, trees, lane, team, seg, s_walk, s_segs[seg & 1]);
@@ -469,6 +470,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
                      wide_idesc<BF16>(kPageTokens), k > 0);
           umma_commit(s_full + 8 * at);
           umma_commit(k_empty + 8 * st);
+          issued = j + 1;
           step();
         }
       } else if (lane == 0) {
@@ -485,12 +487,17 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             umma_f16_ta(tmem + O, tmem + 64 * at + 8 * k, vd + k * 2, wide_idesc<BF16>(D));
           umma_commit(pv_done + 8 * at);
           umma_commit(v_empty + 8 * st);
+          issued = j + 1;
           step();
         }
       }
       __syncwarp();
       base = end;
     }
+    // the block outlives its arrivals: nobody waits for the last pages' places
+    if (lane == 0 && (warp == kScoreWarp || warp == kValueWarp))
+      for (int j = max(0, issued - ST); j < issued; ++j)
+        wait_for((warp == kScoreWarp ? k_empty : v_empty) + 8 * (j % ST), (j / ST) & 1, a.err);
   } else {
     asm volatile("setmaxnreg.inc.sync.aligned.u32 %0;" ::"n"(kSoftRegs));
     for (int seg = 0;; ++seg) {
