@@ -56,6 +56,20 @@ __device__ __forceinline__ float held_max(float x, float scale_log2) {
   return BF16 ? m : __fsub_ru(m, kHeld<BF16>);
 }
 
+// The weight of score s against the running maximum m (finite_max of it), 2^(scale (s - m)),
+// and as much more as m is held low.  Maxima are kept as they come from the products, before
+// scaling: the difference of two scores is exact where they are near each other, however
+// large they are, while scale * s is rounded by more than a weight's range from 2^27 on.  P is
+// at most 2^15 (or 1).
+template <bool BF16>
+__device__ __forceinline__ float weight_of(float s, float m, float scale_log2) {
+  return ex2(fmaf(s - m, scale_log2, kHeld<BF16>));
+}
+// What sums against maximum `from` are multiplied by against `to`, which is no less.
+__device__ __forceinline__ float moved_max(float from, float to, float scale_log2) {
+  return ex2((from - finite_max(to)) * scale_log2);
+}
+
 // acc += f v, l += f l_v: products rounded before they are added, so that the
 // two ways of joining items give the same bits.
 __device__ __forceinline__ void add_scaled(float4& acc, float& l, const float4& v, float l_v, float f) {

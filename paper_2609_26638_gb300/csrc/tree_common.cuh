@@ -27,8 +27,9 @@ struct TreeArgs {
   int Hq, G, nodes, tiles, window, split, items;
   int cluster;        // the items of a tile are one cluster, and join there
   float scale_log2;
+  float light;        // 1 over the weight of a row's largest score: 2^-15, 2^-7 or 1
   float* part_o;      // [row][head][item][D]
-  float2* part_ml;    // [row][head][item]
+  float2* part_ml;    // [row][head][item]: the largest score (before scaling), the sum
   TreePart* part_n;   // [tree]
   int64_t* part_all;  // pages of all work, blocks that share it (wide kernel, open split)
   int* err;
@@ -87,6 +88,10 @@ __device__ __forceinline__ uint32_t not_finite(uint32_t v) {
   return ((v & E) == E ? 0x0000FFFFu : 0u) | ((v & (E << 16)) == (E << 16) ? 0xFFFF0000u : 0u);
 }
 
+__device__ __forceinline__ float row_lse(const TreeArgs& a, float m, float l) {
+  return l != 0.f ? fmaf(finite_max(m), a.scale_log2, log2f(l * a.light)) * kLn2 : -INFINITY;
+}
+
 // Four dims of a row's output, and with the first of them its log-sum-exp.
 template <bool BF16, int D>
 __device__ __forceinline__ void store_row(const TreeArgs& a, int64_t row, int head, int d, float m,
@@ -94,10 +99,7 @@ __device__ __forceinline__ void store_row(const TreeArgs& a, int64_t row, int he
   const float inv = l != 0.f ? 1.f / l : 0.f;
   *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(head) * D + d) =
       make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-  if (d == 0 && a.lse)     // (the 15 go out of m and l first, without a rounding)
-    a.lse[row * a.Hq + head] =
-        l != 0.f ? (finite_max(m) + kHeld<BF16> + log2f(l * (BF16 ? 1.f : 0x1p-15f))) * kLn2
-                 : -INFINITY;
+  if (d == 0 && a.lse) a.lse[row * a.Hq + head] = row_lse(a, m, l);
 }
 
 }  // namespace

@@ -28,10 +28,10 @@
 // multicast each page the teams were slower, one document of 65,001 tokens and 264 rows
 // 97 us: fewer blocks fit, and each waits for the others at every page.)
 //
-// m moves only when a row's maximum rises by more than 2^8 (O is rescaled then; the result
-// does not depend on m but for rounding).  In fp16 it is set 7 below the
-// maximum, so P stays below 2^15 and a weight of 2^-21 of the largest has all its
-// bits, one of 2^-31 some.  P is rounded to the cache's type for the product, the
+// m is a score as it comes from the product (see weight_of), and moves only when a row's maximum
+// rises by more than 8 in the exponent (O is rescaled then; the result does not depend on m but for
+// rounding).  In fp16 its own weight is 2^7, so P is at most 2^15, whatever the scores' size,
+// and a weight of 2^-21 of the largest has all its bits, one of 2^-31 some.  P is rounded to the cache's type for the product, the
 // sum takes it unrounded, in fp32.
 //
 // Pages that hold masked tokens clear, in shared memory, the values that no row
@@ -67,6 +67,8 @@ constexpr int kTmemCols = 256;                       // the places of S (and P),
 constexpr int kMostShared = 1024;                    // trees whose pages are shared evenly
 constexpr int kFewPages = 4;                         // the least share of a block
 constexpr float kRise = 8.f;                         // log2 units
+template <bool BF16>
+constexpr float kSet = BF16 ? 0.f : 7.f;             // the weight of the score that m was set to
 
 template <int D>
 struct WideSmem {
@@ -553,8 +555,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         if (ok) ok = __all_sync(0xFFFFFFFFu, wait_for(bar, phase, a.err)) != 0;
         return ok;
       };
-      constexpr float kSet = BF16 ? 0.f : 7.f;         // how far below the maximum m is set
-      const F32x2 scale2 = join2(a.scale_log2, a.scale_log2);
+      const F32x2 scale2 = join2(a.scale_log2, a.scale_log2), set2 = join2(kSet<BF16>, kSet<BF16>);
       float m = -INFINITY, l = 0.f;
       for (int j = 0; j < pages; ++j) {
         const int tok0 = (page0 + j) * kPageTokens;
@@ -586,13 +587,12 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
             for (int i = 4; i < 32; i += 4)
               x[e] = max3(x[e], __uint_as_float(s[0][i + e]), __uint_as_float(s[1][i + e]));
           }
-          const float mx = fmaxf(max3(x[0], x[1], x[2]), x[3]) * a.scale_log2;
-          const bool rise = live && (mx - kSet > m + kRise || (m == -INFINITY && mx > m));
+          const float mx = fmaxf(max3(x[0], x[1], x[2]), x[3]);
+          const bool rise = live && (mx - m) * a.scale_log2 > kRise;   // (m = -inf: any score)
           if (__any_sync(0xFFFFFFFFu, rise)) {
-            const float set = rise ? mx - kSet : m;
-            const float f = rise ? ex2(m - set) : 1.f;   // (m = -inf: 0)
+            const float f = rise ? moved_max(m, mx, a.scale_log2) : 1.f;
             l *= f;
-            m = set;
+            if (rise) m = mx;
             if (j > 0 && wait(pv_done + 8 * was, was_turn)) {
               tc_fence_after();
 #pragma unroll 1
@@ -614,7 +614,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
 #pragma unroll
             for (int i = 0; i < 16; ++i) {
               const float2 e = split2(fma2(
-                  join2(__uint_as_float(s[h][2 * i]), __uint_as_float(s[h][2 * i + 1])), scale2, z2));
+                  add2(join2(__uint_as_float(s[h][2 * i]), __uint_as_float(s[h][2 * i + 1])), z2), scale2, set2));
               const float u = ex2(e.x), w = ex2(e.y);
               sum2[i & 1] = add2(sum2[i & 1], join2(u, w));
               p[i] = pack2<BF16>(u, w);
@@ -745,7 +745,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
         }
       } else {
         if (live) {
-          if (a.lse) a.lse[out_at] = l != 0.f ? (finite_max(m) + log2f(l)) * kLn2 : -INFINITY;
+          if (a.lse) a.lse[out_at] = row_lse(a, m, l);
           s_place[r] = row * a.ld_out + static_cast<int64_t>(q_head) * D;
         }
         soft_barrier();
