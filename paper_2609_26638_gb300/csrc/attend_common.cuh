@@ -44,30 +44,26 @@ __device__ __forceinline__ uint4 load_once(const uint16_t* p) {
 // exponentials are 2^-inf = 0 and not 2^(inf - inf).
 __device__ __forceinline__ float finite_max(float m) { return m == -INFINITY ? 0.f : m; }
 
-// The max that a step's largest score (before scaling) asks for.  In fp16 it is
-// held 15 too low, so that light keys keep their bits.  Both roundings are upwards, so P is at most 2^15 (or 1) however large
-// the scores are: with 1.4 times that fp16 would come near its end, and scores
-// beyond 2^24 could pass it.
+// How far below the largest exponent the max is held: in fp16 15, so that light keys keep
+// their bits.
 template <bool BF16>
 constexpr float kHeld = BF16 ? 0.f : 15.f;
-template <bool BF16>
-__device__ __forceinline__ float held_max(float x, float scale_log2) {
-  const float m = __fmul_ru(x, scale_log2);
-  return BF16 ? m : __fsub_ru(m, kHeld<BF16>);
-}
 
-// The weight of score s against the running maximum m (finite_max of it), 2^(scale (s - m)),
+// The weights of two scores against the running maximum m (finite_max of it), 2^(scale (s - m)),
 // and as much more as m is held low.  Maxima are kept as they come from the products, before
 // scaling: the difference of two scores is exact where they are near each other, however
 // large they are, while scale * s is rounded by more than a weight's range from 2^27 on.  P is
 // at most 2^15 (or 1).
 template <bool BF16>
-__device__ __forceinline__ float weight_of(float s, float m, float scale_log2) {
-  return ex2(fmaf(s - m, scale_log2, kHeld<BF16>));
+__device__ __forceinline__ float2 weights_of(float s0, float s1, float m, float scale_log2) {
+  const float2 e = split2(fma2(add2(join2(s0, s1), join2(-m, -m)), join2(scale_log2, scale_log2),
+                               join2(kHeld<BF16>, kHeld<BF16>)));
+  return make_float2(ex2(e.x), ex2(e.y));
 }
-// What sums against maximum `from` are multiplied by against `to`, which is no less.
-__device__ __forceinline__ float moved_max(float from, float to, float scale_log2) {
-  return ex2((from - finite_max(to)) * scale_log2);
+// What sums against maximum `from` are multiplied by against one no less, of which z is the
+// finite_max (found outside of loops: within the joining kernel's, one of 131,001 tokens took 0.9 us more).
+__device__ __forceinline__ float moved_max(float from, float z, float scale_log2) {
+  return ex2((from - z) * scale_log2);
 }
 
 // acc += f v, l += f l_v: products rounded before they are added, so that the

@@ -3,7 +3,7 @@
 //
 //   s_j = scale * q . k_j over the visible keys j in [max(0, n - window), n)
 //   o = sum_j 2^(s_j' - m) v_j / l,  l = sum_j 2^(s_j' - m),  s' = s log2(e)
-//   (m the running maximum of s'; in fp16 15 less, see below)
+//   (m the running maximum of s'; in fp16 15 less, see below; kept before scaling, see weights_of)
 //
 // Each key and value is read once for a group of up to 16 query heads (once for
 // every 16 of a larger one), with 4 flops per query head and element of 2 bytes, so
@@ -28,7 +28,7 @@
 // which the accumulators of one lane are again the P operand of the 8 tokens
 // whose values it reads, so P needs no exchange either.
 //
-// Running max (log2 units), sum and accumulators are fp32.  P is rounded to
+// Running max, sum and accumulators are fp32.  P is rounded to
 // the cache's type for the second product, relative error 2^-11 (fp16) or 2^-8
 // (bf16) at most, like the output's own rounding and averaged over the keys; the
 // sum l takes the unrounded P.  fp16 has no exponents for light keys (below 2^-14 it
@@ -115,9 +115,9 @@ __device__ __forceinline__ void store_row(const DecodeArgs& a, int row, int head
   const float inv = l != 0.f ? 1.f / l : 0.f;
   *reinterpret_cast<uint2*>(a.out + row * a.ld_out + static_cast<int64_t>(head) * D + d) =
       make_uint2(pack2<BF16>(acc.x * inv, acc.y * inv), pack2<BF16>(acc.z * inv, acc.w * inv));
-  if (d == 0 && a.lse)     // (the 15 go out of m and l first, without a rounding)
+  if (d == 0 && a.lse)     // (the 15 go out of l first, without a rounding)
     a.lse[static_cast<int64_t>(row) * a.Hq + head] =
-        l != 0.f ? (finite_max(m) + kHeld<BF16> + log2f(l * (BF16 ? 1.f : 0x1p-15f))) * kLn2
+        l != 0.f ? fmaf(finite_max(m), a.scale_log2, log2f(l * (BF16 ? 1.f : 0x1p-15f))) * kLn2
                  : -INFINITY;
 }
 
@@ -255,11 +255,11 @@ decode_attention_kernel(const DecodeArgs a) {
       x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 1));
       x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
     }
-    const float n0 = fmaxf(m0, held_max<BF16>(x0, a.scale_log2)),
-                n1 = fmaxf(m1, held_max<BF16>(x1, a.scale_log2));
+    const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
     const bool rises = n0 != m0 || (WIDE && n1 != m1);
     if (__any_sync(0xFFFFFFFFu, rises)) {
-      const float f0 = ex2(m0 - finite_max(n0)), f1 = WIDE ? ex2(m1 - finite_max(n1)) : 1.f;
+      const float f0 = moved_max(m0, finite_max(n0), a.scale_log2),
+                  f1 = WIDE ? moved_max(m1, finite_max(n1), a.scale_log2) : 1.f;
       l0 *= f0;
       l1 *= f1;
 #pragma unroll
@@ -275,15 +275,14 @@ decode_attention_kernel(const DecodeArgs a) {
     uint32_t pa[4], pb[4];
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float u = ex2(fmaf(s[i][0], a.scale_log2, -z0)), v = ex2(fmaf(s[i][1], a.scale_log2, -z0));
-      l0 += u + v;
-      pa[i] = pack2<BF16>(u, v);
+      const float2 u = weights_of<BF16>(s[i][0], s[i][1], z0, a.scale_log2);
+      l0 += u.x + u.y;
+      pa[i] = pack2<BF16>(u.x, u.y);
       pb[i] = 0u;
       if (WIDE) {
-        const float w = ex2(fmaf(s[i][2], a.scale_log2, -z1)),
-                    y = ex2(fmaf(s[i][3], a.scale_log2, -z1));
-        l1 += w + y;
-        pb[i] = pack2<BF16>(w, y);
+        const float2 w = weights_of<BF16>(s[i][2], s[i][3], z1, a.scale_log2);
+        l1 += w.x + w.y;
+        pb[i] = pack2<BF16>(w.x, w.y);
       }
     }
     // ---- O += P V
@@ -341,7 +340,7 @@ decode_attention_kernel(const DecodeArgs a) {
     for (int w = 0; w < used; ++w) m = fmaxf(m, s_ml[w][r].x);
     const float z = finite_max(m);
     for (int w = 0; w < used; ++w) {
-      const float f = ex2(s_ml[w][r].x - z);
+      const float f = moved_max(s_ml[w][r].x, z, a.scale_log2);
       const float4 v = *reinterpret_cast<const float4*>(so + (w * kRows + r) * P + d);
       l = fmaf(f, s_ml[w][r].y, l);
       acc.x = fmaf(f, v.x, acc.x);
@@ -385,7 +384,7 @@ decode_attention_kernel(const DecodeArgs a) {
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < kMostCluster; ++i)
-        if (i < items) add_scaled(acc, l, v[i], ml[i].y, ex2(ml[i].x - z));
+        if (i < items) add_scaled(acc, l, v[i], ml[i].y, moved_max(ml[i].x, z, a.scale_log2));
       store_row<BF16, D>(a, row, h0 + r, d, m, l, acc);
     }
   }
@@ -420,14 +419,14 @@ __global__ void __launch_bounds__(kJoinThreads) decode_join_kernel(const DecodeA
   __syncthreads();
 #pragma unroll
   for (int w = 0; w < kJoinThreads / 32; ++w) m = fmaxf(m, s_max[w]);
-  const float z = finite_max(m);
+  const float z = finite_max(m), scale_log2 = a.scale_log2;
   const int grp = threadIdx.x / L, d = threadIdx.x % L;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
 #pragma unroll 4
   for (int i = grp; i < items; i += NG) {
     const float2 x = ml[i];
-    add_scaled(acc, l, po[static_cast<int64_t>(i) * L + d], x.y, ex2(x.x - z));
+    add_scaled(acc, l, po[static_cast<int64_t>(i) * L + d], x.y, moved_max(x.x, z, scale_log2));
   }
   s_acc[grp][d] = acc;
   if (d == 0) s_l[grp] = l;

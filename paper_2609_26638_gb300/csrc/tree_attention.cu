@@ -5,7 +5,7 @@
 //          (the window's, where there is one) and the nodes of its mask
 //   o_i = sum_j 2^(s'_ij - m_i) v_j / l_i,  l_i = sum_j 2^(s'_ij - m_i)
 //
-// (s' = s log2(e), m the running maximum, 15 less in fp16; see weight_of.)  A query row is one
+// (s' = s log2(e), m the running maximum, 15 less in fp16; see weights_of.)  A query row is one
 // query head of one node.  Up to 16 rows of a KV head, node by node, are one tile of the
 // narrow kernel below, more are tiles of 128 for the one in tree_wide.cuh (fp16, 16 / 8
 // heads of 64, 32 trees of 1024 to 6144 tokens: 16 rows 50 us here; 32 and 48 rows 77 and
@@ -228,7 +228,8 @@ tree_attention_kernel(const TreeArgs a) {
     x1 = fmaxf(x1, __shfl_xor_sync(0xFFFFFFFFu, x1, 2));
     const float n0 = fmaxf(m0, x0), n1 = fmaxf(m1, x1);
     if (__any_sync(0xFFFFFFFFu, n0 != m0 || n1 != m1)) {
-      const float f0 = moved_max(m0, n0, a.scale_log2), f1 = moved_max(m1, n1, a.scale_log2);
+      const float f0 = moved_max(m0, finite_max(n0), a.scale_log2),
+                  f1 = moved_max(m1, finite_max(n1), a.scale_log2);
       l0 *= f0;
       l1 *= f1;
 #pragma unroll
@@ -244,14 +245,12 @@ tree_attention_kernel(const TreeArgs a) {
     const float z0 = finite_max(m0), z1 = finite_max(m1);
 #pragma unroll
     for (int i = 0; i < 4; ++i) {
-      const float e0 = weight_of<BF16>(s[i][0], z0, a.scale_log2),
-                  e1 = weight_of<BF16>(s[i][1], z0, a.scale_log2),
-                  e2 = weight_of<BF16>(s[i][2], z1, a.scale_log2),
-                  e3 = weight_of<BF16>(s[i][3], z1, a.scale_log2);
-      l0 += e0 + e1;
-      l1 += e2 + e3;
-      pa[i] = pack2<BF16>(e0, e1);
-      pb[i] = pack2<BF16>(e2, e3);
+      const float2 u = weights_of<BF16>(s[i][0], s[i][1], z0, a.scale_log2),
+                   w = weights_of<BF16>(s[i][2], s[i][3], z1, a.scale_log2);
+      l0 += u.x + u.y;
+      l1 += w.x + w.y;
+      pa[i] = pack2<BF16>(u.x, u.y);
+      pb[i] = pack2<BF16>(w.x, w.y);
     }
     const uint16_t* v_now = v_at;
     find_step(j + 1);
@@ -346,8 +345,9 @@ tree_attention_kernel(const TreeArgs a) {
     float m = -INFINITY, l = 0.f;
     float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
     for (int w = 0; w < used; ++w) m = fmaxf(m, sm.ml[w][r].x);
+    const float z = finite_max(m);
     for (int w = 0; w < used; ++w) {
-      const float f = moved_max(sm.ml[w][r].x, m, a.scale_log2);
+      const float f = moved_max(sm.ml[w][r].x, z, a.scale_log2);
       const float4 x = *reinterpret_cast<const float4*>(sm.so + (w * 16 + r) * P + d);
       l = fmaf(f, sm.ml[w][r].y, l);
       acc.x = fmaf(f, x.x, acc.x);
@@ -387,11 +387,12 @@ tree_attention_kernel(const TreeArgs a) {
 #pragma unroll
       for (int i = 0; i < kMostCluster; ++i)
         if (i < items) m = fmaxf(m, ml[i].x);
+      const float z = finite_max(m);
       float l = 0.f;
       float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
 #pragma unroll
       for (int i = 0; i < kMostCluster; ++i)
-        if (i < items) add_scaled(acc, l, x[i], ml[i].y, moved_max(ml[i].x, m, a.scale_log2));
+        if (i < items) add_scaled(acc, l, x[i], ml[i].y, moved_max(ml[i].x, z, a.scale_log2));
       store_row<BF16, D>(a, row0 + node_of(r), q_head(r), d, m, l, acc);
     }
   }
@@ -452,6 +453,7 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows, int team) {
   for (int i = d; i < parts; i += L) m = fmaxf(m, a.part_ml[part_at(i)].x);
 #pragma unroll
   for (int x = L / 2; x; x >>= 1) m = fmaxf(m, __shfl_xor_sync(0xFFFFFFFFu, m, x));
+  const float z = finite_max(m), scale_log2 = a.scale_log2;
   const float4* po = reinterpret_cast<const float4*>(a.part_o) + d;
   float4 acc = make_float4(0.f, 0.f, 0.f, 0.f);
   float l = 0.f;
@@ -471,7 +473,7 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows, int team) {
       for (int i = 0; i < 4; ++i)
         if (first_of + h + i < parts) {
           const float2 x = a.part_ml[part_at(first_of + h + i)];
-          add_scaled(part, pl, v[i], x.y, moved_max(x.x, m, a.scale_log2));
+          add_scaled(part, pl, v[i], x.y, moved_max(x.x, z, scale_log2));
         }
     }
     if (groups == 1) {

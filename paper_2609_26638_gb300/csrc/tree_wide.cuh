@@ -28,7 +28,7 @@
 // multicast each page the teams were slower, one document of 65,001 tokens and 264 rows
 // 97 us: fewer blocks fit, and each waits for the others at every page.)
 //
-// m is a score as it comes from the product (see weight_of), and moves only when a row's maximum
+// m is a score as it comes from the product (see weights_of), and moves only when a row's maximum
 // rises by more than 8 in the exponent (O is rescaled then; the result does not depend on m but for
 // rounding).  In fp16 its own weight is 2^7, so P is at most 2^15, whatever the scores' size,
 // and a weight of 2^-21 of the largest has all its bits, one of 2^-31 some.  P is rounded to the cache's type for the product, the
@@ -590,7 +590,7 @@ tree_wide_kernel(const __grid_constant__ CUtensorMap map_k, const __grid_constan
           const float mx = fmaxf(max3(x[0], x[1], x[2]), x[3]);
           const bool rise = live && (mx - m) * a.scale_log2 > kRise;   // (m = -inf: any score)
           if (__any_sync(0xFFFFFFFFu, rise)) {
-            const float f = rise ? moved_max(m, mx, a.scale_log2) : 1.f;
+            const float f = rise ? moved_max(m, mx, a.scale_log2) : 1.f;   // (mx is above -inf)
             l *= f;
             if (rise) m = mx;
             if (j > 0 && wait(pv_done + 8 * was, was_turn)) {

@@ -13,7 +13,7 @@ import numpy as np
 import pytest
 import torch
 
-from tests.test_gpu_tree_attention import DEV, TYPES, _case, _check, _run
+from tests.test_gpu_tree_attention import DEV, TYPES, _cache, _case, _check, _dev, _run
 
 pytestmark = pytest.mark.gpu
 SIZES = [("fp16", x) for x in (20, 24, 25, 26, 27, 28, 30, 32, 34)] + [
@@ -65,4 +65,26 @@ def test_trees(gs, dtype, x, D, nodes):
         for split in (0, 1, 4):
             out, lse, err = _run(gs, c, split=split)
             assert err == 0
+            _check(c, out, lse, **tol)
+
+
+@pytest.mark.parametrize("dtype,x", SIZES)
+@pytest.mark.parametrize("D", [64, 128])
+def test_single_tokens(gs, dtype, x, D):
+    ns = [0, 5, 64, 700, 300]
+    for rise in (0, 4, 9, 12, 16):
+        c = _case(dtype, ns, 1, 8, 2, D, seed=x + rise)
+        tol = _large(c, x, rise)
+        cache = _cache(gs, c["pool"], c["table"], 2, D, dtype)
+        n = _dev(np.array(ns) + 1)
+        for split in (0, 1, 4):
+            out = torch.zeros(5, 8 * D, dtype=TYPES[dtype], device=DEV)
+            lse = torch.zeros(5, 8, device=DEV)
+            scratch = torch.zeros(gs.gs_decode_attention_scratch_bytes(cache, 5, 8, split), dtype=torch.uint8,
+                                  device=DEV)
+            gs.gs_decode_attention(cache, c["q"].data_ptr(), 8 * D, 0, n.data_ptr(), 5, 8, D ** -0.5, 0,
+                                   out.data_ptr(), 8 * D, lse.data_ptr(), split, scratch.data_ptr(),
+                                   scratch.numel(), torch.cuda.current_stream().cuda_stream)
+            torch.cuda.synchronize()
+            assert int(scratch[:4].view(torch.int32).item()) == 0
             _check(c, out, lse, **tol)
