@@ -62,7 +62,8 @@ def tree_decode(dec: StepDecoder, prompts: List[List[int]], new: int, *, max_nod
     every position, or drawn from ``seed``; a position's token is drawn with the number of
     the position that it follows, whatever tree it was drafted in.  ``settings`` are
     ``Sampler``'s (temperature 0: the most likely token).  ``draft`` makes (tokens, parents)
-    from (history, max_nodes, depth, ngram)."""
+    from (history, max_nodes, depth, ngram); its max_nodes is less than the call's where the
+    context or the pool's free pages end, so a pool that holds the texts is enough."""
     b = len(prompts)
     if not b or any(not p for p in prompts) or new < 1 or not 1 <= max_nodes <= MAX_NODES:
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "no prompt, an empty one, new < 1 or max_nodes beyond 1 .. 64")
@@ -77,6 +78,7 @@ def tree_decode(dec: StepDecoder, prompts: List[List[int]], new: int, *, max_nod
     text = [list(p) for p in prompts]
     left = [new] * b
     seqs: List[int] = []
+    table = dec.pool.table
     steps = 0
     try:
         for p in prompts:                    # all but the last token, which is the first root
@@ -86,10 +88,16 @@ def tree_decode(dec: StepDecoder, prompts: List[List[int]], new: int, *, max_nod
         while any(left):
             live = [i for i in range(b) if left[i]]
             trees = []
-            for i in live:
-                room = min(max_nodes, dec.pool.table.max_ctx - len(text[i]) + 1)
+            cached = [len(text[i]) - 1 for i in live]
+            # pages beyond every root's: drafts may have these, and give back what is not kept
+            spare = table.free_pages - sum(max(0, n // PAGE_TOKENS + 1 - len(table.pages(seqs[i])))
+                                           for i, n in zip(live, cached))
+            for i, n in zip(live, cached):
+                have = max(len(table.pages(seqs[i])), n // PAGE_TOKENS + 1)
+                room = min(max_nodes, table.max_ctx - n, (have + max(spare, 0)) * PAGE_TOKENS - n)
                 tokens, parents = draft(text[i], room, min(depth, left[i] - 1), ngram)
-                trees.append((seqs[i], len(text[i]) - 1, tokens, parents))
+                spare -= max(0, -(-(n + len(tokens)) // PAGE_TOKENS) - have)
+                trees.append((seqs[i], n, tokens, parents))
             logits = dec.feed_trees(trees)
             nodes = logits.shape[1]
             number = torch.zeros(len(live), nodes)
@@ -107,6 +115,7 @@ def tree_decode(dec: StepDecoder, prompts: List[List[int]], new: int, *, max_nod
                     dec.check()
                     raise gs.GsError(gs.GS_ERR_DEVICE_CHECK, "no token could be chosen")
                 text[i] += got
+                dec.pool.truncate(seqs[i], len(text[i]) - 1)
                 left[i] = 0 if got[-1] == eos else left[i] - len(got)
             steps += 1
         dec.check()
