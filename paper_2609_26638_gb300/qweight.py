@@ -28,7 +28,12 @@ def quantize(w: torch.Tensor, group: int = 64, zeros: bool = False
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "an infinite or NaN weight")
     x = w.float().view(w.shape[0], -1, group)
     lo, hi = x.amin(-1).clamp(max=0), x.amax(-1).clamp(min=0)
-    scale = ((hi - lo) / 15 if zeros else torch.maximum(-lo / 8, hi / 7)).to(w.dtype)
+    exact = (hi - lo) / 15 if zeros else torch.maximum(-lo / 8, hi / 7)
+    exact = torch.where(torch.isinf(exact), hi / 15 - lo / 15, exact)
+    scale = exact.to(w.dtype)
+    # below the type's normal numbers a rounding down could leave the largest weights out of reach
+    short = scale.float() < exact * (1 - torch.finfo(w.dtype).eps)
+    scale = torch.where(short, (scale.view(torch.int16) + 1).view(w.dtype), scale)
     step = torch.where(scale == 0, 1, scale.float())
     zero = (-lo / step).round().clamp(0, 15) if zeros else torch.full_like(step, 8.0)
     q = (x / step[..., None] + zero[..., None]).round().clamp(0, 15).to(torch.uint8).flatten(1)
