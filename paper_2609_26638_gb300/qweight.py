@@ -26,7 +26,7 @@ def quantize(w: torch.Tensor, group: int = 64, zeros: bool = False
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "a 16-bit [N, K] matrix with K a multiple of the group needed")
     if not torch.isfinite(w).all():
         raise gs.GsError(gs.GS_ERR_INVALID_ARG, "an infinite or NaN weight")
-    x = w.float().view(w.shape[0], -1, group)
+    x = w.contiguous().float().view(w.shape[0], -1, group)
     lo, hi = x.amin(-1).clamp(max=0), x.amax(-1).clamp(min=0)
     exact = (hi - lo) / 15 if zeros else torch.maximum(-lo / 8, hi / 7)
     exact = torch.where(torch.isinf(exact), hi / 15 - lo / 15, exact)

@@ -38,3 +38,13 @@ def test_the_largest_weights(qweight, dtype, zeros):
     most = torch.finfo(dtype).max
     w[0, 0], w[0, 1], w[1, 5], w[2, 7] = most, -most, most, -most
     _check(qweight, w, zeros)
+
+
+@pytest.mark.parametrize("zeros", [False, True])
+def test_strided_matrices(qweight, zeros):
+    """A transposed matrix, and columns of a wider one, as their copies."""
+    w = torch.randn(128, 96, generator=torch.Generator().manual_seed(3)).half()
+    for view in (w.t(), w[:, :64], w.t()[::2, 32:96]):
+        for a, b in zip(qweight.quantize(view, 64 if view.shape[1] % 64 == 0 else 32, zeros),
+                        qweight.quantize(view.contiguous(), 64 if view.shape[1] % 64 == 0 else 32, zeros)):
+            assert a is b is None or torch.equal(a, b) and a.is_contiguous()
