@@ -15,9 +15,12 @@
 // Packed weights are copied to shared memory seven stages ahead: two stages ahead in
 // registers held the whole to 1.4 TB/s.  What bounds it now is the time that an unpacking
 // warp takes for a stage, some 250 instructions one after another with two warps on a scheduler:
-// bf16, 8192 x 8192, 128 tokens 34 us, of which the products' own time is a quarter.
+// bf16, 8192 x 8192, 128 tokens 34 us, of which the products' own time is a quarter.  Every 128
+// tokens unpack the weights again (544 tokens 157 us): beyond 256 tokens gs_linear's 16-bit
+// weights are faster (64 to 256 tokens 60 to 64 us, 544 93).
 // Unpacking and adding by the same eight warps 36 us; 16 unpacking warps, for want of
-// registers, 41.
+// registers, 41.  Groups of 32 are four sums a stage to read from tensor memory and add instead of
+// one: fp16, 128 tokens 51 us, 32 with groups of 128.
 #pragma once
 #include "qlinear_common.cuh"
 #include "qlinear_places.h"

@@ -111,8 +111,8 @@ __global__ void __launch_bounds__(kAcceptWarps * 32) tree_accept_kernel(const Ac
 // transposed, so a moved token is one element of each of D rows of 64: lanes
 // are dealt to the (row, token) pairs, and reads and writes are sectors of 32
 // bytes for elements of 2.  These sectors bound it: 64 trees, 12 layers, 8 heads of 128, paths
-// of up to 16 tokens 38 us, for which DRAM reads 120 MB and writes 62 where 51 MB
-// are moved.  (Blocks that take 2, 4 or 12 layers each, so that paths and pages are
+// of up to 16 tokens 38 us, for which DRAM reads 120 MB and writes 27, and 35 more stay in L2,
+// where 51 MB are moved.  (Blocks that take 2, 4 or 12 layers each, so that paths and pages are
 // looked up less often: 38, 40 and 50 us.)
 constexpr int kCommitThreads = 128;
 constexpr int kCommitWarps = kCommitThreads / 32;

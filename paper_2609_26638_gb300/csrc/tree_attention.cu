@@ -9,12 +9,15 @@
 // query head of one node.  Up to 16 rows of a KV head, node by node, are one tile of the
 // narrow kernel below, more are tiles of 128 for the one in tree_wide.cuh (fp16, 16 / 8
 // heads of 64, 32 trees of 1024 to 6144 tokens: 16 rows 50 us here; 32 and 48 rows 77 and
-// 104 us with two and three tiles to a warp here, for want of registers, 62 and 68 there).
+// 104 us with two and three tiles to a warp here, for want of registers, 57 and 62 there).
 //
 // A narrow block takes one KV head and one item of `split` pages; its warps take
 // the item's half pages in turn, straight from global memory into the operand
 // registers of m16n8k16 instructions, and are joined at the item's end.  Every byte of
 // the cache is read once, and bounds it.
+//
+// P is rounded to the cache's type for the product with V, as the output is, and the sums are
+// not: the reasons, and what that loses, are gs_decode_attention's.
 //
 // Only steps that reach the tree's nodes, or a window's start, look at masks: a row's
 // view of the step's 32 tokens is one word, the cached range or'ed with its
@@ -495,9 +498,17 @@ tree_join_kernel(const TreeArgs a, int groups, int64_t rows, int team) {
 // wave of blocks shares the cache evenly, or eight items that join in a cluster where that is
 // not long.  Several trees, which may differ in length: items of at most 16 pages, so
 // that the tail behind the longest is short, or 32 where the trees' heads alone fill the
-// GPU, as every part of 16 rows is written and read again (fp16, 16 / 8 heads of 64, 8
-// nodes: 64 trees of 8192 tokens 171 us with 33 pages, 184 with 16, 191 with 12; four
-// of 20,000 25 with 16, 30 with 32; 32 of 1024 to 6144 49 with 12 to 24).
+// GPU, as every part of 16 rows is written and read again.  The host does not know the
+// lengths, and no cap is the best for all; us by pages of an item, the choice with a star:
+//   tokens            nodes, heads            12     16     24     32     48     64
+//   32 x 1024-6144    4, 16 / 8 x 64, fp16    45.8   46.7*  47.2   49.3   44.8   51.8
+//   the same          8                       49.5   50.1*  49.5   52.1   46.6   53.1
+//   16 x 100-6144     5                       30.4   25.9*  26.5   29.7   36.7   42.4
+//   4 x 20,000        8                       37.0   39.3*  33.2   33.7   37.0   44.5
+//   64 x 8192         8                       191    184    171    170*   172    178
+//   48 x 1024-6144    4, 16 / 4 x 128, bf16   84.1   80.8*  76.0   86.6   75.8   83.7
+//   16 x 1024-6144    4, 32 / 8 x 128, bf16   61.4   56.4*  62.7   50.8   63.7   76.8
+// (up to 18 per cent from the best: a caller who knows the lengths can give a split).
 constexpr int64_t wave_of(int head_dim) { return head_dim == 64 ? 320 : 256; }
 constexpr int kMostPages = 16;
 int auto_split(int pages, int trees, int64_t blocks_per_item, int head_dim) {

@@ -1,8 +1,8 @@
 // tree_wide.cuh -- tree attention for many query rows of a KV head: tcgen05
 // products on tiles of 128 rows.
 //
-// With R rows per KV head a byte of the cache takes R flops or more, and beyond some
-// tens the tensor cores bound it.  A block takes 128 rows, one KV head and one
+// With R rows per KV head a byte of the cache takes R flops or more: beyond 16 rows more
+// than tiles of 16 keep up with.  A block takes 128 rows, one KV head and one
 // item of pages, a page of 64 tokens a step:
 //
 //   S = Q K^T    [128 rows][64 tokens] in tensor memory; Q and K from shared memory
@@ -12,8 +12,8 @@
 //
 // Four more warps fetch K and V^T by TMA (both lie in the cache as K-major operands)
 // and issue the S and the O products: to issue a copy takes a thread 300 to 400
-// cycles, a product about 110, so that one thread for two of these tasks would bound
-// the block (1580 cycles a page instead of 1100).  S has three places (two
+// cycles, a product about 110, so that one thread for all of them would bound the block
+// (1580 cycles a page at head dim 64, for which the softmax takes 1250).  S has three places (two
 // at head dim 128), so that the products of the next pages run during the
 // softmax of this one.  The softmax warps take over registers of the other four: at
 // 128 to a thread they would spill.
@@ -31,23 +31,26 @@
 // m is a score as it comes from the product (see weights_of), and moves only when a row's maximum
 // rises by more than 8 in the exponent (O is rescaled then; the result does not depend on m but for
 // rounding).  In fp16 its own weight is 2^7, so P is at most 2^15, whatever the scores' size,
-// and a weight of 2^-21 of the largest has all its bits, one of 2^-31 some.  P is rounded to the cache's type for the product, the
-// sum takes it unrounded, in fp32.
+// and a weight of 2^-21 of the largest has all its bits, one of 2^-31 some.  P is rounded to the
+// cache's type for the product (2^-11 in fp16, 2^-8 in bf16, as the output is; the tensor cores
+// take no wider operand at their full rate), the sum takes it unrounded, in fp32.
 //
 // Pages that hold masked tokens clear, in shared memory, the values that no row
 // sees.  Values that some rows see and that are not finite are taken out and added to
 // those rows' O by hand.
 //
-// Measured: fp16, 16 / 8 heads of 64, 32 trees of 17 nodes over 1024 to 6144 tokens 55 us (a
-// floor of 35 by the cache's bytes); bf16, 32 / 4 heads of 128, one tree over 65,001 tokens 39
-// us with 4 nodes (32 rows), 42 with 16, 57 with 33, 70 with 64 (floors of 20, and of 36 by the
+// Measured: fp16, 16 / 8 heads of 64, 32 trees of 17 nodes over 1024 to 6144 tokens 56.5 us (a
+// floor of 35 by the cache's bytes); bf16, 32 / 4 heads of 128, one tree over 65,001 tokens 40
+// us with 4 nodes (32 rows), 43 with 16, 57 with 33, 71 with 64 (floors of 20, and of 36 by the
 // products for the last).  With 16 nodes the pages come in at 90 per cent of the memory's rate,
-// for 22 of the 42 us; the rest is a block's start, its end and the joining.  With 17 a page takes a block 1200 to 1500 cycles, most of them the softmax
-// warps' chain: wait 180, scores 100, maximum 220, powers 430, the rest to pass P on and to go
-// round; a block's start takes 5000, a change of segment 5500.  What shortened the chain was
-// less code (waits written out in a few instructions, 61 to 57 us; the next segment found
-// during the last one, 55), not fewer powers: two or four threads to a row where the tile's
-// rows leave room came to 54, and to 2 us more at head dim 128.
+// for 22 of the 43 us; the rest is a block's start, its end and the joining.  With 17 (the 32
+// trees) the softmax warps' chain bounds a page, 1250 cycles: wait 180, scores 100, maximum 220,
+// powers 430, P passed on 100, the way round 190 (stamped before the maxima were kept unscaled, which
+// changed no time by more than 0.5 per cent); a block's start takes 5300, a change of segment
+// 5500.  What shortened the chain was less code (waits written out in a few instructions, 61 to
+// 57 us; the next segment found during the last one, 55; waiting for the last arrivals added
+// one), not fewer powers: two or four threads to a row where the tile's rows leave room took 1
+// us off, and added 2 at head dim 128.
 #pragma once
 #include "internal.h"
 #include "tree_common.cuh"
